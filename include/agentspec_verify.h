@@ -35,6 +35,14 @@
  *                       fly, never stored.
  *   verify_check_batch -- the batch descriptor's preconditions, checked on the
  *                       device.
+ *   verify_rotary, verify_rotary_append -- the scored rows' queries and keys
+ *                       rotated to explicit positions on one or several axes;
+ *                       the second stores the keys and values like
+ *                       verify_kv_append.
+ *   verify_key_weights, verify_evict_plan, verify_kv_compact -- a bound on each
+ *                       request's cached keys: the attention weight that every
+ *                       cached key has gathered, the keys to keep, and the moves
+ *                       that bring them to the front of the cache.
  *
  * Conventions shared by the calls
  * --------------------------------
@@ -115,7 +123,9 @@ typedef struct verify_attn_params {
  *   q            [total_q][Hq][D]                     (dtype)
  *   k_cache      [num_blocks][Hkv][D/x][16][x]        x = 16 bytes / element
  *                (token t, dim d of a block at [d/x][t][d%x])
- *   v_cache      [num_blocks][Hkv][D][16]             (token t, dim d at [d][t])
+ *   v_cache      [num_blocks][Hkv][D][16]             (token t, dim d at [d][t]);
+ *                slots behind a request's last key in its last block are read with
+ *                weights of zero, so they must not hold infinities or NaN
  *   block_tables [num_seqs][max_blocks_per_seq] int32 physical block ids; the
  *                first ceil(S_i/16) entries of row i are read, ids outside
  *                [0, num_blocks) are skipped (their keys contribute nothing)
@@ -452,12 +462,192 @@ int verify_check_batch(int32_t num_seqs, int32_t total_q, int32_t max_q_len,
                        int32_t max_seq_len, const int32_t *seq_lens,
                        const int32_t *block_tables, int32_t *counts, hipStream_t stream);
 
+/*
+ * Rotary positions.  Dims f and f + R/2 of a head (interleaved: 2f and 2f + 1) are
+ * a pair (a, b) for each frequency f < R/2, R = rotary_dim.  With the angle
+ * x = positions[axis[f]][row] * inv_freq[f] the pair becomes
+ *     (scale (a cos x - b sin x), scale (a sin x + b cos x));
+ * dims R .. D-1 stay as they are.  One axis is the usual rotary embedding; text,
+ * images and video place a token on a time, a height and a width axis, each of
+ * which turns some of the frequencies.  The angle's turns are taken in binary64
+ * (a position of 10^6 in fp32 leaves a few hundredths of a radian), the rotation
+ * in fp32.
+ */
+#define VERIFY_ROTARY_MAX_AXES 4
+typedef struct verify_rotary_params {
+    int32_t head_dim;    /* D: 64 or 128                                        */
+    int32_t rotary_dim;  /* R: even, 2 <= R <= D                                */
+    int32_t num_axes;    /* 1 .. VERIFY_ROTARY_MAX_AXES                         */
+    int32_t interleaved; /* 0: a pair is (f, f + R/2); 1: (2f, 2f + 1)          */
+    float scale;         /* factor of the rotated pairs; 0 selects 1            */
+    int32_t dtype;       /* verify_dtype of q, k and v                          */
+    uint8_t axis[64];    /* axis[f] < num_axes for f < R/2; the rest is not read */
+} verify_rotary_params;
+
+/*
+ * verify_rotary -- the queries and keys of all packed rows, rotated.
+ *
+ *   q           row r's head h at q + r * q_stride + h * D (elements): a row
+ *               stride of num_q_heads * D, or that of a wider row (a projection
+ *               that holds q, k and v side by side)
+ *   k           likewise with num_kv_heads and k_stride; NULL with num_kv_heads 0
+ *   positions   [num_axes][total_q] int32 (any values)
+ *   inv_freq    [R/2] double, radians per position
+ *   q_out, k_out  written with strides q_out_stride and k_out_stride; may be q and
+ *               k themselves (with the same strides) and must not overlap them
+ *               otherwise
+ * No workspace.  VERIFY_EINVAL for strides below heads * D, an axis out of range, a
+ * scale that is negative or not finite.
+ */
+int verify_rotary(const verify_rotary_params *params, int32_t total_q, int32_t num_q_heads,
+                  int32_t num_kv_heads, const void *q, int64_t q_stride, const void *k,
+                  int64_t k_stride, const int32_t *positions, const double *inv_freq, void *q_out,
+                  int64_t q_out_stride, void *k_out, int64_t k_out_stride, hipStream_t stream);
+
+/*
+ * verify_rotary_append -- verify_rotary with the rotated keys, and the values,
+ * written into the paged cache in the same launch: bit for bit what verify_rotary
+ * followed by verify_kv_append writes.
+ *
+ *   attn        the layer's shape and cache, as for verify_kv_append (head_dim and
+ *               dtype equal to params')
+ *   v_new       the new tokens' values, with row stride v_stride
+ *   block_tables, seq_lens, q_start, k_cache, v_cache  as for verify_kv_append:
+ *               row j of request i goes to position S_i - n_i + j, rows with a
+ *               negative position or an unmapped block are not stored.  q_start
+ *               describes total_q rows; rows outside it are not stored.
+ *   k_cache     16-byte aligned (VERIFY_EINVAL otherwise)
+ * All other arguments as for verify_rotary.  No workspace.
+ */
+int verify_rotary_append(const verify_attn_params *attn, const verify_rotary_params *params,
+                         int32_t total_q, const void *q, int64_t q_stride, const void *k_new,
+                         int64_t k_stride, const void *v_new, int64_t v_stride,
+                         const int32_t *positions, const double *inv_freq,
+                         const int32_t *block_tables, const int32_t *seq_lens,
+                         const int32_t *q_start, void *q_out, int64_t q_out_stride, void *k_cache,
+                         void *v_cache, hipStream_t stream);
+
+/*
+ * A bounded cache.  Beside k_cache and v_cache a layer keeps, for every slot and KV
+ * head, the attention weight its key has gathered and the ordinal of its token:
+ *     key_weights [num_blocks][Hkv][16] float
+ *     key_order   [num_blocks][Hkv][16] int32
+ * After each step verify_key_weights adds the step's weights; where a request
+ * exceeds its bound, verify_evict_plan chooses the keys to keep (each KV head its
+ * own) and verify_kv_compact moves them to the request's first slots, whose number
+ * is then its S_i.  The blocks behind them are free.
+ *
+ * From then on a key's slot says nothing of its token's position: keys are stored
+ * rotated (verify_rotary_append takes the positions), and the window of a
+ * sliding-window layer, which is counted in slots, has no meaning.  These calls
+ * refuse params with sliding_window > 0 (VERIFY_EUNSUPPORTED); such a layer's cache
+ * is bounded by its window.
+ * No block may belong to two requests, or twice to one: all three calls write per
+ * block.
+ */
+
+/*
+ * verify_key_weights -- adds the attention weights of the step's rows to the cached
+ * keys' sums.
+ *
+ * Request i counts its rows j < c_i, c_i = min(num_rows[i], n_i) (NULL: all n_i):
+ * after an acceptance num_emitted is the number of rows whose tokens stand, and the
+ * rows of rejected drafts leave no trace.  For KV head g and key t < S_i, with
+ * p = S_i - n_i + j the position of row j and G = Hq / Hkv,
+ *     w[t] = sum_{j < c_i, p >= t} sum_{h = gG}^{gG+G-1} softmax_t'(scale <q[j][h], K_g[t']>)[t],
+ * the softmax over the keys t' <= p and, with sinks, the head's sink logit (as in
+ * verify_attention).  Then
+ *     old keys, t < S_i - n_i:  key_weights = decay * key_weights + w[t]
+ *                               (decay 0: = w[t], the sum is not read)
+ *     new keys:                 key_weights = w[t], key_order = N_i - S_i + t,
+ * N_i = num_tokens[i], the request's tokens so far with the n_i new ones (NULL: S_i,
+ * a cache that has lost no key).  Keys of unmapped blocks take no part and nothing
+ * of theirs is written; slots from S_i on are left as they are.  Sums are taken in a
+ * fixed order (the same call gives the same bits).
+ *
+ *   q, k_cache, block_tables, seq_lens, q_start, sinks   as for verify_attention,
+ *                after the new keys were appended; k_cache 16-byte aligned
+ *                (VERIFY_EINVAL otherwise)
+ *   max_q_len, max_seq_len   host bounds of n_i and S_i (S_i is clamped to
+ *                max_seq_len and to 16 * max_blocks_per_seq; n_i may exceed
+ *                max_q_len, which only sizes the launch)
+ *   decay        finite, >= 0
+ *   workspace    at least verify_key_weights_workspace_size() bytes for the same
+ *                arguments, or for those of a batch of more requests and rows with
+ *                the same other arguments; its contents on entry are ignored
+ */
+int verify_key_weights_workspace_size(const verify_attn_params *params, int32_t total_q,
+                                      int32_t max_q_len, int32_t max_seq_len, size_t *bytes);
+
+int verify_key_weights(const verify_attn_params *params, int32_t total_q, int32_t max_q_len,
+                       int32_t max_seq_len, const void *q, const void *k_cache,
+                       const int32_t *block_tables, const int32_t *seq_lens,
+                       const int32_t *q_start, const int32_t *num_rows, const int32_t *num_tokens,
+                       const float *sinks, float decay, float *key_weights, int32_t *key_order,
+                       void *workspace, size_t workspace_bytes, hipStream_t stream);
+
+/*
+ * verify_evict_plan -- the keys to keep of requests that hold more than max_keys.
+ *
+ * c_i = min(S_i, max_keys) keys stay for every KV head.  Always kept are the tokens
+ * of ordinal < keep_first and those of ordinal >= N_i - keep_recent; then the keys
+ * of the largest key_weights (a NaN above all, -0 equal to +0), the lower slot first
+ * among equals.  A kept key in a slot < c_i stays there; the others, in ascending
+ * order, take the slots < c_i that fall free, in ascending order.  The plan is for
+ * one layer's cache; it changes nothing.
+ *
+ *   params       num_seqs, num_kv_heads, block_size, max_blocks_per_seq, num_blocks
+ *                (head_dim, dtype and the others are validated, not used)
+ *   max_keys     >= 1, keep_first >= 0, keep_recent >= 0, keep_first + keep_recent
+ *                <= max_keys (VERIFY_EINVAL otherwise)
+ *   max_seq_len  host bound of S_i (clamped to it and to 16 * max_blocks_per_seq)
+ *   key_order    or NULL: the slot is the ordinal (a cache that has lost no key)
+ *   num_tokens   [num_seqs] int32 N_i, or NULL: S_i
+ *   source       [num_seqs][Hkv][max_keys] int32: source[i][g][d] = the slot whose
+ *                key slot d is to hold, d itself if it stays; -1 for d >= c_i
+ *   new_lens     [num_seqs] int32: c_i
+ * A slot of an unmapped block counts as kept below c_i and as evicted above: no key
+ * is moved out of one or into one.  If more keys are always kept than max_keys (by
+ * ordinals that are no ordinals), the lower slots of them stay.
+ *   workspace    at least verify_evict_plan_workspace_size() bytes (may be NULL if
+ *                that is 0); its contents on entry are ignored
+ */
+int verify_evict_plan_workspace_size(const verify_attn_params *params, int32_t max_seq_len,
+                                     int32_t max_keys, size_t *bytes);
+
+int verify_evict_plan(const verify_attn_params *params, int32_t max_seq_len, int32_t max_keys,
+                      int32_t keep_first, int32_t keep_recent, const float *key_weights,
+                      const int32_t *key_order, const int32_t *block_tables,
+                      const int32_t *seq_lens, const int32_t *num_tokens, int32_t *source,
+                      int32_t *new_lens, void *workspace, size_t workspace_bytes,
+                      hipStream_t stream);
+
+/*
+ * verify_kv_compact -- moves the kept keys, in place: for every request i, KV head g
+ * and slot d < min(new_lens[i], max_keys) with s = source[i][g][d] != d, the key, the
+ * value, the weight and the ordinal of slot s are copied to slot d.
+ *
+ *   source, new_lens, max_keys   as verify_evict_plan leaves them, or a plan of the
+ *                caller's own in which every slot that is moved from is not moved to
+ *                (moves run at the same time)
+ *   k_cache, v_cache   in params' dtype; k_cache and v_cache 16-byte aligned
+ *                (VERIFY_EINVAL otherwise).  Element bits are copied unchanged.
+ *   key_weights, key_order   moved likewise; each may be NULL
+ * Slots s outside [0, 16 * max_blocks_per_seq) and slots of unmapped blocks are
+ * skipped.  No workspace.
+ */
+int verify_kv_compact(const verify_attn_params *params, int32_t max_keys,
+                      const int32_t *block_tables, const int32_t *source,
+                      const int32_t *new_lens, void *k_cache, void *v_cache, float *key_weights,
+                      int32_t *key_order, hipStream_t stream);
+
 /* Static, human-readable name of a status code. */
 const char *verify_status_string(int status);
 
 /* Library ABI version (major * 10000 + minor * 100 + patch): 1.9.0.  Since 1.9.0
  * verify_attention_plan reports whole pairs (-1), and the size that
- * verify_attention_workspace_size returns covers batches of fewer requests. */
+ * verify_attention_workspace_size returns covers batches of fewer requests.  The
+ * rotary and bounded-cache calls were added to it without a change to any other. */
 int verify_abi_version(void);
 
 #ifdef __cplusplus

@@ -14,6 +14,13 @@ If the library is missing, every entry point raises -- there is no fallback.
     check_batch(...)           the batch descriptor's preconditions, checked on
                                the device (the calls above take ``check=True``,
                                or every call does with AGENTSPEC_VERIFY_CHECK=1)
+    verify_rotary(...), verify_rotary_append(...)
+                               queries and keys rotated to positions on one or
+                               several axes, alone or with the append
+    verify_key_weights(...), verify_evict_plan(...), verify_kv_compact(...)
+                               a bound on a request's cached keys: the attention
+                               weight each has gathered, the keys to keep, their
+                               moves
 """
 from __future__ import annotations
 
@@ -28,7 +35,9 @@ __all__ = ["verify_attention", "verify_accept", "verify_accept_noalloc", "verify
            "verify_budget", "verify_kv_append", "verify_attention_append",
            "attention_workspace_size", "attention_plan",
            "accept_workspace_size",
-           "lmhead_accept_workspace_size", "check_batch", "BatchError", "VerifyError", "library",
+           "lmhead_accept_workspace_size", "verify_rotary", "verify_rotary_append",
+           "verify_key_weights", "verify_evict_plan", "verify_kv_compact",
+           "key_weights_workspace_size", "evict_plan_workspace_size", "check_batch", "BatchError", "VerifyError", "library",
            "abi_version", "F32", "BF16"]
 
 OK, EINVAL, EUNSUPPORTED, EWORKSPACE, EHIP = 0, -1, -2, -3, -4
@@ -38,6 +47,7 @@ F32, BF16 = 0, 1
 # then the first offending request (VERIFY_CHECK_FIRST)
 CHECK_KINDS = ("rows", "q_len", "short_seq", "long_seq", "block_id")
 CHECK_COUNTS = 6
+ROTARY_MAX_AXES = 4  # VERIFY_ROTARY_MAX_AXES
 CHECK_BY_DEFAULT = os.environ.get("AGENTSPEC_VERIFY_CHECK", "0") == "1"
 
 
@@ -71,6 +81,18 @@ class AttnParams(ctypes.Structure):
         ("scale", ctypes.c_float),
         ("dtype", ctypes.c_int32),
         ("kv_split_blocks", ctypes.c_int32),
+    ]
+
+
+class RotaryParams(ctypes.Structure):
+    _fields_ = [
+        ("head_dim", ctypes.c_int32),
+        ("rotary_dim", ctypes.c_int32),
+        ("num_axes", ctypes.c_int32),
+        ("interleaved", ctypes.c_int32),
+        ("scale", ctypes.c_float),
+        ("dtype", ctypes.c_int32),
+        ("axis", ctypes.c_uint8 * 64),
     ]
 
 
@@ -120,6 +142,22 @@ def library(path: Optional[str] = None):
     lib.verify_budget.restype = ctypes.c_int
     lib.verify_check_batch.argtypes = [i32, i32, i32, vp, P, i32, vp, vp, vp, vp]
     lib.verify_check_batch.restype = ctypes.c_int
+    RP, f32 = ctypes.POINTER(RotaryParams), ctypes.c_float
+    lib.verify_rotary.argtypes = [RP, i32, i32, i32, vp, i64, vp, i64, vp, vp, vp, i64, vp, i64, vp]
+    lib.verify_rotary.restype = ctypes.c_int
+    lib.verify_rotary_append.argtypes = [P, RP, i32, vp, i64, vp, i64, vp, i64, vp, vp, vp, vp, vp, vp, i64, vp,
+                                         vp, vp]
+    lib.verify_rotary_append.restype = ctypes.c_int
+    lib.verify_key_weights_workspace_size.argtypes = [P, i32, i32, i32, ctypes.POINTER(sz)]
+    lib.verify_key_weights_workspace_size.restype = ctypes.c_int
+    lib.verify_key_weights.argtypes = [P, i32, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp, f32, vp, vp, vp, sz, vp]
+    lib.verify_key_weights.restype = ctypes.c_int
+    lib.verify_evict_plan_workspace_size.argtypes = [P, i32, i32, ctypes.POINTER(sz)]
+    lib.verify_evict_plan_workspace_size.restype = ctypes.c_int
+    lib.verify_evict_plan.argtypes = [P, i32, i32, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.verify_evict_plan.restype = ctypes.c_int
+    lib.verify_kv_compact.argtypes = [P, i32, vp, vp, vp, vp, vp, vp, vp, vp]
+    lib.verify_kv_compact.restype = ctypes.c_int
     lib.verify_status_string.argtypes = [ctypes.c_int]
     lib.verify_status_string.restype = ctypes.c_char_p
     lib.verify_abi_version.argtypes = []
@@ -662,3 +700,296 @@ def verify_kv_append(k_new, v_new, k_cache, v_cache, block_tables, seq_lens, q_s
         _dev_ptr(k_new, "k_new")
     rc = library().verify_kv_append(ctypes.byref(params), T, p_k, p_v, *desc, p_kc, p_vc, _stream_ptr(stream, dev))
     _check(rc, "verify_kv_append")
+
+
+def _scratch(shape, dtype, dev, stream):
+    """A tensor that a call on `stream` (None: the current one) uses: memory freed
+    before the call is done is not handed to the current stream meanwhile."""
+    import torch
+    t = torch.empty(shape, dtype=dtype, device=dev)
+    if stream is not None and t.is_cuda:
+        t.record_stream(stream)
+    return t
+
+
+def _launch(where, idx, *args):
+    """The library's call `where` with the tensors' device current, as a launch on
+    one of its streams needs."""
+    import torch
+    call = getattr(library(), where)
+    if torch.cuda.current_device() == idx:
+        rc = call(*args)
+    else:
+        with torch.cuda.device(idx):
+            rc = call(*args)
+    _check(rc, where)
+
+
+def _rows_arg(t, name, heads, D, dtype, idx, device, T=None):
+    """Address and row stride of packed rows [T, heads, D]: contiguous, or a slice
+    of wider rows (heads and dims adjacent, any row stride that holds them)."""
+    shape = (t.shape[0] if T is None else T, heads, D)
+    if t.is_contiguous():
+        return _arg(t, name, shape, dtype, idx, device), heads * D
+    _expect(t, name, shape, dtype, device)
+    st, row = t.stride(), t.stride(0) if shape[0] > 1 else heads * D
+    if (D > 1 and st[2] != 1) or (heads > 1 and st[1] != D) or row < heads * D:
+        raise ValueError("%s must be rows of %d x %d adjacent elements, got strides %s" % (name, heads, D, tuple(st)))
+    return t.data_ptr(), row
+
+
+_rotary_params = {}
+
+
+def _rotary_args(q, positions, inv_freq, axes, interleaved, scale, idx, dev):
+    """RotaryParams of a call, and the addresses of positions and inv_freq."""
+    import torch
+    T, _, D = q.shape
+    if inv_freq.dim() != 1:
+        raise ValueError("inv_freq must be [rotary_dim / 2], got %s" % (tuple(inv_freq.shape),))
+    F = inv_freq.shape[0]
+    num_axes = 1 if positions.dim() == 1 else positions.shape[0]
+    axes = (0,) * F if axes is None and num_axes == 1 else axes
+    if axes is None or len(axes) != F:
+        raise ValueError("axes must name the axis of each of the %d frequencies" % F)
+    p_pos = _arg(positions, "positions", (T,) if positions.dim() == 1 else (num_axes, T), torch.int32, idx, dev)
+    p_freq = _arg(inv_freq, "inv_freq", None, torch.float64, idx, dev)
+    key = (D, num_axes, bool(interleaved), float(scale), q.dtype, tuple(axes))
+    params = _rotary_params.get(key)
+    if params is None:
+        if not (2 <= 2 * F <= D and all(0 <= int(x) < num_axes for x in axes)):
+            raise ValueError("rotary_dim %d of head dim %d, axes %s of %d" % (2 * F, D, sorted(set(axes)), num_axes))
+        params = RotaryParams(D, 2 * F, num_axes, int(bool(interleaved)), float(scale), _dtype_code(q))
+        for f, x in enumerate(axes):
+            if f < len(params.axis):
+                params.axis[f] = int(x)
+        if len(_rotary_params) > 64:
+            _rotary_params.clear()
+        _rotary_params[key] = params
+    return params, p_pos, p_freq
+
+
+def verify_rotary(q, k, positions, inv_freq, *, axes=None, interleaved: bool = False, scale: float = 0.0,
+                  q_out=None, k_out=None, stream=None):
+    """Queries and keys rotated to their rows' positions.
+
+    q [T, Hq, D] and k [T, Hkv, D] or None (bf16 or fp32, D 64 or 128), contiguous
+    or slices of wider rows; positions [A, T] (or [T]) int32; inv_freq [R / 2]
+    float64, radians per position; axes: the axis (0 .. A-1) of each of the R / 2
+    frequencies, needed with more than one.  A pair is dims (f, f + R / 2), or
+    (2f, 2f + 1) if interleaved; dims from R on are copied.  scale: a factor of the
+    rotated dims (0: 1).  q_out and k_out may be q and k.  Returns (q_out, k_out)."""
+    import torch
+    if q.dim() != 3 or k is not None and k.dim() != 3:
+        raise ValueError("q must be [T, Hq, D] and k [T, Hkv, D]")
+    T, Hq, D = q.shape
+    dtype, dev = q.dtype, q.device
+    idx = dev.index if dev.type == "cuda" else -1
+    Hkv = 0 if k is None else k.shape[1]
+    p_q, s_q = _rows_arg(q, "q", Hq, D, dtype, idx, dev)
+    p_k, s_k = (None, 0) if k is None else _rows_arg(k, "k", Hkv, D, dtype, idx, dev, T)
+    params, p_pos, p_freq = _rotary_args(q, positions, inv_freq, axes, interleaved, scale, idx, dev)
+    if q_out is None:
+        q_out = _scratch((T, Hq, D), dtype, dev, stream)
+    if k_out is None and k is not None:
+        k_out = _scratch((T, Hkv, D), dtype, dev, stream)
+    p_qo, s_qo = _rows_arg(q_out, "q_out", Hq, D, dtype, idx, dev, T)
+    p_ko, s_ko = (None, 0) if k is None else _rows_arg(k_out, "k_out", Hkv, D, dtype, idx, dev, T)
+    if idx < 0:
+        _dev_ptr(q, "q")
+    _launch("verify_rotary", idx, ctypes.byref(params), T, Hq, Hkv, p_q, s_q, p_k, s_k, p_pos, p_freq, p_qo, s_qo,
+            p_ko, s_ko, _stream_ptr(stream, dev))
+    return q_out, k_out
+
+
+def verify_rotary_append(q, k_new, v_new, positions, inv_freq, k_cache, v_cache, block_tables, seq_lens, q_start, *,
+                         axes=None, interleaved: bool = False, scale: float = 0.0, q_out=None, stream=None,
+                         check=None):
+    """verify_rotary with the rotated keys and the values written into their
+    paged-cache slots in the same launch (as verify_kv_append writes them).  q [T,
+    Hq, D], k_new and v_new [T, Hkv, D], contiguous or slices of wider rows.  check:
+    as for verify_kv_append.  Returns q_out."""
+    import torch
+    if q.dim() != 3 or k_new.dim() != 3 or v_new.dim() != 3:
+        raise ValueError("q must be [T, Hq, D], k_new and v_new [T, Hkv, D]")
+    T, Hq, D = q.shape
+    dtype, dev = q.dtype, q.device
+    idx = dev.index if dev.type == "cuda" else -1
+    p_q, s_q = _rows_arg(q, "q", Hq, D, dtype, idx, dev)
+    (p_kc, p_vc, *desc), attn = _layer_args(Hq, D, dtype, q.element_size(), idx, dev, k_cache, v_cache, block_tables,
+                                            seq_lens, q_start)
+    Hkv = k_cache.shape[1]
+    p_k, s_k = _rows_arg(k_new, "k_new", Hkv, D, dtype, idx, dev, T)
+    p_v, s_v = _rows_arg(v_new, "v_new", Hkv, D, dtype, idx, dev, T)
+    params, p_pos, p_freq = _rotary_args(q, positions, inv_freq, axes, interleaved, scale, idx, dev)
+    if check or check is None and CHECK_BY_DEFAULT:
+        _checked(check, "verify_rotary_append", q_start=q_start, total_q=T, seq_lens=seq_lens,
+                 block_tables=block_tables, num_blocks=k_cache.shape[0],
+                 max_seq_len=16 * block_tables.shape[1], sliding_window=1, stream=stream)
+    if q_out is None:
+        q_out = _scratch((T, Hq, D), dtype, dev, stream)
+    p_qo, s_qo = _rows_arg(q_out, "q_out", Hq, D, dtype, idx, dev, T)
+    if idx < 0:
+        _dev_ptr(q, "q")
+    _launch("verify_rotary_append", idx, ctypes.byref(attn), ctypes.byref(params), T, p_q, s_q, p_k, s_k, p_v, s_v,
+            p_pos, p_freq, *desc, p_qo, s_qo, p_kc, p_vc, _stream_ptr(stream, dev))
+    return q_out
+
+
+def key_weights_workspace_size(q, k_cache, block_tables, *, max_q_len: int, max_seq_len: int) -> int:
+    params = _attn_params(q, k_cache, block_tables, 0, 0.0, 0)
+    n = ctypes.c_size_t(0)
+    _check(library().verify_key_weights_workspace_size(ctypes.byref(params), q.shape[0], int(max_q_len),
+                                                       int(max_seq_len), ctypes.byref(n)),
+           "verify_key_weights_workspace_size")
+    return int(n.value)
+
+
+def verify_key_weights(q, k_cache, key_weights, key_order, block_tables, seq_lens, q_start, *, max_q_len: int,
+                       max_seq_len: int, num_rows=None, num_tokens=None, sinks=None, scale: float = 0.0,
+                       decay: float = 1.0, workspace=None, stream=None, check=None):
+    """Adds the attention weights of the step's rows to the cached keys' sums.
+
+    key_weights [num_blocks, Hkv, 16] float32 and key_order [num_blocks, Hkv, 16]
+    int32 are updated in place: a key held before the step gets decay * its sum plus
+    its weight in the rows' softmaxes (summed over the rows and the query heads of
+    its KV head), a new one that weight and the ordinal of its token.  num_rows [B]:
+    only the first num_rows[i] rows of request i count (after an acceptance,
+    num_emitted).  num_tokens [B]: the request's tokens so far with the new ones
+    (None: seq_lens).  Other arguments as for verify_attention, after the append.
+    Returns key_weights."""
+    import torch
+    if q.dim() != 3:
+        raise ValueError("q must be [T, Hq, D], got %s" % (tuple(q.shape),))
+    T, Hq, D = q.shape
+    dtype, dev = q.dtype, q.device
+    idx = dev.index if dev.type == "cuda" else -1
+    p_q = _arg(q, "q", None, dtype, idx, dev)
+    p_kc, params = _key_cache_arg(k_cache, Hq, D, dtype, q.element_size(), idx, dev)
+    nb, hkv = k_cache.shape[0], k_cache.shape[1]
+    p_bt, p_sl, B = _table_args(params, block_tables, seq_lens, idx, dev)
+    p_qs = _arg(q_start, "q_start", (B + 1,), torch.int32, idx, dev)
+    p_w, p_o = _key_state(key_weights, key_order, nb, hkv, idx, dev)
+    p_rows = None if num_rows is None else _arg(num_rows, "num_rows", (B,), torch.int32, idx, dev)
+    p_tok = None if num_tokens is None else _arg(num_tokens, "num_tokens", (B,), torch.int32, idx, dev)
+    p_sinks = None if sinks is None else _arg(sinks, "sinks", (Hq,), torch.float32, idx, dev)
+    p_ws, ws_have = _workspace_arg(workspace, idx, dev)
+    if check or check is None and CHECK_BY_DEFAULT:
+        _checked(check, "verify_key_weights", q_start=q_start, total_q=T, max_q_len=max_q_len, seq_lens=seq_lens,
+                 block_tables=block_tables, num_blocks=nb, max_seq_len=max_seq_len, stream=stream)
+    params.scale = float(scale)
+    if workspace is None:
+        ws_have = key_weights_workspace_size(q, k_cache, block_tables, max_q_len=max_q_len, max_seq_len=max_seq_len)
+        if ws_have > 0:
+            workspace = _scratch(ws_have, torch.uint8, dev, stream)
+            p_ws = workspace.data_ptr()
+    if idx < 0:
+        _dev_ptr(q, "q")
+    _launch("verify_key_weights", idx, ctypes.byref(params), T, int(max_q_len), int(max_seq_len), p_q, p_kc, p_bt,
+            p_sl, p_qs, p_rows, p_tok, p_sinks, float(decay), p_w, p_o, p_ws, ws_have, _stream_ptr(stream, dev))
+    return key_weights
+
+
+def _key_cache_arg(k_cache, Hq, D, dtype, esize, idx, dev):
+    """Address of a key cache, and its AttnParams (num_seqs and the table's width are
+    _table_args')."""
+    if k_cache.dim() != 5:
+        raise ValueError("k_cache must be [num_blocks, Hkv, D/x, 16, x], got %s" % (tuple(k_cache.shape),))
+    nb, hkv = k_cache.shape[0], k_cache.shape[1]
+    x = 16 // esize
+    p = _arg(k_cache, "k_cache", (nb, hkv, D // x, 16, x), dtype, idx, dev)
+    return p, AttnParams(0, Hq, hkv, D, 16, 0, nb, 0, 0.0, _dtype_code(k_cache), 0)
+
+
+def _table_args(params, block_tables, lens, idx, dev, name="seq_lens"):
+    """Addresses of block_tables and of the requests' lengths, and their number."""
+    import torch
+    if block_tables.dim() != 2:
+        raise ValueError("block_tables must be [B, max_blocks], got %s" % (tuple(block_tables.shape),))
+    B, params.max_blocks_per_seq = block_tables.shape
+    params.num_seqs = B
+    return (_arg(block_tables, "block_tables", None, torch.int32, idx, dev),
+            _arg(lens, name, (B,), torch.int32, idx, dev), B)
+
+
+def _key_state(key_weights, key_order, nb, hkv, idx, dev):
+    import torch
+    return (None if key_weights is None else _arg(key_weights, "key_weights", (nb, hkv, 16), torch.float32, idx, dev),
+            None if key_order is None else _arg(key_order, "key_order", (nb, hkv, 16), torch.int32, idx, dev))
+
+
+def evict_plan_workspace_size(num_seqs: int, num_kv_heads: int, max_blocks: int, *, max_seq_len: int,
+                              max_keys: int) -> int:
+    params = AttnParams(int(num_seqs), int(num_kv_heads), int(num_kv_heads), 128, 16, int(max_blocks), 0, 0, 0.0, BF16, 0)
+    n = ctypes.c_size_t(0)
+    _check(library().verify_evict_plan_workspace_size(ctypes.byref(params), int(max_seq_len), int(max_keys),
+                                                      ctypes.byref(n)), "verify_evict_plan_workspace_size")
+    return int(n.value)
+
+
+def verify_evict_plan(key_weights, key_order, block_tables, seq_lens, *, max_keys: int, keep_first: int = 0,
+                      keep_recent: int = 0, max_seq_len: int, num_tokens=None, source=None, new_lens=None,
+                      workspace=None, stream=None):
+    """The keys to keep of requests that hold more than max_keys: for every KV head
+    the tokens of the first keep_first and the last keep_recent ordinals, then the
+    keys of the largest key_weights (the lower slot among equals).
+
+    key_weights and key_order (None: the slot is the ordinal) as for
+    verify_key_weights; num_tokens [B] or None (seq_lens).  Returns (source [B, Hkv,
+    max_keys] int32: the slot whose key slot d is to hold, -1 from the request's new
+    length on; new_lens [B] int32: min(seq_lens, max_keys)).  Nothing is moved."""
+    import torch
+    i32 = torch.int32
+    if key_weights.dim() != 3:
+        raise ValueError("key_weights must be [num_blocks, Hkv, 16], got %s" % (tuple(key_weights.shape),))
+    dev = key_weights.device
+    idx = dev.index if dev.type == "cuda" else -1
+    nb, hkv = key_weights.shape[:2]
+    p_w, p_o = _key_state(key_weights, key_order, nb, hkv, idx, dev)
+    # the plan depends neither on the head dim nor on the storage type
+    params = AttnParams(0, hkv, hkv, 128, 16, 0, nb, 0, 0.0, BF16, 0)
+    p_bt, p_sl, B = _table_args(params, block_tables, seq_lens, idx, dev)
+    p_tok = None if num_tokens is None else _arg(num_tokens, "num_tokens", (B,), i32, idx, dev)
+    max_keys = int(max_keys)
+    if source is None:
+        source = _scratch((B, hkv, max(max_keys, 0)), i32, dev, stream)
+    if new_lens is None:
+        new_lens = _scratch((B,), i32, dev, stream)
+    p_src = _arg(source, "source", (B, hkv, max(max_keys, 0)), i32, idx, dev)
+    p_new = _arg(new_lens, "new_lens", (B,), i32, idx, dev)
+    p_ws, ws_have = _workspace_arg(workspace, idx, dev)
+    if workspace is None:
+        ws_have = evict_plan_workspace_size(B, hkv, block_tables.shape[1], max_seq_len=max_seq_len, max_keys=max_keys)
+        if ws_have > 0:
+            workspace = _scratch(ws_have, torch.uint8, dev, stream)
+            p_ws = workspace.data_ptr()
+    if idx < 0:
+        _dev_ptr(key_weights, "key_weights")
+    _launch("verify_evict_plan", idx, ctypes.byref(params), int(max_seq_len), max_keys, int(keep_first),
+            int(keep_recent), p_w, p_o, p_bt, p_sl, p_tok, p_src, p_new, p_ws, ws_have, _stream_ptr(stream, dev))
+    return source, new_lens
+
+
+def verify_kv_compact(k_cache, v_cache, block_tables, source, new_lens, *, key_weights=None, key_order=None,
+                      stream=None):
+    """Moves the kept keys, in place: slot d of every request and KV head receives
+    the key, value (and weight and ordinal) of slot source[i, g, d] for d <
+    new_lens[i].  source and new_lens as verify_evict_plan returns them, or a plan of
+    the caller's own in which no slot that is moved from is moved to."""
+    import torch
+    i32 = torch.int32
+    if k_cache.dim() != 5 or source.dim() != 3:
+        raise ValueError("k_cache must be [num_blocks, Hkv, D/x, 16, x] and source [B, Hkv, max_keys]")
+    dtype, dev = k_cache.dtype, k_cache.device
+    idx = dev.index if dev.type == "cuda" else -1
+    nb, hkv = k_cache.shape[:2]
+    D = k_cache.shape[2] * k_cache.shape[4]
+    p_kc, params = _key_cache_arg(k_cache, hkv, D, dtype, k_cache.element_size(), idx, dev)
+    p_vc = _arg(v_cache, "v_cache", (nb, hkv, D, 16), dtype, idx, dev)
+    p_bt, p_new, B = _table_args(params, block_tables, new_lens, idx, dev, "new_lens")
+    p_src = _arg(source, "source", (B, hkv, source.shape[2]), i32, idx, dev)
+    p_w, p_o = _key_state(key_weights, key_order, nb, hkv, idx, dev)
+    if idx < 0:
+        _dev_ptr(k_cache, "k_cache")
+    _launch("verify_kv_compact", idx, ctypes.byref(params), source.shape[2], p_bt, p_src, p_new, p_kc, p_vc, p_w,
+            p_o, _stream_ptr(stream, dev))

@@ -5,6 +5,7 @@
 #include <stdint.h>
 
 #include <algorithm>
+#include <atomic>
 
 #include "agentspec_verify.h"
 
@@ -184,6 +185,36 @@ int launch_accept_scan(int num_seqs, const int32_t* q_start, const int32_t* toke
 
 inline int check_launch() {
     return hipGetLastError() == hipSuccess ? VERIFY_OK : VERIFY_EHIP;
+}
+
+// The checks of a layer's params that every call taking them makes.
+inline int validate(const verify_attn_params* p, int32_t total_q, int32_t max_q_len, int32_t max_seq_len) {
+    if (!p) return VERIFY_EINVAL;
+    if (p->dtype != VERIFY_F32 && p->dtype != VERIFY_BF16) return VERIFY_EUNSUPPORTED;
+    if (p->head_dim != 64 && p->head_dim != 128) return VERIFY_EUNSUPPORTED;
+    if (p->block_size != kBlockTokens) return VERIFY_EUNSUPPORTED;
+    if (p->num_seqs < 0 || p->num_q_heads <= 0 || p->num_kv_heads <= 0) return VERIFY_EINVAL;
+    if (p->num_q_heads % p->num_kv_heads != 0) return VERIFY_EINVAL;
+    if (p->max_blocks_per_seq <= 0 || p->num_blocks < 0 || p->sliding_window < 0) return VERIFY_EINVAL;
+    if (p->kv_split_blocks < 0 || !(p->scale >= 0.f) || p->scale > 3.0e38f) return VERIFY_EINVAL;
+    if (total_q < 0 || max_q_len < 0 || max_seq_len < 0) return VERIFY_EINVAL;
+    if (p->num_seqs > 65535) return VERIFY_EUNSUPPORTED;
+    return VERIFY_OK;
+}
+
+// Compute units of the current device (cached per device; 256 when none is visible).
+inline int device_cus() {
+    static std::atomic<int> cache[64];
+    int dev = 0;
+    if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 64) { (void)hipGetLastError(); return 256; }
+    int v = cache[dev].load(std::memory_order_relaxed);
+    if (v > 0) return v;
+    if (hipDeviceGetAttribute(&v, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || v <= 0) {
+        (void)hipGetLastError();
+        v = 256;
+    }
+    cache[dev].store(v, std::memory_order_relaxed);
+    return v;
 }
 
 inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
