@@ -6,12 +6,16 @@
 // r runs over the (row, head of the group) pairs of a (request, KV head), m_r is about
 // the row's maximum.  A key's weight needs every row's l_r, so the keys are read
 // twice, in two launches:
-//   weight_stats  rows stay, keys stream past: each lane keeps a running maximum and
-//                 sum per row over the keys of its own columns, joined at the end of
-//                 a split of the keys into one (maximum, sum) per row and split;
-//   weight_sums   keys stay in registers, rows stream past from LDS: a key's weights
-//                 are added up within its lane; the splits' sums are joined into m_r
-//                 and 1 / l_r as the rows are staged.
+//   weight_stats  each lane keeps a running maximum and sum per row over the keys of
+//                 its own columns, joined at the end of a split of the keys into one
+//                 (maximum, sum) per row and split;
+//   weight_sums   a key's weights are added up within its lane; the splits' parts are
+//                 joined into m_r and 1 / l_r as the rows are staged in LDS.
+// In both the rows stay and the keys stream past, the next step's loads in flight.
+// With more rows than LDS holds the second becomes
+//   weight_join, weight_sums_rows   the parts joined once, then the keys stay in
+//                 registers and the rows stream past (a prompt's rows are read once
+//                 per 64 keys, which the second level cache answers).
 // (A row's logarithm log2 l_r + m_r in the place of the two would be rounded at the
 // size of the scores, and every weight of the row with it.)
 // Scores are MFMA products, the queries the first operand and 16 keys the second, so
@@ -26,9 +30,10 @@ namespace {
 
 constexpr int kWgtWaves = 4;
 constexpr int kWgtThreads = kWgtWaves * kWave;
+constexpr int kRowWaves = 8;   // of a weight_sums_rows workgroup
 constexpr float kWgtLog2e = 1.4426950408889634f;
 // 16-row tiles of a weight_stats workgroup at most
-constexpr int stat_tiles(bool bf16) { return bf16 ? 8 : 4; }
+constexpr int kStatTiles = 4;
 
 typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
@@ -47,14 +52,20 @@ struct WgtArgs {
     const float* sinks;
     float* key_weights;
     int32_t* key_order;
-    float2* part;  // [total_q][Hq][splits] (maximum, sum relative to it) of each split
+    float2* part;  // (maximum, sum relative to it) of each row and split, see part_of
     int num_seqs, total_q, hq, hkv, group, max_blocks, num_blocks, max_seq_len;
     float scale_log2, decay;
+    uint32_t group_magic;        // ceil(2^32 / group)
     int splits, split_blocks;    // of weight_stats
     int chunks;                  // row chunks in its grid
     int sum_blocks;              // blocks of a weight_sums workgroup
     int lds_tiles;               // row tiles that weight_sums holds in LDS
 };
+
+// r / group: exact below 2^32 / group, far above any number of rows.
+__device__ __forceinline__ int by_group(const WgtArgs& a, int r) {
+    return a.group == 1 ? r : (int)__umulhi((uint32_t)r, a.group_magic);
+}
 
 struct WgtGeom {
     int q0, n, S, rows, blocks;  // rows: counted rows times the group
@@ -69,6 +80,11 @@ __device__ __forceinline__ WgtGeom wgt_geom(const WgtArgs& a, int i) {
     g.rows = counted * a.group;
     g.blocks = (g.S + kBlockTokens - 1) / kBlockTokens;
     return g;
+}
+
+// The parts of row r of KV head g: [request][KV head][row][splits].
+__device__ __forceinline__ float2* part_of(const WgtArgs& a, const WgtGeom& geo, int g, int r) {
+    return a.part + ((int64_t)geo.q0 * a.hq + (int64_t)g * geo.rows + r) * a.splits;
 }
 
 // Operands of 16 rows or keys over the head dim: NC 16-byte chunks per lane, chunk c
@@ -114,14 +130,14 @@ __device__ __forceinline__ void stage_rows(const WgtArgs& a, const WgtGeom& geo,
         const int lane = e % kWave, c = e / kWave % NC, tile = e / kWave / NC;
         int r = first + tile * 16 + lane % 16;
         if (r >= geo.rows) r = first;
-        const int j = r / a.group, h = r - j * a.group;
+        const int j = by_group(a, r), h = r - j * a.group;
         const T* src = static_cast<const T*>(a.q) + ((int64_t)(geo.q0 + j) * a.hq + g * a.group + h) * D +
                        (4 * c + lane / 16) * (16 / (int)sizeof(T));
         const u32x4u_t v = *reinterpret_cast<const u32x4u_t*>(src);
         lds[e] = make_uint4(v.x, v.y, v.z, v.w);
     }
     for (int t = threadIdx.x; t < tiles * 16; t += kWgtThreads)
-        pos[t] = first + t < geo.rows ? geo.S - geo.n + (first + t) / a.group : -1;
+        pos[t] = first + t < geo.rows ? geo.S - geo.n + by_group(a, first + t) : -1;
 }
 
 // K tile of block `phys`, KV head g.
@@ -133,12 +149,57 @@ __device__ __forceinline__ void load_keys(const WgtArgs& a, int g, int phys, Ope
     for (int c = 0; c < Operand<T, D>::NC; ++c) k.v[c] = src[c * kWave];
 }
 
-// Blocks of a wavefront's step: 8 to 16 KiB of keys in flight.
-constexpr int step_blocks(int d, bool bf16) { return d == 128 && !bf16 ? 2 : 4; }
+// Blocks of a wavefront's step where keys stream past (two such steps are in
+// registers, 8 or 16 KiB of loads in flight), and where they stay.
+constexpr int step_blocks(int d, bool bf16) { return d == 128 && !bf16 ? 1 : 2; }
+constexpr int held_blocks(int d, bool bf16) { return d == 128 && !bf16 ? 2 : 4; }
 
 // Row slack: a row's sum is kept relative to a maximum that may be exceeded by this
 // many powers of two before the sum is rescaled (rarely, then).
 constexpr float kSlackLog2 = 8.f;
+// The maximum of no score: finite, so that it needs no case of its own (2^(-inf - m)
+// is 0, 2^(m - m) is 1, and any score exceeds it).
+constexpr float kNoScore = -3.0e38f;
+
+// The blocks of a wavefront, NB at a time and kWgtWaves * NB apart, their ids read 64
+// at a time (one per lane) and their K tiles a step ahead of their use.
+template <typename T, int D, int NB>
+struct Walk {
+    const WgtArgs& a;
+    const int32_t* table;
+    int g, b, b_hi;   // next blocks to load: [b, b + NB), below b_hi
+    int ids, at;      // ids of the wavefront's next blocks from lane `at` on
+
+    __device__ Walk(const WgtArgs& a, const int32_t* table, int g, int b, int b_hi)
+        : a(a), table(table), g(g), b(b), b_hi(b_hi), ids(-1), at(kWave) {}
+
+    // The blocks' bits in the result: valid ids.  `phys` receives the ids, and K tiles
+    // are loaded from those it then holds: the loads are the same in number whatever
+    // is valid, so that a wait for the step before need not wait for them.
+    __device__ __forceinline__ uint32_t load(Operand<T, D> (&k)[NB], int (&phys)[NB]) {
+        uint32_t ok = 0;
+        if (b < b_hi) {
+            if (at >= kWave) {
+                const int lane = threadIdx.x & (kWave - 1);
+                const int bl = b + lane / NB * (kWgtWaves * NB) + lane % NB;
+                ids = bl < b_hi ? table[bl] : -1;
+                at = 0;
+            }
+#pragma unroll
+            for (int x = 0; x < NB; ++x) {
+                const int id = __builtin_amdgcn_readlane(ids, at + x);
+                const bool valid = id >= 0 && id < a.num_blocks;
+                ok |= (uint32_t)valid << x;
+                phys[x] = valid ? id : 0;
+            }
+            at += NB;
+            b += kWgtWaves * NB;
+        }
+#pragma unroll
+        for (int x = 0; x < NB; ++x) load_keys<T, D>(a, g, phys[x], k[x]);
+        return ok;
+    }
+};
 
 // Grid (row chunks x KV heads x splits, requests).
 template <typename T, int D, int RT>
@@ -159,11 +220,8 @@ __global__ __launch_bounds__(kWgtThreads) void weight_stats(WgtArgs a) {
     const int p0 = geo.S - geo.n;  // position of row 0
     for (int first = chunk0 * (RT * 16); first < geo.rows; first += a.chunks * (RT * 16)) {
         const int tiles = min(RT, (geo.rows - first + 15) / 16);
-        __syncthreads();
-        stage_rows<T, D>(a, geo, g, first, tiles, s_q, s_pos);
-        __syncthreads();
-        const int p_first = p0 + first / a.group;
-        const int p_last = p0 + (min(first + RT * 16, geo.rows) - 1) / a.group;
+        const int p_first = p0 + by_group(a, first);
+        const int p_last = p0 + by_group(a, min(first + RT * 16, geo.rows) - 1);
         // blocks that a row of the chunk sees
         const int b_hi = min(min(b_lo + a.split_blocks, geo.blocks), p_last < 0 ? 0 : p_last / kBlockTokens + 1);
         float m[RT][4], l[RT][4];
@@ -171,17 +229,11 @@ __global__ __launch_bounds__(kWgtThreads) void weight_stats(WgtArgs a) {
         for (int r = 0; r < RT; ++r)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                m[r][e] = -INFINITY;
+                m[r][e] = kNoScore;
                 l[r][e] = 0.f;
             }
-        for (int b = b_lo + w * NB; b < b_hi; b += kWgtWaves * NB) {
-            const int id = lane < NB && b + lane < b_hi ? table[b + lane] : -1;
-            const bool valid = id >= 0 && id < a.num_blocks;
-            const uint32_t ok = (uint32_t)__ballot(valid);
-            if (ok == 0) continue;
-            Operand<T, D> k[NB];
-#pragma unroll
-            for (int x = 0; x < NB; ++x) load_keys<T, D>(a, g, __builtin_amdgcn_readlane(valid ? id : 0, x), k[x]);
+        auto compute = [&](const Operand<T, D> (&k)[NB], uint32_t ok, int b) {
+            if (ok == 0) return;
             const bool masked = ok != (1u << NB) - 1 || (b + NB) * kBlockTokens - 1 > p_first;
             // keeps the query operands in LDS: hoisted out of the loop they would take
             // D / 8 (bf16) or D / 4 registers per tile
@@ -205,22 +257,45 @@ __global__ __launch_bounds__(kWgtThreads) void weight_stats(WgtArgs a) {
                         for (int e = 0; e < 4; ++e) s[x][e] = t <= pos[e] ? s[x][e] : -INFINITY;
                     }
                 }
+                float top[4];
+                bool over = false;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    float top = s[0][e];
+                    top[e] = s[0][e];
 #pragma unroll
-                    for (int x = 1; x < NB; ++x) top = fmaxf(top, s[x][e]);
-                    top *= a.scale_log2;
-                    if (__any(top > m[r][e] + kSlackLog2)) {
-                        const float mn = fmaxf(m[r][e], top);
-                        l[r][e] *= m[r][e] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[r][e] - mn);
+                    for (int x = 1; x < NB; ++x) top[e] = fmaxf(top[e], s[x][e]);
+                    top[e] *= a.scale_log2;
+                    over |= top[e] > m[r][e] + kSlackLog2;
+                }
+                if (__any(over)) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float mn = fmaxf(m[r][e], top[e]);
+                        l[r][e] *= __builtin_amdgcn_exp2f(m[r][e] - mn);
                         m[r][e] = mn;
                     }
-                    const float ref = m[r][e] == -INFINITY ? 0.f : m[r][e];
-#pragma unroll
-                    for (int x = 0; x < NB; ++x) l[r][e] += __builtin_amdgcn_exp2f(fmaf(s[x][e], a.scale_log2, -ref));
                 }
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+#pragma unroll
+                    for (int x = 0; x < NB; ++x) l[r][e] += __builtin_amdgcn_exp2f(fmaf(s[x][e], a.scale_log2, -m[r][e]));
             }
+        };
+        Walk<T, D, NB> walk(a, table, g, b_lo + w * NB, b_hi);
+        Operand<T, D> k0[NB], k1[NB];
+        int phys[NB] = {}, b = walk.b;
+        uint32_t ok0 = walk.load(k0, phys), ok1;
+        __syncthreads();  // the chunk before is done with the rows
+        stage_rows<T, D>(a, geo, g, first, tiles, s_q, s_pos);
+        __syncthreads();
+        while (b < b_hi) {
+            ok1 = walk.load(k1, phys);
+            compute(k0, ok0, b);
+            b += kWgtWaves * NB;
+            if (b >= b_hi) break;
+            ok0 = walk.load(k0, phys);
+            compute(k1, ok1, b);
+            b += kWgtWaves * NB;
         }
         // join the 16 columns, then the wavefronts
 #pragma unroll
@@ -228,7 +303,7 @@ __global__ __launch_bounds__(kWgtThreads) void weight_stats(WgtArgs a) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const float M = wave_max_xor(m[r][e], 16);
-                const float L = wave_sum_xor(m[r][e] == -INFINITY ? l[r][e] : l[r][e] * __builtin_amdgcn_exp2f(m[r][e] - M), 16);
+                const float L = wave_sum_xor(l[r][e] * __builtin_amdgcn_exp2f(m[r][e] - M), 16);
                 if (l16 == 0) {
                     s_m[w][r * 16 + lg * 4 + e] = M;
                     s_l[w][r * 16 + lg * 4 + e] = L;
@@ -237,30 +312,80 @@ __global__ __launch_bounds__(kWgtThreads) void weight_stats(WgtArgs a) {
         __syncthreads();
         const int r = first + tid;
         if (tid < RT * 16 && r < geo.rows) {
-            float M = -INFINITY, L = 0.f;
+            float M = kNoScore, L = 0.f;
 #pragma unroll
             for (int x = 0; x < kWgtWaves; ++x) M = fmaxf(M, s_m[x][tid]);
 #pragma unroll
-            for (int x = 0; x < kWgtWaves; ++x)
-                L += s_m[x][tid] == -INFINITY ? s_l[x][tid] : s_l[x][tid] * __builtin_amdgcn_exp2f(s_m[x][tid] - M);
-            const int j = r / a.group, h = r - j * a.group;
-            a.part[((int64_t)(geo.q0 + j) * a.hq + g * a.group + h) * a.splits + split] = make_float2(M, L);
+            for (int x = 0; x < kWgtWaves; ++x) L += s_l[x][tid] * __builtin_amdgcn_exp2f(s_m[x][tid] - M);
+            part_of(a, geo, g, r)[split] = make_float2(M, L);
         }
     }
 }
 
-// Grid (KV heads x ranges of sum_blocks blocks, requests).  Where the request's
-// counted rows fit the LDS tiles they are staged once; otherwise every step of the
-// keys stages them in turn.
+// A row's (m, 1 / l) from its splits' parts, and its head's sink.  A row without a
+// key has (inf, 0), and so has a place without a row: 2^(s - inf) * 0.
+__device__ __forceinline__ float2 join_parts(const WgtArgs& a, const float2* part, int nsplit, int h) {
+    float M = kNoScore, L = 0.f;
+    for (int s = 0; s < nsplit; ++s) {
+        const float2 p = part[s];
+        const float mn = fmaxf(M, p.x);
+        L = L * __builtin_amdgcn_exp2f(M - mn) + p.y * __builtin_amdgcn_exp2f(p.x - mn);
+        M = mn;
+    }
+    if (M == kNoScore) return make_float2(L == 0.f ? INFINITY : L, 0.f);  // (or every score was NaN)
+    if (a.sinks) L += exp2f(a.sinks[h] * kWgtLog2e - M);
+    return make_float2(M, 1.f / L);
+}
+
+// Adds the weights of 16 rows to sum[x], key l16 of block b + x; `pos` are the four
+// rows' positions (-1: none), read where some row does not see some key.
 template <typename T, int D, int NB>
+__device__ __forceinline__ void add_tile(const WgtArgs& a, const uint4* qv, const Operand<T, D> (&k)[NB], const f32x4_t& m,
+                                         const f32x4_t& inv, bool masked, const i32x4_t& pos, int b, float (&sum)[NB]) {
+    const int l16 = threadIdx.x & 15;
+    if (masked) {
+#pragma unroll
+        for (int x = 0; x < NB; ++x) {
+            const f32x4_t s = product<D>(qv, k[x].v, T{});
+            const int t = (b + x) * kBlockTokens + l16;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float p = __builtin_amdgcn_exp2f(fmaf(s[e], a.scale_log2, -m[e])) * inv[e];
+                sum[x] += t <= pos[e] ? p : 0.f;
+            }
+        }
+    } else {
+#pragma unroll
+        for (int x = 0; x < NB; ++x) {
+            const f32x4_t s = product<D>(qv, k[x].v, T{});
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                sum[x] = fmaf(__builtin_amdgcn_exp2f(fmaf(s[e], a.scale_log2, -m[e])), inv[e], sum[x]);
+        }
+    }
+}
+
+// Writes the sums of key t: added to `old` (its decayed sum), or a new key's first.
+__device__ __forceinline__ void store_weight(const WgtArgs& a, const WgtGeom& geo, int i, int64_t at, int t, float sum,
+                                             float old) {
+    const bool fresh = t >= geo.S - geo.n;
+    if (fresh) a.key_order[at] = (a.num_tokens ? a.num_tokens[i] : geo.S) - geo.S + t;
+    a.key_weights[at] = fresh || a.decay == 0.f ? sum : sum + a.decay * old;
+}
+
+// Few rows: grid (KV heads x ranges of sum_blocks blocks, requests).  The request's
+// row tiles stay in LDS, its keys stream past.
+template <typename T, int D>
 __global__ __launch_bounds__(kWgtThreads) void weight_sums(WgtArgs a) {
-    constexpr int NC = Operand<T, D>::NC;
+    constexpr int NB = step_blocks(D, sizeof(T) == 2), NC = Operand<T, D>::NC;
     extern __shared__ uint4 s_dyn[];  // the row tiles, then their rows' m, 1 / l and positions
     uint4* s_q = s_dyn;
     float* s_m = reinterpret_cast<float*>(s_dyn + a.lds_tiles * NC * kWave);
     float* s_inv = s_m + a.lds_tiles * 16;
     int* s_pos = reinterpret_cast<int*>(s_inv + a.lds_tiles * 16);
-    const int i = blockIdx.y;
+    // backwards: the keys that weight_stats read last are still in the last-level cache
+    // (32 requests of 475 MB: 112 -> 97 us)
+    const int i = a.num_seqs - 1 - blockIdx.y;
     const int g = blockIdx.x % a.hkv, range = blockIdx.x / a.hkv;
     const WgtGeom geo = wgt_geom(a, i);
     const int b_lo = range * a.sum_blocks;
@@ -269,124 +394,195 @@ __global__ __launch_bounds__(kWgtThreads) void weight_sums(WgtArgs a) {
     const int tid = threadIdx.x, lane = tid & (kWave - 1), l16 = lane & 15, lg = lane >> 4;
     const int w = __builtin_amdgcn_readfirstlane(tid / kWave);
     const int32_t* table = a.block_tables + (int64_t)i * a.max_blocks;
-    const int p0 = geo.S - geo.n;
     const int nsplit = (geo.blocks + a.split_blocks - 1) / a.split_blocks;
-    auto stage = [&](int first, int tiles) {
-        stage_rows<T, D>(a, geo, g, first, tiles, s_q, s_pos);
-        for (int t = tid; t < tiles * 16; t += kWgtThreads) {
-            // a place without a row, a row without a key: 2^(s - inf) * 0
-            float m = INFINITY, inv = 0.f;
-            const int r = first + t;
-            if (r < geo.rows) {
-                const int j = r / a.group, h = g * a.group + r - j * a.group;
-                const float2* part = a.part + ((int64_t)(geo.q0 + j) * a.hq + h) * a.splits;
-                float M = -INFINITY, L = 0.f;
-                for (int s = 0; s < nsplit; ++s) {
-                    const float2 p = part[s];
-                    const float mn = fmaxf(M, p.x);
-                    if (mn == -INFINITY) {
-                        L += p.y;  // 0, or a NaN
-                    } else {
-                        L = L * __builtin_amdgcn_exp2f(M - mn) + p.y * __builtin_amdgcn_exp2f(p.x - mn);
-                        M = mn;
-                    }
-                }
-                if (a.sinks && M != -INFINITY) L += exp2f(a.sinks[h] * kWgtLog2e - M);
-                if (M != -INFINITY) {
-                    m = M;
-                    inv = 1.f / L;
-                } else if (L != 0.f) {  // every score was NaN
-                    m = L;
-                }
-            }
-            s_m[t] = m;
-            s_inv[t] = inv;
-        }
-    };
     const int all_tiles = (geo.rows + 15) / 16;
-    const bool once = all_tiles <= a.lds_tiles;
-    if (once) {
-        stage(0, all_tiles);
-        __syncthreads();
-    }
-    for (int b0 = b_lo; b0 < b_hi; b0 += kWgtWaves * NB) {
-        const int b = b0 + w * NB;
-        const int id = lane < NB && b + lane < b_hi ? table[b + lane] : -1;
-        const bool valid = id >= 0 && id < a.num_blocks;
-        const uint32_t ok = (uint32_t)__ballot(valid);
-        Operand<T, D> k[NB];
-        float sum[NB];
+    Walk<T, D, NB> walk(a, table, g, b_lo + w * NB, b_hi);
+    // lane group lg holds the weights of block x = lg of a step
+    auto load_old = [&](uint32_t ok, const int (&phys)[NB], int b) {
+        float old = 0.f;
 #pragma unroll
-        for (int x = 0; x < NB; ++x) sum[x] = 0.f;
-        if (ok) {
-#pragma unroll
-            for (int x = 0; x < NB; ++x) load_keys<T, D>(a, g, __builtin_amdgcn_readlane(valid ? id : 0, x), k[x]);
+        for (int x = 0; x < NB; ++x)
+            if (lg == x && ((ok >> x) & 1u) && (b + x) * kBlockTokens + l16 < geo.S - geo.n)
+                old = a.key_weights[((int64_t)phys[x] * a.hkv + g) * kBlockTokens + l16];
+        return old;
+    };
+    // rows beyond the LDS tiles (a request with more rows than announced) go by in
+    // further rounds over the keys, which add to what the first has written
+    for (int first = 0; first == 0 || first < all_tiles; first += a.lds_tiles) {
+        const int tiles = min(a.lds_tiles, all_tiles - first);
+        Walk<T, D, NB> go = walk;
+        Operand<T, D> k0[NB], k1[NB];
+        int phys0[NB] = {}, phys1[NB] = {}, b = go.b;
+        uint32_t ok0 = go.load(k0, phys0), ok1;
+        if (first > 0) __syncthreads();
+        stage_rows<T, D>(a, geo, g, first * 16, tiles, s_q, s_pos);
+        for (int t = tid; t < tiles * 16; t += kWgtThreads) {
+            float2 mi = make_float2(INFINITY, 0.f);
+            const int r = first * 16 + t;
+            if (r < geo.rows) {
+                mi = join_parts(a, part_of(a, geo, g, r), nsplit, g * a.group + r - by_group(a, r) * a.group);
+            }
+            s_m[t] = mi.x;
+            s_inv[t] = mi.y;
         }
-        auto add_tiles = [&](int first, int tiles) {
+        __syncthreads();
+        auto step = [&](const Operand<T, D> (&k)[NB], const int (&phys)[NB], uint32_t ok, int b) {
+            if (ok == 0) return;
+            const float old = load_old(ok, phys, b);
+            float sum[NB];
+#pragma unroll
+            for (int x = 0; x < NB; ++x) sum[x] = 0.f;
             for (int r = 0; r < tiles; ++r) {
-                const int row = r * 16;
-                const int p_lo = __builtin_amdgcn_readfirstlane(s_pos[row]);
-                const int p_hi = __builtin_amdgcn_readfirstlane(s_pos[min(row + 16, geo.rows - first) - 1]);
-                if (p_hi < b * kBlockTokens) continue;  // none of its rows sees the step's keys
+                const int last = min(r * 16 + 16, geo.rows - first * 16) - 1;
+                if (__builtin_amdgcn_readfirstlane(s_pos[last]) < b * kBlockTokens) continue;  // sees none of the keys
+                const bool masked = (b + NB) * kBlockTokens - 1 > __builtin_amdgcn_readfirstlane(s_pos[r * 16]);
                 uint4 qv[NC];
 #pragma unroll
                 for (int c = 0; c < NC; ++c) qv[c] = s_q[(r * NC + c) * kWave + lane];
                 const f32x4_t m = *reinterpret_cast<const f32x4_t*>(s_m + r * 16 + lg * 4);
                 const f32x4_t inv = *reinterpret_cast<const f32x4_t*>(s_inv + r * 16 + lg * 4);
-                if ((b + NB) * kBlockTokens - 1 > p_lo) {
-                    // keys that some of the rows do not see
-                    const i32x4_t pos = *reinterpret_cast<const i32x4_t*>(s_pos + r * 16 + lg * 4);
+                const i32x4_t pos = *reinterpret_cast<const i32x4_t*>(s_pos + r * 16 + lg * 4);
+                add_tile<T, D, NB>(a, qv, k, m, inv, masked, pos, b, sum);
+            }
+            // the four lane groups hold different rows of the same 16 keys
+            float mine = 0.f;
+            int block = 0;
+            bool store = false;
 #pragma unroll
-                    for (int x = 0; x < NB; ++x) {
-                        const f32x4_t s = product<D>(qv, k[x].v, T{});
-                        const int t = (b + x) * kBlockTokens + l16;
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const float p = __builtin_amdgcn_exp2f(fmaf(s[e], a.scale_log2, -m[e])) * inv[e];
-                            sum[x] += t <= pos[e] ? p : 0.f;
-                        }
-                    }
-                } else {
-#pragma unroll
-                    for (int x = 0; x < NB; ++x) {
-                        const f32x4_t s = product<D>(qv, k[x].v, T{});
-#pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            sum[x] = fmaf(__builtin_amdgcn_exp2f(fmaf(s[e], a.scale_log2, -m[e])), inv[e], sum[x]);
-                    }
+            for (int x = 0; x < NB; ++x) {
+                sum[x] += __shfl_xor(sum[x], 16);
+                sum[x] += __shfl_xor(sum[x], 32);
+                if (lg == x) {
+                    mine = sum[x];
+                    block = phys[x];
+                    store = (ok >> x) & 1u;
                 }
             }
+            const int t = (b + lg) * kBlockTokens + l16;
+            if (store && t < geo.S) {
+                const int64_t at = ((int64_t)block * a.hkv + g) * kBlockTokens + l16;
+                if (first == 0) store_weight(a, geo, i, at, t, mine, old);
+                else a.key_weights[at] += mine;
+            }
         };
-        if (once) {
-            if (ok) add_tiles(0, all_tiles);
-        } else {
-            // from the first row that sees the step's first key
-            const int64_t skip = max((int64_t)0, (int64_t)b0 * kBlockTokens - p0) * a.group;
-            for (int64_t f = skip / 16 * 16; f < geo.rows; f += a.lds_tiles * 16) {
-                const int first = (int)f, tiles = min(a.lds_tiles, (geo.rows - first + 15) / 16);
-                __syncthreads();
-                stage(first, tiles);
-                __syncthreads();
-                if (ok) add_tiles(first, tiles);
-            }
+        while (b < b_hi) {
+            ok1 = go.load(k1, phys1);
+            step(k0, phys0, ok0, b);
+            b += kWgtWaves * NB;
+            if (b >= b_hi) break;
+            ok0 = go.load(k0, phys0);
+            step(k1, phys1, ok1, b);
+            b += kWgtWaves * NB;
         }
-        if (!ok) continue;
-        // four lane groups hold different rows of the same 16 keys; afterwards lane
-        // group lg stores the blocks x with x % 4 == lg
+    }
+}
+
+// Many rows: the parts of every row joined, once, into the first of them.
+__global__ __launch_bounds__(kWgtThreads) void weight_join(WgtArgs a) {
+    const int i = blockIdx.y;
+    const WgtGeom geo = wgt_geom(a, i);
+    const int nsplit = (geo.blocks + a.split_blocks - 1) / a.split_blocks;
+    const int g = blockIdx.x % a.hkv;
+    for (int r = blockIdx.x / a.hkv * kWgtThreads + threadIdx.x; r < geo.rows; r += gridDim.x / a.hkv * kWgtThreads) {
+        float2* part = part_of(a, geo, g, r);
+        part[0] = join_parts(a, part, nsplit, g * a.group + r - by_group(a, r) * a.group);
+    }
+}
+
+// Many rows: grid (KV heads x steps of NB blocks, requests).  The wavefronts hold the
+// same keys and share out the row tiles, which stream past from memory (the second
+// level cache, where the steps of a KV head meet); their sums meet at the end.
+template <typename T, int D>
+__global__ __launch_bounds__(kRowWaves * kWave) void weight_sums_rows(WgtArgs a) {
+    constexpr int NB = held_blocks(D, sizeof(T) == 2), NC = Operand<T, D>::NC;
+    __shared__ float s_sum[kRowWaves][NB * kBlockTokens];
+    const int i = blockIdx.y;
+    const int g = blockIdx.x % a.hkv, b = blockIdx.x / a.hkv * NB;
+    const WgtGeom geo = wgt_geom(a, i);
+    if (b >= geo.blocks) return;
+    const int tid = threadIdx.x, lane = tid & (kWave - 1), l16 = lane & 15, lg = lane >> 4;
+    const int w = __builtin_amdgcn_readfirstlane(tid / kWave);
+    const int32_t* table = a.block_tables + (int64_t)i * a.max_blocks;
+    const int p0 = geo.S - geo.n;
+    Walk<T, D, NB> walk(a, table, g, b, geo.blocks);
+    Operand<T, D> k[NB];
+    int phys[NB] = {};
+    const uint32_t ok = walk.load(k, phys);
+    if (ok == 0) return;
+    float sum[NB];
 #pragma unroll
-        for (int x = 0; x < NB; ++x) {
-            sum[x] += __shfl_xor(sum[x], 16);
-            sum[x] += __shfl_xor(sum[x], 32);
-            const int phys = __builtin_amdgcn_readlane(valid ? id : 0, x);
-            const int t = (b + x) * kBlockTokens + l16;
-            if (lg == x % 4 && ((ok >> x) & 1u) && t < geo.S) {
-                const int64_t at = ((int64_t)phys * a.hkv + g) * kBlockTokens + l16;
-                float v = sum[x];
-                if (t >= p0) a.key_order[at] = (a.num_tokens ? a.num_tokens[i] : geo.S) - geo.S + t;
-                else if (a.decay != 0.f) v += a.decay * a.key_weights[at];
-                a.key_weights[at] = v;
+    for (int x = 0; x < NB; ++x) sum[x] = 0.f;
+    // from the tile of the first row that sees the first key
+    const int64_t skip = max((int64_t)0, (int64_t)b * kBlockTokens - p0) * a.group;
+    const int all_tiles = (geo.rows + 15) / 16;
+    const float2* part = part_of(a, geo, g, 0);
+    struct Rows {
+        uint4 q[NC];
+        f32x4_t m, inv;
+    };
+    auto load = [&](int tile, Rows& v) {
+        // a place without a row: the tile's first row, with weight 0
+        int r = tile * 16 + l16;
+        if (r >= geo.rows) r = tile * 16;
+        const int j = by_group(a, r), h = r - j * a.group;
+        const T* src = static_cast<const T*>(a.q) + ((int64_t)(geo.q0 + j) * a.hq + g * a.group + h) * D +
+                       lg * (16 / (int)sizeof(T));
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+            const u32x4u_t x = *reinterpret_cast<const u32x4u_t*>(src + c * (64 / (int)sizeof(T)));
+            v.q[c] = make_uint4(x.x, x.y, x.z, x.w);
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int rr = tile * 16 + lg * 4 + e;
+            const float2 mi = part[(int64_t)min(rr, geo.rows - 1) * a.splits];
+            v.m[e] = rr < geo.rows ? mi.x : INFINITY;
+            v.inv[e] = rr < geo.rows ? mi.y : 0.f;
+        }
+    };
+    auto add = [&](int tile, const Rows& v) {
+        const bool masked = (b + NB) * kBlockTokens - 1 > p0 + by_group(a, tile * 16);
+        i32x4_t pos = {};
+        if (masked) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int rr = tile * 16 + lg * 4 + e;
+                pos[e] = rr < geo.rows ? p0 + by_group(a, rr) : -1;
             }
         }
+        add_tile<T, D, NB>(a, v.q, k, v.m, v.inv, masked, pos, b, sum);
+    };
+    // the loads of the next tile in flight, the last one's again at the end
+    int tile = (int)min(skip / 16, (int64_t)all_tiles) + w;
+    if (tile < all_tiles) {
+        Rows r0, r1;
+        load(tile, r0);
+        for (;;) {
+            const int next = tile + kRowWaves;
+            load(min(next, all_tiles - 1), r1);
+            add(tile, r0);
+            if (next >= all_tiles) break;
+            tile = next + kRowWaves;
+            load(min(tile, all_tiles - 1), r0);
+            add(next, r1);
+            if (tile >= all_tiles) break;
+        }
+    }
+#pragma unroll
+    for (int x = 0; x < NB; ++x) {
+        sum[x] += __shfl_xor(sum[x], 16);
+        sum[x] += __shfl_xor(sum[x], 32);
+        if (lg == 0) s_sum[w][x * kBlockTokens + l16] = sum[x];
+    }
+    __syncthreads();
+    const int t = b * kBlockTokens + tid;
+    if (tid < NB * kBlockTokens && t < geo.S && ((ok >> (tid / kBlockTokens)) & 1u)) {
+        float v = 0.f;
+#pragma unroll
+        for (int x = 0; x < kRowWaves; ++x) v += s_sum[x][tid];
+        const int64_t at = ((int64_t)table[t / kBlockTokens] * a.hkv + g) * kBlockTokens + l16;
+        const float old = t < p0 && a.decay != 0.f ? a.key_weights[at] : 0.f;
+        store_weight(a, geo, i, at, t, v, old);
     }
 }
 
@@ -396,6 +592,7 @@ struct WgtPlan {
     int chunks, stat_tiles;  // weight_stats: row chunks, tiles per chunk
     int splits, split_blocks;
     int lds_tiles, sum_blocks, ranges;
+    int stat_rows;           // rows times the group of a request, about
     bool once;
     size_t bytes, cover;
 };
@@ -412,12 +609,11 @@ int make_plan(const verify_attn_params& p, int32_t total_q, int32_t max_q_len, i
         1, std::min<int64_t>(((int64_t)max_seq_len + kBlockTokens - 1) / kBlockTokens, p.max_blocks_per_seq));
     const bool bf16 = p.dtype == VERIFY_BF16;
     const int64_t step = kWgtWaves * step_blocks(p.head_dim, bf16);  // blocks of a workgroup's step
-    const int most_tiles = stat_tiles(bf16);
-    pl.stat_tiles = (int)std::min<int64_t>(tiles, most_tiles);
-    pl.chunks = (int)std::min<int64_t>((tiles + most_tiles - 1) / most_tiles, 4096);
+    pl.stat_tiles = (int)std::min<int64_t>(tiles, kStatTiles);
+    pl.chunks = (int)std::min<int64_t>((tiles + kStatTiles - 1) / kStatTiles, 4096);
     // a split has at most 128 blocks, and at least a step, towards four workgroups per
     // compute unit
-    const int64_t want = 4 * 256, most = (blocks + step - 1) / step, least = (blocks + 127) / 128;
+    const int64_t want = 4 * 256, most = (blocks + step - 1) / step, least = pl.chunks > 1 ? (blocks + 1023) / 1024 : (blocks + 127) / 128;
     const int64_t wgs = (int64_t)p.num_kv_heads * pl.chunks;
     auto splits = [&](int64_t seqs) { return std::max(least, std::min(most, (want + seqs * wgs - 1) / (seqs * wgs))); };
     const int64_t ns = splits(std::max(1, p.num_seqs));
@@ -428,8 +624,8 @@ int make_plan(const verify_attn_params& p, int32_t total_q, int32_t max_q_len, i
         pl.lds_tiles = (int)tiles;
         pl.sum_blocks = pl.split_blocks;
     } else {
-        pl.lds_tiles = (int)(16 * 1024 / tile_bytes(p));
-        pl.sum_blocks = kWgtWaves;
+        pl.sum_blocks = held_blocks(p.head_dim, bf16);
+        pl.stat_rows = pl.chunks * kStatTiles * 16;
     }
     // a grid dimension holds fewer than 2^32 threads
     const int64_t ranges = (blocks + pl.sum_blocks - 1) / pl.sum_blocks;
@@ -446,8 +642,9 @@ int make_plan(const verify_attn_params& p, int32_t total_q, int32_t max_q_len, i
 }
 
 template <typename T, int D>
-void launch(const WgtArgs& a, const WgtPlan& pl, int seqs, hipStream_t stream) {
-    const dim3 stats((unsigned)((int64_t)a.hkv * pl.chunks * pl.splits), (unsigned)seqs);
+void launch(const WgtArgs& a, const WgtPlan& pl, hipStream_t stream) {
+    const unsigned seqs = (unsigned)a.num_seqs;
+    const dim3 stats((unsigned)((int64_t)a.hkv * pl.chunks * pl.splits), seqs), sums((unsigned)pl.ranges * a.hkv, seqs);
     auto run = [&](auto rt) {
         hipLaunchKernelGGL((weight_stats<T, D, decltype(rt)::value>), stats, dim3(kWgtThreads), 0, stream, a);
     };
@@ -455,17 +652,16 @@ void launch(const WgtArgs& a, const WgtPlan& pl, int seqs, hipStream_t stream) {
         case 1: run(std::integral_constant<int, 1>{}); break;
         case 2: run(std::integral_constant<int, 2>{}); break;
         case 3: run(std::integral_constant<int, 3>{}); break;
-        case 4: run(std::integral_constant<int, 4>{}); break;
-        default:
-            if constexpr (sizeof(T) == 2) {
-                if (pl.stat_tiles <= 6) run(std::integral_constant<int, 6>{});
-                else run(std::integral_constant<int, 8>{});
-            }
+        default: run(std::integral_constant<int, kStatTiles>{});
     }
-    const dim3 sums((unsigned)pl.ranges * a.hkv, (unsigned)seqs);
-    const size_t lds = (size_t)pl.lds_tiles * (Operand<T, D>::NC * kWave * sizeof(uint4) + 3 * 16 * sizeof(float));
-    if (pl.once) hipLaunchKernelGGL((weight_sums<T, D, step_blocks(D, sizeof(T) == 2)>), sums, dim3(kWgtThreads), lds, stream, a);
-    else hipLaunchKernelGGL((weight_sums<T, D, 1>), sums, dim3(kWgtThreads), lds, stream, a);
+    if (pl.once) {
+        const size_t lds = (size_t)pl.lds_tiles * (Operand<T, D>::NC * kWave * sizeof(uint4) + 3 * 16 * sizeof(float));
+        hipLaunchKernelGGL((weight_sums<T, D>), sums, dim3(kWgtThreads), lds, stream, a);
+        return;
+    }
+    const dim3 join((unsigned)((pl.stat_rows + kWgtThreads - 1) / kWgtThreads * a.hkv), seqs);
+    hipLaunchKernelGGL(weight_join, join, dim3(kWgtThreads), 0, stream, a);
+    hipLaunchKernelGGL((weight_sums_rows<T, D>), sums, dim3(kRowWaves * kWave), 0, stream, a);
 }
 
 int check(const verify_attn_params* p, int32_t total_q, int32_t max_q_len, int32_t max_seq_len) {
@@ -532,14 +728,15 @@ extern "C" int verify_key_weights(const verify_attn_params* params, int32_t tota
     a.max_seq_len = max_seq_len;
     a.scale_log2 = (p.scale > 0.f ? p.scale : 1.0f / sqrtf((float)p.head_dim)) * kWgtLog2e;
     a.decay = decay;
+    a.group_magic = (uint32_t)((((uint64_t)1 << 32) + a.group - 1) / a.group);
     a.splits = pl.splits;
     a.split_blocks = pl.split_blocks;
     a.chunks = pl.chunks;
     a.sum_blocks = pl.sum_blocks;
     a.lds_tiles = pl.lds_tiles;
     if (p.dtype == VERIFY_BF16)
-        p.head_dim == 128 ? launch<uint16_t, 128>(a, pl, p.num_seqs, stream) : launch<uint16_t, 64>(a, pl, p.num_seqs, stream);
+        p.head_dim == 128 ? launch<uint16_t, 128>(a, pl, stream) : launch<uint16_t, 64>(a, pl, stream);
     else
-        p.head_dim == 128 ? launch<float, 128>(a, pl, p.num_seqs, stream) : launch<float, 64>(a, pl, p.num_seqs, stream);
+        p.head_dim == 128 ? launch<float, 128>(a, pl, stream) : launch<float, 64>(a, pl, stream);
     return check_launch();
 }
