@@ -609,8 +609,10 @@ int verify_key_weights(const verify_attn_params *params, int32_t total_q, int32_
  * A slot of an unmapped block counts as kept below c_i and as evicted above: no key
  * is moved out of one or into one.  If more keys are always kept than max_keys (by
  * ordinals that are no ordinals), the lower slots of them stay.
+ *   key_weights and key_order 16-byte aligned (VERIFY_EINVAL otherwise)
  *   workspace    at least verify_evict_plan_workspace_size() bytes (may be NULL if
  *                that is 0); its contents on entry are ignored
+ * VERIFY_EUNSUPPORTED beyond 2^24 slots per request.
  */
 int verify_evict_plan_workspace_size(const verify_attn_params *params, int32_t max_seq_len,
                                      int32_t max_keys, size_t *bytes);

@@ -1,14 +1,23 @@
 // verify_evict.hip -- the keys that a bounded cache keeps, and their moves.
 //
-//   evict_plan   one workgroup per (request, KV head): the c-th largest sort key of
-//                the request's S slots by a radix select (three digits, histograms in
-//                LDS), then one sweep in slot order that finds the kept slots, the
-//                holes among the first c and the kept slots behind them.  A thread
-//                takes a 16-slot block at a time, 64 contiguous bytes of each array.
-//   kv_compact   one wavefront per 16-slot block that keys move into.
+// The plan.  For each (request, KV head): the c-th largest of the S slots' sort keys
+// by a radix select (digits of 11, 11 and 10 bits, histograms in LDS), then the kept
+// slots in slot order, the holes among the first c and the kept slots behind them.  A
+// slot's sort key is one 32-bit word: the order key of its weight, above all of them
+// 0xffffffff for what is always kept, 0 for what never is.  At least c keys are not 0
+// (every slot below c has one), so a key of 0 counts nowhere.
+//   evict_plan    caches of up to kChunk slots: one workgroup, one launch, the keys in
+//                 registers, 16 per thread, from the first pass to the last;
+//   evict_hist (three launches), evict_lists, evict_join
+//                 longer caches: a workgroup per chunk of them, the histograms and
+//                 lists in the workspace between the launches (a single workgroup
+//                 took 543 us for 131072 slots).
+// The call is a chain of latencies.  What it reads is 8 bytes per slot, in pieces of 64
+// contiguous bytes; four lanes take a block's four quarters, so that a load touches 16
+// lines (a block per lane: 64, and the keys' arrival took 9 us of the plan's 40).
 //
-// A slot's sort key is one 32-bit word: the order key of its weight, above all of
-// them 0xffffffff for what is always kept, 0 for what never is.
+// The moves.
+//   kv_compact    one wavefront per 16-slot block that keys move into.
 #include "common.h"
 
 namespace averify {
@@ -16,8 +25,13 @@ namespace {
 
 constexpr int kPlanThreads = 1024;
 constexpr int kPlanWaves = kPlanThreads / kWave;
+constexpr int kSlots = 16;                      // of a thread
+constexpr int kChunk = kPlanThreads * kSlots;
 constexpr int kDigitBits = 11;
 constexpr int kBins = 1 << kDigitBits;
+constexpr int kMaxChunks = 1024;                // of a request
+constexpr uint32_t kAlways = 0xffffffffu;
+typedef int32_t i32x4u_t __attribute__((ext_vector_type(4), aligned(4)));
 
 struct PlanArgs {
     const float* key_weights;
@@ -27,151 +41,394 @@ struct PlanArgs {
     const int32_t* num_tokens;
     int32_t* source;
     int32_t* new_lens;
-    int32_t* lists;  // [pairs][2][list_len]: holes, and kept slots behind c
-    int64_t list_len;
-    int hkv, max_blocks, num_blocks, max_seq_len, max_keys, keep_first, keep_recent;
+    // long caches: [pairs][chunks] histograms of two passes, lists and their lengths
+    int32_t* hist;    // [2][pairs][chunks][kBins]
+    uint16_t* lists;  // [pairs][chunks][kChunk]: holes from the front, movers from the back
+    int2* counts;     // [pairs][chunks] holes and movers
+    uint2* state;     // [pairs][2] digits found and keys still needed, after one and two passes
+    int64_t pairs;
+    int hkv, chunks, max_blocks, num_blocks, max_seq_len, max_keys, keep_first, keep_recent;
 };
 
-// Exclusive prefix sum over the workgroup; the total in `total`.
-__device__ __forceinline__ int scan_exclusive(int v, int* wave_sums, int& total) {
-    const int lane = threadIdx.x & (kWave - 1), wv = threadIdx.x / kWave;
-    int x = v;
-#pragma unroll
-    for (int o = 1; o < kWave; o <<= 1) {
-        const int y = __shfl_up(x, o);
-        if (lane >= o) x += y;
-    }
-    __syncthreads();  // the sums of the scan before are read
-    if (lane == kWave - 1) wave_sums[wv] = x;
-    __syncthreads();
-    int before = 0, all = 0;
-#pragma unroll
-    for (int w = 0; w < kPlanWaves; ++w) {
-        const int s = wave_sums[w];
-        before += w < wv ? s : 0;
-        all += s;
-    }
-    total = all;
-    return before + x - v;
+struct PlanGeom {
+    int i, g, S, c;
+    int64_t pair, recent;  // ordinals from `recent` on are always kept
+};
+
+__device__ __forceinline__ PlanGeom plan_geom(const PlanArgs& a, int g, int i) {
+    PlanGeom p;
+    p.i = i;
+    p.g = g;
+    p.S = (int)max((int64_t)0, min((int64_t)a.seq_lens[i], min((int64_t)a.max_seq_len, (int64_t)a.max_blocks * kBlockTokens)));
+    p.c = min(p.S, a.max_keys);
+    p.pair = (int64_t)i * a.hkv + g;
+    p.recent = (int64_t)(a.num_tokens ? a.num_tokens[i] : p.S) - a.keep_recent;
+    return p;
 }
 
-__global__ __launch_bounds__(kPlanThreads) void evict_plan(PlanArgs a) {
-    __shared__ int hist[kBins];
-    __shared__ int wave_sums[kPlanWaves];
-    __shared__ int s_digit, s_above;
-    const int g = blockIdx.x, i = blockIdx.y, tid = threadIdx.x;
-    const int S = (int)max((int64_t)0, min((int64_t)a.seq_lens[i], min((int64_t)a.max_seq_len, (int64_t)a.max_blocks * kBlockTokens)));
-    const int c = min(S, a.max_keys);
-    const int64_t pair = (int64_t)i * a.hkv + g;
-    int32_t* source = a.source + pair * a.max_keys;
-    if (g == 0 && tid == 0) a.new_lens[i] = c;
-    if (S == c) {
-        for (int d = tid; d < a.max_keys; d += kPlanThreads) source[d] = d < c ? d : -1;
-        return;
+// First slot of this thread's quarter k of a chunk: wavefront, quarter, lane in order.
+__device__ __forceinline__ int slot_of(int chunk, int k) {
+    const int lane = threadIdx.x & (kWave - 1), wv = threadIdx.x / kWave;
+    return ((chunk * kPlanThreads + wv * kWave + 16 * k + lane / 4) * kBlockTokens) + lane % 4 * 4;
+}
+
+// Sort keys of this thread's slots: key[4 k + e] that of slot_of(k) + e.
+__device__ __forceinline__ void load_keys(const PlanArgs& a, const PlanGeom& p, int chunk, uint32_t (&key)[kSlots]) {
+    const int32_t* table = a.block_tables + (int64_t)p.i * a.max_blocks;
+    const int blocks = (p.S + kBlockTokens - 1) / kBlockTokens;
+    int id[4];
+    float4 w[4];
+    int4 o[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const int b = slot_of(chunk, k) / kBlockTokens;
+        id[k] = b < blocks ? table[b] : -1;
     }
-    const int32_t* table = a.block_tables + (int64_t)i * a.max_blocks;
-    const int64_t recent = (int64_t)(a.num_tokens ? a.num_tokens[i] : S) - a.keep_recent;
-    const int blocks = (S + kBlockTokens - 1) / kBlockTokens;
-    const int rounds = (blocks + kPlanThreads - 1) / kPlanThreads;
-
-    // the sort keys of this thread's block of a round, and how many of them count
-    uint32_t key[kBlockTokens];
-    int cnt = 0;
-    auto load = [&](int round) {
-        const int b = round * kPlanThreads + tid, s0 = b * kBlockTokens;
-        cnt = b < blocks ? min(kBlockTokens, S - s0) : 0;
-        if (cnt == 0) return;
-        const int id = table[b];
-        if (id < 0 || id >= a.num_blocks) {
 #pragma unroll
-            for (int e = 0; e < kBlockTokens; ++e) key[e] = s0 + e < c ? 0xffffffffu : 0u;
-            return;
-        }
-        const int64_t at = ((int64_t)id * a.hkv + g) * kBlockTokens;
-#pragma unroll
-        for (int e = 0; e < kBlockTokens; ++e) {
-            const uint32_t k = min(order_key(__float_as_uint(a.key_weights[at + e])), 0xfffffffeu);
-            const int o = a.key_order ? a.key_order[at + e] : s0 + e;
-            key[e] = o < a.keep_first || o >= recent ? 0xffffffffu : k;
-        }
-    };
-
-    // the c-th largest key: its digits from the top, `need` of the keys that share the
-    // digits so far being among the c largest
-    uint32_t prefix = 0, known = 0;  // known: mask of the digits found
-    int need = c;
-    if (rounds == 1) load(0);
-    for (int shift = 32 - kDigitBits; ; shift = max(0, shift - kDigitBits)) {
-        const uint32_t digits = ~known & (0xffffffffu << shift);  // of this pass
-        for (int e = tid; e < kBins; e += kPlanThreads) hist[e] = 0;
-        __syncthreads();
-        for (int round = 0; round < rounds; ++round) {
-            if (rounds > 1) load(round);
-#pragma unroll
-            for (int e = 0; e < kBlockTokens; ++e)
-                if (e < cnt && (key[e] & known) == prefix) atomicAdd(&hist[(key[e] & digits) >> shift], 1);
-        }
-        __syncthreads();
-        // two bins per thread, the highest first
-        const int top = kBins - 1 - 2 * tid;
-        const int h1 = hist[top], h0 = hist[top - 1];
-        int total;
-        const int above = scan_exclusive(h1 + h0, wave_sums, total);
-        if (above < need && need <= above + h1) {
-            s_digit = top;
-            s_above = above;
-        } else if (above + h1 < need && need <= above + h1 + h0) {
-            s_digit = top - 1;
-            s_above = above + h1;
-        }
-        __syncthreads();
-        prefix |= (uint32_t)s_digit << shift;
-        need -= s_above;
-        known |= digits;
-        __syncthreads();
-        if (shift == 0) break;
+    for (int k = 0; k < 4; ++k) {
+        const bool mapped = id[k] >= 0 && id[k] < a.num_blocks;
+        const int64_t at = ((int64_t)(mapped ? id[k] : 0) * a.hkv + p.g) * kBlockTokens + threadIdx.x % 4 * 4;
+        if (!mapped) continue;
+        w[k] = *reinterpret_cast<const float4*>(a.key_weights + at);
+        if (a.key_order) o[k] = *reinterpret_cast<const int4*>(a.key_order + at);
     }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const bool mapped = id[k] >= 0 && id[k] < a.num_blocks;
+        const int s0 = slot_of(chunk, k);
+        const float wk[4] = {w[k].x, w[k].y, w[k].z, w[k].w};
+        const int ok[4] = {o[k].x, o[k].y, o[k].z, o[k].w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int s = s0 + e, ord = a.key_order ? ok[e] : s;
+            uint32_t v = min(order_key(__float_as_uint(wk[e])), kAlways - 1);
+            if (ord < a.keep_first || ord >= p.recent) v = kAlways;
+            if (!mapped) v = s < p.c ? kAlways : 0u;
+            key[4 * k + e] = s < p.S ? v : 0u;
+        }
+    }
+}
 
-    // slots in order: kept are the keys above prefix and the first `need` equal to it
-    int32_t* holes = a.lists + pair * 2 * a.list_len;
-    int32_t* movers = holes + a.list_len;
-    int ties = 0, nholes = 0, nmovers = 0;
-    for (int round = 0; round < rounds; ++round) {
-        if (rounds > 1) load(round);
-        const int s0 = (round * kPlanThreads + tid) * kBlockTokens;
-        int eq = 0, total;
+// Inclusive prefix sum over the wavefront.
+__device__ __forceinline__ int wave_scan(int x) {
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);  // row_shr 1, 2, 4, 8
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);  // row_bcast 15, 31
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);
+    return x;
+}
+
+// Lanes below this one whose bit of `mask` is set.
+__device__ __forceinline__ int lanes_below(uint64_t mask) {
+    return __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0));
+}
+
+// A pass of the select: the digits found so far are in prefix, under the mask known.
+struct Digits {
+    uint32_t prefix, known;
+    int need;  // of the keys that share them, this many are among the c largest
+    __device__ uint32_t mask(int pass) const { return pass == 0 ? 0xffe00000u : pass == 1 ? 0x001ffc00u : 0x000003ffu; }
+    __device__ int shift(int pass) const { return pass == 0 ? 21 : pass == 1 ? 10 : 0; }
+};
+
+// Adds the thread's keys that share the digits to the histogram of the next one.  The
+// lanes that agree with the first of them go as one addition: weights that are equal
+// (zeros, what is always kept) would otherwise wait for each other.
+__device__ __forceinline__ void add_keys(const Digits& d, int pass, const uint32_t (&key)[kSlots], int* hist) {
+    const int lane = threadIdx.x & (kWave - 1);
 #pragma unroll
-        for (int e = 0; e < kBlockTokens; ++e) eq += e < cnt && key[e] == prefix;
-        int rank = ties + scan_exclusive(eq, wave_sums, total);
-        ties += total;
-        uint32_t hole = 0, mover = 0;
-#pragma unroll
-        for (int e = 0; e < kBlockTokens; ++e) {
-            if (e >= cnt) continue;
-            bool kept = key[e] > prefix;
-            if (key[e] == prefix) kept = rank++ < need;
-            if (s0 + e < c) {
-                if (kept) source[s0 + e] = s0 + e;
-                else hole |= 1u << e;
-            } else if (kept) {
-                mover |= 1u << e;
-            }
-        }
-        // both counts in one scan: a round has 2^14 slots
-        const int mine = __popc(hole) | (__popc(mover) << 16);
-        const int before = scan_exclusive(mine, wave_sums, total);
-        int h = nholes + (before & 0xffff), m = nmovers + (before >> 16);
-#pragma unroll
-        for (int e = 0; e < kBlockTokens; ++e) {
-            if ((hole >> e) & 1u) holes[h++] = s0 + e;
-            if ((mover >> e) & 1u) movers[m++] = s0 + e;
-        }
-        nholes += total & 0xffff;
-        nmovers += total >> 16;
+    for (int e = 0; e < kSlots; ++e) {
+        const bool in = key[e] != 0 && (key[e] & d.known) == d.prefix;
+        const uint64_t mask = __ballot(in);
+        if (mask == 0) continue;
+        const int bin = (int)((key[e] & d.mask(pass)) >> d.shift(pass));
+        const int leader = __builtin_ctzll(mask);
+        const bool same = in && bin == __builtin_amdgcn_readlane(bin, leader);
+        const uint64_t agree = __ballot(same);
+        if (lane == leader) atomicAdd(&hist[bin], __popcll(agree));
+        if (in && !same) atomicAdd(&hist[bin], 1);
+    }
+}
+
+struct PlanShared {
+    int hist[kBins];
+    int sums[kPlanWaves];
+    int digit, above, count;
+};
+
+__device__ __forceinline__ void clear_hist(PlanShared& sh) {
+    for (int e = threadIdx.x; e < kBins; e += kPlanThreads) sh.hist[e] = 0;
+    __syncthreads();
+}
+
+// The digit of the c-th largest key, from the whole histogram (every thread's
+// additions done), added to d.  Returns the keys that share all digits now.
+__device__ __forceinline__ int find_digit(PlanShared& sh, Digits& d, int pass) {
+    const int tid = threadIdx.x, lane = tid & (kWave - 1), wv = tid / kWave;
+    __syncthreads();
+    // two bins per thread, the highest first
+    const int top = kBins - 1 - 2 * tid;
+    const int h1 = sh.hist[top], h0 = sh.hist[top - 1];
+    const int x = wave_scan(h1 + h0);
+    if (lane == kWave - 1) sh.sums[wv] = x;
+    __syncthreads();
+    int above = x - h1 - h0;
+    for (int w = 0; w < wv; ++w) above += sh.sums[w];
+    const bool hi = above < d.need && d.need <= above + h1;
+    const bool lo = above + h1 < d.need && d.need <= above + h1 + h0;
+    if (hi || lo) {
+        sh.digit = hi ? top : top - 1;
+        sh.above = hi ? above : above + h1;
+        sh.count = hi ? h1 : h0;
     }
     __syncthreads();
-    for (int u = tid; u < nholes; u += kPlanThreads) source[holes[u]] = movers[u];
-    for (int d = c + tid; d < a.max_keys; d += kPlanThreads) source[d] = -1;
+    d.prefix |= (uint32_t)sh.digit << d.shift(pass);
+    d.known |= d.mask(pass);
+    d.need -= sh.above;
+    return sh.count;
+}
+
+// Which of the thread's keys are kept: those above the c-th largest, and of those
+// equal to it the first d.need in slot order, of `count` in all and `before` in
+// earlier chunks.
+__device__ __forceinline__ uint32_t kept_bits(PlanShared& sh, const Digits& d, const uint32_t (&key)[kSlots], int count,
+                                              int before) {
+    uint32_t kept = 0, equal = 0;
+#pragma unroll
+    for (int e = 0; e < kSlots; ++e) {
+        kept |= (uint32_t)(key[e] > d.prefix) << e;
+        equal |= (uint32_t)(key[e] == d.prefix) << e;
+    }
+    if (count == d.need) return kept | equal;
+    // ranks among the equal ones: wavefronts, quarters, lanes, elements in order
+    int rank[4], total = 0;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        rank[k] = total;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const uint64_t m = __ballot((equal >> (4 * k + e)) & 1u);
+            rank[k] += lanes_below(m);
+            total += __popcll(m);
+        }
+    }
+    const int wv = threadIdx.x / kWave;
+    __syncthreads();
+    if ((threadIdx.x & (kWave - 1)) == 0) sh.sums[wv] = total;
+    __syncthreads();
+    for (int w = 0; w < wv; ++w) before += sh.sums[w];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        int r = before + rank[k];
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if ((equal >> (4 * k + e)) & 1u) kept |= (uint32_t)(r++ < d.need) << (4 * k + e);
+    }
+    return kept;
+}
+
+// Writes the plan of the kept slots that stay, and lists the holes below c and the
+// kept slots from c on in slot order: hole(n, slot), mover(n, slot) for the n-th of
+// each.  Returns their numbers.
+template <typename Hole, typename Mover>
+__device__ __forceinline__ int2 list_slots(PlanShared& sh, const PlanGeom& p, int chunk, uint32_t kept, int32_t* source,
+                                           Hole hole, Mover mover) {
+    const int lane = threadIdx.x & (kWave - 1), wv = threadIdx.x / kWave;
+    uint32_t front = 0, inside = 0;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const int s0 = slot_of(chunk, k);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            front |= (uint32_t)(s0 + e < p.c) << (4 * k + e);
+            inside |= (uint32_t)(s0 + e < p.S) << (4 * k + e);
+        }
+        // holes are written over after a barrier, by whoever fills them
+        const int four = (front >> (4 * k)) & 0xf;
+        if (four == 0xf) {
+            *reinterpret_cast<i32x4u_t*>(source + s0) = i32x4u_t{s0, s0 + 1, s0 + 2, s0 + 3};
+        } else {
+#pragma unroll
+            for (int e = 0; e < 3; ++e)
+                if ((four >> e) & 1) source[s0 + e] = s0 + e;
+        }
+    }
+    const uint32_t bits[2] = {front & ~kept, inside & kept & ~front};
+    int rank[2][4], total[2] = {0, 0};
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        const bool some = __any(bits[j] != 0);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            rank[j][k] = total[j];
+            if (!some) continue;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const uint64_t m = __ballot((bits[j] >> (4 * k + e)) & 1u);
+                rank[j][k] += lanes_below(m);
+                total[j] += __popcll(m);
+            }
+        }
+    }
+    __syncthreads();
+    // both in one word: a chunk has 2^14 slots
+    if (lane == 0) sh.sums[wv] = total[0] | total[1] << 16;
+    __syncthreads();
+    int before = 0, all = 0;
+    for (int w = 0; w < kPlanWaves; ++w) {
+        before += w < wv ? sh.sums[w] : 0;
+        all += sh.sums[w];
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const int s0 = slot_of(chunk, k);
+        int h = (before & 0xffff) + rank[0][k], m = (before >> 16) + rank[1][k];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if ((bits[0] >> (4 * k + e)) & 1u) hole(h++, s0 + e);
+            if ((bits[1] >> (4 * k + e)) & 1u) mover(m++, s0 + e);
+        }
+    }
+    return make_int2(all & 0xffff, all >> 16);
+}
+
+// What a plan needs whoever is kept; true where that is all of it.
+__device__ __forceinline__ bool plan_ends(const PlanArgs& a, const PlanGeom& p, int32_t* source) {
+    if (p.g == 0 && threadIdx.x == 0) a.new_lens[p.i] = p.c;
+    for (int d = p.c + threadIdx.x; d < a.max_keys; d += kPlanThreads) source[d] = -1;
+    if (p.S != p.c) return false;
+    for (int d = threadIdx.x; d < p.c; d += kPlanThreads) source[d] = d;
+    return true;
+}
+
+// Grid (KV heads, requests).
+__global__ __launch_bounds__(kPlanThreads) void evict_plan(PlanArgs a) {
+    __shared__ PlanShared sh;
+    __shared__ uint16_t s_hole[kChunk / 2], s_mover[kChunk / 2];  // at most min(c, S - c) each
+    const PlanGeom p = plan_geom(a, blockIdx.x, blockIdx.y);
+    int32_t* source = a.source + p.pair * a.max_keys;
+    if (plan_ends(a, p, source)) return;
+    uint32_t key[kSlots];
+    load_keys(a, p, 0, key);
+    Digits d{0, 0, p.c};
+    int count = 0;
+    for (int pass = 0; pass < 3; ++pass) {
+        clear_hist(sh);
+        add_keys(d, pass, key, sh.hist);
+        count = find_digit(sh, d, pass);
+    }
+    const uint32_t kept = kept_bits(sh, d, key, count, 0);
+    const int2 n = list_slots(
+        sh, p, 0, kept, source, [&](int k, int s) { s_hole[k] = (uint16_t)s; }, [&](int k, int s) { s_mover[k] = (uint16_t)s; });
+    __syncthreads();
+    for (int u = threadIdx.x; u < n.x; u += kPlanThreads) source[s_hole[u]] = s_mover[u];
+}
+
+// The histogram of a pass, summed over the request's chunks; `before` receives the
+// counts of `bin` in the chunks before `chunk`, once that bin is known.
+__device__ __forceinline__ const int32_t* chunk_hists(const PlanArgs& a, const PlanGeom& p, int pass) {
+    return a.hist + ((pass & 1) * a.pairs + p.pair) * a.chunks * kBins;
+}
+__device__ __forceinline__ void sum_hists(const PlanArgs& a, const PlanGeom& p, int pass, PlanShared& sh) {
+    const int32_t* h = chunk_hists(a, p, pass);
+    const int chunks = (p.S + kChunk - 1) / kChunk;
+    for (int e = threadIdx.x; e < kBins; e += kPlanThreads) {
+        int v = 0;
+        for (int k = 0; k < chunks; ++k) v += h[(int64_t)k * kBins + e];
+        sh.hist[e] = v;
+    }
+}
+// The digits after `pass` passes: those before from the state, the last one's from the
+// histograms.
+__device__ __forceinline__ int digits_after(const PlanArgs& a, const PlanGeom& p, int passes, PlanShared& sh, Digits& d) {
+    d = Digits{0, 0, p.c};
+    if (passes > 1) {
+        const uint2 s = a.state[p.pair * 2 + passes - 2];
+        d.prefix = s.x;
+        d.need = (int)s.y;
+        d.known = passes == 2 ? d.mask(0) : d.mask(0) | d.mask(1);
+    }
+    sum_hists(a, p, passes - 1, sh);
+    return find_digit(sh, d, passes - 1);
+}
+
+// Grid (KV heads x chunks, requests), as the two kernels after it.
+template <int PASS>
+__global__ __launch_bounds__(kPlanThreads) void evict_hist(PlanArgs a) {
+    __shared__ PlanShared sh;
+    const PlanGeom p = plan_geom(a, blockIdx.x % a.hkv, blockIdx.y);
+    const int chunk = blockIdx.x / a.hkv;
+    if (p.S == p.c || (int64_t)chunk * kChunk >= p.S) return;
+    uint32_t key[kSlots];
+    load_keys(a, p, chunk, key);
+    Digits d{0, 0, p.c};
+    if (PASS > 0) {
+        digits_after(a, p, PASS, sh, d);
+        if (chunk == 0 && threadIdx.x == 0) a.state[p.pair * 2 + PASS - 1] = make_uint2(d.prefix, (uint32_t)d.need);
+        __syncthreads();
+    }
+    clear_hist(sh);
+    add_keys(d, PASS, key, sh.hist);
+    __syncthreads();
+    int32_t* out = a.hist + (((PASS & 1) * a.pairs + p.pair) * a.chunks + chunk) * kBins;
+    for (int e = threadIdx.x; e < kBins; e += kPlanThreads) out[e] = sh.hist[e];
+}
+
+__global__ __launch_bounds__(kPlanThreads) void evict_lists(PlanArgs a) {
+    __shared__ PlanShared sh;
+    const PlanGeom p = plan_geom(a, blockIdx.x % a.hkv, blockIdx.y);
+    const int chunk = blockIdx.x / a.hkv;
+    int32_t* source = a.source + p.pair * a.max_keys;
+    if (chunk == 0 && plan_ends(a, p, source)) return;
+    if (p.S == p.c || (int64_t)chunk * kChunk >= p.S) return;
+    uint32_t key[kSlots];
+    load_keys(a, p, chunk, key);
+    Digits d;
+    const int count = digits_after(a, p, 3, sh, d);
+    int before = 0;
+    const int32_t* h = chunk_hists(a, p, 2) + (d.prefix & d.mask(2));
+    for (int k = 0; k < chunk; ++k) before += h[(int64_t)k * kBins];
+    const uint32_t kept = kept_bits(sh, d, key, count, before);
+    uint16_t* list = a.lists + (p.pair * a.chunks + chunk) * kChunk;
+    const int s0 = chunk * kChunk;
+    const int2 n = list_slots(
+        sh, p, chunk, kept, source, [&](int k, int s) { list[k] = (uint16_t)(s - s0); },
+        [&](int k, int s) { list[kChunk - 1 - k] = (uint16_t)(s - s0); });
+    if (threadIdx.x == 0) a.counts[p.pair * a.chunks + chunk] = n;
+}
+
+// The n-th hole of the request takes its n-th mover.
+__global__ __launch_bounds__(kPlanThreads) void evict_join(PlanArgs a) {
+    __shared__ int s_movers[kMaxChunks];  // before and in each chunk
+    __shared__ int s_holes;
+    const PlanGeom p = plan_geom(a, blockIdx.x % a.hkv, blockIdx.y);
+    const int chunk = blockIdx.x / a.hkv, chunks = (p.S + kChunk - 1) / kChunk;
+    if (p.S == p.c || chunk >= chunks) return;
+    const int2* counts = a.counts + p.pair * a.chunks;
+    const int holes = counts[chunk].x;
+    if (holes == 0) return;
+    if (threadIdx.x == 0) {
+        int before = 0, sum = 0;
+        for (int k = 0; k < chunks; ++k) {
+            const int2 n = counts[k];
+            before += k < chunk ? n.x : 0;
+            sum += n.y;
+            s_movers[k] = sum;
+        }
+        s_holes = before;
+    }
+    __syncthreads();
+    const uint16_t* lists = a.lists + p.pair * a.chunks * kChunk;
+    int32_t* source = a.source + p.pair * a.max_keys;
+    int k = 0;
+    for (int u = threadIdx.x; u < holes; u += kPlanThreads) {
+        const int n = s_holes + u;
+        while (k < chunks - 1 && s_movers[k] <= n) ++k;
+        const int m = n - (k > 0 ? s_movers[k - 1] : 0);
+        source[chunk * kChunk + lists[(int64_t)chunk * kChunk + u]] = k * kChunk + lists[(int64_t)k * kChunk + kChunk - 1 - m];
+    }
 }
 
 struct CompactArgs {
@@ -234,14 +491,25 @@ int check(const verify_attn_params* p, int32_t max_seq_len, int32_t max_keys) {
     return max_keys < 1 ? VERIFY_EINVAL : VERIFY_OK;
 }
 
-// Holes of a (request, KV head) at most.
-int64_t list_len(const verify_attn_params& p, int32_t max_seq_len, int32_t max_keys) {
+// Chunks of the longest request; 1: evict_plan alone, without a workspace.
+int64_t plan_chunks(const verify_attn_params& p, int32_t max_seq_len) {
     const int64_t longest = std::min<int64_t>(max_seq_len, (int64_t)p.max_blocks_per_seq * kBlockTokens);
-    return std::max<int64_t>(0, std::min<int64_t>(max_keys, longest - max_keys));
+    return std::max<int64_t>(1, (longest + kChunk - 1) / kChunk);
 }
 
-size_t plan_bytes(const verify_attn_params& p, int32_t max_seq_len, int32_t max_keys) {
-    return align_up((size_t)p.num_seqs * p.num_kv_heads * 2 * (size_t)list_len(p, max_seq_len, max_keys) * sizeof(int32_t), 256);
+struct PlanSpace {
+    size_t lists, counts, state, total;  // offsets behind the histograms
+};
+
+PlanSpace plan_space(const verify_attn_params& p, int32_t max_seq_len, int32_t max_keys) {
+    PlanSpace w{};
+    const size_t chunks = (size_t)plan_chunks(p, max_seq_len), pairs = (size_t)p.num_seqs * p.num_kv_heads;
+    if (chunks == 1 || max_keys >= max_seq_len) return w;
+    w.lists = align_up(2 * pairs * chunks * kBins * sizeof(int32_t), 256);
+    w.counts = w.lists + align_up(pairs * chunks * kChunk * sizeof(uint16_t), 256);
+    w.state = w.counts + align_up(pairs * chunks * sizeof(int2), 256);
+    w.total = w.state + align_up(pairs * 2 * sizeof(uint2), 256);
+    return w;
 }
 
 }  // namespace
@@ -253,8 +521,10 @@ extern "C" int verify_evict_plan_workspace_size(const verify_attn_params* params
                                                 int32_t max_keys, size_t* bytes) {
     if (!bytes) return VERIFY_EINVAL;
     const int rc = check(params, max_seq_len, max_keys);
-    if (rc == VERIFY_OK) *bytes = plan_bytes(*params, max_seq_len, max_keys);
-    return rc;
+    if (rc != VERIFY_OK) return rc;
+    if (plan_chunks(*params, max_seq_len) > kMaxChunks) return VERIFY_EUNSUPPORTED;
+    *bytes = plan_space(*params, max_seq_len, max_keys).total;
+    return VERIFY_OK;
 }
 
 extern "C" int verify_evict_plan(const verify_attn_params* params, int32_t max_seq_len, int32_t max_keys,
@@ -268,8 +538,11 @@ extern "C" int verify_evict_plan(const verify_attn_params* params, int32_t max_s
     if (keep_first < 0 || keep_recent < 0 || (int64_t)keep_first + keep_recent > max_keys) return VERIFY_EINVAL;
     if (p.num_seqs > 0 && (!block_tables || !seq_lens || !source || !new_lens)) return VERIFY_EINVAL;
     if (p.num_seqs > 0 && p.num_blocks > 0 && !key_weights) return VERIFY_EINVAL;
-    const size_t need = plan_bytes(p, max_seq_len, max_keys);
-    if (workspace_bytes < need || (need > 0 && !workspace)) return VERIFY_EWORKSPACE;
+    if (((uintptr_t)key_weights | (uintptr_t)key_order) & 15) return VERIFY_EINVAL;
+    const int64_t chunks = plan_chunks(p, max_seq_len);
+    if (chunks > kMaxChunks || chunks * p.num_kv_heads >= (1 << 22)) return VERIFY_EUNSUPPORTED;
+    const PlanSpace space = plan_space(p, max_seq_len, max_keys);
+    if (workspace_bytes < space.total || (space.total > 0 && !workspace)) return VERIFY_EWORKSPACE;
     if (p.num_seqs == 0) return VERIFY_OK;
     PlanArgs a{};
     a.key_weights = key_weights;
@@ -279,8 +552,8 @@ extern "C" int verify_evict_plan(const verify_attn_params* params, int32_t max_s
     a.num_tokens = num_tokens;
     a.source = source;
     a.new_lens = new_lens;
-    a.lists = static_cast<int32_t*>(workspace);
-    a.list_len = list_len(p, max_seq_len, max_keys);
+    a.pairs = (int64_t)p.num_seqs * p.num_kv_heads;
+    a.chunks = (int)chunks;
     a.hkv = p.num_kv_heads;
     a.max_blocks = p.max_blocks_per_seq;
     a.num_blocks = p.num_blocks;
@@ -288,7 +561,22 @@ extern "C" int verify_evict_plan(const verify_attn_params* params, int32_t max_s
     a.max_keys = max_keys;
     a.keep_first = keep_first;
     a.keep_recent = keep_recent;
-    hipLaunchKernelGGL(evict_plan, dim3((unsigned)p.num_kv_heads, (unsigned)p.num_seqs), dim3(kPlanThreads), 0, stream, a);
+    dim3 grid((unsigned)p.num_kv_heads, (unsigned)p.num_seqs);
+    if (space.total == 0) {  // (also where no request can exceed max_keys)
+        hipLaunchKernelGGL(evict_plan, grid, dim3(kPlanThreads), 0, stream, a);
+        return check_launch();
+    }
+    char* ws = static_cast<char*>(workspace);
+    a.hist = reinterpret_cast<int32_t*>(ws);
+    a.lists = reinterpret_cast<uint16_t*>(ws + space.lists);
+    a.counts = reinterpret_cast<int2*>(ws + space.counts);
+    a.state = reinterpret_cast<uint2*>(ws + space.state);
+    grid.x *= (unsigned)chunks;
+    hipLaunchKernelGGL(evict_hist<0>, grid, dim3(kPlanThreads), 0, stream, a);
+    hipLaunchKernelGGL(evict_hist<1>, grid, dim3(kPlanThreads), 0, stream, a);
+    hipLaunchKernelGGL(evict_hist<2>, grid, dim3(kPlanThreads), 0, stream, a);
+    hipLaunchKernelGGL(evict_lists, grid, dim3(kPlanThreads), 0, stream, a);
+    hipLaunchKernelGGL(evict_join, grid, dim3(kPlanThreads), 0, stream, a);
     return check_launch();
 }
 

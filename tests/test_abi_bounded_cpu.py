@@ -143,8 +143,14 @@ def test_evict_plan_arguments():
     query = av.library().verify_evict_plan_workspace_size
     size = ctypes.c_size_t(0)
     assert query(ctypes.byref(_attn()), 1000, 100, ctypes.byref(size)) == av.OK
+    assert size.value == 0                                    # a workgroup's own memory holds it
+    long = _attn(max_blocks_per_seq=4096)
+    assert query(ctypes.byref(long), 40000, 100, ctypes.byref(size)) == av.OK and size.value > 0
     need = size.value
-    assert query(ctypes.byref(_attn()), 100, 100, ctypes.byref(size)) == av.OK and size.value == 0  # nobody exceeds it
+    assert query(ctypes.byref(long), 40000, 40000, ctypes.byref(size)) == av.OK and size.value == 0  # nobody exceeds it
+    far = _attn(max_blocks_per_seq=1 << 25)
+    assert query(ctypes.byref(far), (1 << 24) + 1, 100, ctypes.byref(size)) == av.EUNSUPPORTED
+    assert _plan(far, ms=(1 << 24) + 1) == av.EUNSUPPORTED
     assert query(ctypes.byref(_attn()), 1000, 100, None) == av.EINVAL
     assert query(None, 1000, 100, ctypes.byref(size)) == av.EINVAL
     assert _plan(None) == av.EINVAL
@@ -154,8 +160,9 @@ def test_evict_plan_arguments():
     for x in (0, 2, 3, 5, 6):
         assert _plan(_attn(), ptrs={x: None}) == av.EINVAL
     assert _plan(_attn(sliding_window=64)) == av.EUNSUPPORTED
-    if need:
-        assert _plan(_attn(), have=need - 1) == _plan(_attn(), ws=None) == av.EWORKSPACE
+    for x in (0, 1):
+        assert _plan(_attn(), ptrs={x: ctypes.c_void_p(0x1004)}) == av.EINVAL
+    assert _plan(long, ms=40000, have=need - 1) == _plan(long, ms=40000, ws=None) == av.EWORKSPACE
     assert _plan(_attn(num_seqs=0), have=0, ws=None) == av.OK
 
 
