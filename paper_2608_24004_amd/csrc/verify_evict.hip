@@ -158,6 +158,15 @@ struct PlanShared {
     int digit, above, count;
 };
 
+// Sum of sh.sums over the wavefronts before this one; over all of them in `total`.
+__device__ __forceinline__ int sums_before(const PlanShared& sh, int& total) {
+    const int lane = threadIdx.x & (kWave - 1);
+    const int wv = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
+    const int x = wave_scan(lane < kPlanWaves ? sh.sums[lane] : 0);
+    total = __builtin_amdgcn_readlane(x, kPlanWaves - 1);
+    return wv > 0 ? __builtin_amdgcn_readlane(x, wv - 1) : 0;
+}
+
 __device__ __forceinline__ void clear_hist(PlanShared& sh) {
     for (int e = threadIdx.x; e < kBins; e += kPlanThreads) sh.hist[e] = 0;
     __syncthreads();
@@ -174,8 +183,8 @@ __device__ __forceinline__ int find_digit(PlanShared& sh, Digits& d, int pass) {
     const int x = wave_scan(h1 + h0);
     if (lane == kWave - 1) sh.sums[wv] = x;
     __syncthreads();
-    int above = x - h1 - h0;
-    for (int w = 0; w < wv; ++w) above += sh.sums[w];
+    int all;
+    const int above = sums_before(sh, all) + x - h1 - h0;
     const bool hi = above < d.need && d.need <= above + h1;
     const bool lo = above + h1 < d.need && d.need <= above + h1 + h0;
     if (hi || lo) {
@@ -218,7 +227,8 @@ __device__ __forceinline__ uint32_t kept_bits(PlanShared& sh, const Digits& d, c
     __syncthreads();
     if ((threadIdx.x & (kWave - 1)) == 0) sh.sums[wv] = total;
     __syncthreads();
-    for (int w = 0; w < wv; ++w) before += sh.sums[w];
+    int all;
+    before += sums_before(sh, all);
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
         int r = before + rank[k];
@@ -276,19 +286,21 @@ __device__ __forceinline__ int2 list_slots(PlanShared& sh, const PlanGeom& p, in
     // both in one word: a chunk has 2^14 slots
     if (lane == 0) sh.sums[wv] = total[0] | total[1] << 16;
     __syncthreads();
-    int before = 0, all = 0;
-    for (int w = 0; w < kPlanWaves; ++w) {
-        before += w < wv ? sh.sums[w] : 0;
-        all += sh.sums[w];
-    }
+    int all;
+    const int before = sums_before(sh, all);
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        const int s0 = slot_of(chunk, k);
-        int h = (before & 0xffff) + rank[0][k], m = (before >> 16) + rank[1][k];
+    for (int j = 0; j < 2; ++j) {
+        if (total[j] == 0) continue;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            if ((bits[0] >> (4 * k + e)) & 1u) hole(h++, s0 + e);
-            if ((bits[1] >> (4 * k + e)) & 1u) mover(m++, s0 + e);
+        for (int k = 0; k < 4; ++k) {
+            const int s0 = slot_of(chunk, k);
+            int n = (j == 0 ? before & 0xffff : before >> 16) + rank[j][k];
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if ((bits[j] >> (4 * k + e)) & 1u) {
+                    if (j == 0) hole(n++, s0 + e);
+                    else mover(n++, s0 + e);
+                }
         }
     }
     return make_int2(all & 0xffff, all >> 16);
@@ -334,11 +346,13 @@ __device__ __forceinline__ const int32_t* chunk_hists(const PlanArgs& a, const P
 __device__ __forceinline__ void sum_hists(const PlanArgs& a, const PlanGeom& p, int pass, PlanShared& sh) {
     const int32_t* h = chunk_hists(a, p, pass);
     const int chunks = (p.S + kChunk - 1) / kChunk;
-    for (int e = threadIdx.x; e < kBins; e += kPlanThreads) {
-        int v = 0;
-        for (int k = 0; k < chunks; ++k) v += h[(int64_t)k * kBins + e];
-        sh.hist[e] = v;
-    }
+    int v[kBins / kPlanThreads] = {};
+#pragma unroll 4
+    for (int k = 0; k < chunks; ++k)
+#pragma unroll
+        for (int e = 0; e < kBins / kPlanThreads; ++e) v[e] += h[(int64_t)k * kBins + e * kPlanThreads + threadIdx.x];
+#pragma unroll
+    for (int e = 0; e < kBins / kPlanThreads; ++e) sh.hist[e * kPlanThreads + threadIdx.x] = v[e];
 }
 // The digits after `pass` passes: those before from the state, the last one's from the
 // histograms.
@@ -409,15 +423,17 @@ __global__ __launch_bounds__(kPlanThreads) void evict_join(PlanArgs a) {
     const int2* counts = a.counts + p.pair * a.chunks;
     const int holes = counts[chunk].x;
     if (holes == 0) return;
-    if (threadIdx.x == 0) {
-        int before = 0, sum = 0;
-        for (int k = 0; k < chunks; ++k) {
-            const int2 n = counts[k];
-            before += k < chunk ? n.x : 0;
-            sum += n.y;
-            s_movers[k] = sum;
+    if (threadIdx.x < kWave) {
+        int holes_before = 0, sum = 0;
+        for (int base = 0; base < chunks; base += kWave) {
+            const int k = base + threadIdx.x;
+            const int2 n = k < chunks ? counts[k] : make_int2(0, 0);
+            const int x = wave_scan(n.y), y = wave_scan(k < chunk ? n.x : 0);
+            if (k < chunks) s_movers[k] = sum + x;
+            sum += __builtin_amdgcn_readlane(x, kWave - 1);
+            holes_before += __builtin_amdgcn_readlane(y, kWave - 1);
         }
-        s_holes = before;
+        if (threadIdx.x == 0) s_holes = holes_before;
     }
     __syncthreads();
     const uint16_t* lists = a.lists + p.pair * a.chunks * kChunk;
