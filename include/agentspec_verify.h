@@ -636,7 +636,9 @@ int verify_evict_plan(const verify_attn_params *params, int32_t max_seq_len, int
  *                (VERIFY_EINVAL otherwise).  Element bits are copied unchanged.
  *   key_weights, key_order   moved likewise; each may be NULL
  * Slots s outside [0, 16 * max_blocks_per_seq) and slots of unmapped blocks are
- * skipped.  No workspace.
+ * skipped.  The other slots of a block that keys move into may be written with the
+ * bits they hold: nothing else may write to the requests' blocks meanwhile.  No
+ * workspace.
  */
 int verify_kv_compact(const verify_attn_params *params, int32_t max_keys,
                       const int32_t *block_tables, const int32_t *source,

@@ -460,7 +460,23 @@ struct CompactArgs {
 
 constexpr int kCompactWaves = 4;
 
-// Grid (KV heads x groups of blocks, requests), a wavefront per block.
+__device__ __forceinline__ uint32_t bits_of(float x) { return __float_as_uint(x); }
+__device__ __forceinline__ uint32_t bits_of(uint16_t x) { return x; }
+__device__ __forceinline__ float of_bits(uint32_t x, float) { return __uint_as_float(x); }
+__device__ __forceinline__ uint16_t of_bits(uint32_t x, uint16_t) { return (uint16_t)x; }
+
+// A block that many keys move into is written whole, the keys that stay as they are
+// included.  Lines that are written in part are read back and merged at the memory,
+// which costs as much as reading them here: 16 caches of 8 to 16 thousand keys brought
+// to 4096 took 242 us with partial writes, 217 with whole ones (1.05 GB at the rate of
+// a copy: a moved key's value lies in D 32-byte pieces of 16 keys, so all of the blocks
+// it leaves and enters passes by).  A block with few moves writes those alone (32 caches
+// with nine moves per head: 12 us, whole 19; the same with 2, 3 and 4 blocks per
+// wavefront, and the long moves slower).
+constexpr int kWholeMoves = 5;
+
+// Grid (KV heads x groups of blocks, requests), a wavefront per block, a lane per slot
+// and quarter of the dims.
 template <typename T, int D>
 __global__ __launch_bounds__(kCompactWaves * kWave) void kv_compact(CompactArgs a) {
     constexpr int N = 16 / (int)sizeof(T);
@@ -476,26 +492,26 @@ __global__ __launch_bounds__(kCompactWaves * kWave) void kv_compact(CompactArgs 
     const int to = table[b];
     int from = -1;
     if (s != d && s >= 0 && s / kBlockTokens < a.max_blocks) from = table[s / kBlockTokens];
-    const bool move = from >= 0 && from < a.num_blocks && to >= 0 && to < a.num_blocks;
-    if (!move) return;
-    const int slot = s % kBlockTokens;
-    const int64_t src = (int64_t)from * a.hkv + g, dst = (int64_t)to * a.hkv + g;
-    const uint4* ks = reinterpret_cast<const uint4*>(static_cast<const T*>(a.kc) + src * TILE) + slot;
-    uint4* kd = reinterpret_cast<uint4*>(static_cast<T*>(a.kc) + dst * TILE) + t;
-    uint4 k[D / N / 4];
+    const bool moved = from >= 0 && from < a.num_blocks && to >= 0 && to < a.num_blocks;
+    const int moves = __popcll(__ballot(moved)) / 4;
+    if (moves == 0 || (!moved && moves < kWholeMoves)) return;
+    const int slot = moved ? s % kBlockTokens : t;
+    const int64_t src = (int64_t)(moved ? from : to) * a.hkv + g, dst = (int64_t)to * a.hkv + g;
+    const u32x4* ks = reinterpret_cast<const u32x4*>(static_cast<const T*>(a.kc) + src * TILE) + slot;
+    u32x4* kd = reinterpret_cast<u32x4*>(static_cast<T*>(a.kc) + dst * TILE) + t;
+    const T* vs = static_cast<const T*>(a.vc) + src * TILE + slot;
+    T* vd = static_cast<T*>(a.vc) + dst * TILE + t;
+    u32x4 k[D / N / 4];
+    uint32_t v[D / 4];
 #pragma unroll
     for (int x = 0; x < D / N / 4; ++x) k[x] = ks[(4 * x + part) * kBlockTokens];
 #pragma unroll
+    for (int x = 0; x < D / 4; ++x) v[x] = bits_of(vs[(4 * x + part) * kBlockTokens]);
+#pragma unroll
     for (int x = 0; x < D / N / 4; ++x) kd[(4 * x + part) * kBlockTokens] = k[x];
-    const T* vs = static_cast<const T*>(a.vc) + src * TILE + slot;
-    T* vd = static_cast<T*>(a.vc) + dst * TILE + t;
-    for (int x0 = 0; x0 < D / 4; x0 += 16) {
-        T v[16];
 #pragma unroll
-        for (int x = 0; x < 16; ++x) v[x] = vs[(4 * (x0 + x) + part) * kBlockTokens];
-#pragma unroll
-        for (int x = 0; x < 16; ++x) vd[(4 * (x0 + x) + part) * kBlockTokens] = v[x];
-    }
+    for (int x = 0; x < D / 4; ++x) vd[(4 * x + part) * kBlockTokens] = of_bits(v[x], T{});
+    if (!moved) return;
     if (part == 0 && a.key_weights) a.key_weights[dst * kBlockTokens + t] = a.key_weights[src * kBlockTokens + slot];
     if (part == 1 && a.key_order) a.key_order[dst * kBlockTokens + t] = a.key_order[src * kBlockTokens + slot];
 }
