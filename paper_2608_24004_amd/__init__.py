@@ -712,17 +712,25 @@ def _scratch(shape, dtype, dev, stream):
     return t
 
 
+_current_device = None
+
+
 def _launch(where, idx, *args):
     """The library's call `where` with the tensors' device current, as a launch on
     one of its streams needs."""
-    import torch
-    call = getattr(library(), where)
-    if torch.cuda.current_device() == idx:
+    global _current_device
+    if _current_device is None:
+        import torch
+        _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+    call = getattr(_lib or library(), where)
+    if _current_device() == idx:
         rc = call(*args)
     else:
+        import torch
         with torch.cuda.device(idx):
             rc = call(*args)
-    _check(rc, where)
+    if rc != OK:
+        _check(rc, where)
 
 
 def _rows_arg(t, name, heads, D, dtype, idx, device, T=None):

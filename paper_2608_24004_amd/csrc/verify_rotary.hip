@@ -11,6 +11,10 @@
 // binary64, its integer part is removed there, and sine and cosine are evaluated in
 // fp32 on a half turn at most.
 //
+// What bounds it: memory, above a few thousand rows (5461 rows of 40 heads of 128, 112
+// MB: 27 us, 4.2 TB/s); below, a launch and the latencies of positions, rows and, for
+// the append, of q_start, the request's length and its block ids.
+//
 // The append.  K goes to its slots in the 16-byte chunks that the cache keeps
 // together; V, which the cache keeps transposed, passes through LDS.  Threads run
 // over a tile's rows first, so that the consecutive slots of a prompt's rows leave in
@@ -40,7 +44,8 @@ struct RotArgs {
     const int32_t* seq_lens;
     const int32_t* q_start;
     int64_t q_stride, k_stride, v_stride, q_out_stride, k_out_stride;
-    int total_q, hq, hkv, num_axes, freqs, heads_per_wg;
+    int total_q, hq, hkv, num_axes, freqs;
+    int key_wgs, value_wgs, heads_per_wg;
     int num_seqs, max_blocks, num_blocks;
     float scale;
     uint8_t axis[kMaxFreqs];
@@ -100,6 +105,13 @@ template <> struct Vec<float> {
     }
 };
 
+// scale (cos, sin) of t turns: their fraction, in binary64, then fp32.
+__device__ __forceinline__ float2 unit_circle(double t, float scale) {
+    float sn, cn;
+    sincospif(2.f * (float)(t - rint(t)), &sn, &cn);
+    return make_float2(scale * cn, scale * sn);
+}
+
 __device__ __forceinline__ void turn(float& x, float& y, const float2& cs) {
     // explicit, so that every layout's code rounds alike
     const float a = x, b = y;
@@ -107,39 +119,49 @@ __device__ __forceinline__ void turn(float& x, float& y, const float2& cs) {
     y = fmaf(b, cs.x, a * cs.y);
 }
 
+// Heads of a workgroup: of K (their chunks pass through registers, all loads before
+// the first store) and of V (through LDS).
+constexpr int kKeyHeads = 4;
+constexpr int value_heads(int esize) { return esize == 2 ? 4 : 2; }
+// Of Q at most: 5461 rows of 32 heads 26.9 us with 8 or fewer, 28.8 with 16, 30.7 with 24.
+constexpr int kQueryHeads = 8;
+constexpr int batch(bool inter) { return inter ? 4 : 1; }  // query items of a thread in flight
+
+// Workgroup (tile, y): y below key_wgs takes keys, below key_wgs + value_wgs values,
+// the others queries.  Keys and values come first: theirs is the longer way.
 // WIDE: all rows and pair halves are 16-byte aligned; otherwise element by element.
 // INTER: the pair of frequency f is (2f, 2f + 1).
 template <typename T, int D, bool APPEND, bool WIDE, bool INTER>
 __global__ __launch_bounds__(kRotThreads) void rotate_rows(RotArgs a) {
     constexpr int N = Vec<T>::N;
     constexpr int CH = D / N;  // 16-byte chunks of a head
+    constexpr int VH = value_heads((int)sizeof(T)), kBatch = batch(INTER);
+    constexpr int PLACE = APPEND ? kSearchEntries / 4 : 0, VALUES = APPEND && WIDE ? VH * kTile * (CH + 1) : 0;
     __shared__ float2 cs[kTile][kMaxFreqs];
     __shared__ Place place[kTile];
-    // the search's entries, then the values of one head
-    __shared__ uint4 scratch[kTile * (CH + 1) > kSearchEntries / 4 ? kTile * (CH + 1) : kSearchEntries / 4];
+    __shared__ uint4 s_start[PLACE ? PLACE : 1];
+    __shared__ uint4 s_val[VALUES ? VALUES : 1];
     const int tid = threadIdx.x, lane = tid & (kWave - 1), wv = tid / kWave;
-    const int row0 = blockIdx.x * kTile;
+    // Workgroups go round the eight XCDs: each takes neighbouring tiles, whose rows share
+    // cache lines of the paged cache (six prompts of 12 thousand rows in all: 60 -> 56 us).
+    const int xq = gridDim.x / 8, xr = gridDim.x % 8, xcd = blockIdx.x % 8;
+    const int row0 = (xcd * xq + min(xcd, xr) + (int)(blockIdx.x / 8)) * kTile;
     const int rows = min(kTile, a.total_q - row0);
-    // heads in the order K, V, Q: the first two have the longer way
-    const int kv_heads = APPEND ? 2 * a.hkv : a.hkv;
-    const int h_lo = blockIdx.y * a.heads_per_wg;
-    const int h_hi = min(h_lo + a.heads_per_wg, kv_heads + a.hq);
+    const int y = blockIdx.y;
+    const bool key = y < a.key_wgs, value = !key && y < a.key_wgs + a.value_wgs;
+    const int per = key ? kKeyHeads : value ? VH : a.heads_per_wg;
+    const int h_lo = (key ? y : value ? y - a.key_wgs : y - a.key_wgs - a.value_wgs) * per;
+    const int h_hi = min(h_lo + per, key || value ? a.hkv : a.hq);
 
-    // angles: a wavefront per row, a frequency per lane
-    if (lane < a.freqs) {
-        const double turns_per = a.inv_freq[lane] * 0.15915494309189533577;  // 1 / 2 pi
-        const int32_t* pos = a.positions + (int64_t)a.axis[lane] * a.total_q + row0;
-        for (int r = wv; r < rows; r += kRotThreads / kWave) {
-            const double t = (double)pos[r] * turns_per;
-            float sn, cn;
-            sincospif(2.f * (float)(t - rint(t)), &sn, &cn);
-            cs[r][lane] = make_float2(cn * a.scale, sn * a.scale);
-        }
-    }
-    if constexpr (APPEND) {
-        if (h_lo < kv_heads) find_places(a, row0, rows, reinterpret_cast<int32_t*>(scratch), place);
-    }
-    __syncthreads();
+    // angles: a frequency per lane; with 32 or fewer of them two rows per wavefront
+    const int fsh = a.freqs <= 32 ? 5 : 6;
+    auto angles = [&]() {
+        const int f = tid & ((1 << fsh) - 1), r0 = tid >> fsh, step = kRotThreads >> fsh;
+        if (f >= a.freqs) return;
+        const double turns_per = a.inv_freq[f] * 0.15915494309189533577;  // 1 / 2 pi
+        const int32_t* pos = a.positions + (int64_t)a.axis[f] * a.total_q + row0;
+        for (int r = r0; r < rows; r += step) cs[r][f] = unit_circle((double)pos[r] * turns_per, a.scale);
+    };
 
     const int half = a.freqs;  // the distance of a pair's dims, unless INTER
     if constexpr (WIDE) {
@@ -152,83 +174,122 @@ __global__ __launch_bounds__(kRotThreads) void rotate_rows(RotArgs a) {
             c1 = !INTER && it < turned ? it + half / N : -1;
             if (it >= turned) c0 = 2 * half / N + (it - turned);
         };
-        auto turn_item = [&](int it, int r, uint4& v0, uint4& v1) {
+        auto load_item = [&](const T* head, int c0, int c1, u32x4& v0, u32x4& v1) {
+            v0 = *reinterpret_cast<const u32x4*>(head + c0 * N);
+            if (!INTER) v1 = *reinterpret_cast<const u32x4*>(head + (c1 >= 0 ? c1 : c0) * N);
+        };
+        auto turn_item = [&](int it, int r, u32x4& v0, u32x4& v1) {
             if (it >= turned) return;
             float x[N], y[N];
-            unpack16(v0, x, T{});
+            unpack16(make_uint4(v0.x, v0.y, v0.z, v0.w), x, T{});
             if constexpr (INTER) {
 #pragma unroll
                 for (int e = 0; e < N; e += 2) turn(x[e], x[e + 1], cs[r][it * (N / 2) + e / 2]);
             } else {
-                unpack16(v1, y, T{});
+                unpack16(make_uint4(v1.x, v1.y, v1.z, v1.w), y, T{});
 #pragma unroll
                 for (int e = 0; e < N; ++e) turn(x[e], y[e], cs[r][it * N + e]);
-                v1 = Vec<T>::pack(y);
+                const uint4 w = Vec<T>::pack(y);
+                v1 = u32x4{w.x, w.y, w.z, w.w};
             }
-            v0 = Vec<T>::pack(x);
+            const uint4 w = Vec<T>::pack(x);
+            v0 = u32x4{w.x, w.y, w.z, w.w};
         };
-        // heads [lo, hi) of rows, row to row: items fastest
-        auto rotate_heads = [&](const T* in, int64_t in_stride, T* out, int64_t out_stride, int lo, int hi) {
-            int sh = 0;
-            while ((1 << sh) < items) ++sh;
-            const int it = tid & ((1 << sh) - 1);
-            if (it >= items) return;
-            int c0, c1;
-            item_chunks(it, c0, c1);
-            for (int u = tid >> sh; u < (hi - lo) * kTile; u += kRotThreads >> sh) {
-                const int r = u % kTile, h = lo + u / kTile;
-                if (r >= rows) continue;
-                const T* src = in + (row0 + r) * in_stride + (int64_t)h * D;
-                uint4 v0 = ld16(src + c0 * N), v1 = make_uint4(0, 0, 0, 0);
-                if (c1 >= 0) v1 = ld16(src + c1 * N);
-                turn_item(it, r, v0, v1);
-                T* dst = out + (row0 + r) * out_stride + (int64_t)h * D;
-                *reinterpret_cast<uint4*>(dst + c0 * N) = v0;
-                if (c1 >= 0) *reinterpret_cast<uint4*>(dst + c1 * N) = v1;
-            }
-        };
-        const int r = tid % kTile;
-        if constexpr (APPEND) {
-            const T* kin = static_cast<const T*>(a.k) + (row0 + r) * a.k_stride;
-            const int64_t tile = (int64_t)D * kBlockTokens;
-            const bool store = r < rows && place[r].block >= 0;
-            const Place p = store ? place[r] : Place{0, 0};
-            for (int h = h_lo; h < min(h_hi, a.hkv); ++h) {
-                T* to = static_cast<T*>(a.k_out) + ((int64_t)p.block * a.hkv + h) * tile + p.slot * N;
-                for (int it = tid / kTile; it < items && store; it += kRotThreads / kTile) {
-                    int c0, c1;
-                    item_chunks(it, c0, c1);
-                    uint4 v0 = ld16(kin + h * D + c0 * N), v1 = make_uint4(0, 0, 0, 0);
-                    if (c1 >= 0) v1 = ld16(kin + h * D + c1 * N);
-                    turn_item(it, r, v0, v1);
-                    *reinterpret_cast<uint4*>(to + c0 * (kBlockTokens * N)) = v0;
-                    if (c1 >= 0) *reinterpret_cast<uint4*>(to + c1 * (kBlockTokens * N)) = v1;
+        if (APPEND && key) {
+            // a thread per row and item, its chunks of every head of the workgroup
+            const int r = tid % kTile, it = tid / kTile;
+            const T* in = static_cast<const T*>(a.k) + (row0 + min(r, rows - 1)) * a.k_stride;
+            for (int base = it; base - it < items; base += kRotThreads / kTile) {
+                const int my = min(base, items - 1);
+                int c0, c1;
+                item_chunks(my, c0, c1);
+                u32x4 v0[kKeyHeads], v1[kKeyHeads];
+#pragma unroll
+                for (int x = 0; x < kKeyHeads; ++x) load_item(in + min(h_lo + x, h_hi - 1) * D, c0, c1, v0[x], v1[x]);
+                if (base == it) {
+                    angles();
+                    find_places(a, row0, rows, reinterpret_cast<int32_t*>(s_start), place);
+                    __syncthreads();
+                }
+                const Place p = r < rows ? place[r] : Place{-1, 0};
+                if (p.block < 0 || base >= items) continue;
+#pragma unroll
+                for (int x = 0; x < kKeyHeads; ++x) {
+                    if (h_lo + x >= h_hi) break;
+                    turn_item(my, r, v0[x], v1[x]);
+                    T* to = static_cast<T*>(a.k_out) + ((int64_t)p.block * a.hkv + h_lo + x) * (D * kBlockTokens) + p.slot * N;
+                    *reinterpret_cast<u32x4*>(to + c0 * (kBlockTokens * N)) = v0[x];
+                    if (c1 >= 0) *reinterpret_cast<u32x4*>(to + c1 * (kBlockTokens * N)) = v1[x];
                 }
             }
-            for (int h = max(h_lo, a.hkv) - a.hkv; h < min(h_hi, kv_heads) - a.hkv; ++h) {
-                __syncthreads();  // the search, or the head before, is done with scratch
-                for (int e = tid; e < rows * CH; e += kRotThreads)
-                    scratch[e / CH * (CH + 1) + e % CH] =
-                        ld16(static_cast<const T*>(a.v) + (row0 + e / CH) * a.v_stride + h * D + e % CH * N);
-                __syncthreads();
-                T* to = static_cast<T*>(a.v_out) + ((int64_t)p.block * a.hkv + h) * tile + p.slot;
-                const T* from = reinterpret_cast<const T*>(scratch + r * (CH + 1));
-                if (store)
-                    for (int d = tid / kTile; d < D; d += kRotThreads / kTile) to[d * kBlockTokens] = from[d];
+        } else if (APPEND && value) {
+            u32x4 v[VH * kTile * CH / kRotThreads];
+#pragma unroll
+            for (int x = 0; x < VH * kTile * CH / kRotThreads; ++x) {
+                const int e = x * kRotThreads + tid, c = e % CH, r = e / CH % kTile, h = e / CH / kTile;
+                v[x] = *reinterpret_cast<const u32x4*>(static_cast<const T*>(a.v) + (row0 + min(r, rows - 1)) * a.v_stride +
+                                                       min(h_lo + h, h_hi - 1) * D + c * N);
             }
-        } else if (a.k) {
-            rotate_heads(static_cast<const T*>(a.k), a.k_stride, static_cast<T*>(a.k_out), a.k_out_stride, h_lo,
-                         min(h_hi, a.hkv));
+            find_places(a, row0, rows, reinterpret_cast<int32_t*>(s_start), place);
+#pragma unroll
+            for (int x = 0; x < VH * kTile * CH / kRotThreads; ++x) {
+                const int e = x * kRotThreads + tid, c = e % CH;
+                s_val[e / CH * (CH + 1) + c] = make_uint4(v[x].x, v[x].y, v[x].z, v[x].w);
+            }
+            __syncthreads();
+            // threads over the rows first: neighbouring slots of a dim are neighbours
+            const int r = tid % kTile;
+            const Place p = r < rows ? place[r] : Place{-1, 0};
+            if (p.block < 0) return;
+            for (int h = h_lo; h < h_hi; ++h) {
+                const T* from = reinterpret_cast<const T*>(s_val + ((h - h_lo) * kTile + r) * (CH + 1));
+                T* to = static_cast<T*>(a.v_out) + ((int64_t)p.block * a.hkv + h) * (D * kBlockTokens) + p.slot;
+#pragma unroll
+                for (int d = 0; d < D; d += kRotThreads / kTile) to[(d + tid / kTile) * kBlockTokens] = from[d + tid / kTile];
+            }
+        } else {
+            // row to row: items fastest, kBatch of a thread in flight (every thread's loads
+            // are made, of the last row and item past the end: with a test before each the
+            // prompts of append took 60 us, 56 without)
+            const T* in = static_cast<const T*>(key ? a.k : a.q);
+            T* out = static_cast<T*>(key ? a.k_out : a.q_out);
+            const int64_t in_stride = key ? a.k_stride : a.q_stride, out_stride = key ? a.k_out_stride : a.q_out_stride;
+            int sh = 0;
+            while ((1 << sh) < items) ++sh;
+            const int my = tid & ((1 << sh) - 1), it = min(my, items - 1);
+            int c0, c1;
+            item_chunks(it, c0, c1);
+            const int step = kRotThreads >> sh, all = (h_hi - h_lo) * kTile;
+            angles();
+            __syncthreads();
+            for (int base = 0; base < all; base += kBatch * step) {
+                const int u0 = base + (tid >> sh);
+                u32x4 v0[kBatch], v1[kBatch];
+#pragma unroll
+                for (int x = 0; x < kBatch; ++x) {
+                    const int u = min(u0 + x * step, all - 1);
+                    load_item(in + (row0 + min(u % kTile, rows - 1)) * in_stride + (int64_t)(h_lo + u / kTile) * D, c0, c1,
+                              v0[x], v1[x]);
+                }
+#pragma unroll
+                for (int x = 0; x < kBatch; ++x) {
+                    const int u = u0 + x * step, r = u % kTile;
+                    if (my >= items || u >= all || r >= rows) continue;
+                    turn_item(it, r, v0[x], v1[x]);
+                    T* dst = out + (row0 + r) * out_stride + (int64_t)(h_lo + u / kTile) * D;
+                    *reinterpret_cast<u32x4*>(dst + c0 * N) = v0[x];
+                    if (c1 >= 0) *reinterpret_cast<u32x4*>(dst + c1 * N) = v1[x];
+                }
+            }
         }
-        rotate_heads(static_cast<const T*>(a.q), a.q_stride, static_cast<T*>(a.q_out), a.q_out_stride,
-                     max(h_lo, kv_heads) - kv_heads, h_hi - kv_heads);
     } else {
+        if (!value) angles();
+        if (APPEND && (key || value)) find_places(a, row0, rows, reinterpret_cast<int32_t*>(s_start), place);
+        __syncthreads();
         // an item is a pair, or two neighbouring dims that pass through
         for (int u = tid; u < (h_hi - h_lo) * kTile * (D / 2); u += kRotThreads) {
-            const int it = u % (D / 2), r = u / (D / 2) % kTile, hh = h_lo + u / (D / 2) / kTile;
+            const int it = u % (D / 2), r = u / (D / 2) % kTile, h = h_lo + u / (D / 2) / kTile;
             if (r >= rows) continue;
-            const bool key = hh < a.hkv, value = !key && hh < kv_heads;
-            const int h = key ? hh : value ? hh - a.hkv : hh - kv_heads;
             const bool turned = it < half && !value;
             const int d0 = turned && !INTER ? it : 2 * it, d1 = turned && !INTER ? it + half : 2 * it + 1;
             const T* src = static_cast<const T*>(key ? a.k : value ? a.v : a.q) +
@@ -274,9 +335,8 @@ int check_params(const verify_rotary_params* p, int32_t total_q, int32_t hq, int
 
 template <typename T, int D, bool APPEND>
 void launch(const RotArgs& a, const verify_rotary_params& p, bool wide, hipStream_t stream) {
-    const int heads = a.hq + (APPEND ? 2 : 1) * a.hkv;
     const dim3 grid((unsigned)(((int64_t)a.total_q + kTile - 1) / kTile),
-                    (unsigned)((heads + a.heads_per_wg - 1) / a.heads_per_wg));
+                    (unsigned)(a.key_wgs + a.value_wgs + (a.hq + a.heads_per_wg - 1) / a.heads_per_wg));
     auto run = [&](auto w, auto inter) {
         hipLaunchKernelGGL((rotate_rows<T, D, APPEND, decltype(w)::value, decltype(inter)::value>), grid,
                            dim3(kRotThreads), 0, stream, a);
@@ -292,15 +352,15 @@ int rotary_call(RotArgs& a, const verify_rotary_params& p, hipStream_t stream) {
     a.freqs = p.rotary_dim / 2;
     a.scale = p.scale > 0.f ? p.scale : 1.f;
     for (int f = 0; f < a.freqs; ++f) a.axis[f] = p.axis[f];
-    // Heads per workgroup: two where the rows are few (more workgroups, each done
-    // sooner), as many as leave four workgroups per compute unit otherwise (every
-    // workgroup computes its tile's angles).
-    const int heads = a.hq + (APPEND ? 2 : 1) * a.hkv;
+    // Query heads per workgroup: two where the rows are few (more workgroups, each done
+    // sooner), up to kQueryHeads otherwise (every workgroup computes its tile's angles).
     const int64_t tiles = ((int64_t)a.total_q + kTile - 1) / kTile;
-    const int64_t chunks = std::max<int64_t>(1, std::min<int64_t>((heads + 1) / 2, 4 * device_cus() / tiles));
-    a.heads_per_wg = (int)((heads + chunks - 1) / chunks);
+    const int64_t chunks = std::max<int64_t>(1, std::min<int64_t>((a.hq + 1) / 2, 8 * device_cus() / tiles));
+    a.heads_per_wg = (int)std::min<int64_t>((a.hq + chunks - 1) / chunks, kQueryHeads);
+    a.key_wgs = (a.hkv + kKeyHeads - 1) / kKeyHeads;
     const int esize = p.dtype == VERIFY_BF16 ? 2 : 4, n = 16 / esize;
-    uint64_t bits = (uint64_t)(uintptr_t)a.q | (uintptr_t)a.k | (uintptr_t)a.v | (uintptr_t)a.q_out | (uintptr_t)a.k_out;
+    if (APPEND) a.value_wgs = (a.hkv + value_heads(esize) - 1) / value_heads(esize);
+    const uint64_t bits = (uint64_t)(uintptr_t)a.q | (uintptr_t)a.k | (uintptr_t)a.v | (uintptr_t)a.q_out | (uintptr_t)a.k_out;
     const int64_t strides = a.q_stride | a.k_stride | a.v_stride | a.q_out_stride | a.k_out_stride;
     const int step = p.interleaved ? p.rotary_dim : a.freqs;
     const bool wide = (bits & 15) == 0 && strides % n == 0 && step % n == 0;
