@@ -13,11 +13,13 @@
 //                 joined into m_r and 1 / l_r as the rows are staged in LDS.
 // In both the rows stay and the keys stream past, the next step's loads in flight.
 // With more rows than LDS holds the second becomes
-//   weight_join, weight_sums_rows   the parts joined once, then the keys stay in
-//                 registers and the rows stream past (a prompt's rows are read once
-//                 per 64 keys, which the second level cache answers).
-// (A row's logarithm log2 l_r + m_r in the place of the two would be rounded at the
-// size of the scores, and every weight of the row with it.)
+//   weight_join, weight_sums_rows, weight_store   the parts joined once, then keys
+//                 stay in registers and the rows stream past through LDS.
+// What bounds it: few rows, the keys' bytes (32 requests of 475 MB of keys, 36 rows each:
+// 93 us per pass, 5.1 TB/s, as fast as a copy; both passes read them); many rows, the
+// exponentials, one per row and key and pass beside four other vector instructions (the
+// prompts named at weight_sums_rows' segments: 72 and 76 us, of which the matrix
+// instructions take 14 each).
 // Scores are MFMA products, the queries the first operand and 16 keys the second, so
 // that a lane holds one key (column) and four rows of every product.  A block's K tile
 // lies in memory as the operand wants it: 16 bytes per lane, 1 KiB per load, no LDS.
@@ -30,16 +32,16 @@ namespace {
 
 constexpr int kWgtWaves = 4;
 constexpr int kWgtThreads = kWgtWaves * kWave;
-constexpr int kRowWaves = 8;   // of a weight_sums_rows workgroup
 constexpr float kWgtLog2e = 1.4426950408889634f;
 // 16-row tiles of a weight_stats workgroup at most
-constexpr int kStatTiles = 4;
+constexpr int kStatTiles = 8;
 
 typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
 typedef int i32x4_t __attribute__((ext_vector_type(4)));
 // queries are aligned to their elements only
 typedef uint32_t u32x4u_t __attribute__((ext_vector_type(4), aligned(2)));
+typedef float f32x4u_t __attribute__((ext_vector_type(4), aligned(8)));
 
 struct WgtArgs {
     const void* q;
@@ -53,12 +55,16 @@ struct WgtArgs {
     float* key_weights;
     int32_t* key_order;
     float2* part;  // (maximum, sum relative to it) of each row and split, see part_of
+    float2* rows;  // (maximum, 1 / sum) of each row: [request][KV head][row], 16 more behind the last
     int num_seqs, total_q, hq, hkv, group, max_blocks, num_blocks, max_seq_len;
     float scale_log2, decay;
     uint32_t group_magic;        // ceil(2^32 / group)
     int splits, split_blocks;    // of weight_stats
     int chunks;                  // row chunks in its grid
     int sum_blocks;              // blocks of a weight_sums workgroup
+    int segments, segment_tiles; // of weight_sums_rows
+    int64_t sum_keys;            // keys of a segment's sums
+    float* sums;                 // [requests][Hkv][segments][sum_keys]
     int lds_tiles;               // row tiles that weight_sums holds in LDS
 };
 
@@ -85,6 +91,10 @@ __device__ __forceinline__ WgtGeom wgt_geom(const WgtArgs& a, int i) {
 // The parts of row r of KV head g: [request][KV head][row][splits].
 __device__ __forceinline__ float2* part_of(const WgtArgs& a, const WgtGeom& geo, int g, int r) {
     return a.part + ((int64_t)geo.q0 * a.hq + (int64_t)g * geo.rows + r) * a.splits;
+}
+
+__device__ __forceinline__ float2* rows_of(const WgtArgs& a, const WgtGeom& geo, int g) {
+    return a.rows + (int64_t)geo.q0 * a.hq + (int64_t)g * geo.rows;
 }
 
 // Operands of 16 rows or keys over the head dim: NC 16-byte chunks per lane, chunk c
@@ -130,6 +140,10 @@ __device__ __forceinline__ void stage_rows(const WgtArgs& a, const WgtGeom& geo,
         const int lane = e % kWave, c = e / kWave % NC, tile = e / kWave / NC;
         int r = first + tile * 16 + lane % 16;
         if (r >= geo.rows) r = first;
+        if (geo.rows == 0) {
+            lds[e] = make_uint4(0, 0, 0, 0);
+            continue;
+        }
         const int j = by_group(a, r), h = r - j * a.group;
         const T* src = static_cast<const T*>(a.q) + ((int64_t)(geo.q0 + j) * a.hq + g * a.group + h) * D +
                        (4 * c + lane / 16) * (16 / (int)sizeof(T));
@@ -153,6 +167,8 @@ __device__ __forceinline__ void load_keys(const WgtArgs& a, int g, int phys, Ope
 // registers, 8 or 16 KiB of loads in flight), and where they stay.
 constexpr int step_blocks(int d, bool bf16) { return d == 128 && !bf16 ? 1 : 2; }
 constexpr int held_blocks(int d, bool bf16) { return d == 128 && !bf16 ? 2 : 4; }
+// Row tiles that then go by together: 16 KiB.
+constexpr int row_tiles(int d, bool bf16) { return 16 * 1024 / (16 * d * (bf16 ? 2 : 4)); }
 
 // Row slack: a row's sum is kept relative to a maximum that may be exceeded by this
 // many powers of two before the sum is rescaled (rarely, then).
@@ -183,6 +199,9 @@ struct Walk {
                 const int lane = threadIdx.x & (kWave - 1);
                 const int bl = b + lane / NB * (kWgtWaves * NB) + lane % NB;
                 ids = bl < b_hi ? table[bl] : -1;
+                // settled here, every 64 blocks: otherwise the compiler waits for it, and
+                // with it for the keys in flight, at every step's reading of the ids
+                __builtin_amdgcn_s_waitcnt(kWaitVmcnt0);
                 at = 0;
             }
 #pragma unroll
@@ -210,7 +229,8 @@ __global__ __launch_bounds__(kWgtThreads) void weight_stats(WgtArgs a) {
     __shared__ __attribute__((aligned(16))) int s_pos[RT * 16];
     const int i = blockIdx.y;
     const int g = blockIdx.x % a.hkv;
-    const int chunk0 = blockIdx.x / a.hkv % a.chunks, split = blockIdx.x / a.hkv / a.chunks;
+    // the last rows first: a prompt's see the most keys
+    const int chunk0 = a.chunks - 1 - blockIdx.x / a.hkv % a.chunks, split = blockIdx.x / a.hkv / a.chunks;
     const WgtGeom geo = wgt_geom(a, i);
     const int b_lo = split * a.split_blocks;
     if (b_lo >= geo.blocks) return;
@@ -232,8 +252,10 @@ __global__ __launch_bounds__(kWgtThreads) void weight_stats(WgtArgs a) {
                 m[r][e] = kNoScore;
                 l[r][e] = 0.f;
             }
+        // (also of a step without a valid block, and with no test before the first tile: if
+        // there is a way past their use, keys are waited for before their registers are
+        // loaded again, and the next step's with them)
         auto compute = [&](const Operand<T, D> (&k)[NB], uint32_t ok, int b) {
-            if (ok == 0) return;
             const bool masked = ok != (1u << NB) - 1 || (b + NB) * kBlockTokens - 1 > p_first;
             // keeps the query operands in LDS: hoisted out of the loop they would take
             // D / 8 (bf16) or D / 4 registers per tile
@@ -241,7 +263,7 @@ __global__ __launch_bounds__(kWgtThreads) void weight_stats(WgtArgs a) {
             asm volatile("" : "+v"(ql));
 #pragma unroll
             for (int r = 0; r < RT; ++r) {
-                if (r >= tiles) break;
+                if (r > 0 && r >= tiles) break;
                 uint4 qv[NC];
 #pragma unroll
                 for (int c = 0; c < NC; ++c) qv[c] = s_q[(r * NC + c) * kWave + ql];
@@ -257,20 +279,20 @@ __global__ __launch_bounds__(kWgtThreads) void weight_stats(WgtArgs a) {
                         for (int e = 0; e < 4; ++e) s[x][e] = t <= pos[e] ? s[x][e] : -INFINITY;
                     }
                 }
-                float top[4];
-                bool over = false;
+                // the scores as they enter the exponentials; one test for all of them
+                float top = -INFINITY;
+                auto relative = [&](int e, int x) { return fmaf(s[x][e], a.scale_log2, -m[r][e]); };
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    top[e] = s[0][e];
+                for (int e = 0; e < 4; ++e)
 #pragma unroll
-                    for (int x = 1; x < NB; ++x) top[e] = fmaxf(top[e], s[x][e]);
-                    top[e] *= a.scale_log2;
-                    over |= top[e] > m[r][e] + kSlackLog2;
-                }
-                if (__any(over)) {
+                    for (int x = 0; x < NB; ++x) top = fmaxf(top, relative(e, x));
+                if (__any(top > kSlackLog2)) {
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        const float mn = fmaxf(m[r][e], top[e]);
+                        float mn = s[0][e];
+#pragma unroll
+                        for (int x = 1; x < NB; ++x) mn = fmaxf(mn, s[x][e]);
+                        mn = fmaxf(m[r][e], mn * a.scale_log2);
                         l[r][e] *= __builtin_amdgcn_exp2f(m[r][e] - mn);
                         m[r][e] = mn;
                     }
@@ -278,7 +300,7 @@ __global__ __launch_bounds__(kWgtThreads) void weight_stats(WgtArgs a) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
 #pragma unroll
-                    for (int x = 0; x < NB; ++x) l[r][e] += __builtin_amdgcn_exp2f(fmaf(s[x][e], a.scale_log2, -m[r][e]));
+                    for (int x = 0; x < NB; ++x) l[r][e] += __builtin_amdgcn_exp2f(relative(e, x));
             }
         };
         Walk<T, D, NB> walk(a, table, g, b_lo + w * NB, b_hi);
@@ -288,15 +310,17 @@ __global__ __launch_bounds__(kWgtThreads) void weight_stats(WgtArgs a) {
         __syncthreads();  // the chunk before is done with the rows
         stage_rows<T, D>(a, geo, g, first, tiles, s_q, s_pos);
         __syncthreads();
-        while (b < b_hi) {
+        // in pairs of steps, without a way out between a step's loads and their use
+        constexpr int STEP = kWgtWaves * NB;
+        int steps = b < b_hi ? (b_hi - b + STEP - 1) / STEP : 0;
+        for (; steps > 1; steps -= 2) {
             ok1 = walk.load(k1, phys);
             compute(k0, ok0, b);
-            b += kWgtWaves * NB;
-            if (b >= b_hi) break;
             ok0 = walk.load(k0, phys);
-            compute(k1, ok1, b);
-            b += kWgtWaves * NB;
+            compute(k1, ok1, b + STEP);
+            b += 2 * STEP;
         }
+        if (steps > 0) compute(k0, ok0, b);
         // join the 16 columns, then the wavefronts
 #pragma unroll
         for (int r = 0; r < RT; ++r)
@@ -325,11 +349,18 @@ __global__ __launch_bounds__(kWgtThreads) void weight_stats(WgtArgs a) {
 // A row's (m, 1 / l) from its splits' parts, and its head's sink.  A row without a
 // key has (inf, 0), and so has a place without a row: 2^(s - inf) * 0.
 __device__ __forceinline__ float2 join_parts(const WgtArgs& a, const float2* part, int nsplit, int h) {
+    constexpr int kRound = 8;  // loads in flight: one by one each cost a memory latency
     float M = kNoScore, L = 0.f;
-    for (int s = 0; s < nsplit; ++s) {
-        const float2 p = part[s];
-        const float mn = fmaxf(M, p.x);
-        L = L * __builtin_amdgcn_exp2f(M - mn) + p.y * __builtin_amdgcn_exp2f(p.x - mn);
+    for (int s0 = 0; s0 < nsplit; s0 += kRound) {
+        float2 p[kRound];
+#pragma unroll
+        for (int x = 0; x < kRound; ++x) p[x] = part[min(s0 + x, nsplit - 1)];
+        float mn = M;
+#pragma unroll
+        for (int x = 0; x < kRound; ++x) mn = fmaxf(mn, p[x].x);
+        L *= __builtin_amdgcn_exp2f(M - mn);
+#pragma unroll
+        for (int x = 0; x < kRound; ++x) L += s0 + x < nsplit ? p[x].y * __builtin_amdgcn_exp2f(p[x].x - mn) : 0.f;
         M = mn;
     }
     if (M == kNoScore) return make_float2(L == 0.f ? INFINITY : L, 0.f);  // (or every score was NaN)
@@ -395,7 +426,7 @@ __global__ __launch_bounds__(kWgtThreads) void weight_sums(WgtArgs a) {
     const int w = __builtin_amdgcn_readfirstlane(tid / kWave);
     const int32_t* table = a.block_tables + (int64_t)i * a.max_blocks;
     const int nsplit = (geo.blocks + a.split_blocks - 1) / a.split_blocks;
-    const int all_tiles = (geo.rows + 15) / 16;
+    const int all_tiles = max(1, (geo.rows + 15) / 16);
     Walk<T, D, NB> walk(a, table, g, b_lo + w * NB, b_hi);
     // lane group lg holds the weights of block x = lg of a step
     auto load_old = [&](uint32_t ok, const int (&phys)[NB], int b) {
@@ -427,14 +458,12 @@ __global__ __launch_bounds__(kWgtThreads) void weight_sums(WgtArgs a) {
         }
         __syncthreads();
         auto step = [&](const Operand<T, D> (&k)[NB], const int (&phys)[NB], uint32_t ok, int b) {
-            if (ok == 0) return;
             const float old = load_old(ok, phys, b);
             float sum[NB];
 #pragma unroll
             for (int x = 0; x < NB; ++x) sum[x] = 0.f;
-            for (int r = 0; r < tiles; ++r) {
-                const int last = min(r * 16 + 16, geo.rows - first * 16) - 1;
-                if (__builtin_amdgcn_readfirstlane(s_pos[last]) < b * kBlockTokens) continue;  // sees none of the keys
+            // (one tile at least, whatever there is: see weight_stats)
+            for (int r = 0; r == 0 || r < tiles; ++r) {
                 const bool masked = (b + NB) * kBlockTokens - 1 > __builtin_amdgcn_readfirstlane(s_pos[r * 16]);
                 uint4 qv[NC];
 #pragma unroll
@@ -465,125 +494,157 @@ __global__ __launch_bounds__(kWgtThreads) void weight_sums(WgtArgs a) {
                 else a.key_weights[at] += mine;
             }
         };
-        while (b < b_hi) {
+        constexpr int STEP = kWgtWaves * NB;
+        int steps = b < b_hi ? (b_hi - b + STEP - 1) / STEP : 0;
+        for (; steps > 1; steps -= 2) {
             ok1 = go.load(k1, phys1);
             step(k0, phys0, ok0, b);
-            b += kWgtWaves * NB;
-            if (b >= b_hi) break;
             ok0 = go.load(k0, phys0);
-            step(k1, phys1, ok1, b);
-            b += kWgtWaves * NB;
+            step(k1, phys1, ok1, b + STEP);
+            b += 2 * STEP;
         }
+        if (steps > 0) step(k0, phys0, ok0, b);
     }
 }
 
-// Many rows: the parts of every row joined, once, into the first of them.
+// Many rows: the parts of every row joined, once.
 __global__ __launch_bounds__(kWgtThreads) void weight_join(WgtArgs a) {
     const int i = blockIdx.y;
     const WgtGeom geo = wgt_geom(a, i);
     const int nsplit = (geo.blocks + a.split_blocks - 1) / a.split_blocks;
     const int g = blockIdx.x % a.hkv;
-    for (int r = blockIdx.x / a.hkv * kWgtThreads + threadIdx.x; r < geo.rows; r += gridDim.x / a.hkv * kWgtThreads) {
-        float2* part = part_of(a, geo, g, r);
-        part[0] = join_parts(a, part, nsplit, g * a.group + r - by_group(a, r) * a.group);
-    }
+    for (int r = blockIdx.x / a.hkv * kWgtThreads + threadIdx.x; r < geo.rows; r += gridDim.x / a.hkv * kWgtThreads)
+        rows_of(a, geo, g)[r] = join_parts(a, part_of(a, geo, g, r), nsplit, g * a.group + r - by_group(a, r) * a.group);
 }
 
-// Many rows: grid (KV heads x steps of NB blocks, requests).  The wavefronts hold the
-// same keys and share out the row tiles, which stream past from memory (the second
-// level cache, where the steps of a KV head meet); their sums meet at the end.
+// Many rows: grid (KV heads x segments of the rows x ranges of sum_blocks blocks,
+// requests).  Every wavefront holds keys of its own, and the segment's rows go by in
+// LDS, 16 KiB at a time, the next ones in flight: read by every wavefront for itself
+// (eight on the same 64 keys) they cost 92 us of the prompts' pass, since a KV head's
+// query rows lie 1 KiB in 8 and meet in a quarter of the second level cache.
+// Prompts are cut into segments because the rows are uneven work: the first keys are
+// seen by all of them, the last by few.  weight_store adds the segments' sums.
 template <typename T, int D>
-__global__ __launch_bounds__(kRowWaves * kWave) void weight_sums_rows(WgtArgs a) {
+__global__ __launch_bounds__(kWgtThreads) void weight_sums_rows(WgtArgs a) {
     constexpr int NB = held_blocks(D, sizeof(T) == 2), NC = Operand<T, D>::NC;
-    __shared__ float s_sum[kRowWaves][NB * kBlockTokens];
+    constexpr int CT = row_tiles(D, sizeof(T) == 2);       // tiles of a chunk
+    constexpr int LD = CT * NC * kWave / kWgtThreads;      // 16-byte pieces of it per thread
+    constexpr int ROWS = CT * 16;
+    __shared__ uint4 s_q[2][CT * NC * kWave];
+    __shared__ __attribute__((aligned(16))) float2 s_mi[2][ROWS];  // the rows' m and 1 / l
     const int i = blockIdx.y;
-    const int g = blockIdx.x % a.hkv, b = blockIdx.x / a.hkv * NB;
+    const int g = blockIdx.x % a.hkv, segment = blockIdx.x / a.hkv % a.segments;
+    const int b_lo = blockIdx.x / a.hkv / a.segments * a.sum_blocks;
     const WgtGeom geo = wgt_geom(a, i);
-    if (b >= geo.blocks) return;
+    if (b_lo >= geo.blocks) return;
     const int tid = threadIdx.x, lane = tid & (kWave - 1), l16 = lane & 15, lg = lane >> 4;
     const int w = __builtin_amdgcn_readfirstlane(tid / kWave);
     const int32_t* table = a.block_tables + (int64_t)i * a.max_blocks;
-    const int p0 = geo.S - geo.n;
+    const int p0 = geo.S - geo.n, b = b_lo + w * NB;
     Walk<T, D, NB> walk(a, table, g, b, geo.blocks);
     Operand<T, D> k[NB];
     int phys[NB] = {};
     const uint32_t ok = walk.load(k, phys);
-    if (ok == 0) return;
     float sum[NB];
 #pragma unroll
     for (int x = 0; x < NB; ++x) sum[x] = 0.f;
-    // from the tile of the first row that sees the first key
-    const int64_t skip = max((int64_t)0, (int64_t)b * kBlockTokens - p0) * a.group;
-    const int all_tiles = (geo.rows + 15) / 16;
-    const float2* part = part_of(a, geo, g, 0);
-    struct Rows {
-        uint4 q[NC];
-        f32x4_t m, inv;
-    };
-    auto load = [&](int tile, Rows& v) {
-        // a place without a row: the tile's first row, with weight 0
-        int r = tile * 16 + l16;
-        if (r >= geo.rows) r = tile * 16;
-        const int j = by_group(a, r), h = r - j * a.group;
-        const T* src = static_cast<const T*>(a.q) + ((int64_t)(geo.q0 + j) * a.hq + g * a.group + h) * D +
-                       lg * (16 / (int)sizeof(T));
+
+    // the segment's tiles, from that of the first row that sees the range's first key
+    const int64_t skip = max((int64_t)0, (int64_t)b_lo * kBlockTokens - p0) * a.group;
+    const int64_t first = max(skip / 16, (int64_t)segment * a.segment_tiles);
+    const int last = (int)min((int64_t)(geo.rows + 15) / 16, (int64_t)(segment + 1) * a.segment_tiles);
+    const int chunks = first < last ? ((int)(last - first) + CT - 1) / CT : 0;
+    const float2* stats = rows_of(a, geo, g);
+    uint4 qr[LD];
+    float2 mr;
+    auto load = [&](int chunk) {
+        const int row0 = ((int)first + chunk * CT) * 16;
 #pragma unroll
-        for (int c = 0; c < NC; ++c) {
-            const u32x4u_t x = *reinterpret_cast<const u32x4u_t*>(src + c * (64 / (int)sizeof(T)));
-            v.q[c] = make_uint4(x.x, x.y, x.z, x.w);
+        for (int x = 0; x < LD; ++x) {
+            const int e = x * kWgtThreads + tid, ln = e % kWave, c = e / kWave % NC, tile = e / kWave / NC;
+            const int r = min(row0 + tile * 16 + ln % 16, geo.rows - 1);  // (a place without a row: the last one)
+            const int j = by_group(a, r), h = r - j * a.group;
+            const T* src = static_cast<const T*>(a.q) + ((int64_t)(geo.q0 + j) * a.hq + g * a.group + h) * D +
+                           (4 * c + ln / 16) * (16 / (int)sizeof(T));
+            const u32x4u_t v = *reinterpret_cast<const u32x4u_t*>(src);
+            qr[x] = make_uint4(v.x, v.y, v.z, v.w);
         }
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const int rr = tile * 16 + lg * 4 + e;
-            const float2 mi = part[(int64_t)min(rr, geo.rows - 1) * a.splits];
-            v.m[e] = rr < geo.rows ? mi.x : INFINITY;
-            v.inv[e] = rr < geo.rows ? mi.y : 0.f;
-        }
+        mr = stats[min(row0 + tid % ROWS, geo.rows - 1)];
     };
-    auto add = [&](int tile, const Rows& v) {
-        const bool masked = (b + NB) * kBlockTokens - 1 > p0 + by_group(a, tile * 16);
-        i32x4_t pos = {};
-        if (masked) {
+    auto put = [&](int buf) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int rr = tile * 16 + lg * 4 + e;
-                pos[e] = rr < geo.rows ? p0 + by_group(a, rr) : -1;
-            }
-        }
-        add_tile<T, D, NB>(a, v.q, k, v.m, v.inv, masked, pos, b, sum);
+        for (int x = 0; x < LD; ++x) s_q[buf][x * kWgtThreads + tid] = qr[x];
+        if (tid < ROWS) s_mi[buf][tid] = mr;
     };
-    // the loads of the next tile in flight, the last one's again at the end
-    int tile = (int)min(skip / 16, (int64_t)all_tiles) + w;
-    if (tile < all_tiles) {
-        Rows r0, r1;
-        load(tile, r0);
-        for (;;) {
-            const int next = tile + kRowWaves;
-            load(min(next, all_tiles - 1), r1);
-            add(tile, r0);
-            if (next >= all_tiles) break;
-            tile = next + kRowWaves;
-            load(min(tile, all_tiles - 1), r0);
-            add(next, r1);
-            if (tile >= all_tiles) break;
-        }
+    if (chunks > 0) {
+        load(0);
+        put(0);
     }
+    __syncthreads();
+    for (int chunk = 0; chunk < chunks; ++chunk) {
+        const int buf = chunk & 1;
+        load(min(chunk + 1, chunks - 1));
+        for (int t = 0; t < CT; ++t) {
+            const int row = ((int)first + chunk * CT + t) * 16;
+            if (row >= last * 16 || row >= geo.rows) break;
+            const int p_lo = p0 + by_group(a, row), p_hi = p0 + by_group(a, min(row + 16, geo.rows) - 1);
+            if (p_hi < b * kBlockTokens) continue;  // none of its rows sees the wavefront's keys
+            const bool masked = (b + NB) * kBlockTokens - 1 > p_lo || row + 16 > geo.rows;
+            i32x4_t pos = {};
+            if (masked) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int rr = row + lg * 4 + e;
+                    pos[e] = rr < geo.rows ? p0 + by_group(a, rr) : -1;
+                }
+            }
+            uint4 qv[NC];
+#pragma unroll
+            for (int c = 0; c < NC; ++c) qv[c] = s_q[buf][(t * NC + c) * kWave + lane];
+            const f32x4_t x = *reinterpret_cast<const f32x4_t*>(&s_mi[buf][t * 16 + lg * 4]);
+            const f32x4_t y = *reinterpret_cast<const f32x4_t*>(&s_mi[buf][t * 16 + lg * 4 + 2]);
+            add_tile<T, D, NB>(a, qv, k, f32x4_t{x[0], x[2], y[0], y[2]}, f32x4_t{x[1], x[3], y[1], y[3]}, masked, pos, b, sum);
+        }
+        put(buf ^ 1);
+        __syncthreads();
+    }
+    // the four lane groups hold different rows of the same 16 keys
+    float mine = 0.f;
+    int block = 0;
+    bool store = false;
 #pragma unroll
     for (int x = 0; x < NB; ++x) {
         sum[x] += __shfl_xor(sum[x], 16);
         sum[x] += __shfl_xor(sum[x], 32);
-        if (lg == 0) s_sum[w][x * kBlockTokens + l16] = sum[x];
+        if (lg == x) {
+            mine = sum[x];
+            block = phys[x];
+            store = (ok >> x) & 1u;
+        }
     }
-    __syncthreads();
-    const int t = b * kBlockTokens + tid;
-    if (tid < NB * kBlockTokens && t < geo.S && ((ok >> (tid / kBlockTokens)) & 1u)) {
-        float v = 0.f;
-#pragma unroll
-        for (int x = 0; x < kRowWaves; ++x) v += s_sum[x][tid];
-        const int64_t at = ((int64_t)table[t / kBlockTokens] * a.hkv + g) * kBlockTokens + l16;
-        const float old = t < p0 && a.decay != 0.f ? a.key_weights[at] : 0.f;
-        store_weight(a, geo, i, at, t, v, old);
+    const int t = (b + lg) * kBlockTokens + l16;
+    if (!store || t >= geo.S) return;
+    if (a.segments > 1) {
+        a.sums[(((int64_t)i * a.hkv + g) * a.segments + segment) * a.sum_keys + t] = mine;
+        return;
     }
+    const int64_t at = ((int64_t)block * a.hkv + g) * kBlockTokens + l16;
+    store_weight(a, geo, i, at, t, mine, t < p0 && a.decay != 0.f ? a.key_weights[at] : 0.f);
+}
+
+// Grid (KV heads x 256 keys, requests).
+__global__ __launch_bounds__(kWgtThreads) void weight_store(WgtArgs a) {
+    const int i = blockIdx.y, g = blockIdx.x % a.hkv, t = blockIdx.x / a.hkv * kWgtThreads + threadIdx.x;
+    const WgtGeom geo = wgt_geom(a, i);
+    if (t >= geo.S) return;
+    const int id = a.block_tables[(int64_t)i * a.max_blocks + t / kBlockTokens];
+    if (id < 0 || id >= a.num_blocks) return;
+    const float* sums = a.sums + ((int64_t)i * a.hkv + g) * a.segments * a.sum_keys + t;
+    float v = 0.f;
+#pragma unroll 4
+    for (int x = 0; x < a.segments; ++x) v += sums[(int64_t)x * a.sum_keys];
+    const int64_t at = ((int64_t)id * a.hkv + g) * kBlockTokens + t % kBlockTokens;
+    store_weight(a, geo, i, at, t, v, a.decay != 0.f && t < geo.S - geo.n ? a.key_weights[at] : 0.f);
 }
 
 // ------------------------------------------------------------------ host side
@@ -594,12 +655,16 @@ struct WgtPlan {
     int lds_tiles, sum_blocks, ranges;
     int stat_rows;           // rows times the group of a request, about
     bool once;
-    size_t bytes, cover;
+    int segments, segment_tiles;
+    int64_t sum_keys;
+    size_t rows_at, sums_at, bytes, cover;
 };
 
 int64_t tile_bytes(const verify_attn_params& p) {
     return 16 * (int64_t)p.head_dim * (p.dtype == VERIFY_BF16 ? 2 : 4);
 }
+
+constexpr int64_t kSumWgs = 2048;  // (request, KV head, range, segment)s that segments are made towards
 
 int make_plan(const verify_attn_params& p, int32_t total_q, int32_t max_q_len, int32_t max_seq_len, WgtPlan* out) {
     WgtPlan pl{};
@@ -609,11 +674,19 @@ int make_plan(const verify_attn_params& p, int32_t total_q, int32_t max_q_len, i
         1, std::min<int64_t>(((int64_t)max_seq_len + kBlockTokens - 1) / kBlockTokens, p.max_blocks_per_seq));
     const bool bf16 = p.dtype == VERIFY_BF16;
     const int64_t step = kWgtWaves * step_blocks(p.head_dim, bf16);  // blocks of a workgroup's step
-    pl.stat_tiles = (int)std::min<int64_t>(tiles, kStatTiles);
-    pl.chunks = (int)std::min<int64_t>((tiles + kStatTiles - 1) / kStatTiles, 4096);
-    // a split has at most 128 blocks, and at least a step, towards four workgroups per
-    // compute unit
-    const int64_t want = 4 * 256, most = (blocks + step - 1) / step, least = pl.chunks > 1 ? (blocks + 1023) / 1024 : (blocks + 127) / 128;
+    // Every row chunk reads the keys again: as few as hold the tiles, evenly (64 requests
+    // of 72 rows, head dim 64: 418 us with four tiles each, 294 with all five).  A
+    // prompt's keys come from the cache, and it is better off with more wavefronts in a
+    // compute unit (139 us with four tiles each, 157 with eight).
+    const int64_t parts = tiles > 32 ? (tiles + 3) / 4 : (tiles + kStatTiles - 1) / kStatTiles;
+    pl.stat_tiles = (int)((tiles + parts - 1) / parts);
+    pl.chunks = (int)std::min<int64_t>(parts, 4096);
+    // A split has at least a step, and at most 128 blocks, towards two workgroups per
+    // compute unit in bf16 (eight requests of 2000 to 4096 keys, 36 rows: 29 us with 512
+    // workgroups, 37 with 1024, 45 with 2048: each stages the rows and joins their parts)
+    // and eight in fp32, whose products take 16 times as long and are better spread (six
+    // requests of 500 to 4100 keys, 40 rows, head dim 64: 38, 38 and 30 us).
+    const int64_t want = bf16 ? 512 : 2048, most = (blocks + step - 1) / step, least = pl.chunks > 1 ? (blocks + 1023) / 1024 : (blocks + 127) / 128;
     const int64_t wgs = (int64_t)p.num_kv_heads * pl.chunks;
     auto splits = [&](int64_t seqs) { return std::max(least, std::min(most, (want + seqs * wgs - 1) / (seqs * wgs))); };
     const int64_t ns = splits(std::max(1, p.num_seqs));
@@ -624,19 +697,34 @@ int make_plan(const verify_attn_params& p, int32_t total_q, int32_t max_q_len, i
         pl.lds_tiles = (int)tiles;
         pl.sum_blocks = pl.split_blocks;
     } else {
-        pl.sum_blocks = held_blocks(p.head_dim, bf16);
-        pl.stat_rows = pl.chunks * kStatTiles * 16;
+        pl.sum_blocks = kWgtWaves * held_blocks(p.head_dim, bf16);
+        pl.stat_rows = (int)std::min<int64_t>(tiles * 16, 1 << 20);
+        // segments of 16 tiles at least, towards eight workgroups per compute unit (of a
+        // prompt's half have nothing to do): two prompts of 2531 and 1300 rows, four heads
+        // per KV head, 96 us in 6 segments, 76 in 12 and 16, 74 in 48, but then 14 instead
+        // of 5 to add them
+        const int64_t whole = std::max<int64_t>(1, p.num_seqs) * p.num_kv_heads * ((blocks + pl.sum_blocks - 1) / pl.sum_blocks);
+        pl.segments = (int)std::max<int64_t>(1, std::min<int64_t>({16, tiles / 16, kSumWgs / whole}));
+        pl.segment_tiles = (int)std::min<int64_t>((tiles + pl.segments - 1) / pl.segments, 1 << 27);
     }
     // a grid dimension holds fewer than 2^32 threads
-    const int64_t ranges = (blocks + pl.sum_blocks - 1) / pl.sum_blocks;
+    const int64_t ranges = (blocks + pl.sum_blocks - 1) / pl.sum_blocks * std::max(1, pl.segments);
     pl.ranges = (int)ranges;
     if (std::max<int64_t>(pl.splits * wgs, ranges * p.num_kv_heads) >= (1 << 24)) return VERIFY_EUNSUPPORTED;
     const size_t row = (size_t)p.num_q_heads * sizeof(float2);
-    pl.bytes = align_up(row * total_q * pl.splits, 256);
+    // the parts, and with many rows what they join into
+    pl.rows_at = align_up(row * total_q * pl.splits, 256);
+    const size_t joined = pl.once || total_q == 0 ? 0 : align_up(row * total_q + 16 * sizeof(float2), 256);
+    pl.sum_keys = blocks * kBlockTokens;
+    const size_t sums = pl.segments > 1 ? align_up((size_t)p.num_seqs * p.num_kv_heads * pl.segments * pl.sum_keys * sizeof(float), 256) : 0;
+    pl.sums_at = pl.rows_at + joined;
+    pl.bytes = pl.sums_at + sums;
     // Any batch of fewer requests: b of them have at most b max_q_len rows and
     // want / (b wgs) + 1 splits, or `least`.
     const int64_t few = ((int64_t)std::max(1, max_q_len) * want + wgs - 1) / wgs + total_q;
-    pl.cover = std::max(pl.bytes, align_up(row * (size_t)std::max(std::min(few, (int64_t)total_q * most), (int64_t)total_q * least), 256));
+    pl.cover = std::max(pl.bytes, align_up(row * (size_t)std::max(std::min(few, (int64_t)total_q * most), (int64_t)total_q * least), 256) + joined);
+    if (!pl.once)  // fewer requests may have more segments: kSumWgs of them at most in all
+        pl.cover += std::max(sums, align_up((size_t)(kSumWgs / ((blocks + pl.sum_blocks - 1) / pl.sum_blocks)) * pl.sum_keys * sizeof(float), 256));
     *out = pl;
     return VERIFY_OK;
 }
@@ -652,6 +740,8 @@ void launch(const WgtArgs& a, const WgtPlan& pl, hipStream_t stream) {
         case 1: run(std::integral_constant<int, 1>{}); break;
         case 2: run(std::integral_constant<int, 2>{}); break;
         case 3: run(std::integral_constant<int, 3>{}); break;
+        case 4: run(std::integral_constant<int, 4>{}); break;
+        case 5: case 6: run(std::integral_constant<int, 6>{}); break;
         default: run(std::integral_constant<int, kStatTiles>{});
     }
     if (pl.once) {
@@ -661,7 +751,9 @@ void launch(const WgtArgs& a, const WgtPlan& pl, hipStream_t stream) {
     }
     const dim3 join((unsigned)((pl.stat_rows + kWgtThreads - 1) / kWgtThreads * a.hkv), seqs);
     hipLaunchKernelGGL(weight_join, join, dim3(kWgtThreads), 0, stream, a);
-    hipLaunchKernelGGL((weight_sums_rows<T, D>), sums, dim3(kRowWaves * kWave), 0, stream, a);
+    hipLaunchKernelGGL((weight_sums_rows<T, D>), sums, dim3(kWgtThreads), 0, stream, a);
+    const dim3 store((unsigned)((pl.sum_keys + kWgtThreads - 1) / kWgtThreads * a.hkv), seqs);
+    if (a.segments > 1) hipLaunchKernelGGL(weight_store, store, dim3(kWgtThreads), 0, stream, a);
 }
 
 int check(const verify_attn_params* p, int32_t total_q, int32_t max_q_len, int32_t max_seq_len) {
@@ -718,6 +810,7 @@ extern "C" int verify_key_weights(const verify_attn_params* params, int32_t tota
     a.key_weights = key_weights;
     a.key_order = key_order;
     a.part = static_cast<float2*>(workspace);
+    a.rows = reinterpret_cast<float2*>(static_cast<char*>(workspace) + pl.rows_at);
     a.num_seqs = p.num_seqs;
     a.total_q = total_q;
     a.hq = p.num_q_heads;
@@ -734,6 +827,10 @@ extern "C" int verify_key_weights(const verify_attn_params* params, int32_t tota
     a.chunks = pl.chunks;
     a.sum_blocks = pl.sum_blocks;
     a.lds_tiles = pl.lds_tiles;
+    a.segments = pl.segments;
+    a.segment_tiles = pl.segment_tiles;
+    a.sum_keys = pl.sum_keys;
+    a.sums = reinterpret_cast<float*>(static_cast<char*>(workspace) + pl.sums_at);
     if (p.dtype == VERIFY_BF16)
         p.head_dim == 128 ? launch<uint16_t, 128>(a, pl, stream) : launch<uint16_t, 64>(a, pl, stream);
     else

@@ -53,6 +53,9 @@ def _weights_case(rng, S, n, hkv, G, d, dtype, *, rows=None, lost=None, sinks=Fa
     ([300, 0, 33, 129], [9, 0, 33, 0], 1, 5, dict(lost=[100, 0, 0, 7], decay=0.5)),
     ([70, 150], [70, 150], 1, 2, dict(sinks=True)),              # whole prompts
     ([260, 31, 5], [40, 31, 5], 1, 8, dict(rows=[37, 1, 9])),    # more rows than one staging holds
+    ([140, 31], [15, 9], 2, 8, {}),                              # eight row tiles, all in one workgroup
+    ([140, 31], [9, 16], 1, 16, {}),                             # ten, in two even parts
+    ([900], [300], 1, 4, dict(rows=[299])),                      # rows in segments
     ([200, 90], [5, 17], 2, 1, dict(unmapped=3, decay=0.0)),
     ([400, 37], [6, 20], 1, 8, dict(size=15.0, sinks=True)),     # peaked rows
     ([100, 80], [30, 40], 2, 8, dict(max_q_len=2)),              # more rows than announced
