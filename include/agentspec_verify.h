@@ -572,6 +572,7 @@ int verify_rotary_append(const verify_attn_params *attn, const verify_rotary_par
  *                max_seq_len and to 16 * max_blocks_per_seq; n_i may exceed
  *                max_q_len, which only sizes the launch)
  *   decay        finite, >= 0
+ *   VERIFY_EUNSUPPORTED from total_q G (G - 1) = 2^32 on, G = Hq / Hkv.
  *   workspace    at least verify_key_weights_workspace_size() bytes for the same
  *                arguments, or for those of a batch of more requests and rows with
  *                the same other arguments; its contents on entry are ignored

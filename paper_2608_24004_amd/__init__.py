@@ -703,13 +703,13 @@ def verify_kv_append(k_new, v_new, k_cache, v_cache, block_tables, seq_lens, q_s
 
 
 def _scratch(shape, dtype, dev, stream):
-    """A tensor that a call on `stream` (None: the current one) uses: memory freed
-    before the call is done is not handed to the current stream meanwhile."""
+    """A tensor that a call on `stream` (None: the current one) uses, from that
+    stream's memory: its last use there is over before this one begins."""
     import torch
-    t = torch.empty(shape, dtype=dtype, device=dev)
-    if stream is not None and t.is_cuda:
-        t.record_stream(stream)
-    return t
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=dev)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=dev)
 
 
 _current_device = None
@@ -733,17 +733,18 @@ def _launch(where, idx, *args):
         _check(rc, where)
 
 
-def _rows_arg(t, name, heads, D, dtype, idx, device, T=None):
+def _rows_arg(t, name, heads, D, dtype, idx, device, T):
     """Address and row stride of packed rows [T, heads, D]: contiguous, or a slice
     of wider rows (heads and dims adjacent, any row stride that holds them)."""
-    shape = (t.shape[0] if T is None else T, heads, D)
-    if t.is_contiguous():
-        return _arg(t, name, shape, dtype, idx, device), heads * D
-    _expect(t, name, shape, dtype, device)
-    st, row = t.stride(), t.stride(0) if shape[0] > 1 else heads * D
-    if (D > 1 and st[2] != 1) or (heads > 1 and st[1] != D) or row < heads * D:
+    shape = (T, heads, D)
+    if not (t is not None and t.dtype is dtype and t.get_device() == idx >= 0 and t.shape == shape):
+        _expect(t, name, shape, dtype, device)
+    st = t.stride()
+    if T <= 1:
+        st = (heads * D,) + st[1:]  # one row has no stride
+    if (st[2] != 1 and D > 1) or (st[1] != D and heads > 1) or st[0] < heads * D:
         raise ValueError("%s must be rows of %d x %d adjacent elements, got strides %s" % (name, heads, D, tuple(st)))
-    return t.data_ptr(), row
+    return t.data_ptr(), st[0]
 
 
 _rotary_params = {}
@@ -794,7 +795,7 @@ def verify_rotary(q, k, positions, inv_freq, *, axes=None, interleaved: bool = F
     dtype, dev = q.dtype, q.device
     idx = dev.index if dev.type == "cuda" else -1
     Hkv = 0 if k is None else k.shape[1]
-    p_q, s_q = _rows_arg(q, "q", Hq, D, dtype, idx, dev)
+    p_q, s_q = _rows_arg(q, "q", Hq, D, dtype, idx, dev, T)
     p_k, s_k = (None, 0) if k is None else _rows_arg(k, "k", Hkv, D, dtype, idx, dev, T)
     params, p_pos, p_freq = _rotary_args(q, positions, inv_freq, axes, interleaved, scale, idx, dev)
     if q_out is None:
@@ -823,7 +824,7 @@ def verify_rotary_append(q, k_new, v_new, positions, inv_freq, k_cache, v_cache,
     T, Hq, D = q.shape
     dtype, dev = q.dtype, q.device
     idx = dev.index if dev.type == "cuda" else -1
-    p_q, s_q = _rows_arg(q, "q", Hq, D, dtype, idx, dev)
+    p_q, s_q = _rows_arg(q, "q", Hq, D, dtype, idx, dev, T)
     (p_kc, p_vc, *desc), attn = _layer_args(Hq, D, dtype, q.element_size(), idx, dev, k_cache, v_cache, block_tables,
                                             seq_lens, q_start)
     Hkv = k_cache.shape[1]

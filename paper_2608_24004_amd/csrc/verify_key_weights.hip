@@ -68,7 +68,7 @@ struct WgtArgs {
     int lds_tiles;               // row tiles that weight_sums holds in LDS
 };
 
-// r / group: exact below 2^32 / group, far above any number of rows.
+// r / group: exact where r (group - 1) < 2^32, which the host checks.
 __device__ __forceinline__ int by_group(const WgtArgs& a, int r) {
     return a.group == 1 ? r : (int)__umulhi((uint32_t)r, a.group_magic);
 }
@@ -552,7 +552,9 @@ __global__ __launch_bounds__(kWgtThreads) void weight_sums_rows(WgtArgs a) {
     // the segment's tiles, from that of the first row that sees the range's first key
     const int64_t skip = max((int64_t)0, (int64_t)b_lo * kBlockTokens - p0) * a.group;
     const int64_t first = max(skip / 16, (int64_t)segment * a.segment_tiles);
-    const int last = (int)min((int64_t)(geo.rows + 15) / 16, (int64_t)(segment + 1) * a.segment_tiles);
+    // (the last segment takes the rows past those announced, too)
+    const int all = (geo.rows + 15) / 16;
+    const int last = segment == a.segments - 1 ? all : (int)min((int64_t)all, (int64_t)(segment + 1) * a.segment_tiles);
     const int chunks = first < last ? ((int)(last - first) + CT - 1) / CT : 0;
     const float2* stats = rows_of(a, geo, g);
     uint4 qr[LD];
@@ -760,6 +762,8 @@ int check(const verify_attn_params* p, int32_t total_q, int32_t max_q_len, int32
     const int rc = validate(p, total_q, max_q_len, max_seq_len);
     if (rc != VERIFY_OK) return rc;
     if (p->sliding_window > 0) return VERIFY_EUNSUPPORTED;
+    const int64_t group = p->num_q_heads / p->num_kv_heads;
+    if (group > 65536 || (total_q + 1) * group * (group - 1) >= ((int64_t)1 << 32)) return VERIFY_EUNSUPPORTED;
     return VERIFY_OK;
 }
 

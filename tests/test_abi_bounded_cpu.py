@@ -128,6 +128,8 @@ def test_key_weights_arguments():
     assert _weights(_attn(), have=0) == _weights(_attn(), ws=None) == av.EWORKSPACE
     # a grid that no launch holds
     assert _weights(_attn(num_q_heads=4096, num_kv_heads=4096, max_blocks_per_seq=1 << 26), ms=(1 << 30)) == av.EUNSUPPORTED
+    # a group that the row arithmetic does not hold
+    assert _weights(_attn(num_q_heads=8192, num_kv_heads=1), T=64) == av.EUNSUPPORTED
     assert _weights(_attn(num_seqs=0), T=0, have=0, ws=None) == av.OK
 
 

@@ -56,6 +56,8 @@ def _weights_case(rng, S, n, hkv, G, d, dtype, *, rows=None, lost=None, sinks=Fa
     ([140, 31], [15, 9], 2, 8, {}),                              # eight row tiles, all in one workgroup
     ([140, 31], [9, 16], 1, 16, {}),                             # ten, in two even parts
     ([900], [300], 1, 4, dict(rows=[299])),                      # rows in segments
+    ([700, 400], [300, 20], 1, 4, dict(max_q_len=130)),          # segments, and more rows than announced
+    ([30, 40], [0, 0], 2, 4, dict(decay=0.75, max_q_len=3)),     # no row at all
     ([200, 90], [5, 17], 2, 1, dict(unmapped=3, decay=0.0)),
     ([400, 37], [6, 20], 1, 8, dict(size=15.0, sinks=True)),     # peaked rows
     ([100, 80], [30, 40], 2, 8, dict(max_q_len=2)),              # more rows than announced
