@@ -12,7 +12,8 @@
 //   weight_sums   a key's weights are added up within its lane; the splits' parts are
 //                 joined into m_r and 1 / l_r as the rows are staged in LDS.
 // In both the rows stay and the keys stream past, the next step's loads in flight.
-// With more rows than LDS holds the second becomes
+// Where the scores themselves are few (a decoding step) weight_stats stores them and
+// weight_sums reads those instead.  With more rows than LDS holds the second becomes
 //   weight_join, weight_sums_rows, weight_store   the parts joined once, then keys
 //                 stay in registers and the rows stream past through LDS.
 // What bounds it: few rows, the keys' bytes (32 requests of 475 MB of keys, 36 rows each:
@@ -65,6 +66,8 @@ struct WgtArgs {
     int segments, segment_tiles; // of weight_sums_rows
     int64_t sum_keys;            // keys of a segment's sums
     float* sums;                 // [requests][Hkv][segments][sum_keys]
+    f32x4_t* scores;             // [requests][Hkv][score_blocks], see scores_of
+    int score_rows, score_blocks;
     int lds_tiles;               // row tiles that weight_sums holds in LDS
 };
 
@@ -220,8 +223,14 @@ struct Walk {
     }
 };
 
-// Grid (row chunks x KV heads x splits, requests).
-template <typename T, int D, int RT>
+// Scores of block b that weight_stats leaves for weight_sums: [row / 4][key][row % 4],
+// the four rows that a lane holds of a product.
+__device__ __forceinline__ f32x4_t* scores_of(const WgtArgs& a, int i, int g, int b) {
+    return a.scores + (((int64_t)i * a.hkv + g) * a.score_blocks + b) * (a.score_rows / 4) * kBlockTokens;
+}
+
+// Grid (row chunks x KV heads x splits, requests).  SCORES: the products are stored.
+template <typename T, int D, int RT, bool SCORES = false>
 __global__ __launch_bounds__(kWgtThreads) void weight_stats(WgtArgs a) {
     constexpr int NB = step_blocks(D, sizeof(T) == 2), NC = Operand<T, D>::NC;
     __shared__ uint4 s_q[RT * NC * kWave];
@@ -270,6 +279,12 @@ __global__ __launch_bounds__(kWgtThreads) void weight_stats(WgtArgs a) {
                 f32x4_t s[NB];
 #pragma unroll
                 for (int x = 0; x < NB; ++x) s[x] = product<D>(qv, k[x].v, T{});
+                if constexpr (SCORES) {
+#pragma unroll
+                    for (int x = 0; x < NB; ++x)
+                        if (((ok >> x) & 1u) && lg * 4 < geo.rows && geo.rows <= a.score_rows)
+                            scores_of(a, i, g, b + x)[lane] = s[x];
+                }
                 if (masked) {
                     const i32x4_t pos = *reinterpret_cast<const i32x4_t*>(s_pos + r * 16 + (ql >> 4) * 4);
 #pragma unroll
@@ -405,8 +420,10 @@ __device__ __forceinline__ void store_weight(const WgtArgs& a, const WgtGeom& ge
 }
 
 // Few rows: grid (KV heads x ranges of sum_blocks blocks, requests).  The request's
-// row tiles stay in LDS, its keys stream past.
-template <typename T, int D>
+// row tiles stay in LDS, its keys stream past.  SCORES: where the rows are no more than
+// score_rows, the scores that weight_stats stored are read in the keys' place, a thread
+// per key.
+template <typename T, int D, bool SCORES>
 __global__ __launch_bounds__(kWgtThreads) void weight_sums(WgtArgs a) {
     constexpr int NB = step_blocks(D, sizeof(T) == 2), NC = Operand<T, D>::NC;
     extern __shared__ uint4 s_dyn[];  // the row tiles, then their rows' m, 1 / l and positions
@@ -426,6 +443,35 @@ __global__ __launch_bounds__(kWgtThreads) void weight_sums(WgtArgs a) {
     const int w = __builtin_amdgcn_readfirstlane(tid / kWave);
     const int32_t* table = a.block_tables + (int64_t)i * a.max_blocks;
     const int nsplit = (geo.blocks + a.split_blocks - 1) / a.split_blocks;
+    if (SCORES && geo.rows <= a.score_rows) {
+        if (tid < geo.rows) {
+            const float2 mi = join_parts(a, part_of(a, geo, g, tid), nsplit, g * a.group + tid - by_group(a, tid) * a.group);
+            s_m[tid] = mi.x;
+            s_inv[tid] = mi.y;
+            s_pos[tid] = geo.S - geo.n + by_group(a, tid);
+        }
+        __syncthreads();
+        for (int t = b_lo * kBlockTokens + tid; t < min(b_hi * kBlockTokens, geo.S); t += kWgtThreads) {
+            const int id = table[t / kBlockTokens];
+            if (id < 0 || id >= a.num_blocks) continue;
+            const int64_t at = ((int64_t)id * a.hkv + g) * kBlockTokens + t % kBlockTokens;
+            const float old = t < geo.S - geo.n && a.decay != 0.f ? a.key_weights[at] : 0.f;
+            const f32x4_t* scores = scores_of(a, i, g, t / kBlockTokens) + t % kBlockTokens;
+            float sum = 0.f;
+            for (int r0 = 0; r0 < geo.rows; r0 += 4) {
+                const f32x4_t x = scores[r0 / 4 * kBlockTokens];
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    if (r0 + r >= geo.rows) break;
+                    // (a key that no row sees has no scores, and is not asked for them)
+                    const float p = __builtin_amdgcn_exp2f(fmaf(x[r], a.scale_log2, -s_m[r0 + r])) * s_inv[r0 + r];
+                    sum += t <= s_pos[r0 + r] ? p : 0.f;
+                }
+            }
+            store_weight(a, geo, i, at, t, sum, old);
+        }
+        return;
+    }
     const int all_tiles = max(1, (geo.rows + 15) / 16);
     Walk<T, D, NB> walk(a, table, g, b_lo + w * NB, b_hi);
     // lane group lg holds the weights of block x = lg of a step
@@ -658,6 +704,7 @@ struct WgtPlan {
     int stat_rows;           // rows times the group of a request, about
     bool once;
     int segments, segment_tiles;
+    int score_rows, score_blocks;  // 0: the keys are read twice
     int64_t sum_keys;
     size_t rows_at, sums_at, bytes, cover;
 };
@@ -719,12 +766,26 @@ int make_plan(const verify_attn_params& p, int32_t total_q, int32_t max_q_len, i
     const size_t joined = pl.once || total_q == 0 ? 0 : align_up(row * total_q + 16 * sizeof(float2), 256);
     pl.sum_keys = blocks * kBlockTokens;
     const size_t sums = pl.segments > 1 ? align_up((size_t)p.num_seqs * p.num_kv_heads * pl.segments * pl.sum_keys * sizeof(float), 256) : 0;
+    // A row tile whose scores are at most a quarter of the keys' bytes to write and read:
+    // 32 requests of 4097 keys, 4 rows, head dim 128: 94 us reading the keys twice, 73;
+    // 16 requests of 2000 to 8000, 8 rows: 59 and 57; the same in fp32, 16 rows: 65 and 51;
+    // 8 rows at head dim 64, where they are half: 63 and 66.  Not where the requests'
+    // bounds exceed the cache twice over, and the scores with them.
+    size_t scores = 0;
+    const int64_t rows = align_up(G * std::max(1, max_q_len), 4), bounds = blocks * p.num_seqs, room = 2 * (int64_t)p.num_blocks;
+    if (rows <= 16 && 4 * (2 * rows * kBlockTokens * (int64_t)sizeof(float)) <= tile_bytes(p)) {
+        scores = (size_t)std::min(bounds, room) * p.num_kv_heads * rows * kBlockTokens * sizeof(float);
+        if (bounds <= room) {
+            pl.score_rows = (int)rows;
+            pl.score_blocks = (int)blocks;
+        }
+    }
     pl.sums_at = pl.rows_at + joined;
-    pl.bytes = pl.sums_at + sums;
+    pl.bytes = pl.sums_at + sums + scores;
     // Any batch of fewer requests: b of them have at most b max_q_len rows and
     // want / (b wgs) + 1 splits, or `least`.
     const int64_t few = ((int64_t)std::max(1, max_q_len) * want + wgs - 1) / wgs + total_q;
-    pl.cover = std::max(pl.bytes, align_up(row * (size_t)std::max(std::min(few, (int64_t)total_q * most), (int64_t)total_q * least), 256) + joined);
+    pl.cover = std::max(pl.bytes, align_up(row * (size_t)std::max(std::min(few, (int64_t)total_q * most), (int64_t)total_q * least), 256) + joined + scores);
     if (!pl.once)  // fewer requests may have more segments: kSumWgs of them at most in all
         pl.cover += std::max(sums, align_up((size_t)(kSumWgs / ((blocks + pl.sum_blocks - 1) / pl.sum_blocks)) * pl.sum_keys * sizeof(float), 256));
     *out = pl;
@@ -738,7 +799,9 @@ void launch(const WgtArgs& a, const WgtPlan& pl, hipStream_t stream) {
     auto run = [&](auto rt) {
         hipLaunchKernelGGL((weight_stats<T, D, decltype(rt)::value>), stats, dim3(kWgtThreads), 0, stream, a);
     };
-    switch (pl.stat_tiles) {
+    if (pl.score_rows > 0) {
+        hipLaunchKernelGGL((weight_stats<T, D, 1, true>), stats, dim3(kWgtThreads), 0, stream, a);
+    } else switch (pl.stat_tiles) {
         case 1: run(std::integral_constant<int, 1>{}); break;
         case 2: run(std::integral_constant<int, 2>{}); break;
         case 3: run(std::integral_constant<int, 3>{}); break;
@@ -748,7 +811,8 @@ void launch(const WgtArgs& a, const WgtPlan& pl, hipStream_t stream) {
     }
     if (pl.once) {
         const size_t lds = (size_t)pl.lds_tiles * (Operand<T, D>::NC * kWave * sizeof(uint4) + 3 * 16 * sizeof(float));
-        hipLaunchKernelGGL((weight_sums<T, D>), sums, dim3(kWgtThreads), lds, stream, a);
+        if (pl.score_rows > 0) hipLaunchKernelGGL((weight_sums<T, D, true>), sums, dim3(kWgtThreads), lds, stream, a);
+        else hipLaunchKernelGGL((weight_sums<T, D, false>), sums, dim3(kWgtThreads), lds, stream, a);
         return;
     }
     const dim3 join((unsigned)((pl.stat_rows + kWgtThreads - 1) / kWgtThreads * a.hkv), seqs);
@@ -835,6 +899,9 @@ extern "C" int verify_key_weights(const verify_attn_params* params, int32_t tota
     a.segment_tiles = pl.segment_tiles;
     a.sum_keys = pl.sum_keys;
     a.sums = reinterpret_cast<float*>(static_cast<char*>(workspace) + pl.sums_at);
+    a.scores = reinterpret_cast<f32x4_t*>(a.sums);  // (either, never both)
+    a.score_rows = pl.score_rows;
+    a.score_blocks = pl.score_blocks;
     if (p.dtype == VERIFY_BF16)
         p.head_dim == 128 ? launch<uint16_t, 128>(a, pl, stream) : launch<uint16_t, 64>(a, pl, stream);
     else

@@ -62,12 +62,16 @@ def _weights_case(rng, S, n, hkv, G, d, dtype, *, rows=None, lost=None, sinks=Fa
     ([400, 37], [6, 20], 1, 8, dict(size=15.0, sinks=True)),     # peaked rows
     ([100, 80], [30, 40], 2, 8, dict(max_q_len=2)),              # more rows than announced
     ([100, 80], [3, 4], 1, 2, dict(max_seq_len=81)),             # more keys than announced
+    ([300, 90, 33, 0], [1, 3, 0, 1], 2, 3, dict(max_q_len=1)),   # one row: its scores; more: its keys again
+    ([200, 90], [1, 1], 1, 2, dict(rows=[0, 1], unmapped=4, sinks=True)),
+    ([700, 1, 2, 17], [1, 1, 1, 1], 1, 1, {}),                   # bounds well beyond what the cache holds
 ])
 def test_key_weights(d, dtype, S, n, hkv, G, kw):
     _weights_case(np.random.default_rng(len(S) * d + G), S, n, hkv, G, d, dtype, **kw)
 
 
-@pytest.mark.parametrize("S,n,kw", [([5000, 40], [2, 1], {}), ([2600], [150], {}), ([2500, 2300], [7, 5], dict(decay=0.25))])
+@pytest.mark.parametrize("S,n,kw", [([5000, 40], [2, 1], {}), ([2600], [150], {}), ([2500, 2300], [7, 5], dict(decay=0.25)),
+                                    ([9000, 4100], [1, 1], dict(decay=0.25, unmapped=5)), ([3000], [2], {})])
 def test_key_weights_of_long_caches(S, n, kw):
     _weights_case(np.random.default_rng(sum(S)), S, n, 1, 4, 128, "bf16", **kw)
 
@@ -382,19 +386,20 @@ def test_on_another_stream_and_side_by_side():
 
 def test_workspace_of_a_larger_batch_serves_smaller_ones():
     """The size asked for one batch covers every batch of fewer requests and rows."""
-    def size(B, T, hq, hkv, mq, ms):
+    def size(B, T, hq, hkv, mq, ms, nb):
         q = torch.empty((T, hq, 128), dtype=torch.bfloat16)
-        kc = torch.empty((1, hkv, 16, 16, 8), dtype=torch.bfloat16)
+        kc = torch.empty((nb, hkv, 16, 16, 8), dtype=torch.bfloat16)
         bt = torch.empty((B, -(-ms // 16)), dtype=torch.int32)
         return av.key_weights_workspace_size(q, kc, bt, max_q_len=mq, max_seq_len=ms)
-    for mq, ms, hq, hkv in ((1, 5000, 8, 8), (9, 16384, 32, 8), (200, 4000, 32, 2), (9, 131072, 8, 1)):
-        large = size(64, 64 * mq, hq, hkv, mq, ms)
+    for mq, ms, hq, hkv, nb in ((1, 5000, 8, 8, 1), (1, 5000, 8, 2, 3200), (9, 16384, 32, 8, 1), (200, 4000, 32, 2, 1),
+                                (9, 131072, 8, 1, 1)):
+        large = size(64, 64 * mq, hq, hkv, mq, ms, nb)
         for B in (1, 2, 3, 7, 20, 63):
             # what the call asks for, not what the query returns
             q = torch.zeros((B * mq, hq, 128), dtype=torch.bfloat16, device=DEV)
-            kc = torch.zeros((1, hkv, 16, 16, 8), dtype=torch.bfloat16, device=DEV)
+            kc = torch.zeros((nb, hkv, 16, 16, 8), dtype=torch.bfloat16, device=DEV)
             bt = torch.zeros((B, -(-ms // 16)), dtype=torch.int32, device=DEV)
-            w, o = torch.zeros((1, hkv, 16), device=DEV), torch.zeros((1, hkv, 16), dtype=torch.int32, device=DEV)
+            w, o = torch.zeros((nb, hkv, 16), device=DEV), torch.zeros((nb, hkv, 16), dtype=torch.int32, device=DEV)
             ws = torch.empty(large, dtype=torch.uint8, device=DEV)
             # requests without keys: the launch has nothing to do
             av.verify_key_weights(q, kc, w, o, bt, torch.zeros(B, dtype=torch.int32, device=DEV),
