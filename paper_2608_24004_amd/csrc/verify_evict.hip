@@ -6,15 +6,18 @@
 // slot's sort key is one 32-bit word: the order key of its weight, above all of them
 // 0xffffffff for what is always kept, 0 for what never is.  At least c keys are not 0
 // (every slot below c has one), so a key of 0 counts nowhere.
-//   evict_plan    caches of up to kChunk slots: one workgroup, one launch, the keys in
-//                 registers, 16 per thread, from the first pass to the last;
+//   evict_plan    caches of up to 16384 slots: one workgroup, one launch, the keys in
+//                 registers, 4, 8 or 16 per thread, from the first pass to the last (32
+//                 requests of 4096 slots, eight heads: 15 us with 16, 10 with 4; of 8192:
+//                 18 with 16, 15 with 8);
 //   evict_hist (three launches), evict_lists, evict_join
-//                 longer caches: a workgroup per chunk of them, the histograms and
-//                 lists in the workspace between the launches (a single workgroup
-//                 took 543 us for 131072 slots).
+//                 longer caches: a workgroup per chunk of them, the sort keys, histograms
+//                 and lists in the workspace between the launches (a single workgroup
+//                 took 543 us for 131072 slots; the five 46 when each read the table,
+//                 the weights and the ordinals again, in chunks of 16384 slots; 30 now).
 // The call is a chain of latencies.  What it reads is 8 bytes per slot, in pieces of 64
 // contiguous bytes; four lanes take a block's four quarters, so that a load touches 16
-// lines (a block per lane: 64, and the keys' arrival took 9 us of the plan's 40).
+// lines (a block per lane: 64, and the keys' arrival took 9 us of a plan of 16384's 40).
 //
 // The moves.
 //   kv_compact    one wavefront per 16-slot block that keys move into.
@@ -25,11 +28,13 @@ namespace {
 
 constexpr int kPlanThreads = 1024;
 constexpr int kPlanWaves = kPlanThreads / kWave;
-constexpr int kSlots = 16;                      // of a thread
-constexpr int kChunk = kPlanThreads * kSlots;
+// Slots of a thread, and of a workgroup: all of a cache in one, or a chunk of a longer
+// one (131072 slots, eight heads: 46 us in chunks of 16 per thread, 36 of 8, 39 of 4).
+constexpr int kSlots = 16, kAlone = kPlanThreads * kSlots;
+constexpr int kPart = 8, kChunk = kPlanThreads * kPart;
 constexpr int kDigitBits = 11;
 constexpr int kBins = 1 << kDigitBits;
-constexpr int kMaxChunks = 1024;                // of a request
+constexpr int kMaxChunks = 2048;                // of a request
 constexpr uint32_t kAlways = 0xffffffffu;
 typedef int32_t i32x4u_t __attribute__((ext_vector_type(4), aligned(4)));
 
@@ -41,13 +46,14 @@ struct PlanArgs {
     const int32_t* num_tokens;
     int32_t* source;
     int32_t* new_lens;
-    // long caches: [pairs][chunks] histograms of two passes, lists and their lengths
-    int32_t* hist;    // [2][pairs][chunks][kBins]
+    // long caches:
+    uint4* keys;      // [pairs][chunks] sort keys, see stored_keys
+    int32_t* hist;    // [2][pairs][hists][kBins]: the chunks', and their sum where evict_sum forms it
     uint16_t* lists;  // [pairs][chunks][kChunk]: holes from the front, movers from the back
     int2* counts;     // [pairs][chunks] holes and movers
     uint2* state;     // [pairs][2] digits found and keys still needed, after one and two passes
     int64_t pairs;
-    int hkv, chunks, max_blocks, num_blocks, max_seq_len, max_keys, keep_first, keep_recent;
+    int hkv, chunks, hists, max_blocks, num_blocks, max_seq_len, max_keys, keep_first, keep_recent;
 };
 
 struct PlanGeom {
@@ -67,25 +73,27 @@ __device__ __forceinline__ PlanGeom plan_geom(const PlanArgs& a, int g, int i) {
 }
 
 // First slot of this thread's quarter k of a chunk: wavefront, quarter, lane in order.
+template <int N>
 __device__ __forceinline__ int slot_of(int chunk, int k) {
     const int lane = threadIdx.x & (kWave - 1), wv = threadIdx.x / kWave;
-    return ((chunk * kPlanThreads + wv * kWave + 16 * k + lane / 4) * kBlockTokens) + lane % 4 * 4;
+    return (chunk * kPlanWaves + wv) * (kWave * N) + (16 * k + lane / 4) * kBlockTokens + lane % 4 * 4;
 }
 
 // Sort keys of this thread's slots: key[4 k + e] that of slot_of(k) + e.
-__device__ __forceinline__ void load_keys(const PlanArgs& a, const PlanGeom& p, int chunk, uint32_t (&key)[kSlots]) {
+template <int N>
+__device__ __forceinline__ void load_keys(const PlanArgs& a, const PlanGeom& p, int chunk, uint32_t (&key)[N]) {
     const int32_t* table = a.block_tables + (int64_t)p.i * a.max_blocks;
     const int blocks = (p.S + kBlockTokens - 1) / kBlockTokens;
-    int id[4];
-    float4 w[4];
-    int4 o[4];
+    int id[N / 4];
+    float4 w[N / 4];
+    int4 o[N / 4];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        const int b = slot_of(chunk, k) / kBlockTokens;
+    for (int k = 0; k < N / 4; ++k) {
+        const int b = slot_of<N>(chunk, k) / kBlockTokens;
         id[k] = b < blocks ? table[b] : -1;
     }
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
+    for (int k = 0; k < N / 4; ++k) {
         const bool mapped = id[k] >= 0 && id[k] < a.num_blocks;
         const int64_t at = ((int64_t)(mapped ? id[k] : 0) * a.hkv + p.g) * kBlockTokens + threadIdx.x % 4 * 4;
         if (!mapped) continue;
@@ -93,9 +101,9 @@ __device__ __forceinline__ void load_keys(const PlanArgs& a, const PlanGeom& p, 
         if (a.key_order) o[k] = *reinterpret_cast<const int4*>(a.key_order + at);
     }
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
+    for (int k = 0; k < N / 4; ++k) {
         const bool mapped = id[k] >= 0 && id[k] < a.num_blocks;
-        const int s0 = slot_of(chunk, k);
+        const int s0 = slot_of<N>(chunk, k);
         const float wk[4] = {w[k].x, w[k].y, w[k].z, w[k].w};
         const int ok[4] = {o[k].x, o[k].y, o[k].z, o[k].w};
 #pragma unroll
@@ -136,10 +144,11 @@ struct Digits {
 // Adds the thread's keys that share the digits to the histogram of the next one.  The
 // lanes that agree with the first of them go as one addition: weights that are equal
 // (zeros, what is always kept) would otherwise wait for each other.
-__device__ __forceinline__ void add_keys(const Digits& d, int pass, const uint32_t (&key)[kSlots], int* hist) {
+template <int N>
+__device__ __forceinline__ void add_keys(const Digits& d, int pass, const uint32_t (&key)[N], int* hist) {
     const int lane = threadIdx.x & (kWave - 1);
 #pragma unroll
-    for (int e = 0; e < kSlots; ++e) {
+    for (int e = 0; e < N; ++e) {
         const bool in = key[e] != 0 && (key[e] & d.known) == d.prefix;
         const uint64_t mask = __ballot(in);
         if (mask == 0) continue;
@@ -202,19 +211,20 @@ __device__ __forceinline__ int find_digit(PlanShared& sh, Digits& d, int pass) {
 // Which of the thread's keys are kept: those above the c-th largest, and of those
 // equal to it the first d.need in slot order, of `count` in all and `before` in
 // earlier chunks.
-__device__ __forceinline__ uint32_t kept_bits(PlanShared& sh, const Digits& d, const uint32_t (&key)[kSlots], int count,
+template <int N>
+__device__ __forceinline__ uint32_t kept_bits(PlanShared& sh, const Digits& d, const uint32_t (&key)[N], int count,
                                               int before) {
     uint32_t kept = 0, equal = 0;
 #pragma unroll
-    for (int e = 0; e < kSlots; ++e) {
+    for (int e = 0; e < N; ++e) {
         kept |= (uint32_t)(key[e] > d.prefix) << e;
         equal |= (uint32_t)(key[e] == d.prefix) << e;
     }
     if (count == d.need) return kept | equal;
     // ranks among the equal ones: wavefronts, quarters, lanes, elements in order
-    int rank[4], total = 0;
+    int rank[N / 4], total = 0;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
+    for (int k = 0; k < N / 4; ++k) {
         rank[k] = total;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
@@ -230,7 +240,7 @@ __device__ __forceinline__ uint32_t kept_bits(PlanShared& sh, const Digits& d, c
     int all;
     before += sums_before(sh, all);
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
+    for (int k = 0; k < N / 4; ++k) {
         int r = before + rank[k];
 #pragma unroll
         for (int e = 0; e < 4; ++e)
@@ -242,14 +252,14 @@ __device__ __forceinline__ uint32_t kept_bits(PlanShared& sh, const Digits& d, c
 // Writes the plan of the kept slots that stay, and lists the holes below c and the
 // kept slots from c on in slot order: hole(n, slot), mover(n, slot) for the n-th of
 // each.  Returns their numbers.
-template <typename Hole, typename Mover>
+template <int N, typename Hole, typename Mover>
 __device__ __forceinline__ int2 list_slots(PlanShared& sh, const PlanGeom& p, int chunk, uint32_t kept, int32_t* source,
                                            Hole hole, Mover mover) {
     const int lane = threadIdx.x & (kWave - 1), wv = threadIdx.x / kWave;
     uint32_t front = 0, inside = 0;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        const int s0 = slot_of(chunk, k);
+    for (int k = 0; k < N / 4; ++k) {
+        const int s0 = slot_of<N>(chunk, k);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             front |= (uint32_t)(s0 + e < p.c) << (4 * k + e);
@@ -266,12 +276,12 @@ __device__ __forceinline__ int2 list_slots(PlanShared& sh, const PlanGeom& p, in
         }
     }
     const uint32_t bits[2] = {front & ~kept, inside & kept & ~front};
-    int rank[2][4], total[2] = {0, 0};
+    int rank[2][N / 4], total[2] = {0, 0};
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
         const bool some = __any(bits[j] != 0);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
+        for (int k = 0; k < N / 4; ++k) {
             rank[j][k] = total[j];
             if (!some) continue;
 #pragma unroll
@@ -292,8 +302,8 @@ __device__ __forceinline__ int2 list_slots(PlanShared& sh, const PlanGeom& p, in
     for (int j = 0; j < 2; ++j) {
         if (total[j] == 0) continue;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const int s0 = slot_of(chunk, k);
+        for (int k = 0; k < N / 4; ++k) {
+            const int s0 = slot_of<N>(chunk, k);
             int n = (j == 0 ? before & 0xffff : before >> 16) + rank[j][k];
 #pragma unroll
             for (int e = 0; e < 4; ++e)
@@ -315,14 +325,15 @@ __device__ __forceinline__ bool plan_ends(const PlanArgs& a, const PlanGeom& p, 
     return true;
 }
 
-// Grid (KV heads, requests).
+// Grid (KV heads, requests), caches of up to N slots per thread.
+template <int N>
 __global__ __launch_bounds__(kPlanThreads) void evict_plan(PlanArgs a) {
     __shared__ PlanShared sh;
-    __shared__ uint16_t s_hole[kChunk / 2], s_mover[kChunk / 2];  // at most min(c, S - c) each
+    __shared__ uint16_t s_hole[kPlanThreads * N / 2], s_mover[kPlanThreads * N / 2];  // at most min(c, S - c) each
     const PlanGeom p = plan_geom(a, blockIdx.x, blockIdx.y);
     int32_t* source = a.source + p.pair * a.max_keys;
     if (plan_ends(a, p, source)) return;
-    uint32_t key[kSlots];
+    uint32_t key[N];
     load_keys(a, p, 0, key);
     Digits d{0, 0, p.c};
     int count = 0;
@@ -332,22 +343,43 @@ __global__ __launch_bounds__(kPlanThreads) void evict_plan(PlanArgs a) {
         count = find_digit(sh, d, pass);
     }
     const uint32_t kept = kept_bits(sh, d, key, count, 0);
-    const int2 n = list_slots(
+    const int2 n = list_slots<N>(
         sh, p, 0, kept, source, [&](int k, int s) { s_hole[k] = (uint16_t)s; }, [&](int k, int s) { s_mover[k] = (uint16_t)s; });
     __syncthreads();
     for (int u = threadIdx.x; u < n.x; u += kPlanThreads) source[s_hole[u]] = s_mover[u];
 }
 
-// The histogram of a pass, summed over the request's chunks; `before` receives the
-// counts of `bin` in the chunks before `chunk`, once that bin is known.
-__device__ __forceinline__ const int32_t* chunk_hists(const PlanArgs& a, const PlanGeom& p, int pass) {
-    return a.hist + ((pass & 1) * a.pairs + p.pair) * a.chunks * kBins;
+// The histograms of a pass.
+__device__ __forceinline__ int32_t* chunk_hists(const PlanArgs& a, const PlanGeom& p, int pass) {
+    return a.hist + ((pass & 1) * a.pairs + p.pair) * a.hists * kBins;
 }
+
+// Their sum over a request of many chunks, which every chunk's workgroup would form for
+// itself.  Grid (KV heads x pieces of 64 bins, requests), 16 wavefronts for the chunks.
+__global__ __launch_bounds__(kPlanThreads) void evict_sum(PlanArgs a, int pass) {
+    __shared__ int s_sum[kPlanWaves][kWave];
+    const PlanGeom p = plan_geom(a, blockIdx.x % a.hkv, blockIdx.y);
+    if (p.S == p.c) return;
+    const int lane = threadIdx.x & (kWave - 1), wv = threadIdx.x / kWave;
+    const int bin = blockIdx.x / a.hkv * kWave + lane, chunks = (p.S + kChunk - 1) / kChunk;
+    int32_t* h = chunk_hists(a, p, pass) + bin;
+    int v = 0;
+#pragma unroll 8
+    for (int k = wv; k < chunks; k += kPlanWaves) v += h[(int64_t)k * kBins];
+    s_sum[wv][lane] = v;
+    __syncthreads();
+    if (wv > 0) return;
+#pragma unroll
+    for (int k = 1; k < kPlanWaves; ++k) v += s_sum[k][lane];
+    h[(int64_t)a.chunks * kBins] = v;
+}
+
 __device__ __forceinline__ void sum_hists(const PlanArgs& a, const PlanGeom& p, int pass, PlanShared& sh) {
-    const int32_t* h = chunk_hists(a, p, pass);
-    const int chunks = (p.S + kChunk - 1) / kChunk;
+    const bool summed = a.hists > a.chunks;
+    const int32_t* h = chunk_hists(a, p, pass) + (summed ? (int64_t)a.chunks * kBins : 0);
+    const int chunks = summed ? 1 : (p.S + kChunk - 1) / kChunk;
     int v[kBins / kPlanThreads] = {};
-#pragma unroll 4
+#pragma unroll 8
     for (int k = 0; k < chunks; ++k)
 #pragma unroll
         for (int e = 0; e < kBins / kPlanThreads; ++e) v[e] += h[(int64_t)k * kBins + e * kPlanThreads + threadIdx.x];
@@ -368,6 +400,20 @@ __device__ __forceinline__ int digits_after(const PlanArgs& a, const PlanGeom& p
     return find_digit(sh, d, passes - 1);
 }
 
+// This thread's sort keys as the first pass leaves them for the others: they then need
+// neither the table nor the ordinals, and arrive while the histograms are added up.
+__device__ __forceinline__ uint4* stored_keys(const PlanArgs& a, const PlanGeom& p, int chunk) {
+    return a.keys + ((p.pair * a.chunks + chunk) * (kPart / 4)) * kPlanThreads + threadIdx.x;
+}
+__device__ __forceinline__ void fetch_keys(const PlanArgs& a, const PlanGeom& p, int chunk, uint32_t (&key)[kPart]) {
+    const uint4* from = stored_keys(a, p, chunk);
+#pragma unroll
+    for (int k = 0; k < kPart / 4; ++k) {
+        const uint4 v = from[k * kPlanThreads];
+        key[4 * k] = v.x, key[4 * k + 1] = v.y, key[4 * k + 2] = v.z, key[4 * k + 3] = v.w;
+    }
+}
+
 // Grid (KV heads x chunks, requests), as the two kernels after it.
 template <int PASS>
 __global__ __launch_bounds__(kPlanThreads) void evict_hist(PlanArgs a) {
@@ -375,8 +421,16 @@ __global__ __launch_bounds__(kPlanThreads) void evict_hist(PlanArgs a) {
     const PlanGeom p = plan_geom(a, blockIdx.x % a.hkv, blockIdx.y);
     const int chunk = blockIdx.x / a.hkv;
     if (p.S == p.c || (int64_t)chunk * kChunk >= p.S) return;
-    uint32_t key[kSlots];
-    load_keys(a, p, chunk, key);
+    uint32_t key[kPart];
+    if constexpr (PASS == 0) {
+        load_keys(a, p, chunk, key);
+        uint4* to = stored_keys(a, p, chunk);
+#pragma unroll
+        for (int k = 0; k < kPart / 4; ++k)
+            to[k * kPlanThreads] = make_uint4(key[4 * k], key[4 * k + 1], key[4 * k + 2], key[4 * k + 3]);
+    } else {
+        fetch_keys(a, p, chunk, key);
+    }
     Digits d{0, 0, p.c};
     if (PASS > 0) {
         digits_after(a, p, PASS, sh, d);
@@ -386,7 +440,7 @@ __global__ __launch_bounds__(kPlanThreads) void evict_hist(PlanArgs a) {
     clear_hist(sh);
     add_keys(d, PASS, key, sh.hist);
     __syncthreads();
-    int32_t* out = a.hist + (((PASS & 1) * a.pairs + p.pair) * a.chunks + chunk) * kBins;
+    int32_t* out = chunk_hists(a, p, PASS) + (int64_t)chunk * kBins;
     for (int e = threadIdx.x; e < kBins; e += kPlanThreads) out[e] = sh.hist[e];
 }
 
@@ -397,17 +451,20 @@ __global__ __launch_bounds__(kPlanThreads) void evict_lists(PlanArgs a) {
     int32_t* source = a.source + p.pair * a.max_keys;
     if (chunk == 0 && plan_ends(a, p, source)) return;
     if (p.S == p.c || (int64_t)chunk * kChunk >= p.S) return;
-    uint32_t key[kSlots];
-    load_keys(a, p, chunk, key);
+    uint32_t key[kPart];
+    fetch_keys(a, p, chunk, key);
     Digits d;
     const int count = digits_after(a, p, 3, sh, d);
     int before = 0;
-    const int32_t* h = chunk_hists(a, p, 2) + (d.prefix & d.mask(2));
-    for (int k = 0; k < chunk; ++k) before += h[(int64_t)k * kBins];
+    if (count != d.need) {  // a lane per earlier chunk
+        const int32_t* h = chunk_hists(a, p, 2) + (d.prefix & d.mask(2));
+        for (int k = threadIdx.x & (kWave - 1); k < chunk; k += kWave) before += h[(int64_t)k * kBins];
+        before = __builtin_amdgcn_readlane(wave_scan(before), kWave - 1);
+    }
     const uint32_t kept = kept_bits(sh, d, key, count, before);
     uint16_t* list = a.lists + (p.pair * a.chunks + chunk) * kChunk;
     const int s0 = chunk * kChunk;
-    const int2 n = list_slots(
+    const int2 n = list_slots<kPart>(
         sh, p, chunk, kept, source, [&](int k, int s) { list[k] = (uint16_t)(s - s0); },
         [&](int k, int s) { list[kChunk - 1 - k] = (uint16_t)(s - s0); });
     if (threadIdx.x == 0) a.counts[p.pair * a.chunks + chunk] = n;
@@ -438,10 +495,14 @@ __global__ __launch_bounds__(kPlanThreads) void evict_join(PlanArgs a) {
     __syncthreads();
     const uint16_t* lists = a.lists + p.pair * a.chunks * kChunk;
     int32_t* source = a.source + p.pair * a.max_keys;
-    int k = 0;
     for (int u = threadIdx.x; u < holes; u += kPlanThreads) {
         const int n = s_holes + u;
-        while (k < chunks - 1 && s_movers[k] <= n) ++k;
+        int k = 0, top = chunks - 1;  // the first chunk with more than n movers up to its end
+        while (k < top) {
+            const int mid = (k + top) / 2;
+            if (s_movers[mid] <= n) k = mid + 1;
+            else top = mid;
+        }
         const int m = n - (k > 0 ? s_movers[k - 1] : 0);
         source[chunk * kChunk + lists[(int64_t)chunk * kChunk + u]] = k * kChunk + lists[(int64_t)k * kChunk + kChunk - 1 - m];
     }
@@ -526,18 +587,24 @@ int check(const verify_attn_params* p, int32_t max_seq_len, int32_t max_keys) {
 // Chunks of the longest request; 1: evict_plan alone, without a workspace.
 int64_t plan_chunks(const verify_attn_params& p, int32_t max_seq_len) {
     const int64_t longest = std::min<int64_t>(max_seq_len, (int64_t)p.max_blocks_per_seq * kBlockTokens);
-    return std::max<int64_t>(1, (longest + kChunk - 1) / kChunk);
+    return longest <= kAlone ? 1 : (longest + kChunk - 1) / kChunk;
 }
 
+// Histograms of a request: evict_sum adds up those of more than 20 chunks (eight heads,
+// each workgroup adding them up for itself and with evict_sum: 131072 slots 30 and 35 us,
+// 196608 40 and 39, a million 183 and 88).
+size_t plan_hists(int64_t chunks) { return chunks + (chunks > 20); }
+
 struct PlanSpace {
-    size_t lists, counts, state, total;  // offsets behind the histograms
+    size_t hist, lists, counts, state, total;  // offsets behind the sort keys
 };
 
 PlanSpace plan_space(const verify_attn_params& p, int32_t max_seq_len, int32_t max_keys) {
     PlanSpace w{};
     const size_t chunks = (size_t)plan_chunks(p, max_seq_len), pairs = (size_t)p.num_seqs * p.num_kv_heads;
     if (chunks == 1 || max_keys >= max_seq_len) return w;
-    w.lists = align_up(2 * pairs * chunks * kBins * sizeof(int32_t), 256);
+    w.hist = pairs * chunks * kChunk * sizeof(uint32_t);
+    w.lists = w.hist + align_up(2 * pairs * plan_hists(chunks) * kBins * sizeof(int32_t), 256);
     w.counts = w.lists + align_up(pairs * chunks * kChunk * sizeof(uint16_t), 256);
     w.state = w.counts + align_up(pairs * chunks * sizeof(int2), 256);
     w.total = w.state + align_up(pairs * 2 * sizeof(uint2), 256);
@@ -586,6 +653,7 @@ extern "C" int verify_evict_plan(const verify_attn_params* params, int32_t max_s
     a.new_lens = new_lens;
     a.pairs = (int64_t)p.num_seqs * p.num_kv_heads;
     a.chunks = (int)chunks;
+    a.hists = (int)plan_hists(chunks);
     a.hkv = p.num_kv_heads;
     a.max_blocks = p.max_blocks_per_seq;
     a.num_blocks = p.num_blocks;
@@ -595,18 +663,29 @@ extern "C" int verify_evict_plan(const verify_attn_params* params, int32_t max_s
     a.keep_recent = keep_recent;
     dim3 grid((unsigned)p.num_kv_heads, (unsigned)p.num_seqs);
     if (space.total == 0) {  // (also where no request can exceed max_keys)
-        hipLaunchKernelGGL(evict_plan, grid, dim3(kPlanThreads), 0, stream, a);
+        const int64_t longest = std::min<int64_t>(max_seq_len, (int64_t)p.max_blocks_per_seq * kBlockTokens);
+        if (longest <= 4 * kPlanThreads) hipLaunchKernelGGL(evict_plan<4>, grid, dim3(kPlanThreads), 0, stream, a);
+        else if (longest <= 8 * kPlanThreads) hipLaunchKernelGGL(evict_plan<8>, grid, dim3(kPlanThreads), 0, stream, a);
+        else hipLaunchKernelGGL(evict_plan<kSlots>, grid, dim3(kPlanThreads), 0, stream, a);
         return check_launch();
     }
     char* ws = static_cast<char*>(workspace);
-    a.hist = reinterpret_cast<int32_t*>(ws);
+    a.keys = reinterpret_cast<uint4*>(ws);
+    a.hist = reinterpret_cast<int32_t*>(ws + space.hist);
     a.lists = reinterpret_cast<uint16_t*>(ws + space.lists);
     a.counts = reinterpret_cast<int2*>(ws + space.counts);
     a.state = reinterpret_cast<uint2*>(ws + space.state);
     grid.x *= (unsigned)chunks;
+    const dim3 sums((unsigned)(p.num_kv_heads * (kBins / kWave)), (unsigned)p.num_seqs);
+    auto sum = [&](int pass) {
+        if (a.hists > a.chunks) hipLaunchKernelGGL(evict_sum, sums, dim3(kPlanThreads), 0, stream, a, pass);
+    };
     hipLaunchKernelGGL(evict_hist<0>, grid, dim3(kPlanThreads), 0, stream, a);
+    sum(0);
     hipLaunchKernelGGL(evict_hist<1>, grid, dim3(kPlanThreads), 0, stream, a);
+    sum(1);
     hipLaunchKernelGGL(evict_hist<2>, grid, dim3(kPlanThreads), 0, stream, a);
+    sum(2);
     hipLaunchKernelGGL(evict_lists, grid, dim3(kPlanThreads), 0, stream, a);
     hipLaunchKernelGGL(evict_join, grid, dim3(kPlanThreads), 0, stream, a);
     return check_launch();

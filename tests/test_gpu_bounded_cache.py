@@ -155,23 +155,25 @@ def test_evict_plan(S, hkv, max_keys, kw, values, lost):
     _plan_case(c, w.to(DEV), o, max_keys=max_keys, tokens=c.tokens if lost else None, **kw)
 
 
-def test_evict_plan_of_long_caches():
+@pytest.mark.parametrize("S,hkv", [([40000, 16385, 16384], 2), ([8193, 4097, 8192], 2), ([4097, 4096], 3),
+                                   ([250000, 100, 170003], 1)])
+def test_evict_plan_of_long_caches(S, hkv):
     """More blocks than the workgroup has threads, and ordinals that are none."""
     rng = np.random.default_rng(4)
-    S = [40000, 16385, 16384]
     c = Cache.__new__(Cache)
     c.S = np.asarray(S, dtype=np.int32)
     blocks = -(-c.S // BLOCK)
     c.nb = int(blocks.sum())
     ids = rng.permutation(c.nb).astype(np.int32)
-    c.block_tables = np.full((3, int(blocks.max())), -1, dtype=np.int32)
+    c.block_tables = np.full((len(S), int(blocks.max())), -1, dtype=np.int32)
     for i, off in enumerate(np.cumsum(blocks) - blocks):
         c.block_tables[i, :blocks[i]] = ids[off:off + blocks[i]]
     c.k = c.v = torch.zeros(1)
-    c.w = torch.as_tensor(rng.integers(0, 5000, size=(c.nb, 2, BLOCK)), dtype=torch.float32)
-    c.o = torch.as_tensor(rng.integers(0, 60000, size=(c.nb, 2, BLOCK)), dtype=torch.int32)
-    for max_keys, kw in ((16384, dict(keep_first=100, keep_recent=1000)), (20001, {}), (5, dict(keep_first=5))):
-        _plan_case(c, c.w.to(DEV), c.o.to(DEV), max_keys=max_keys, tokens=[60000] * 3, **kw)
+    c.w = torch.as_tensor(rng.integers(0, 5000, size=(c.nb, hkv, BLOCK)), dtype=torch.float32)
+    c.o = torch.as_tensor(rng.integers(0, 60000, size=(c.nb, hkv, BLOCK)), dtype=torch.int32)
+    for max_keys, kw in ((16384, dict(keep_first=100, keep_recent=1000)), (20001, {}), (3000, dict(keep_recent=64)),
+                         (5, dict(keep_first=5))):
+        _plan_case(c, c.w.to(DEV), c.o.to(DEV), max_keys=max_keys, tokens=[60000] * len(S), **kw)
 
 
 def test_evict_plan_with_unmapped_blocks_and_a_tighter_bound():
