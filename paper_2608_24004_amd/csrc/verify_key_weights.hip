@@ -17,7 +17,7 @@
 //   weight_join, weight_sums_rows, weight_store   the parts joined once, then keys
 //                 stay in registers and the rows stream past through LDS.
 // What bounds it: few rows, the keys' bytes (32 requests of 475 MB of keys, 36 rows each:
-// 93 us per pass, 5.1 TB/s, as fast as a copy; both passes read them); many rows, the
+// 181 us for two passes that both read them, 5.2 TB/s, the rate of a copy); many rows, the
 // exponentials, one per row and key and pass beside four other vector instructions (the
 // prompts named at weight_sums_rows' segments: 72 and 76 us, of which the matrix
 // instructions take 14 each).
@@ -157,13 +157,15 @@ __device__ __forceinline__ void stage_rows(const WgtArgs& a, const WgtGeom& geo,
         pos[t] = first + t < geo.rows ? geo.S - geo.n + by_group(a, first + t) : -1;
 }
 
-// K tile of block `phys`, KV head g.
-template <typename T, int D>
+// K tile of block `phys`, KV head g.  ONCE: read for the last time in the call, and kept
+// out of the way of what is read again (the second pass of the 32 requests above: 187 ->
+// 181 us for both; the only one of a decoding step, 32 requests of 4097 keys: 70 -> 63).
+template <typename T, int D, bool ONCE>
 __device__ __forceinline__ void load_keys(const WgtArgs& a, int g, int phys, Operand<T, D>& k) {
     const uint4* src = static_cast<const uint4*>(a.kc) + ((int64_t)phys * a.hkv + g) * (Operand<T, D>::NC * kWave) +
                        (threadIdx.x & (kWave - 1));
 #pragma unroll
-    for (int c = 0; c < Operand<T, D>::NC; ++c) k.v[c] = src[c * kWave];
+    for (int c = 0; c < Operand<T, D>::NC; ++c) k.v[c] = ONCE ? ld16_stream(src + c * kWave) : src[c * kWave];
 }
 
 // Blocks of a wavefront's step where keys stream past (two such steps are in
@@ -182,7 +184,7 @@ constexpr float kNoScore = -3.0e38f;
 
 // The blocks of a wavefront, NB at a time and kWgtWaves * NB apart, their ids read 64
 // at a time (one per lane) and their K tiles a step ahead of their use.
-template <typename T, int D, int NB>
+template <typename T, int D, int NB, bool ONCE = false>
 struct Walk {
     const WgtArgs& a;
     const int32_t* table;
@@ -218,7 +220,7 @@ struct Walk {
             b += kWgtWaves * NB;
         }
 #pragma unroll
-        for (int x = 0; x < NB; ++x) load_keys<T, D>(a, g, phys[x], k[x]);
+        for (int x = 0; x < NB; ++x) load_keys<T, D, ONCE>(a, g, phys[x], k[x]);
         return ok;
     }
 };
@@ -318,7 +320,7 @@ __global__ __launch_bounds__(kWgtThreads) void weight_stats(WgtArgs a) {
                     for (int x = 0; x < NB; ++x) l[r][e] += __builtin_amdgcn_exp2f(relative(e, x));
             }
         };
-        Walk<T, D, NB> walk(a, table, g, b_lo + w * NB, b_hi);
+        Walk<T, D, NB, SCORES> walk(a, table, g, b_lo + w * NB, b_hi);
         Operand<T, D> k0[NB], k1[NB];
         int phys[NB] = {}, b = walk.b;
         uint32_t ok0 = walk.load(k0, phys), ok1;
@@ -473,7 +475,7 @@ __global__ __launch_bounds__(kWgtThreads) void weight_sums(WgtArgs a) {
         return;
     }
     const int all_tiles = max(1, (geo.rows + 15) / 16);
-    Walk<T, D, NB> walk(a, table, g, b_lo + w * NB, b_hi);
+    Walk<T, D, NB, true> walk(a, table, g, b_lo + w * NB, b_hi);
     // lane group lg holds the weights of block x = lg of a step
     auto load_old = [&](uint32_t ok, const int (&phys)[NB], int b) {
         float old = 0.f;
@@ -487,7 +489,7 @@ __global__ __launch_bounds__(kWgtThreads) void weight_sums(WgtArgs a) {
     // further rounds over the keys, which add to what the first has written
     for (int first = 0; first == 0 || first < all_tiles; first += a.lds_tiles) {
         const int tiles = min(a.lds_tiles, all_tiles - first);
-        Walk<T, D, NB> go = walk;
+        Walk<T, D, NB, true> go = walk;
         Operand<T, D> k0[NB], k1[NB];
         int phys0[NB] = {}, phys1[NB] = {}, b = go.b;
         uint32_t ok0 = go.load(k0, phys0), ok1;
@@ -767,10 +769,10 @@ int make_plan(const verify_attn_params& p, int32_t total_q, int32_t max_q_len, i
     pl.sum_keys = blocks * kBlockTokens;
     const size_t sums = pl.segments > 1 ? align_up((size_t)p.num_seqs * p.num_kv_heads * pl.segments * pl.sum_keys * sizeof(float), 256) : 0;
     // A row tile whose scores are at most a quarter of the keys' bytes to write and read:
-    // 32 requests of 4097 keys, 4 rows, head dim 128: 94 us reading the keys twice, 73;
-    // 16 requests of 2000 to 8000, 8 rows: 59 and 57; the same in fp32, 16 rows: 65 and 51;
-    // 8 rows at head dim 64, where they are half: 63 and 66.  Not where the requests'
-    // bounds exceed the cache twice over, and the scores with them.
+    // 32 requests of 4097 keys, 4 rows, head dim 128: 94 us reading the keys twice, 63;
+    // 16 requests of 2000 to 8000, 8 rows: 59 and 52; the same in fp32, 16 rows: 65 and 52;
+    // where they are half, 8 rows at head dim 64: 59 and 60; 15 rows, four heads: 31 and 37.
+    // Not where the requests' bounds exceed the cache twice over, and the scores with them.
     size_t scores = 0;
     const int64_t rows = align_up(G * std::max(1, max_q_len), 4), bounds = blocks * p.num_seqs, room = 2 * (int64_t)p.num_blocks;
     if (rows <= 16 && 4 * (2 * rows * kBlockTokens * (int64_t)sizeof(float)) <= tile_bytes(p)) {
