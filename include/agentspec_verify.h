@@ -572,8 +572,10 @@ int verify_rotary_append(const verify_attn_params *attn, const verify_rotary_par
  *                max_seq_len and to 16 * max_blocks_per_seq; n_i may exceed
  *                max_q_len, which only sizes the launch)
  *   decay        finite, >= 0
- *   VERIFY_EUNSUPPORTED from total_q G (G - 1) = 2^32 on, G = Hq / Hkv.
- *   workspace    at least verify_key_weights_workspace_size() bytes for the same
+ *   VERIFY_EUNSUPPORTED where (total_q + 1) G reaches 2^30 or (total_q + 1) G (G - 1)
+ *                2^32, G = Hq / Hkv.
+ *   workspace    16-byte aligned (VERIFY_EINVAL otherwise), at least
+ *                verify_key_weights_workspace_size() bytes for the same
  *                arguments, or for those of a batch of more requests and rows with
  *                the same other arguments; its contents on entry are ignored
  */
@@ -611,9 +613,10 @@ int verify_key_weights(const verify_attn_params *params, int32_t total_q, int32_
  * is moved out of one or into one.  If more keys are always kept than max_keys (by
  * ordinals that are no ordinals), the lower slots of them stay.
  *   key_weights and key_order 16-byte aligned (VERIFY_EINVAL otherwise)
- *   workspace    at least verify_evict_plan_workspace_size() bytes (may be NULL if
- *                that is 0); its contents on entry are ignored
- * VERIFY_EUNSUPPORTED beyond 2^24 slots per request.
+ *   workspace    16-byte aligned (VERIFY_EINVAL otherwise), at least
+ *                verify_evict_plan_workspace_size() bytes (may be NULL if that is 0);
+ *                its contents on entry are ignored
+ * VERIFY_EUNSUPPORTED beyond 2^24 slots per request and from 131072 KV heads on.
  */
 int verify_evict_plan_workspace_size(const verify_attn_params *params, int32_t max_seq_len,
                                      int32_t max_keys, size_t *bytes);

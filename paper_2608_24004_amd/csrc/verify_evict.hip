@@ -595,6 +595,11 @@ int64_t plan_chunks(const verify_attn_params& p, int32_t max_seq_len) {
 // 196608 40 and 39, a million 183 and 88).
 size_t plan_hists(int64_t chunks) { return chunks + (chunks > 20); }
 
+// A grid dimension holds fewer than 2^32 threads: those of the chunks and of evict_sum.
+bool plan_fits(const verify_attn_params& p, int64_t chunks) {
+    return chunks <= kMaxChunks && std::max<int64_t>(chunks, kBins / kWave) * p.num_kv_heads < (1 << 22);
+}
+
 struct PlanSpace {
     size_t hist, lists, counts, state, total;  // offsets behind the sort keys
 };
@@ -621,7 +626,7 @@ extern "C" int verify_evict_plan_workspace_size(const verify_attn_params* params
     if (!bytes) return VERIFY_EINVAL;
     const int rc = check(params, max_seq_len, max_keys);
     if (rc != VERIFY_OK) return rc;
-    if (plan_chunks(*params, max_seq_len) > kMaxChunks) return VERIFY_EUNSUPPORTED;
+    if (!plan_fits(*params, plan_chunks(*params, max_seq_len))) return VERIFY_EUNSUPPORTED;
     *bytes = plan_space(*params, max_seq_len, max_keys).total;
     return VERIFY_OK;
 }
@@ -637,9 +642,9 @@ extern "C" int verify_evict_plan(const verify_attn_params* params, int32_t max_s
     if (keep_first < 0 || keep_recent < 0 || (int64_t)keep_first + keep_recent > max_keys) return VERIFY_EINVAL;
     if (p.num_seqs > 0 && (!block_tables || !seq_lens || !source || !new_lens)) return VERIFY_EINVAL;
     if (p.num_seqs > 0 && p.num_blocks > 0 && !key_weights) return VERIFY_EINVAL;
-    if (((uintptr_t)key_weights | (uintptr_t)key_order) & 15) return VERIFY_EINVAL;
+    if (((uintptr_t)key_weights | (uintptr_t)key_order | (uintptr_t)workspace) & 15) return VERIFY_EINVAL;
     const int64_t chunks = plan_chunks(p, max_seq_len);
-    if (chunks > kMaxChunks || chunks * p.num_kv_heads >= (1 << 22)) return VERIFY_EUNSUPPORTED;
+    if (!plan_fits(p, chunks)) return VERIFY_EUNSUPPORTED;
     const PlanSpace space = plan_space(p, max_seq_len, max_keys);
     if (workspace_bytes < space.total || (space.total > 0 && !workspace)) return VERIFY_EWORKSPACE;
     if (p.num_seqs == 0) return VERIFY_OK;

@@ -829,7 +829,8 @@ int check(const verify_attn_params* p, int32_t total_q, int32_t max_q_len, int32
     if (rc != VERIFY_OK) return rc;
     if (p->sliding_window > 0) return VERIFY_EUNSUPPORTED;
     const int64_t group = p->num_q_heads / p->num_kv_heads;
-    if (group > 65536 || (total_q + 1) * group * (group - 1) >= ((int64_t)1 << 32)) return VERIFY_EUNSUPPORTED;
+    const int64_t rows = ((int64_t)total_q + 1) * group;  // see by_group
+    if (rows >= (1 << 30) || rows * (group - 1) >= ((int64_t)1 << 32)) return VERIFY_EUNSUPPORTED;
     return VERIFY_OK;
 }
 
@@ -862,7 +863,7 @@ extern "C" int verify_key_weights(const verify_attn_params* params, int32_t tota
     if (p.num_seqs > 0 && (!block_tables || !seq_lens || !q_start)) return VERIFY_EINVAL;
     if (p.num_blocks > 0 && p.num_seqs > 0 && (!k_cache || !key_weights || !key_order)) return VERIFY_EINVAL;
     if (total_q > 0 && !q) return VERIFY_EINVAL;
-    if ((uintptr_t)k_cache & 15) return VERIFY_EINVAL;
+    if (((uintptr_t)k_cache | (uintptr_t)workspace) & 15) return VERIFY_EINVAL;
     WgtPlan pl;
     rc = make_plan(p, total_q, max_q_len, max_seq_len, &pl);
     if (rc != VERIFY_OK) return rc;

@@ -130,6 +130,10 @@ def test_key_weights_arguments():
     assert _weights(_attn(num_q_heads=4096, num_kv_heads=4096, max_blocks_per_seq=1 << 26), ms=(1 << 30)) == av.EUNSUPPORTED
     # a group that the row arithmetic does not hold
     assert _weights(_attn(num_q_heads=8192, num_kv_heads=1), T=64) == av.EUNSUPPORTED
+    for T in (1 << 30, 2 ** 31 - 1):
+        assert _weights(_attn(num_q_heads=2, num_kv_heads=2), T=T) == av.EUNSUPPORTED
+        assert _weights(_attn(num_q_heads=4, num_kv_heads=2), T=T // 2 + 1) == av.EUNSUPPORTED
+    assert _weights(_attn(), ws=ctypes.c_void_p(0x1008)) == av.EINVAL
     assert _weights(_attn(num_seqs=0), T=0, have=0, ws=None) == av.OK
 
 
@@ -164,6 +168,9 @@ def test_evict_plan_arguments():
     assert _plan(_attn(sliding_window=64)) == av.EUNSUPPORTED
     for x in (0, 1):
         assert _plan(_attn(), ptrs={x: ctypes.c_void_p(0x1004)}) == av.EINVAL
+    many = _attn(num_q_heads=1 << 17, num_kv_heads=1 << 17, max_blocks_per_seq=4096)
+    assert query(ctypes.byref(many), 40000, 100, ctypes.byref(size)) == _plan(many, ms=40000) == av.EUNSUPPORTED
+    assert _plan(long, ms=40000, ws=ctypes.c_void_p(0x1008)) == av.EINVAL
     assert _plan(long, ms=40000, have=need - 1) == _plan(long, ms=40000, ws=None) == av.EWORKSPACE
     assert _plan(_attn(num_seqs=0), have=0, ws=None) == av.OK
 
