@@ -739,6 +739,8 @@ def _rows_arg(t, name, heads, D, dtype, idx, device, T):
     shape = (T, heads, D)
     if not (t is not None and t.dtype is dtype and t.get_device() == idx >= 0 and t.shape == shape):
         _expect(t, name, shape, dtype, device)
+    if t.is_contiguous():
+        return t.data_ptr(), heads * D
     st = t.stride()
     if T <= 1:
         st = (heads * D,) + st[1:]  # one row has no stride
@@ -758,14 +760,14 @@ def _rotary_args(q, positions, inv_freq, axes, interleaved, scale, idx, dev):
         raise ValueError("inv_freq must be [rotary_dim / 2], got %s" % (tuple(inv_freq.shape),))
     F = inv_freq.shape[0]
     num_axes = 1 if positions.dim() == 1 else positions.shape[0]
-    axes = (0,) * F if axes is None and num_axes == 1 else axes
-    if axes is None or len(axes) != F:
+    if num_axes != 1 if axes is None else len(axes) != F:
         raise ValueError("axes must name the axis of each of the %d frequencies" % F)
     p_pos = _arg(positions, "positions", (T,) if positions.dim() == 1 else (num_axes, T), torch.int32, idx, dev)
     p_freq = _arg(inv_freq, "inv_freq", None, torch.float64, idx, dev)
-    key = (D, num_axes, bool(interleaved), float(scale), q.dtype, tuple(axes))
+    key = (D, F, num_axes, bool(interleaved), float(scale), q.dtype, None if axes is None else tuple(axes))
     params = _rotary_params.get(key)
     if params is None:
+        axes = (0,) * F if axes is None else axes
         if not (2 <= 2 * F <= D and all(0 <= int(x) < num_axes for x in axes)):
             raise ValueError("rotary_dim %d of head dim %d, axes %s of %d" % (2 * F, D, sorted(set(axes)), num_axes))
         params = RotaryParams(D, 2 * F, num_axes, int(bool(interleaved)), float(scale), _dtype_code(q))
@@ -792,8 +794,7 @@ def verify_rotary(q, k, positions, inv_freq, *, axes=None, interleaved: bool = F
     if q.dim() != 3 or k is not None and k.dim() != 3:
         raise ValueError("q must be [T, Hq, D] and k [T, Hkv, D]")
     T, Hq, D = q.shape
-    dtype, dev = q.dtype, q.device
-    idx = dev.index if dev.type == "cuda" else -1
+    dtype, dev, idx = q.dtype, q.device, q.get_device()
     Hkv = 0 if k is None else k.shape[1]
     p_q, s_q = _rows_arg(q, "q", Hq, D, dtype, idx, dev, T)
     p_k, s_k = (None, 0) if k is None else _rows_arg(k, "k", Hkv, D, dtype, idx, dev, T)
@@ -822,8 +823,7 @@ def verify_rotary_append(q, k_new, v_new, positions, inv_freq, k_cache, v_cache,
     if q.dim() != 3 or k_new.dim() != 3 or v_new.dim() != 3:
         raise ValueError("q must be [T, Hq, D], k_new and v_new [T, Hkv, D]")
     T, Hq, D = q.shape
-    dtype, dev = q.dtype, q.device
-    idx = dev.index if dev.type == "cuda" else -1
+    dtype, dev, idx = q.dtype, q.device, q.get_device()
     p_q, s_q = _rows_arg(q, "q", Hq, D, dtype, idx, dev, T)
     (p_kc, p_vc, *desc), attn = _layer_args(Hq, D, dtype, q.element_size(), idx, dev, k_cache, v_cache, block_tables,
                                             seq_lens, q_start)
@@ -845,13 +845,16 @@ def verify_rotary_append(q, k_new, v_new, positions, inv_freq, k_cache, v_cache,
     return q_out
 
 
-def key_weights_workspace_size(q, k_cache, block_tables, *, max_q_len: int, max_seq_len: int) -> int:
-    params = _attn_params(q, k_cache, block_tables, 0, 0.0, 0)
+def _workspace_size(where, params, *bounds):
+    """The size query `where`, in bytes."""
     n = ctypes.c_size_t(0)
-    _check(library().verify_key_weights_workspace_size(ctypes.byref(params), q.shape[0], int(max_q_len),
-                                                       int(max_seq_len), ctypes.byref(n)),
-           "verify_key_weights_workspace_size")
+    _check(getattr(library(), where)(ctypes.byref(params), *bounds, ctypes.byref(n)), where)
     return int(n.value)
+
+
+def key_weights_workspace_size(q, k_cache, block_tables, *, max_q_len: int, max_seq_len: int) -> int:
+    return _workspace_size("verify_key_weights_workspace_size", _attn_params(q, k_cache, block_tables, 0, 0.0, 0),
+                           q.shape[0], int(max_q_len), int(max_seq_len))
 
 
 def verify_key_weights(q, k_cache, key_weights, key_order, block_tables, seq_lens, q_start, *, max_q_len: int,
@@ -871,8 +874,7 @@ def verify_key_weights(q, k_cache, key_weights, key_order, block_tables, seq_len
     if q.dim() != 3:
         raise ValueError("q must be [T, Hq, D], got %s" % (tuple(q.shape),))
     T, Hq, D = q.shape
-    dtype, dev = q.dtype, q.device
-    idx = dev.index if dev.type == "cuda" else -1
+    dtype, dev, idx = q.dtype, q.device, q.get_device()
     p_q = _arg(q, "q", None, dtype, idx, dev)
     p_kc, params = _key_cache_arg(k_cache, Hq, D, dtype, q.element_size(), idx, dev)
     nb, hkv = k_cache.shape[0], k_cache.shape[1]
@@ -888,7 +890,7 @@ def verify_key_weights(q, k_cache, key_weights, key_order, block_tables, seq_len
                  block_tables=block_tables, num_blocks=nb, max_seq_len=max_seq_len, stream=stream)
     params.scale = float(scale)
     if workspace is None:
-        ws_have = key_weights_workspace_size(q, k_cache, block_tables, max_q_len=max_q_len, max_seq_len=max_seq_len)
+        ws_have = _workspace_size("verify_key_weights_workspace_size", params, T, int(max_q_len), int(max_seq_len))
         if ws_have > 0:
             workspace = _scratch(ws_have, torch.uint8, dev, stream)
             p_ws = workspace.data_ptr()
@@ -930,10 +932,7 @@ def _key_state(key_weights, key_order, nb, hkv, idx, dev):
 def evict_plan_workspace_size(num_seqs: int, num_kv_heads: int, max_blocks: int, *, max_seq_len: int,
                               max_keys: int) -> int:
     params = AttnParams(int(num_seqs), int(num_kv_heads), int(num_kv_heads), 128, 16, int(max_blocks), 0, 0, 0.0, BF16, 0)
-    n = ctypes.c_size_t(0)
-    _check(library().verify_evict_plan_workspace_size(ctypes.byref(params), int(max_seq_len), int(max_keys),
-                                                      ctypes.byref(n)), "verify_evict_plan_workspace_size")
-    return int(n.value)
+    return _workspace_size("verify_evict_plan_workspace_size", params, int(max_seq_len), int(max_keys))
 
 
 def verify_evict_plan(key_weights, key_order, block_tables, seq_lens, *, max_keys: int, keep_first: int = 0,
@@ -951,8 +950,7 @@ def verify_evict_plan(key_weights, key_order, block_tables, seq_lens, *, max_key
     i32 = torch.int32
     if key_weights.dim() != 3:
         raise ValueError("key_weights must be [num_blocks, Hkv, 16], got %s" % (tuple(key_weights.shape),))
-    dev = key_weights.device
-    idx = dev.index if dev.type == "cuda" else -1
+    dev, idx = key_weights.device, key_weights.get_device()
     nb, hkv = key_weights.shape[:2]
     p_w, p_o = _key_state(key_weights, key_order, nb, hkv, idx, dev)
     # the plan depends neither on the head dim nor on the storage type
@@ -968,7 +966,7 @@ def verify_evict_plan(key_weights, key_order, block_tables, seq_lens, *, max_key
     p_new = _arg(new_lens, "new_lens", (B,), i32, idx, dev)
     p_ws, ws_have = _workspace_arg(workspace, idx, dev)
     if workspace is None:
-        ws_have = evict_plan_workspace_size(B, hkv, block_tables.shape[1], max_seq_len=max_seq_len, max_keys=max_keys)
+        ws_have = _workspace_size("verify_evict_plan_workspace_size", params, int(max_seq_len), max_keys)
         if ws_have > 0:
             workspace = _scratch(ws_have, torch.uint8, dev, stream)
             p_ws = workspace.data_ptr()
@@ -989,8 +987,7 @@ def verify_kv_compact(k_cache, v_cache, block_tables, source, new_lens, *, key_w
     i32 = torch.int32
     if k_cache.dim() != 5 or source.dim() != 3:
         raise ValueError("k_cache must be [num_blocks, Hkv, D/x, 16, x] and source [B, Hkv, max_keys]")
-    dtype, dev = k_cache.dtype, k_cache.device
-    idx = dev.index if dev.type == "cuda" else -1
+    dtype, dev, idx = k_cache.dtype, k_cache.device, k_cache.get_device()
     nb, hkv = k_cache.shape[:2]
     D = k_cache.shape[2] * k_cache.shape[4]
     p_kc, params = _key_cache_arg(k_cache, hkv, D, dtype, k_cache.element_size(), idx, dev)
