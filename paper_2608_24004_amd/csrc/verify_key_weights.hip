@@ -157,6 +157,19 @@ __device__ __forceinline__ void stage_rows(const WgtArgs& a, const WgtGeom& geo,
         pos[t] = first + t < geo.rows ? geo.S - geo.n + by_group(a, first + t) : -1;
 }
 
+// op over the 16 lanes of a row, by rotations of it within the vector unit (shuffles
+// go through LDS, one latency each).
+template <typename Op>
+__device__ __forceinline__ float of_16_lanes(float x, Op op) {
+    auto turn = [](float x, auto n) {
+        return __uint_as_float(__builtin_amdgcn_update_dpp(0u, __float_as_uint(x), 0x120 + decltype(n)::value, 0xf, 0xf, false));
+    };
+    x = op(x, turn(x, std::integral_constant<int, 8>{}));
+    x = op(x, turn(x, std::integral_constant<int, 4>{}));
+    x = op(x, turn(x, std::integral_constant<int, 2>{}));
+    return op(x, turn(x, std::integral_constant<int, 1>{}));
+}
+
 // K tile of block `phys`, KV head g.  ONCE: read for the last time in the call, and kept
 // out of the way of what is read again (the second pass of the 32 requests above: 187 ->
 // 181 us for both; the only one of a decoding step, 32 requests of 4097 keys: 70 -> 63).
@@ -343,8 +356,8 @@ __global__ __launch_bounds__(kWgtThreads) void weight_stats(WgtArgs a) {
         for (int r = 0; r < RT; ++r)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const float M = wave_max_xor(m[r][e], 16);
-                const float L = wave_sum_xor(l[r][e] * __builtin_amdgcn_exp2f(m[r][e] - M), 16);
+                const float M = of_16_lanes(m[r][e], [](float x, float y) { return fmaxf(x, y); });
+                const float L = of_16_lanes(l[r][e] * __builtin_amdgcn_exp2f(m[r][e] - M), [](float x, float y) { return x + y; });
                 if (l16 == 0) {
                     s_m[w][r * 16 + lg * 4 + e] = M;
                     s_l[w][r * 16 + lg * 4 + e] = L;
