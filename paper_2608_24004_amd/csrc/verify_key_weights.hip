@@ -170,6 +170,14 @@ __device__ __forceinline__ float of_16_lanes(float x, Op op) {
     return op(x, turn(x, std::integral_constant<int, 1>{}));
 }
 
+// The sum over the four rows of 16 lanes.
+__device__ __forceinline__ float of_4_rows(float x) {
+    const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = __uint_as_float(a[0]) + __uint_as_float(a[1]);  // rows 0 + 1 twice, 2 + 3 twice
+    const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float(b[0]) + __uint_as_float(b[1]);
+}
+
 // K tile of block `phys`, KV head g.  ONCE: read for the last time in the call, and kept
 // out of the way of what is read again (the second pass of the 32 requests above: 187 ->
 // 181 us for both; the only one of a decoding step, 32 requests of 4097 keys: 70 -> 63).
@@ -540,8 +548,7 @@ __global__ __launch_bounds__(kWgtThreads) void weight_sums(WgtArgs a) {
             bool store = false;
 #pragma unroll
             for (int x = 0; x < NB; ++x) {
-                sum[x] += __shfl_xor(sum[x], 16);
-                sum[x] += __shfl_xor(sum[x], 32);
+                sum[x] = of_4_rows(sum[x]);
                 if (lg == x) {
                     mine = sum[x];
                     block = phys[x];
@@ -677,8 +684,7 @@ __global__ __launch_bounds__(kWgtThreads) void weight_sums_rows(WgtArgs a) {
     bool store = false;
 #pragma unroll
     for (int x = 0; x < NB; ++x) {
-        sum[x] += __shfl_xor(sum[x], 16);
-        sum[x] += __shfl_xor(sum[x], 32);
+        sum[x] = of_4_rows(sum[x]);
         if (lg == x) {
             mine = sum[x];
             block = phys[x];
