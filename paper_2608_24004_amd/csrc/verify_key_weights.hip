@@ -17,10 +17,10 @@
 //   weight_join, weight_sums_rows, weight_store   the parts joined once, then keys
 //                 stay in registers and the rows stream past through LDS.
 // What bounds it: few rows, the keys' bytes (32 requests of 475 MB of keys, 36 rows each:
-// 181 us for two passes that both read them, 5.2 TB/s, the rate of a copy); many rows, the
-// exponentials, one per row and key and pass beside four other vector instructions (the
-// prompts named at weight_sums_rows' segments: 72 and 76 us, of which the matrix
-// instructions take 14 each).
+// 179 us for two passes that both read them, 5.3 TB/s, the rate of a copy); many rows, the
+// vector instructions, an exponential per row and key and pass among them (the prompts
+// named at weight_sums_rows' segments: 65 and 74 us, of which the matrix instructions
+// take 14 each).
 // Scores are MFMA products, the queries the first operand and 16 keys the second, so
 // that a lane holds one key (column) and four rows of every product.  A block's K tile
 // lies in memory as the operand wants it: 16 bytes per lane, 1 KiB per load, no LDS.
@@ -747,15 +747,15 @@ int make_plan(const verify_attn_params& p, int32_t total_q, int32_t max_q_len, i
     // Every row chunk reads the keys again: as few as hold the tiles, evenly (64 requests
     // of 72 rows, head dim 64: 418 us with four tiles each, 294 with all five).  A
     // prompt's keys come from the cache, and it is better off with more wavefronts in a
-    // compute unit (139 us with four tiles each, 157 with eight).
+    // compute unit (133 us with four tiles each, 146 with eight).
     const int64_t parts = tiles > 32 ? (tiles + 3) / 4 : (tiles + kStatTiles - 1) / kStatTiles;
     pl.stat_tiles = (int)((tiles + parts - 1) / parts);
     pl.chunks = (int)std::min<int64_t>(parts, 4096);
     // A split has at least a step, and at most 128 blocks, towards two workgroups per
-    // compute unit in bf16 (eight requests of 2000 to 4096 keys, 36 rows: 29 us with 512
-    // workgroups, 37 with 1024, 45 with 2048: each stages the rows and joins their parts)
-    // and eight in fp32, whose products take 16 times as long and are better spread (six
-    // requests of 500 to 4100 keys, 40 rows, head dim 64: 38, 38 and 30 us).
+    // compute unit in bf16 (eight requests of 2000 to 4096 keys, 36 rows: 28 us with 512
+    // workgroups, 33 with 1024: each stages the rows and joins their parts) and eight in
+    // fp32, whose products take 16 times as long and are better spread (six requests of
+    // 500 to 4100 keys, 40 rows, head dim 64: 36 us with 1024, 27 with 2048).
     const int64_t want = bf16 ? 512 : 2048, most = (blocks + step - 1) / step, least = pl.chunks > 1 ? (blocks + 1023) / 1024 : (blocks + 127) / 128;
     const int64_t wgs = (int64_t)p.num_kv_heads * pl.chunks;
     auto splits = [&](int64_t seqs) { return std::max(least, std::min(most, (want + seqs * wgs - 1) / (seqs * wgs))); };
