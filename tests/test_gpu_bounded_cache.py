@@ -408,3 +408,79 @@ def test_workspace_of_a_larger_batch_serves_smaller_ones():
                                   torch.zeros(B + 1, dtype=torch.int32, device=DEV), max_q_len=mq, max_seq_len=ms,
                                   workspace=ws)
     torch.cuda.synchronize()
+
+
+def _least(call, most):
+    """The fewest bytes of workspace that `call` takes."""
+    low, high = 0, most  # high is taken
+    while low < high:
+        mid = (low + high) // 2
+        try:
+            call(mid)
+            high = mid
+        except av.VerifyError as e:
+            assert e.status == av.EWORKSPACE
+            low = mid + 1
+    return high
+
+
+@pytest.mark.parametrize("S,n,G,dtype", [
+    ([300, 40, 1], [1, 1, 1], 4, "bf16"),      # scores in the workspace
+    ([500, 77], [9, 3], 4, "bf16"),
+    ([700, 400], [300, 220], 4, "bf16"),       # segments
+    ([260, 31], [40, 31], 8, "f32"),
+])
+def test_key_weights_keep_to_their_workspace(S, n, G, dtype):
+    """Nothing is written behind the least size that the call takes, and nothing
+    depends on what it held."""
+    rng = np.random.default_rng(S[0])
+    c = Cache(rng, S, hkv=2, d=128, dtype=dtype)
+    q = torch.as_tensor(rng.standard_normal((sum(n), 2 * G, 128))).to(workload.torch_dtype(dtype)).to(DEV)
+    kc, _, w0, o0, bt, sl = c.to(DEV)
+    kw = dict(max_q_len=max(n), max_seq_len=max(S))
+    most = av.key_weights_workspace_size(q, kc, bt, **kw)
+    buf = torch.empty(most + 4096, dtype=torch.uint8, device=DEV)
+    out = []
+
+    def call(size):
+        w, o = w0.clone(), o0.clone()
+        av.verify_key_weights(q, kc, w, o, bt, sl, _dev(q_start_of(n)), workspace=buf[:size], **kw)
+        out.append((bits(w), bits(o)))
+
+    least = _least(call, most)
+    for fill in (0xFF, 0x3C):
+        buf.fill_(fill)
+        call(least)
+        assert (buf[least:] == fill).all()
+    for w, o in out[-2:]:
+        np.testing.assert_array_equal(w, out[0][0])
+        np.testing.assert_array_equal(o, out[0][1])
+
+
+@pytest.mark.parametrize("S", [[40000, 17000], [200000, 90]])
+def test_evict_plan_keeps_to_its_workspace(S):
+    rng = np.random.default_rng(7)
+    blocks = [-(-s // BLOCK) for s in S]
+    bt = torch.full((len(S), max(blocks)), -1, dtype=torch.int32)
+    for i, b in enumerate(blocks):
+        bt[i, :b] = torch.arange(b) + sum(blocks[:i])
+    w = torch.as_tensor(rng.integers(0, 300, size=(sum(blocks), 2, BLOCK)), dtype=torch.float32, device=DEV)
+    args = (w, None, bt.to(DEV), _dev(S))
+    kw = dict(max_keys=5000, keep_recent=100, max_seq_len=max(S))
+    most = av.evict_plan_workspace_size(len(S), 2, max(blocks), max_seq_len=max(S), max_keys=5000)
+    buf = torch.empty(most + 4096, dtype=torch.uint8, device=DEV)
+    out = []
+
+    def call(size):
+        src, lens = av.verify_evict_plan(*args, workspace=buf[:size], **kw)
+        out.append((src.cpu().numpy(), lens.cpu().numpy()))
+
+    least = _least(call, most)
+    for fill in (0xFF, 0x3C):
+        buf.fill_(fill)
+        call(least)
+        assert (buf[least:] == fill).all()
+    rs, rl = bounded.evict_plan(w.double().cpu().numpy(), None, bt.numpy(), S, sum(blocks), max_keys=5000, keep_recent=100)
+    for src, lens in out[-2:]:
+        np.testing.assert_array_equal(src, rs)
+        np.testing.assert_array_equal(lens, rl)
