@@ -616,7 +616,7 @@ int verify_key_weights(const verify_attn_params *params, int32_t total_q, int32_
  *   workspace    16-byte aligned (VERIFY_EINVAL otherwise), at least
  *                verify_evict_plan_workspace_size() bytes (may be NULL if that is 0);
  *                its contents on entry are ignored
- * VERIFY_EUNSUPPORTED beyond 2^24 slots per request and from 131072 KV heads on.
+ * VERIFY_EUNSUPPORTED beyond 2^24 slots per request and from 65536 KV heads on.
  */
 int verify_evict_plan_workspace_size(const verify_attn_params *params, int32_t max_seq_len,
                                      int32_t max_keys, size_t *bytes);

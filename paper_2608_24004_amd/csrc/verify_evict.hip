@@ -7,9 +7,9 @@
 // 0xffffffff for what is always kept, 0 for what never is.  At least c keys are not 0
 // (every slot below c has one), so a key of 0 counts nowhere.
 //   evict_plan    caches of up to 16384 slots: one workgroup, one launch, the keys in
-//                 registers, 4, 8 or 16 per thread, from the first pass to the last (32
-//                 requests of 4096 slots, eight heads: 15 us with 16, 10 with 4; of 8192:
-//                 18 with 16, 15 with 8);
+//                 registers, 4, 8 or 16 per thread, from the first pass to the last (one
+//                 request of 1024 slots, eight heads: 11.7 us with 16, 6.3 with 4;
+//                 of 8192: 12.3 with 16, 9.6 with 8);
 //   evict_hist (three launches), evict_lists, evict_join
 //                 longer caches: a workgroup per chunk of them, the sort keys, histograms
 //                 and lists in the workspace between the launches (a single workgroup
@@ -325,12 +325,15 @@ __device__ __forceinline__ bool plan_ends(const PlanArgs& a, const PlanGeom& p, 
     return true;
 }
 
-// Grid (KV heads, requests), caches of up to N slots per thread.
+// Grid (requests, KV heads), caches of up to N slots per thread.  Workgroups go round the
+// eight XCDs: where the requests are a multiple of eight, a request's heads meet in one,
+// whose L2 then serves the lines that hold two heads' slots (32 requests of 16384 slots,
+// eight heads: 24 us with the heads first, 20; of 4096: 9.9 and 8.4).
 template <int N>
 __global__ __launch_bounds__(kPlanThreads) void evict_plan(PlanArgs a) {
     __shared__ PlanShared sh;
     __shared__ uint16_t s_hole[kPlanThreads * N / 2], s_mover[kPlanThreads * N / 2];  // at most min(c, S - c) each
-    const PlanGeom p = plan_geom(a, blockIdx.x, blockIdx.y);
+    const PlanGeom p = plan_geom(a, blockIdx.y, blockIdx.x);
     int32_t* source = a.source + p.pair * a.max_keys;
     if (plan_ends(a, p, source)) return;
     uint32_t key[N];
@@ -595,9 +598,10 @@ int64_t plan_chunks(const verify_attn_params& p, int32_t max_seq_len) {
 // 196608 40 and 39, a million 183 and 88).
 size_t plan_hists(int64_t chunks) { return chunks + (chunks > 20); }
 
-// A grid dimension holds fewer than 2^32 threads: those of the chunks and of evict_sum.
+// A grid's first dimension holds fewer than 2^32 threads, those of the chunks and of
+// evict_sum; its second fewer than 2^16 workgroups, evict_plan's heads.
 bool plan_fits(const verify_attn_params& p, int64_t chunks) {
-    return chunks <= kMaxChunks && std::max<int64_t>(chunks, kBins / kWave) * p.num_kv_heads < (1 << 22);
+    return chunks <= kMaxChunks && p.num_kv_heads < (1 << 16) && std::max<int64_t>(chunks, kBins / kWave) * p.num_kv_heads < (1 << 22);
 }
 
 struct PlanSpace {
@@ -666,8 +670,8 @@ extern "C" int verify_evict_plan(const verify_attn_params* params, int32_t max_s
     a.max_keys = max_keys;
     a.keep_first = keep_first;
     a.keep_recent = keep_recent;
-    dim3 grid((unsigned)p.num_kv_heads, (unsigned)p.num_seqs);
     if (space.total == 0) {  // (also where no request can exceed max_keys)
+        const dim3 grid((unsigned)p.num_seqs, (unsigned)p.num_kv_heads);
         const int64_t longest = std::min<int64_t>(max_seq_len, (int64_t)p.max_blocks_per_seq * kBlockTokens);
         if (longest <= 4 * kPlanThreads) hipLaunchKernelGGL(evict_plan<4>, grid, dim3(kPlanThreads), 0, stream, a);
         else if (longest <= 8 * kPlanThreads) hipLaunchKernelGGL(evict_plan<8>, grid, dim3(kPlanThreads), 0, stream, a);
@@ -680,7 +684,7 @@ extern "C" int verify_evict_plan(const verify_attn_params* params, int32_t max_s
     a.lists = reinterpret_cast<uint16_t*>(ws + space.lists);
     a.counts = reinterpret_cast<int2*>(ws + space.counts);
     a.state = reinterpret_cast<uint2*>(ws + space.state);
-    grid.x *= (unsigned)chunks;
+    const dim3 grid((unsigned)(p.num_kv_heads * chunks), (unsigned)p.num_seqs);
     const dim3 sums((unsigned)(p.num_kv_heads * (kBins / kWave)), (unsigned)p.num_seqs);
     auto sum = [&](int pass) {
         if (a.hists > a.chunks) hipLaunchKernelGGL(evict_sum, sums, dim3(kPlanThreads), 0, stream, a, pass);

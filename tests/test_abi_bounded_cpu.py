@@ -168,8 +168,10 @@ def test_evict_plan_arguments():
     assert _plan(_attn(sliding_window=64)) == av.EUNSUPPORTED
     for x in (0, 1):
         assert _plan(_attn(), ptrs={x: ctypes.c_void_p(0x1004)}) == av.EINVAL
-    many = _attn(num_q_heads=1 << 17, num_kv_heads=1 << 17, max_blocks_per_seq=4096)
-    assert query(ctypes.byref(many), 40000, 100, ctypes.byref(size)) == _plan(many, ms=40000) == av.EUNSUPPORTED
+    for heads in (1 << 16, 1 << 17):
+        many = _attn(num_q_heads=heads, num_kv_heads=heads, max_blocks_per_seq=4096)
+        for ms in (1000, 40000):
+            assert query(ctypes.byref(many), ms, 100, ctypes.byref(size)) == _plan(many, ms=ms) == av.EUNSUPPORTED
     assert _plan(long, ms=40000, ws=ctypes.c_void_p(0x1008)) == av.EINVAL
     assert _plan(long, ms=40000, have=need - 1) == _plan(long, ms=40000, ws=None) == av.EWORKSPACE
     assert _plan(_attn(num_seqs=0), have=0, ws=None) == av.OK
