@@ -758,9 +758,11 @@ int make_plan(const verify_attn_params& p, int32_t total_q, int32_t max_q_len, i
     // 500 to 4100 keys, 40 rows, head dim 64: 36 us with 1024, 27 with 2048).
     const int64_t want = bf16 ? 512 : 2048, most = (blocks + step - 1) / step, least = pl.chunks > 1 ? (blocks + 1023) / 1024 : (blocks + 127) / 128;
     const int64_t wgs = (int64_t)p.num_kv_heads * pl.chunks;
-    auto splits = [&](int64_t seqs) { return std::max(least, std::min(most, (want + seqs * wgs - 1) / (seqs * wgs))); };
-    const int64_t ns = splits(std::max(1, p.num_seqs));
-    pl.split_blocks = (int)(((blocks + ns - 1) / ns + step - 1) / step * step);
+    auto split_of = [&](int64_t seqs) {  // its blocks, in a batch of `seqs` requests
+        const int64_t ns = std::max(least, std::min(most, (want + seqs * wgs - 1) / (seqs * wgs)));
+        return ((blocks + ns - 1) / ns + step - 1) / step * step;
+    };
+    pl.split_blocks = (int)split_of(std::max(1, p.num_seqs));
     pl.splits = (int)((blocks + pl.split_blocks - 1) / pl.split_blocks);
     pl.once = tiles * tile_bytes(p) <= 56 * 1024;
     if (pl.once) {
@@ -803,12 +805,13 @@ int make_plan(const verify_attn_params& p, int32_t total_q, int32_t max_q_len, i
     }
     pl.sums_at = pl.rows_at + joined;
     pl.bytes = pl.sums_at + sums + scores;
-    // Any batch of fewer requests: b of them have at most b max_q_len rows and
-    // want / (b wgs) + 1 splits, or `least`.
-    const int64_t few = ((int64_t)std::max(1, max_q_len) * want + wgs - 1) / wgs + total_q;
-    pl.cover = std::max(pl.bytes, align_up(row * (size_t)std::max(std::min(few, (int64_t)total_q * most), (int64_t)total_q * least), 256) + joined + scores);
-    if (!pl.once)  // fewer requests may have more segments: kSumWgs of them at most in all
-        pl.cover += std::max(sums, align_up((size_t)(kSumWgs / ((blocks + pl.sum_blocks - 1) / pl.sum_blocks)) * pl.sum_keys * sizeof(float), 256));
+    // Any batch of fewer requests and rows: one request alone is cut into the most splits,
+    // and all total_q rows may be its own, whatever max_q_len says.  Fewer requests may also
+    // have more segments: kSumWgs of them at most in all.
+    const size_t most_parts = row * total_q * (size_t)((blocks + split_of(1) - 1) / split_of(1));
+    const int64_t key_ranges = (blocks + pl.sum_blocks - 1) / pl.sum_blocks;
+    const size_t most_sums = pl.once ? 0 : align_up((size_t)(kSumWgs / key_ranges) * pl.sum_keys * sizeof(float), 256);
+    pl.cover = align_up(most_parts, 256) + joined + std::max(sums, most_sums) + scores;
     *out = pl;
     return VERIFY_OK;
 }

@@ -137,6 +137,25 @@ def test_key_weights_arguments():
     assert _weights(_attn(num_seqs=0), T=0, have=0, ws=None) == av.OK
 
 
+@pytest.mark.parametrize("dtype", [av.BF16, av.F32])
+@pytest.mark.parametrize("hq,hkv,d,mq,ms", [(32, 8, 128, 9, 16384), (8, 8, 128, 1, 5000), (64, 1, 64, 1, 4000),
+                                            (32, 2, 128, 200, 4000), (8, 1, 128, 9, 131072), (32, 8, 64, 600, 900)])
+def test_key_weights_workspace_covers_fewer_requests_with_as_many_rows(dtype, hq, hkv, d, mq, ms):
+    """The size asked for a batch serves every batch of fewer requests and rows, also
+    one with more rows than its requests announce (max_q_len only sizes the launch).  A
+    cache of no blocks: the call ends after its checks."""
+    size = ctypes.c_size_t(0)
+    attn = lambda B: _attn(num_seqs=B, num_q_heads=hq, num_kv_heads=hkv, head_dim=d, dtype=dtype, num_blocks=0,
+                           max_blocks_per_seq=-(-ms // 16))
+    for B, T in ((32, 32 * mq), (32, 7), (5, 500), (1, 1)):
+        assert av.library().verify_key_weights_workspace_size(ctypes.byref(attn(B)), T, mq, ms,
+                                                              ctypes.byref(size)) == av.OK
+        for b in sorted({1, 2, 3, (B + 1) // 2, B}):
+            for t in sorted({1, T // 3, T - 1, T}):
+                if b <= B:
+                    assert _weights(attn(b), T=t, mq=mq, ms=ms, have=size.value) == av.OK, (B, T, b, t)
+
+
 def _plan(attn, ms=1000, keys=100, first=4, recent=10, ptrs=None, ws=DUMMY, have=1 << 30):
     p = [DUMMY] * 7  # weights, order, bt, sl, tokens, source, lens
     for k, v in (ptrs or {}).items():
