@@ -132,9 +132,10 @@ __device__ __forceinline__ f32x4_t product(const uint4* q, const uint4* k, float
 }
 
 // Stages rows [first, first + 16 tiles) of (request, KV head) in LDS in operand
-// order.  Places behind the last row repeat the chunk's first row: their products are
-// finite wherever that row's are, so what is multiplied by zero later stays zero.
-// `pos` receives the rows' positions (-1 without a row).
+// order.  Places behind the last row repeat it.  Where no row of a tile is masked, their
+// products are multiplied by zero, which leaves a NaN of a row or key that is not finite:
+// the last row sees every key that any row of its tile sees, so that such a key's weight
+// is NaN by that row itself.  `pos` receives the rows' positions (-1 without a row).
 template <typename T, int D>
 __device__ __forceinline__ void stage_rows(const WgtArgs& a, const WgtGeom& geo, int g, int first, int tiles, uint4* lds,
                                            int* pos) {
@@ -142,7 +143,7 @@ __device__ __forceinline__ void stage_rows(const WgtArgs& a, const WgtGeom& geo,
     for (int e = threadIdx.x; e < tiles * NC * kWave; e += kWgtThreads) {
         const int lane = e % kWave, c = e / kWave % NC, tile = e / kWave / NC;
         int r = first + tile * 16 + lane % 16;
-        if (r >= geo.rows) r = first;
+        if (r >= geo.rows) r = geo.rows - 1;
         if (geo.rows == 0) {
             lds[e] = make_uint4(0, 0, 0, 0);
             continue;
