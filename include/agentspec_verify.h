@@ -497,7 +497,8 @@ typedef struct verify_rotary_params {
  *               k themselves (with the same strides) and must not overlap them
  *               otherwise
  * No workspace.  VERIFY_EINVAL for strides below heads * D, an axis out of range, a
- * scale that is negative or not finite.
+ * scale that is negative or not finite; VERIFY_EUNSUPPORTED for more than 2^28 - 16
+ * rows, more than 32768 query or 16384 KV heads.
  */
 int verify_rotary(const verify_rotary_params *params, int32_t total_q, int32_t num_q_heads,
                   int32_t num_kv_heads, const void *q, int64_t q_stride, const void *k,

@@ -330,6 +330,7 @@ int check_params(const verify_rotary_params* p, int32_t total_q, int32_t hq, int
         if (p->axis[f] >= p->num_axes) return VERIFY_EINVAL;
     if (total_q < 0 || hq < 1 || hkv < 0) return VERIFY_EINVAL;
     if (hq > 32768 || hkv > 16384) return VERIFY_EUNSUPPORTED;  // grid y
+    if (((int64_t)total_q + kTile - 1) / kTile >= (1 << 24)) return VERIFY_EUNSUPPORTED;  // fewer than 2^32 threads in x
     return VERIFY_OK;
 }
 

@@ -79,6 +79,14 @@ def test_rotary_arguments(kw, want):
     assert _rotary(None) == av.EINVAL
 
 
+@pytest.mark.parametrize("T", [(1 << 28) - 15, 1 << 28, 2 ** 31 - 15, 2 ** 31 - 1])
+def test_rotary_of_more_rows_than_a_launch_holds(T):
+    assert _rotary(_rot(), T=T) == av.EUNSUPPORTED
+    for attn in (_attn(), _attn(num_seqs=0)):
+        args = (ctypes.byref(attn), ctypes.byref(_rot()), T, DUMMY, 1024, DUMMY, 256, DUMMY, 256) + (DUMMY,) * 6
+        assert av.library().verify_rotary_append(*args, 1024, DUMMY, DUMMY, None) == av.EUNSUPPORTED
+
+
 def test_rotary_append_arguments():
     lib = av.library()
 
