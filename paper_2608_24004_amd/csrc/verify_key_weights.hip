@@ -42,7 +42,6 @@ typedef float f32x4_t __attribute__((ext_vector_type(4)));
 typedef int i32x4_t __attribute__((ext_vector_type(4)));
 // queries are aligned to their elements only
 typedef uint32_t u32x4u_t __attribute__((ext_vector_type(4), aligned(2)));
-typedef float f32x4u_t __attribute__((ext_vector_type(4), aligned(8)));
 
 struct WgtArgs {
     const void* q;
@@ -56,7 +55,7 @@ struct WgtArgs {
     float* key_weights;
     int32_t* key_order;
     float2* part;  // (maximum, sum relative to it) of each row and split, see part_of
-    float2* rows;  // (maximum, 1 / sum) of each row: [request][KV head][row], 16 more behind the last
+    float2* rows;  // (maximum, 1 / sum) of each row: [request][KV head][row]
     int num_seqs, total_q, hq, hkv, group, max_blocks, num_blocks, max_seq_len;
     float scale_log2, decay;
     uint32_t group_magic;        // ceil(2^32 / group)
@@ -528,7 +527,7 @@ __global__ __launch_bounds__(kWgtThreads) void weight_sums(WgtArgs a) {
         }
         __syncthreads();
         auto step = [&](const Operand<T, D> (&k)[NB], const int (&phys)[NB], uint32_t ok, int b) {
-            const float old = load_old(ok, phys, b);
+            const float old = first == 0 ? load_old(ok, phys, b) : 0.f;
             float sum[NB];
 #pragma unroll
             for (int x = 0; x < NB; ++x) sum[x] = 0.f;
@@ -787,7 +786,7 @@ int make_plan(const verify_attn_params& p, int32_t total_q, int32_t max_q_len, i
     const size_t row = (size_t)p.num_q_heads * sizeof(float2);
     // the parts, and with many rows what they join into
     pl.rows_at = align_up(row * total_q * pl.splits, 256);
-    const size_t joined = pl.once || total_q == 0 ? 0 : align_up(row * total_q + 16 * sizeof(float2), 256);
+    const size_t joined = pl.once ? 0 : align_up(row * total_q, 256);
     pl.sum_keys = blocks * kBlockTokens;
     const size_t sums = pl.segments > 1 ? align_up((size_t)p.num_seqs * p.num_kv_heads * pl.segments * pl.sum_keys * sizeof(float), 256) : 0;
     // A row tile whose scores are at most a quarter of the keys' bytes to write and read:

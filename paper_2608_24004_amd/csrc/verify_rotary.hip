@@ -44,7 +44,7 @@ struct RotArgs {
     const int32_t* seq_lens;
     const int32_t* q_start;
     int64_t q_stride, k_stride, v_stride, q_out_stride, k_out_stride;
-    int total_q, hq, hkv, num_axes, freqs;
+    int total_q, hq, hkv, freqs;
     int key_wgs, value_wgs, heads_per_wg;
     int num_seqs, max_blocks, num_blocks;
     float scale;
@@ -141,7 +141,7 @@ __global__ __launch_bounds__(kRotThreads) void rotate_rows(RotArgs a) {
     __shared__ Place place[kTile];
     __shared__ uint4 s_start[PLACE ? PLACE : 1];
     __shared__ uint4 s_val[VALUES ? VALUES : 1];
-    const int tid = threadIdx.x, lane = tid & (kWave - 1), wv = tid / kWave;
+    const int tid = threadIdx.x;
     // Workgroups go round the eight XCDs: each takes neighbouring tiles, whose rows share
     // cache lines of the paged cache (six prompts of 12 thousand rows in all: 60 -> 56 us).
     const int xq = gridDim.x / 8, xr = gridDim.x % 8, xcd = blockIdx.x % 8;
@@ -349,7 +349,6 @@ void launch(const RotArgs& a, const verify_rotary_params& p, bool wide, hipStrea
 // Fills in what both calls share and launches.
 template <bool APPEND>
 int rotary_call(RotArgs& a, const verify_rotary_params& p, hipStream_t stream) {
-    a.num_axes = p.num_axes;
     a.freqs = p.rotary_dim / 2;
     a.scale = p.scale > 0.f ? p.scale : 1.f;
     for (int f = 0; f < a.freqs; ++f) a.axis[f] = p.axis[f];
