@@ -565,6 +565,11 @@ int verify_rotary_append(const verify_attn_params *attn, const verify_rotary_par
  * a cache that has lost no key).  Keys of unmapped blocks take no part and nothing
  * of theirs is written; slots from S_i on are left as they are.  Sums are taken in a
  * fixed order (the same call gives the same bits).
+ * The ordinals of keys below S_i - n_i are not written: a caller that passes only the
+ * last rows of a prompt (to weigh its keys by a window of them, with decay 0) writes
+ * those of the rows before itself.
+ * A row or key that is not finite makes NaN the weights of the keys that such a row,
+ * or a row that sees such a key, sees (a key that scores -inf weighs nothing).
  *
  *   q, k_cache, block_tables, seq_lens, q_start, sinks   as for verify_attention,
  *                after the new keys were appended; k_cache 16-byte aligned
@@ -656,7 +661,8 @@ const char *verify_status_string(int status);
 /* Library ABI version (major * 10000 + minor * 100 + patch): 1.9.0.  Since 1.9.0
  * verify_attention_plan reports whole pairs (-1), and the size that
  * verify_attention_workspace_size returns covers batches of fewer requests.  The
- * rotary and bounded-cache calls were added to it without a change to any other. */
+ * rotary and bounded-cache calls were added to it without a change to any other: a
+ * caller that may load a library of 1.9.0 without them looks for their symbols. */
 int verify_abi_version(void);
 
 #ifdef __cplusplus

@@ -868,8 +868,9 @@ def verify_key_weights(q, k_cache, key_weights, key_order, block_tables, seq_len
     its KV head), a new one that weight and the ordinal of its token.  num_rows [B]:
     only the first num_rows[i] rows of request i count (after an acceptance,
     num_emitted).  num_tokens [B]: the request's tokens so far with the new ones
-    (None: seq_lens).  Other arguments as for verify_attention, after the append.
-    Returns key_weights."""
+    (None: seq_lens).  Other arguments as for verify_attention, after the append
+    (check=True also refuses a request of more than max_q_len rows, which the call
+    itself takes).  Returns key_weights."""
     import torch
     if q.dim() != 3:
         raise ValueError("q must be [T, Hq, D], got %s" % (tuple(q.shape),))
