@@ -17,10 +17,11 @@
 //   weight_join, weight_sums_rows, weight_store   the parts joined once, then keys
 //                 stay in registers and the rows stream past through LDS.
 // What bounds it: few rows, the keys' bytes (32 requests of 475 MB of keys, 36 rows each:
-// 179 us for two passes that both read them, 5.3 TB/s, the rate of a copy); many rows, the
-// vector instructions, an exponential per row and key and pass among them (the prompts
-// named at weight_sums_rows' segments: 65 and 74 us, of which the matrix instructions
-// take 14 each).
+// 179 us for two passes that both read them, 5.3 TB/s, the rate of a copy); many rows, in
+// the first pass the vector instructions, an exponential per row and key among them, in the
+// second uneven rows and waits as much (the prompts named at weight_sums_rows' segments: 65
+// and 74 us, in which a compute unit has work for 50 and 46, its vector units then active
+// 77 and 53 % of the time; the matrix instructions take 14 us of each).
 // Scores are MFMA products, the queries the first operand and 16 keys the second, so
 // that a lane holds one key (column) and four rows of every product.  A block's K tile
 // lies in memory as the operand wants it: 16 bytes per lane, 1 KiB per load, no LDS.
@@ -754,8 +755,8 @@ int make_plan(const verify_attn_params& p, int32_t total_q, int32_t max_q_len, i
     // A split has at least a step, and at most 128 blocks, towards two workgroups per
     // compute unit in bf16 (eight requests of 2000 to 4096 keys, 36 rows: 28 us with 512
     // workgroups, 33 with 1024: each stages the rows and joins their parts) and eight in
-    // fp32, whose products take 16 times as long and are better spread (six requests of
-    // 500 to 4100 keys, 40 rows, head dim 64: 36 us with 1024, 27 with 2048).
+    // fp32 (six requests of 500 to 4100 keys, 40 rows, head dim 64: 36 us with 1024, 27
+    // with 2048; the products are 2.5 us of each pass, the rest those starts and ends).
     const int64_t want = bf16 ? 512 : 2048, most = (blocks + step - 1) / step, least = pl.chunks > 1 ? (blocks + 1023) / 1024 : (blocks + 127) / 128;
     const int64_t wgs = (int64_t)p.num_kv_heads * pl.chunks;
     auto split_of = [&](int64_t seqs) {  // its blocks, in a batch of `seqs` requests
