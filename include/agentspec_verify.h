@@ -39,6 +39,12 @@
  *                       rotated to explicit positions on one or several axes;
  *                       the second stores the keys and values like
  *                       verify_kv_append.
+ *   verify_norm_rotary, verify_norm_rotary_append -- the same two with each
+ *                       head's query and key normalised first.
+ *   verify_adjust_logits, verify_count_tokens -- penalties, biases and grammar
+ *                       masks applied to the logits before an acceptance call
+ *                       reads them, and the counts of tokens that the penalties
+ *                       read.
  *   verify_key_weights, verify_evict_plan, verify_kv_compact -- a bound on each
  *                       request's cached keys: the attention weight that every
  *                       cached key has gathered, the keys to keep, and the moves
@@ -527,6 +533,114 @@ int verify_rotary_append(const verify_attn_params *attn, const verify_rotary_par
                          const int32_t *block_tables, const int32_t *seq_lens,
                          const int32_t *q_start, void *q_out, int64_t q_out_stride, void *k_cache,
                          void *v_cache, hipStream_t stream);
+
+/*
+ * verify_norm_rotary, verify_norm_rotary_append -- verify_rotary and
+ * verify_rotary_append with a norm before the rotation: every head x of a row's query
+ * (key) becomes
+ *     x * w / sqrt(sum_d x[d]^2 / D + eps),    w = q_weight (k_weight),
+ * over all D dims, and is then rotated.  Values are not normalised.  Everything between
+ * the load and the store is in fp32: one rounding.
+ *
+ *   q_weight, k_weight  [D] float, or NULL: all ones
+ *   eps                 finite, >= 0 (VERIFY_EINVAL otherwise)
+ * All other arguments and refusals as for verify_rotary and verify_rotary_append.  No
+ * workspace.
+ */
+int verify_norm_rotary(const verify_rotary_params *params, int32_t total_q, int32_t num_q_heads,
+                       int32_t num_kv_heads, const void *q, int64_t q_stride, const void *k,
+                       int64_t k_stride, const float *q_weight, const float *k_weight, float eps,
+                       const int32_t *positions, const double *inv_freq, void *q_out,
+                       int64_t q_out_stride, void *k_out, int64_t k_out_stride, hipStream_t stream);
+
+int verify_norm_rotary_append(const verify_attn_params *attn, const verify_rotary_params *params,
+                              int32_t total_q, const void *q, int64_t q_stride, const void *k_new,
+                              int64_t k_stride, const void *v_new, int64_t v_stride,
+                              const float *q_weight, const float *k_weight, float eps,
+                              const int32_t *positions, const double *inv_freq,
+                              const int32_t *block_tables, const int32_t *seq_lens,
+                              const int32_t *q_start, void *q_out, int64_t q_out_stride,
+                              void *k_cache, void *v_cache, hipStream_t stream);
+
+/*
+ * Changed logits.  Every request of a batch owns a slot of a state of
+ *     counts [num_slots][vocab] int32: how often each token was put out, and
+ *     seen   [num_slots][2][ceil(vocab / 32)] uint32: bit v % 32 of word v / 32 tells
+ *            in the first row whether token v was in the prompt, in the second whether
+ *            its count is not zero (a count whose bit is 0 is taken as zero).
+ * A slot whose counts and bits are zeroed is that of a new request; verify_count_tokens
+ * enters its prompt, and after each step the tokens that the step emitted.
+ */
+typedef struct verify_adjust_params {
+    /* [num_seqs] float each, or NULL: r = 1, f = 0, p = 0.  With all three NULL the
+       state is not read. */
+    const float *repetition, *frequency, *presence;
+    const int32_t *counts;
+    const uint32_t *seen;
+    const int32_t *slots; /* [num_seqs] each request's slot (outside [0, num_slots): a
+                             request that had no token yet), or NULL: slot i          */
+    int32_t num_slots;
+    /* request i's biases are entries bias_start[i] .. bias_start[i + 1] - 1 (clamped to
+       [0, num_biases]) of the other two; bias_start NULL: none.  Tokens outside the
+       vocabulary are passed over; a token named more than once gets its values' sum,
+       taken in their order. */
+    const int32_t *bias_start, *bias_tokens;
+    const float *bias_values;
+    int32_t num_biases;
+    /* mask [num_masks][ceil(vocab / 32)]: bit v % 32 of word v / 32 tells whether token
+       v may follow; mask_rows [total_q]: each row's mask (outside [0, num_masks): every
+       token may follow), or NULL: no masks. */
+    int32_t num_masks;
+    const uint32_t *mask;
+    const int32_t *mask_rows;
+} verify_adjust_params;
+
+/*
+ * verify_adjust_logits -- penalties, biases and masks, for the logits that
+ * verify_accept or verify_accept_sampled then reads.
+ *
+ * Row j of request i is scored behind the drafts tokens[q_start[i] + 1 .. q_start[i] + j],
+ * which therefore count as put out: with c = counts[slot][v] plus the occurrences of v
+ * among them, token v's logit x becomes, in fp32,
+ *     x <- x > 0 ? x (1 / r) : x r        if v was in the prompt or c > 0
+ *     x <- x + (b - (f c + p))            b its bias; f c + p only if c > 0
+ *     x <- -inf                           if the row's mask lacks v
+ * (the first two as one fused multiply-add) and is rounded once to logits_dtype.  Logits
+ * to which none of the three applies keep their value.
+ *
+ *   logits    [total_q][row_stride], vocab entries used; row_stride = 0 means vocab
+ *   tokens, q_start   as for verify_accept; tokens (needed with a penalty) outside the
+ *             vocabulary are passed over
+ *   out       [total_q][out_stride] likewise; may be logits itself (with the same
+ *             stride; what does not change is then not moved) and must not overlap it
+ *             otherwise.  Rows outside the requests' are not written.
+ * No workspace.  VERIFY_EINVAL where a penalty is given without counts, seen or tokens,
+ * entries without their list, masks without mask; VERIFY_EUNSUPPORTED for vocab from
+ * 2^31 - 2049 on.
+ */
+int verify_adjust_logits(int32_t num_seqs, int32_t total_q, int64_t vocab, int64_t row_stride,
+                         int32_t logits_dtype, const void *logits, const int32_t *tokens,
+                         const int32_t *q_start, const verify_adjust_params *params, void *out,
+                         int64_t out_stride, hipStream_t stream);
+
+/*
+ * verify_count_tokens -- enters tokens into the state that verify_adjust_logits reads.
+ *
+ * Request i's tokens are tokens[token_start[i] + j], j < min(num_tokens[i],
+ * token_start[i + 1] - token_start[i]) (num_tokens NULL: all of them): after an
+ * acceptance tokens = emitted, token_start = q_start, num_tokens = num_emitted.  Each is
+ * added to its count and its bit of seen's second row is set; with prompt = 1 its bit of
+ * the first row is set instead.  Tokens outside [0, vocab) and requests whose slot lies
+ * outside [0, num_slots) are passed over.  Two requests may name the same slot.
+ *
+ *   total_tokens  entries of tokens (token_start is clamped to [0, total_tokens])
+ *   counts        may be NULL with prompt = 1
+ * No workspace.
+ */
+int verify_count_tokens(int32_t num_seqs, int32_t total_tokens, int64_t vocab, int32_t num_slots,
+                        const int32_t *tokens, const int32_t *token_start,
+                        const int32_t *num_tokens, const int32_t *slots, int32_t prompt,
+                        int32_t *counts, uint32_t *seen, hipStream_t stream);
 
 /*
  * A bounded cache.  Beside k_cache and v_cache a layer keeps, for every slot and KV

@@ -17,6 +17,11 @@ If the library is missing, every entry point raises -- there is no fallback.
     verify_rotary(...), verify_rotary_append(...)
                                queries and keys rotated to positions on one or
                                several axes, alone or with the append
+    verify_norm_rotary(...), verify_norm_rotary_append(...)
+                               the same behind a norm of each head's query and key
+    verify_adjust_logits(...), verify_count_tokens(...)
+                               penalties, biases and grammar masks on the logits, and
+                               the token counts that the penalties read
     verify_key_weights(...), verify_evict_plan(...), verify_kv_compact(...)
                                a bound on a request's cached keys: the attention
                                weight each has gathered, the keys to keep, their
@@ -36,6 +41,7 @@ __all__ = ["verify_attention", "verify_accept", "verify_accept_noalloc", "verify
            "attention_workspace_size", "attention_plan",
            "accept_workspace_size",
            "lmhead_accept_workspace_size", "verify_rotary", "verify_rotary_append",
+           "verify_norm_rotary", "verify_norm_rotary_append", "verify_adjust_logits", "verify_count_tokens",
            "verify_key_weights", "verify_evict_plan", "verify_kv_compact",
            "key_weights_workspace_size", "evict_plan_workspace_size", "check_batch", "BatchError", "VerifyError", "library",
            "abi_version", "F32", "BF16"]
@@ -96,6 +102,25 @@ class RotaryParams(ctypes.Structure):
     ]
 
 
+class AdjustParams(ctypes.Structure):
+    _fields_ = [
+        ("repetition", ctypes.c_void_p),
+        ("frequency", ctypes.c_void_p),
+        ("presence", ctypes.c_void_p),
+        ("counts", ctypes.c_void_p),
+        ("seen", ctypes.c_void_p),
+        ("slots", ctypes.c_void_p),
+        ("num_slots", ctypes.c_int32),
+        ("bias_start", ctypes.c_void_p),
+        ("bias_tokens", ctypes.c_void_p),
+        ("bias_values", ctypes.c_void_p),
+        ("num_biases", ctypes.c_int32),
+        ("num_masks", ctypes.c_int32),
+        ("mask", ctypes.c_void_p),
+        ("mask_rows", ctypes.c_void_p),
+    ]
+
+
 _lib = None
 
 
@@ -148,6 +173,15 @@ def library(path: Optional[str] = None):
     lib.verify_rotary_append.argtypes = [P, RP, i32, vp, i64, vp, i64, vp, i64, vp, vp, vp, vp, vp, vp, i64, vp,
                                          vp, vp]
     lib.verify_rotary_append.restype = ctypes.c_int
+    lib.verify_norm_rotary.argtypes = [RP, i32, i32, i32, vp, i64, vp, i64, vp, vp, f32, vp, vp, vp, i64, vp, i64, vp]
+    lib.verify_norm_rotary.restype = ctypes.c_int
+    lib.verify_norm_rotary_append.argtypes = [P, RP, i32, vp, i64, vp, i64, vp, i64, vp, vp, f32, vp, vp, vp, vp, vp,
+                                              vp, i64, vp, vp, vp]
+    lib.verify_norm_rotary_append.restype = ctypes.c_int
+    lib.verify_adjust_logits.argtypes = [i32, i32, i64, i64, i32, vp, vp, vp, ctypes.POINTER(AdjustParams), vp, i64, vp]
+    lib.verify_adjust_logits.restype = ctypes.c_int
+    lib.verify_count_tokens.argtypes = [i32, i32, i64, i32, vp, vp, vp, vp, i32, vp, vp, vp]
+    lib.verify_count_tokens.restype = ctypes.c_int
     lib.verify_key_weights_workspace_size.argtypes = [P, i32, i32, i32, ctypes.POINTER(sz)]
     lib.verify_key_weights_workspace_size.restype = ctypes.c_int
     lib.verify_key_weights.argtypes = [P, i32, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp, f32, vp, vp, vp, sz, vp]
@@ -790,7 +824,29 @@ def verify_rotary(q, k, positions, inv_freq, *, axes=None, interleaved: bool = F
     frequencies, needed with more than one.  A pair is dims (f, f + R / 2), or
     (2f, 2f + 1) if interleaved; dims from R on are copied.  scale: a factor of the
     rotated dims (0: 1).  q_out and k_out may be q and k.  Returns (q_out, k_out)."""
+    return _rotary_call("verify_rotary", None, q, k, positions, inv_freq, axes, interleaved, scale, q_out, k_out, stream)
+
+
+def verify_norm_rotary(q, k, positions, inv_freq, *, q_weight=None, k_weight=None, eps: float = 1e-6, axes=None,
+                       interleaved: bool = False, scale: float = 0.0, q_out=None, k_out=None, stream=None):
+    """verify_rotary behind a norm of each head: x * weight / sqrt(mean(x^2) + eps) over
+    the head's D dims, with q_weight and k_weight [D] float32 (None: ones).  Norm and
+    rotation are rounded once.  Other arguments and the result as for verify_rotary."""
+    return _rotary_call("verify_norm_rotary", (q_weight, k_weight, eps), q, k, positions, inv_freq, axes, interleaved,
+                        scale, q_out, k_out, stream)
+
+
+def _norm_args(norm, D, idx, dev):
+    """The norm's arguments of a call: none for a call without one."""
+    if norm is None:
+        return ()
     import torch
+    q_weight, k_weight, eps = norm
+    return (None if q_weight is None else _arg(q_weight, "q_weight", (D,), torch.float32, idx, dev),
+            None if k_weight is None else _arg(k_weight, "k_weight", (D,), torch.float32, idx, dev), float(eps))
+
+
+def _rotary_call(where, norm, q, k, positions, inv_freq, axes, interleaved, scale, q_out, k_out, stream):
     if q.dim() != 3 or k is not None and k.dim() != 3:
         raise ValueError("q must be [T, Hq, D] and k [T, Hkv, D]")
     T, Hq, D = q.shape
@@ -799,6 +855,7 @@ def verify_rotary(q, k, positions, inv_freq, *, axes=None, interleaved: bool = F
     p_q, s_q = _rows_arg(q, "q", Hq, D, dtype, idx, dev, T)
     p_k, s_k = (None, 0) if k is None else _rows_arg(k, "k", Hkv, D, dtype, idx, dev, T)
     params, p_pos, p_freq = _rotary_args(q, positions, inv_freq, axes, interleaved, scale, idx, dev)
+    norm = _norm_args(norm, D, idx, dev)
     if q_out is None:
         q_out = _scratch((T, Hq, D), dtype, dev, stream)
     if k_out is None and k is not None:
@@ -807,7 +864,7 @@ def verify_rotary(q, k, positions, inv_freq, *, axes=None, interleaved: bool = F
     p_ko, s_ko = (None, 0) if k is None else _rows_arg(k_out, "k_out", Hkv, D, dtype, idx, dev, T)
     if idx < 0:
         _dev_ptr(q, "q")
-    _launch("verify_rotary", idx, ctypes.byref(params), T, Hq, Hkv, p_q, s_q, p_k, s_k, p_pos, p_freq, p_qo, s_qo,
+    _launch(where, idx, ctypes.byref(params), T, Hq, Hkv, p_q, s_q, p_k, s_k, *norm, p_pos, p_freq, p_qo, s_qo,
             p_ko, s_ko, _stream_ptr(stream, dev))
     return q_out, k_out
 
@@ -819,7 +876,22 @@ def verify_rotary_append(q, k_new, v_new, positions, inv_freq, k_cache, v_cache,
     paged-cache slots in the same launch (as verify_kv_append writes them).  q [T,
     Hq, D], k_new and v_new [T, Hkv, D], contiguous or slices of wider rows.  check:
     as for verify_kv_append.  Returns q_out."""
-    import torch
+    return _rotary_append_call("verify_rotary_append", None, q, k_new, v_new, positions, inv_freq, k_cache, v_cache,
+                               block_tables, seq_lens, q_start, axes, interleaved, scale, q_out, stream, check)
+
+
+def verify_norm_rotary_append(q, k_new, v_new, positions, inv_freq, k_cache, v_cache, block_tables, seq_lens, q_start,
+                              *, q_weight=None, k_weight=None, eps: float = 1e-6, axes=None,
+                              interleaved: bool = False, scale: float = 0.0, q_out=None, stream=None, check=None):
+    """verify_rotary_append behind a norm of each head's query and key (see
+    verify_norm_rotary; the values are stored as they are).  Returns q_out."""
+    return _rotary_append_call("verify_norm_rotary_append", (q_weight, k_weight, eps), q, k_new, v_new, positions,
+                               inv_freq, k_cache, v_cache, block_tables, seq_lens, q_start, axes, interleaved, scale,
+                               q_out, stream, check)
+
+
+def _rotary_append_call(where, norm, q, k_new, v_new, positions, inv_freq, k_cache, v_cache, block_tables, seq_lens,
+                        q_start, axes, interleaved, scale, q_out, stream, check):
     if q.dim() != 3 or k_new.dim() != 3 or v_new.dim() != 3:
         raise ValueError("q must be [T, Hq, D], k_new and v_new [T, Hkv, D]")
     T, Hq, D = q.shape
@@ -831,8 +903,9 @@ def verify_rotary_append(q, k_new, v_new, positions, inv_freq, k_cache, v_cache,
     p_k, s_k = _rows_arg(k_new, "k_new", Hkv, D, dtype, idx, dev, T)
     p_v, s_v = _rows_arg(v_new, "v_new", Hkv, D, dtype, idx, dev, T)
     params, p_pos, p_freq = _rotary_args(q, positions, inv_freq, axes, interleaved, scale, idx, dev)
+    norm = _norm_args(norm, D, idx, dev)
     if check or check is None and CHECK_BY_DEFAULT:
-        _checked(check, "verify_rotary_append", q_start=q_start, total_q=T, seq_lens=seq_lens,
+        _checked(check, where, q_start=q_start, total_q=T, seq_lens=seq_lens,
                  block_tables=block_tables, num_blocks=k_cache.shape[0],
                  max_seq_len=16 * block_tables.shape[1], sliding_window=1, stream=stream)
     if q_out is None:
@@ -840,9 +913,131 @@ def verify_rotary_append(q, k_new, v_new, positions, inv_freq, k_cache, v_cache,
     p_qo, s_qo = _rows_arg(q_out, "q_out", Hq, D, dtype, idx, dev, T)
     if idx < 0:
         _dev_ptr(q, "q")
-    _launch("verify_rotary_append", idx, ctypes.byref(attn), ctypes.byref(params), T, p_q, s_q, p_k, s_k, p_v, s_v,
-            p_pos, p_freq, *desc, p_qo, s_qo, p_kc, p_vc, _stream_ptr(stream, dev))
+    _launch(where, idx, ctypes.byref(attn), ctypes.byref(params), T, p_q, s_q, p_k, s_k, p_v, s_v, *norm, p_pos,
+            p_freq, *desc, p_qo, s_qo, p_kc, p_vc, _stream_ptr(stream, dev))
     return q_out
+
+
+def _row_matrix(t, name, shape, dtype, idx, device):
+    """Address and row stride of a matrix whose rows are contiguous."""
+    if not (t is not None and t.dtype is dtype and t.get_device() == idx >= 0 and t.shape == shape):
+        _expect(t, name, shape, dtype, device)
+    stride = t.stride(0) if t.shape[0] > 1 else t.shape[1]
+    if t.shape[1] > 1 and t.stride(1) != 1 or stride < t.shape[1]:
+        raise ValueError("%s must have rows of %d adjacent elements, got strides %s" % (name, t.shape[1], tuple(t.stride())))
+    return t.data_ptr(), stride
+
+
+def _token_state(counts, seen, slots, vocab, B, idx, dev):
+    """Addresses of a state of token counts and bits and of the requests' slots in it,
+    and its number of slots."""
+    import torch
+    i32 = torch.int32
+    if counts.dim() != 2:
+        raise ValueError("counts must be [slots, V], got %s" % (tuple(counts.shape),))
+    n = counts.shape[0]
+    if slots is None and n < B:
+        raise ValueError("%d requests have %d slots: name them in slots" % (B, n))
+    return (_arg(counts, "counts", (n, vocab), i32, idx, dev),
+            _arg(seen, "seen", (n, 2, (vocab + 31) // 32), i32, idx, dev),
+            None if slots is None else _arg(slots, "slots", (B,), i32, idx, dev), n)
+
+
+def verify_adjust_logits(logits, tokens, q_start, *, counts=None, seen=None, slots=None, repetition=None,
+                         frequency=None, presence=None, bias_start=None, bias_tokens=None, bias_values=None,
+                         mask=None, mask_rows=None, out=None, stream=None, check=None):
+    """Penalties, biases and grammar masks, before verify_accept or verify_accept_sampled
+    reads the logits.
+
+    logits [T, V] (bf16 or fp32, rows may be strided), tokens [T] and q_start [B + 1] as
+    for verify_accept: row j of a request is scored behind its drafts 1 .. j, which
+    count.  repetition, frequency, presence [B] float32 or None; with any of them counts
+    [slots, V] int32 and seen [slots, 2, ceil(V / 32)] int32 are the state that
+    verify_count_tokens keeps (zeros for a new request), slots [B] int32 the requests'
+    rows in it (None: 0 .. B-1).  bias_start [B + 1], bias_tokens and bias_values: each
+    request's list of biased tokens.  mask [M, ceil(V / 32)] int32 bits (token v: bit
+    v % 32 of word v // 32) of the tokens that may follow, mask_rows [T] each row's mask
+    (-1: all may).  out: None for a new tensor; logits to change them in place.  Returns
+    out."""
+    import torch
+    i32, f32 = torch.int32, torch.float32
+    if logits.dim() != 2:
+        raise ValueError("logits must be [T, V], got %s" % (tuple(logits.shape),))
+    T, V = logits.shape
+    dev, dtype, idx = logits.device, logits.dtype, logits.get_device()
+    if q_start.dim() != 1 or q_start.shape[0] < 1:
+        raise ValueError("q_start must be [B + 1], got %s" % (tuple(q_start.shape),))
+    B = q_start.shape[0] - 1
+    code = _dtype_code(logits)
+    p_logits, stride = _row_matrix(logits, "logits", (T, V), dtype, idx, dev)
+    p_qs = _arg(q_start, "q_start", None, i32, idx, dev)
+    p_tok = None if tokens is None else _arg(tokens, "tokens", (T,), i32, idx, dev)
+    params = AdjustParams()
+    if repetition is not None or frequency is not None or presence is not None:
+        if counts is None or seen is None or tokens is None:
+            raise ValueError("a penalty needs counts, seen and tokens")
+        if repetition is not None:
+            params.repetition = _arg(repetition, "repetition", (B,), f32, idx, dev)
+        if frequency is not None:
+            params.frequency = _arg(frequency, "frequency", (B,), f32, idx, dev)
+        if presence is not None:
+            params.presence = _arg(presence, "presence", (B,), f32, idx, dev)
+        params.counts, params.seen, params.slots, params.num_slots = _token_state(counts, seen, slots, V, B, idx, dev)
+    if bias_start is not None:
+        params.bias_start = _arg(bias_start, "bias_start", (B + 1,), i32, idx, dev)
+        if bias_tokens is None or bias_values is None or bias_tokens.dim() != 1:
+            raise ValueError("bias_start needs bias_tokens and bias_values of one dim")
+        m = bias_tokens.shape[0]
+        params.bias_tokens = _arg(bias_tokens, "bias_tokens", None, i32, idx, dev)
+        params.bias_values = _arg(bias_values, "bias_values", (m,), f32, idx, dev)
+        params.num_biases = m
+    elif bias_tokens is not None or bias_values is not None:
+        raise ValueError("bias_tokens and bias_values need bias_start")
+    if mask_rows is not None:
+        if mask is None or mask.dim() != 2:
+            raise ValueError("mask_rows needs mask [M, ceil(V / 32)]")
+        params.mask_rows = _arg(mask_rows, "mask_rows", (T,), i32, idx, dev)
+        params.mask = _arg(mask, "mask", (mask.shape[0], (V + 31) // 32), i32, idx, dev)
+        params.num_masks = mask.shape[0]
+    elif mask is not None:
+        raise ValueError("mask needs mask_rows")
+    if check or check is None and CHECK_BY_DEFAULT:
+        _checked(check, "verify_adjust_logits", q_start=q_start, total_q=T, stream=stream)
+    if out is None:
+        out = _scratch((T, V), dtype, dev, stream)
+    p_out, out_stride = _row_matrix(out, "out", (T, V), dtype, idx, dev)
+    if idx < 0:
+        _dev_ptr(logits, "logits")
+    _launch("verify_adjust_logits", idx, B, T, V, stride, code, p_logits, p_tok, p_qs, ctypes.byref(params), p_out,
+            out_stride, _stream_ptr(stream, dev))
+    return out
+
+
+def verify_count_tokens(counts, seen, tokens, token_start, *, num_tokens=None, slots=None, prompt: bool = False,
+                        stream=None):
+    """Enters tokens into the state that verify_adjust_logits reads, in place.
+
+    counts [slots, V] and seen [slots, 2, ceil(V / 32)] int32 (zeros for a new request).
+    Request i's tokens are the first num_tokens[i] (None: all) of tokens[token_start[i]
+    : token_start[i + 1]]: after an acceptance tokens = emitted, token_start = q_start
+    and num_tokens = num_emitted.  prompt: they belong to the request's prompt, which
+    only the repetition penalty regards.  Tokens outside the vocabulary are passed
+    over.  slots [B] int32: the requests' rows of the state (None: 0 .. B-1)."""
+    import torch
+    i32 = torch.int32
+    if token_start.dim() != 1 or token_start.shape[0] < 1:
+        raise ValueError("token_start must be [B + 1], got %s" % (tuple(token_start.shape),))
+    if tokens.dim() != 1:
+        raise ValueError("tokens must be packed in one dim, got %s" % (tuple(tokens.shape),))
+    B, dev, idx = token_start.shape[0] - 1, counts.device, counts.get_device()
+    p_counts, p_seen, p_slots, n = _token_state(counts, seen, slots, counts.shape[-1], B, idx, dev)
+    p_tok = _arg(tokens, "tokens", None, i32, idx, dev)
+    p_start = _arg(token_start, "token_start", None, i32, idx, dev)
+    p_num = None if num_tokens is None else _arg(num_tokens, "num_tokens", (B,), i32, idx, dev)
+    if idx < 0:
+        _dev_ptr(counts, "counts")
+    _launch("verify_count_tokens", idx, B, tokens.shape[0], counts.shape[1], n, p_tok, p_start, p_num, p_slots,
+            int(bool(prompt)), p_counts, p_seen, _stream_ptr(stream, dev))
 
 
 def _workspace_size(where, params, *bounds):

@@ -1,0 +1,395 @@
+// verify_logits.hip -- logits changed before tokens are accepted from them: penalties
+// for tokens that a request has had, biases and grammar masks; and the counts of
+// tokens that the penalties read.
+//
+// Row j of a request stands behind its drafts 1 .. j, so a token's count there is the
+// stored one and those of these drafts.  With h[v] whether v was in the prompt or has
+// a count c[v] > 0:
+//     x *= x > 0 ? 1 / repetition : repetition   where h[v]
+//     x += bias[v] - frequency c[v] - presence [c[v] > 0]
+//     x  = -inf                                  where the row's mask lacks v
+//
+// What bounds it: memory, 2 V bytes in and out per row.  The request's state is small
+// beside them: a bit per token tells whether a count need be read at all, so V / 4
+// bytes of bits and the counts of the few tokens that were had.  A workgroup takes
+// kSpan tokens of one request and all of its rows: state and biases become a factor
+// and a summand per token in registers, eight tokens to a thread, and a row costs a
+// compare, a select and a fused multiply-add per element; a draft changes one token's
+// summand on the way to the next row.
+#include <type_traits>
+
+#include "common.h"
+
+namespace averify {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kPer = 8;                  // tokens of a thread
+constexpr int kSpan = kThreads * kPer;   // tokens of a workgroup
+constexpr int kRows = 4;                 // rows in flight
+
+struct AdjustArgs {
+    const void* logits;
+    void* out;
+    const int32_t* tokens;
+    const int32_t* q_start;
+    const float* repetition;
+    const float* frequency;
+    const float* presence;
+    const int32_t* counts;
+    const uint8_t* seen;
+    const int32_t* slots;
+    const int32_t* bias_start;
+    const int32_t* bias_tokens;
+    const float* bias_values;
+    const uint8_t* mask;
+    const int32_t* mask_rows;
+    int64_t row_stride, out_stride;
+    int vocab, words, total_q, num_slots, num_biases, num_masks;
+};
+
+// A thread's eight logits.  WIDE: neighbours, in 16-byte loads; otherwise kThreads
+// apart, so that a wavefront's lanes are neighbours whatever a row's alignment.
+template <typename T, bool WIDE> struct Group {
+    static constexpr int kVecs = kPer * (int)sizeof(T) / 16;
+    uint4 v[WIDE ? kVecs : 1];
+    T s[WIDE ? 1 : kPer];
+
+    // tokens from `room` on are behind the vocabulary
+    __device__ __forceinline__ void load(const T* row, int tok, int room) {
+        if constexpr (WIDE) {
+            if (room >= kPer) {
+#pragma unroll
+                for (int k = 0; k < kVecs; ++k) v[k] = ld16_stream(row + tok + k * (16 / (int)sizeof(T)));
+            } else {
+                T t[kPer] = {};
+#pragma unroll
+                for (int e = 0; e < kPer; ++e) if (e < room) t[e] = row[tok + e];
+                __builtin_memcpy(v, t, sizeof(t));
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < kPer; ++e) if (tok + e * kThreads < room) s[e] = row[tok + e * kThreads];
+        }
+    }
+    __device__ __forceinline__ void store(T* row, int tok, int room) const {
+        if constexpr (WIDE) {
+            if (room >= kPer) {
+#pragma unroll
+                for (int k = 0; k < kVecs; ++k) reinterpret_cast<uint4*>(row + tok)[k] = v[k];
+            } else {
+                T t[kPer];
+                __builtin_memcpy(t, v, sizeof(t));
+#pragma unroll
+                for (int e = 0; e < kPer; ++e) if (e < room) row[tok + e] = t[e];
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < kPer; ++e) if (tok + e * kThreads < room) row[tok + e * kThreads] = s[e];
+        }
+    }
+    __device__ __forceinline__ void get(float* x) const {
+        if constexpr (WIDE) {
+#pragma unroll
+            for (int k = 0; k < kVecs; ++k) unpack16(v[k], x + k * (16 / (int)sizeof(T)), T{});
+        } else {
+#pragma unroll
+            for (int e = 0; e < kPer; ++e) x[e] = Storage<T>::load(s, e);
+        }
+    }
+    __device__ __forceinline__ void set(const float* x) {
+        if constexpr (WIDE && sizeof(T) == 2) {
+            v[0] = make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]),
+                              pack_bf16x2(x[6], x[7]));
+        } else if constexpr (WIDE) {
+            __builtin_memcpy(v, x, kPer * sizeof(float));
+        } else {
+#pragma unroll
+            for (int e = 0; e < kPer; ++e) Storage<T>::store(s, e, x[e]);
+        }
+    }
+};
+
+// Workgroup (x, i, z): tokens x kSpan .. of request i, the z-th part of its rows.
+template <typename T, bool WIDE, bool IN_PLACE>
+__global__ __launch_bounds__(kThreads) void adjust_rows(AdjustArgs a) {
+    __shared__ int s_token[kThreads];
+    __shared__ float s_value[kThreads];
+    __shared__ int s_found[kThreads / kWave];
+    const int tid = threadIdx.x, i = blockIdx.y;
+    const int q0 = max(0, min(a.q_start[i], a.total_q)), n = max(0, min(a.q_start[i + 1], a.total_q) - q0);
+    const int part = (n + (int)gridDim.z - 1) / (int)gridDim.z;
+    const int j0 = min(n, (int)blockIdx.z * part), j1 = min(n, j0 + part);
+    if (j0 >= j1) return;
+    const int span0 = blockIdx.x * kSpan;
+    const int tok0 = span0 + (WIDE ? tid * kPer : tid);
+    auto token = [&](int e) { return tok0 + (WIDE ? e : e * kThreads); };
+    const int room = WIDE ? a.vocab - tok0 : a.vocab;  // Group's bound
+    const bool live = tok0 < a.vocab;
+    // eight bits of a bit array, bit e for token(e); bits behind the vocabulary are 0
+    auto bits_of = [&](const uint8_t* bits) -> uint32_t {
+        if (!live) return 0;
+        if constexpr (WIDE) return bits[tok0 >> 3];
+        uint32_t b = 0;
+#pragma unroll
+        for (int e = 0; e < kPer; ++e)
+            if (token(e) < a.vocab) b |= (bits[token(e) >> 3] >> (token(e) & 7) & 1u) << e;
+        return b;
+    };
+
+    // the request's state: tokens had (a bit each), their counts, biases
+    uint32_t had = 0, biased = 0;
+    int32_t c[kPer];
+    float bias[kPer];
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) c[e] = 0, bias[e] = -0.f;  // -0: a sum's neutral element
+    const bool penal = a.counts != nullptr;
+    float rep = 1.f, inv = 1.f, freq = 0.f, pres = 0.f;
+    if (penal) {
+        if (a.repetition) rep = a.repetition[i], inv = 1.f / rep;
+        if (a.frequency) freq = a.frequency[i];
+        if (a.presence) pres = a.presence[i];
+        const int slot = a.slots ? a.slots[i] : i;
+        if (slot >= 0 && slot < a.num_slots) {
+            const uint8_t* seen = a.seen + (int64_t)slot * 2 * a.words * 4;
+            const uint32_t prompt = bits_of(seen), out = bits_of(seen + (int64_t)a.words * 4);
+            if (out) {
+                const int32_t* counts = a.counts + (int64_t)slot * a.vocab;
+#pragma unroll
+                for (int e = 0; e < kPer; ++e)
+                    if ((out >> e & 1u) && token(e) < a.vocab) c[e] = max(0, counts[token(e)]);
+            }
+            had = prompt;
+#pragma unroll
+            for (int e = 0; e < kPer; ++e) had |= (uint32_t)(c[e] > 0) << e;
+        }
+    }
+    if (a.bias_start) {
+        // the list's entries of this span, kThreads of the list at a time, in its order
+        const int b0 = max(0, min(a.bias_start[i], a.num_biases)), b1 = min(a.bias_start[i + 1], a.num_biases);
+        for (int base = b0; base < b1; base += kThreads) {
+            const int at = base + tid, tok = at < b1 ? a.bias_tokens[at] : -1;
+            const bool here = tok >= span0 && tok - span0 < kSpan && tok < a.vocab;
+            const uint64_t vote = __ballot(here);
+            if (tid % kWave == 0) s_found[tid / kWave] = __popcll(vote);
+            __syncthreads();
+            int before = 0, all = 0;
+#pragma unroll
+            for (int w = 0; w < kThreads / kWave; ++w) {
+                before += w < tid / kWave ? s_found[w] : 0;
+                all += s_found[w];
+            }
+            if (here) {
+                const int p = before + __popcll(vote & ((1ull << (tid % kWave)) - 1));
+                s_token[p] = tok;
+                s_value[p] = a.bias_values[at];
+            }
+            __syncthreads();
+            for (int p = 0; p < all; ++p) {
+                const int d = s_token[p];
+#pragma unroll
+                for (int e = 0; e < kPer; ++e)
+                    if (d == token(e)) bias[e] += s_value[p], biased |= 1u << e;
+            }
+            __syncthreads();
+        }
+    }
+    // token e: x becomes fma(x, x > 0 ? up[e] : down[e], add[e])
+    float up[kPer], down[kPer], add[kPer];
+    auto settle = [&](int e) {
+        up[e] = had >> e & 1u ? inv : 1.f;
+        down[e] = had >> e & 1u ? rep : 1.f;
+        add[e] = bias[e];
+        if (c[e] > 0) add[e] -= fmaf(freq, (float)c[e], pres);
+    };
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) settle(e);
+    // the draft that row j stands behind (no draft: -1)
+    auto draft = [&](int j) {
+        const int d = j > 0 ? a.tokens[q0 + j] : -1;
+        if (d < span0 || d - span0 >= kSpan || d >= a.vocab) return;
+#pragma unroll
+        for (int e = 0; e < kPer; ++e)
+            if (d == token(e)) {
+                ++c[e];
+                had |= 1u << e;
+                settle(e);
+            }
+    };
+    if (penal)
+        for (int j = 1; j < j0; ++j) draft(j);
+
+    const T* in = static_cast<const T*>(a.logits) + (int64_t)q0 * a.row_stride;
+    T* to = static_cast<T*>(a.out) + (int64_t)q0 * a.out_stride;
+    for (int base = j0; base < j1; base += kRows) {
+        Group<T, WIDE> g[kRows];
+        uint32_t allowed[kRows];
+        // In place a group that nothing changes is neither read nor written.  The
+        // drafts of these rows may change it: those rows' groups are read too.
+        uint32_t coming = 0;
+        if (IN_PLACE && penal) {
+            uint32_t had_by = 0;
+#pragma unroll
+            for (int x = 0; x < kRows; ++x) {
+                const int j = base + x, d = j > 0 && j < j1 ? a.tokens[q0 + j] : -1;
+#pragma unroll
+                for (int e = 0; e < kPer; ++e) had_by |= d == token(e) && d < a.vocab;
+                coming |= had_by << x;
+            }
+        }
+#pragma unroll
+        for (int x = 0; x < kRows; ++x) {
+            const int j = base + x;
+            allowed[x] = 0xffu;
+            if (a.mask_rows && j < j1) {
+                const int m = a.mask_rows[q0 + j];
+                if (m >= 0 && m < a.num_masks) allowed[x] = bits_of(a.mask + (int64_t)m * a.words * 4);
+            }
+        }
+#pragma unroll
+        for (int x = 0; x < kRows; ++x) {
+            const int j = base + x;
+            // what is masked whole need not be read
+            const bool changed = !IN_PLACE || had || biased || allowed[x] != 0xffu || (coming >> x & 1u);
+            if (j < j1 && live && allowed[x] && changed) g[x].load(in + (int64_t)j * a.row_stride, tok0, room);
+        }
+#pragma unroll
+        for (int x = 0; x < kRows; ++x) {
+            const int j = base + x;
+            if (j >= j1) break;
+            if (penal) draft(j);
+            const bool changed = had || biased || allowed[x] != 0xffu;
+            if (changed) {
+                float v[kPer];
+                if (allowed[x]) g[x].get(v);
+#pragma unroll
+                for (int e = 0; e < kPer; ++e) {
+                    const float y = fmaf(v[e], v[e] > 0.f ? up[e] : down[e], add[e]);
+                    v[e] = allowed[x] >> e & 1u ? y : -INFINITY;
+                }
+                g[x].set(v);
+            }
+            if (live && (!IN_PLACE || changed)) g[x].store(to + (int64_t)j * a.out_stride, tok0, room);
+        }
+    }
+}
+
+struct CountArgs {
+    int32_t* counts;
+    uint32_t* seen;
+    const int32_t* tokens;
+    const int32_t* start;
+    const int32_t* num;
+    const int32_t* slots;
+    int vocab, words, total, num_slots, prompt;
+};
+
+// Workgroup (x, i): request i's tokens, kThreads at a time.  Integer sums and bits:
+// the order in which they arrive changes nothing.
+__global__ __launch_bounds__(kThreads) void count_tokens(CountArgs a) {
+    const int i = blockIdx.y;
+    const int slot = a.slots ? a.slots[i] : i;
+    if (slot < 0 || slot >= a.num_slots) return;
+    const int t0 = max(0, min(a.start[i], a.total));
+    int n = max(0, min(a.start[i + 1], a.total) - t0);
+    if (a.num) n = min(n, a.num[i]);
+    uint32_t* seen = a.seen + ((int64_t)slot * 2 + (a.prompt ? 0 : 1)) * a.words;
+    int32_t* counts = a.counts + (int64_t)slot * a.vocab;
+    for (int64_t j = blockIdx.x * kThreads + threadIdx.x; j < n; j += (int64_t)gridDim.x * kThreads) {
+        const int tok = a.tokens[t0 + j];
+        if (tok < 0 || tok >= a.vocab) continue;
+        if (!a.prompt) atomicAdd(counts + tok, 1);
+        atomicOr(seen + (tok >> 5), 1u << (tok & 31));
+    }
+}
+
+template <typename T, bool IN_PLACE>
+void launch_adjust(const AdjustArgs& a, const dim3& grid, bool wide, hipStream_t stream) {
+    if (wide) hipLaunchKernelGGL((adjust_rows<T, true, IN_PLACE>), grid, dim3(kThreads), 0, stream, a);
+    else hipLaunchKernelGGL((adjust_rows<T, false, IN_PLACE>), grid, dim3(kThreads), 0, stream, a);
+}
+
+}  // namespace
+}  // namespace averify
+
+using namespace averify;
+
+extern "C" int verify_adjust_logits(int32_t num_seqs, int32_t total_q, int64_t vocab, int64_t row_stride,
+                                    int32_t logits_dtype, const void* logits, const int32_t* tokens,
+                                    const int32_t* q_start, const verify_adjust_params* params, void* out,
+                                    int64_t out_stride, hipStream_t stream) {
+    if (!params || num_seqs < 0 || total_q < 0 || vocab < 1) return VERIFY_EINVAL;
+    if (logits_dtype != VERIFY_F32 && logits_dtype != VERIFY_BF16) return VERIFY_EUNSUPPORTED;
+    // a span's tokens are counted in 32 bits
+    if (vocab >= (int64_t)INT32_MAX - kSpan || num_seqs > 65535) return VERIFY_EUNSUPPORTED;
+    if (row_stride == 0) row_stride = vocab;
+    if (out_stride == 0) out_stride = vocab;
+    if (row_stride < vocab || out_stride < vocab) return VERIFY_EINVAL;
+    const bool penal = params->repetition || params->frequency || params->presence;
+    const bool biases = params->bias_start, masks = params->mask_rows;
+    if (penal && (!params->counts || !params->seen || !tokens)) return VERIFY_EINVAL;
+    if (biases && ((!params->bias_tokens || !params->bias_values) && params->num_biases > 0)) return VERIFY_EINVAL;
+    if (masks && !params->mask && params->num_masks > 0) return VERIFY_EINVAL;
+    if (params->num_slots < 0 || params->num_biases < 0 || params->num_masks < 0) return VERIFY_EINVAL;
+    if (num_seqs == 0 || total_q == 0) return VERIFY_OK;
+    if (!logits || !out || !q_start) return VERIFY_EINVAL;
+    const bool in_place = logits == out;
+    if (in_place && row_stride != out_stride) return VERIFY_EINVAL;
+    AdjustArgs a{};
+    a.logits = logits;
+    a.out = out;
+    a.tokens = tokens;
+    a.q_start = q_start;
+    if (penal) {
+        a.repetition = params->repetition;
+        a.frequency = params->frequency;
+        a.presence = params->presence;
+        a.counts = params->counts;
+        a.seen = reinterpret_cast<const uint8_t*>(params->seen);
+        a.slots = params->slots;
+        a.num_slots = params->num_slots;
+    }
+    if (biases && params->num_biases > 0) {
+        a.bias_start = params->bias_start;
+        a.bias_tokens = params->bias_tokens;
+        a.bias_values = params->bias_values;
+        a.num_biases = params->num_biases;
+    }
+    if (masks && params->num_masks > 0) {
+        a.mask = reinterpret_cast<const uint8_t*>(params->mask);
+        a.mask_rows = params->mask_rows;
+        a.num_masks = params->num_masks;
+    }
+    a.row_stride = row_stride;
+    a.out_stride = out_stride;
+    a.vocab = (int)vocab;
+    a.words = (int)((vocab + 31) / 32);
+    a.total_q = total_q;
+    // a request's rows are divided where there would be few workgroups otherwise
+    const int64_t spans = (vocab + kSpan - 1) / kSpan, wgs = spans * num_seqs, rows = (total_q + num_seqs - 1) / num_seqs;
+    const int64_t parts = std::max<int64_t>(1, std::min<int64_t>({(1024 + wgs - 1) / wgs, rows, 65535}));
+    const dim3 grid((unsigned)spans, (unsigned)num_seqs, (unsigned)parts);
+    const int esize = logits_dtype == VERIFY_BF16 ? 2 : 4, n = 16 / esize;
+    const bool wide = (((uintptr_t)logits | (uintptr_t)out) & 15) == 0 && row_stride % n == 0 && out_stride % n == 0;
+    if (logits_dtype == VERIFY_BF16)
+        in_place ? launch_adjust<uint16_t, true>(a, grid, wide, stream) : launch_adjust<uint16_t, false>(a, grid, wide, stream);
+    else
+        in_place ? launch_adjust<float, true>(a, grid, wide, stream) : launch_adjust<float, false>(a, grid, wide, stream);
+    return check_launch();
+}
+
+extern "C" int verify_count_tokens(int32_t num_seqs, int32_t total_tokens, int64_t vocab, int32_t num_slots,
+                                   const int32_t* tokens, const int32_t* token_start, const int32_t* num_tokens,
+                                   const int32_t* slots, int32_t prompt, int32_t* counts, uint32_t* seen,
+                                   hipStream_t stream) {
+    if (num_seqs < 0 || total_tokens < 0 || num_slots < 0 || vocab < 1 || (prompt != 0 && prompt != 1)) return VERIFY_EINVAL;
+    if (vocab > INT32_MAX - 31 || num_seqs > 65535) return VERIFY_EUNSUPPORTED;
+    if (num_seqs == 0 || total_tokens == 0 || num_slots == 0) return VERIFY_OK;
+    if (!tokens || !token_start || !seen || (!prompt && !counts)) return VERIFY_EINVAL;
+    const CountArgs a{counts, seen, tokens, token_start, num_tokens, slots, (int)vocab, (int)((vocab + 31) / 32),
+                      total_tokens, num_slots, prompt};
+    const int64_t per = ((int64_t)total_tokens + num_seqs - 1) / num_seqs;
+    const dim3 grid((unsigned)std::min<int64_t>((per + kThreads - 1) / kThreads, 256), (unsigned)num_seqs);
+    hipLaunchKernelGGL(count_tokens, grid, dim3(kThreads), 0, stream, a);
+    return check_launch();
+}

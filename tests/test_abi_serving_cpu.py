@@ -1,0 +1,128 @@
+"""Norms with the rotation, changed logits and token counts on the host: every refusal
+comes before the GPU is touched, from the library and from the binding."""
+from __future__ import annotations
+
+import ctypes
+
+import pytest
+import torch
+
+import paper_2608_24004_amd as av
+from test_abi_bounded_cpu import DUMMY, _attn, _rot
+
+
+def _norm(p, T=3, hq=8, hkv=2, q=DUMMY, qs=1024, k=DUMMY, ks=256, qw=DUMMY, kw=None, eps=1e-6, pos=DUMMY, freq=DUMMY,
+          qo=DUMMY, qos=1024, ko=DUMMY, kos=256):
+    return av.library().verify_norm_rotary(ctypes.byref(p) if p is not None else None, T, hq, hkv, q, qs, k, ks, qw, kw,
+                                           eps, pos, freq, qo, qos, ko, kos, None)
+
+
+def _norm_append(attn=None, p=None, T=3, eps=1e-6, kc=DUMMY, v=DUMMY, qos=1024, bt=DUMMY):
+    return av.library().verify_norm_rotary_append(
+        ctypes.byref(attn or _attn()), ctypes.byref(p or _rot()), T, DUMMY, 1024, DUMMY, 256, v, 256, None, DUMMY, eps,
+        DUMMY, DUMMY, bt, DUMMY, DUMMY, DUMMY, qos, kc, DUMMY, None)
+
+
+@pytest.mark.parametrize("kw,want", [
+    (dict(eps=-1.0), av.EINVAL), (dict(eps=float("nan")), av.EINVAL), (dict(eps=float("inf")), av.EINVAL),
+    (dict(T=-1), av.EINVAL), (dict(hq=0), av.EINVAL), (dict(q=None), av.EINVAL), (dict(pos=None), av.EINVAL),
+    (dict(k=None), av.EINVAL), (dict(ko=None), av.EINVAL), (dict(qs=1023), av.EINVAL), (dict(kos=255), av.EINVAL),
+    (dict(qs=2048), av.EINVAL), (dict(hq=40000, qs=1 << 40, qos=1 << 40), av.EUNSUPPORTED),
+    (dict(T=2 ** 31 - 1), av.EUNSUPPORTED), (dict(T=0, q=None), av.OK),
+])
+def test_norm_rotary(kw, want):
+    assert _norm(_rot(), **kw) == want
+    assert _norm(None) == av.EINVAL and _norm(_rot(head_dim=96)) == av.EUNSUPPORTED
+
+
+@pytest.mark.parametrize("kw,want", [
+    (dict(eps=-1.0), av.EINVAL), (dict(kc=ctypes.c_void_p(0x1008)), av.EINVAL), (dict(v=None), av.EINVAL),
+    (dict(bt=None), av.EINVAL), (dict(qos=1000), av.EINVAL), (dict(qos=2048), av.EINVAL),
+    (dict(p=_rot(dtype=av.F32)), av.EINVAL), (dict(attn=_attn(head_dim=64)), av.EINVAL),
+    (dict(attn=_attn(block_size=32)), av.EUNSUPPORTED), (dict(T=0), av.OK),
+])
+def test_norm_rotary_append(kw, want):
+    assert _norm_append(**kw) == want
+
+
+def _adjust(B=2, T=5, V=100, rs=0, dtype=av.BF16, logits=DUMMY, tokens=DUMMY, qs=DUMMY, out=ctypes.c_void_p(0x9000), os=0,
+            params=True, **kw):
+    p = av.AdjustParams()
+    for k, v in kw.items():
+        setattr(p, k, v)
+    return av.library().verify_adjust_logits(B, T, V, rs, dtype, logits, tokens, qs, ctypes.byref(p) if params else None,
+                                             out, os, None)
+
+
+@pytest.mark.parametrize("kw,want", [
+    (dict(params=False), av.EINVAL), (dict(B=-1), av.EINVAL), (dict(T=-1), av.EINVAL), (dict(V=0), av.EINVAL),
+    (dict(V=2 ** 31 - 2049), av.EUNSUPPORTED), (dict(V=2 ** 33), av.EUNSUPPORTED), (dict(dtype=2), av.EUNSUPPORTED),
+    (dict(B=65536), av.EUNSUPPORTED), (dict(rs=99), av.EINVAL), (dict(os=-1), av.EINVAL),
+    (dict(logits=None), av.EINVAL), (dict(qs=None), av.EINVAL), (dict(out=None), av.EINVAL),
+    (dict(out=DUMMY, rs=128), av.EINVAL),                       # in place with two strides
+    (dict(repetition=0x1000), av.EINVAL),                       # no state
+    (dict(frequency=0x1000, counts=0x1000), av.EINVAL),
+    (dict(presence=0x1000, counts=0x1000, seen=0x1000, tokens=None), av.EINVAL),
+    (dict(presence=0x1000, counts=0x1000, seen=0x1000, num_slots=-1), av.EINVAL),
+    (dict(bias_start=0x1000, num_biases=1), av.EINVAL), (dict(bias_start=0x1000, num_biases=-1), av.EINVAL),
+    (dict(mask_rows=0x1000, num_masks=1), av.EINVAL), (dict(mask_rows=0x1000, num_masks=-1), av.EINVAL),
+    (dict(T=0, logits=None), av.OK), (dict(B=0, qs=None), av.OK),
+])
+def test_adjust_logits(kw, want):
+    assert _adjust(**kw) == want
+
+
+def _count(B=2, total=5, V=100, slots_n=3, tokens=DUMMY, start=DUMMY, prompt=0, counts=DUMMY, seen=DUMMY):
+    return av.library().verify_count_tokens(B, total, V, slots_n, tokens, start, None, None, prompt, counts, seen, None)
+
+
+@pytest.mark.parametrize("kw,want", [
+    (dict(B=-1), av.EINVAL), (dict(total=-1), av.EINVAL), (dict(V=0), av.EINVAL), (dict(slots_n=-1), av.EINVAL),
+    (dict(prompt=2), av.EINVAL), (dict(V=2 ** 31), av.EUNSUPPORTED), (dict(B=65536), av.EUNSUPPORTED),
+    (dict(tokens=None), av.EINVAL), (dict(start=None), av.EINVAL), (dict(seen=None), av.EINVAL),
+    (dict(counts=None), av.EINVAL), (dict(B=0), av.OK), (dict(total=0, counts=None), av.OK), (dict(slots_n=0), av.OK),
+])
+def test_count_tokens(kw, want):
+    assert _count(**kw) == want
+
+
+def test_the_binding_refuses():
+    i32 = torch.int32
+    x, tok, qs = torch.zeros((5, 100)), torch.zeros(5, dtype=i32), torch.zeros(3, dtype=i32)
+    counts, seen, one = torch.zeros((3, 100), dtype=i32), torch.zeros((3, 2, 4), dtype=i32), torch.ones(2)
+    state = dict(counts=counts, seen=seen, repetition=one)
+    bad = [
+        dict(x=torch.zeros(5)), dict(x=torch.zeros((100, 5)).t()), dict(x=torch.zeros((1, 100)).expand(5, 100)),
+        dict(qs=torch.zeros((3, 1), dtype=i32)), dict(tok=tok[:4], **state),
+        dict(repetition=one), dict(**{**state, "seen": seen[:, :1]}), dict(**{**state, "counts": counts[:, :99]}),
+        dict(**{**state, "repetition": torch.ones(3)}), dict(**state, slots=torch.zeros(3, dtype=i32)),
+        dict(**{**state, "counts": counts[:1], "seen": seen[:1]}),  # two requests, one slot
+        dict(bias_start=qs), dict(bias_tokens=tok, bias_values=one),
+        dict(bias_start=qs, bias_tokens=tok, bias_values=torch.ones(4)),
+        dict(mask=seen[:, 0]), dict(mask_rows=tok), dict(mask=seen[:, 0, :3].contiguous(), mask_rows=tok),
+        dict(mask=seen[:, 0].contiguous(), mask_rows=tok[:3]), dict(out=torch.zeros((5, 99))),
+        dict(x=torch.zeros((5, 100), dtype=torch.float16)),
+    ]
+    for kw in bad:
+        kw = dict(kw)
+        args = kw.pop("x", x), kw.pop("tok", tok), kw.pop("qs", qs)
+        with pytest.raises((ValueError, TypeError)):
+            av.verify_adjust_logits(*args, **kw)
+    with pytest.raises(ValueError, match="device"):
+        av.verify_adjust_logits(x, tok, qs)
+    for args, kw in [((counts[0], seen, tok, qs), {}), ((counts, seen[0], tok, qs), {}), ((counts, seen, tok, qs[:0]), {}),
+                     ((counts, seen, tok[None], qs), {}), ((counts, seen, tok, qs), dict(num_tokens=tok)),
+                     ((counts[:1], seen[:1], tok, qs), {}), ((counts.long(), seen, tok, qs), {}),
+                     ((counts, seen, tok, qs), {})]:
+        with pytest.raises((ValueError, TypeError)):
+            av.verify_count_tokens(*args, **kw)
+    q, pos, freq = torch.zeros((5, 2, 64)), torch.zeros(5, dtype=i32), torch.zeros(32, dtype=torch.float64)
+    for kw in (dict(q_weight=torch.ones(63)), dict(k_weight=torch.ones(64, dtype=torch.bfloat16)), {}):
+        with pytest.raises((ValueError, TypeError)):
+            av.verify_norm_rotary(q, None, pos, freq, **kw)
+
+
+def test_the_structs_agree_with_c():
+    # 6 pointers, an int and its padding, 3 pointers, two ints, 2 pointers
+    assert ctypes.sizeof(av.AdjustParams) == 6 * 8 + 8 + 3 * 8 + 8 + 2 * 8
+    assert av.AdjustParams.num_masks.offset == 84 and av.AdjustParams.mask.offset == 88
