@@ -41,6 +41,9 @@
  *                       verify_kv_append.
  *   verify_norm_rotary, verify_norm_rotary_append -- the same two with each
  *                       head's query and key normalised first.
+ *   verify_attention_shared -- verify_attention where groups of requests begin with
+ *                       the same cached tokens: the keys of a common prefix are read
+ *                       once for all rows of its group.
  *   verify_adjust_logits, verify_count_tokens -- penalties, biases and grammar
  *                       masks applied to the logits before an acceptance call
  *                       reads them, and the counts of tokens that the penalties
@@ -561,6 +564,46 @@ int verify_norm_rotary_append(const verify_attn_params *attn, const verify_rotar
                               const int32_t *block_tables, const int32_t *seq_lens,
                               const int32_t *q_start, void *q_out, int64_t q_out_stride,
                               void *k_cache, void *v_cache, hipStream_t stream);
+
+/*
+ * verify_attention_shared -- verify_attention of a batch in which groups of requests
+ * begin with the same cached tokens (agents of one kind: the same instructions and tool
+ * descriptions).  The result is verify_attention's, up to rounding; the keys of a common
+ * prefix are read once for all rows of its group instead of once per request.
+ *
+ *   group_start  [num_groups + 1] int32, non-decreasing: requests group_start[k] ..
+ *                group_start[k + 1] - 1 form group k.  Requests in front of the first
+ *                and behind the last group share nothing.
+ *   prefix_lens  [num_groups] int32 (clamped to [0, max_prefix_len]): the requests of
+ *                group k have the same first prefix_lens[k] / 16 (rounded down) entries
+ *                in block_tables, and that many blocks of cached keys at least.  Those of
+ *                the group's first request are read.
+ *   max_prefix_len   host upper bound on prefix_lens; below 16, or with no group, the
+ *                call is verify_attention (with its workspace)
+ *   max_q_len    host upper bound on n_i (sizes the launch; a request may exceed it)
+ *   k_cache, v_cache   16-byte aligned (VERIFY_EINVAL otherwise).  Slots behind a
+ *                request's last key may hold anything.
+ *   sinks and all other arguments as for verify_attention.  A row may stand inside the
+ *                prefix (a prompt that is still being read): it sees the keys up to its
+ *                own.
+ *   workspace    16-byte aligned (VERIFY_EINVAL otherwise), at least
+ *                verify_attention_shared_workspace_size() bytes for the same arguments;
+ *                its contents on entry are ignored
+ * VERIFY_EUNSUPPORTED for params with sliding_window > 0 (a window does not see a long
+ * prefix) or kv_split_blocks > 0, and where total_q Hq / Hkv reaches 2^30.
+ */
+int verify_attention_shared_workspace_size(const verify_attn_params *params, int32_t total_q,
+                                           int32_t max_q_len, int32_t max_seq_len,
+                                           int32_t num_groups, int32_t max_prefix_len,
+                                           size_t *bytes);
+
+int verify_attention_shared(const verify_attn_params *params, int32_t total_q, int32_t max_q_len,
+                            int32_t max_seq_len, int32_t num_groups, int32_t max_prefix_len,
+                            const void *q, const void *k_cache, const void *v_cache,
+                            const int32_t *block_tables, const int32_t *seq_lens,
+                            const int32_t *q_start, const int32_t *group_start,
+                            const int32_t *prefix_lens, const float *sinks, void *out,
+                            void *workspace, size_t workspace_bytes, hipStream_t stream);
 
 /*
  * Changed logits.  Every request of a batch owns a slot of a state of

@@ -19,6 +19,9 @@ If the library is missing, every entry point raises -- there is no fallback.
                                several axes, alone or with the append
     verify_norm_rotary(...), verify_norm_rotary_append(...)
                                the same behind a norm of each head's query and key
+    verify_attention_shared(...)
+                               verify_attention where groups of requests begin with the
+                               same cached tokens, whose keys are read once
     verify_adjust_logits(...), verify_count_tokens(...)
                                penalties, biases and grammar masks on the logits, and
                                the token counts that the penalties read
@@ -42,6 +45,7 @@ __all__ = ["verify_attention", "verify_accept", "verify_accept_noalloc", "verify
            "accept_workspace_size",
            "lmhead_accept_workspace_size", "verify_rotary", "verify_rotary_append",
            "verify_norm_rotary", "verify_norm_rotary_append", "verify_adjust_logits", "verify_count_tokens",
+           "verify_attention_shared", "attention_shared_workspace_size",
            "verify_key_weights", "verify_evict_plan", "verify_kv_compact",
            "key_weights_workspace_size", "evict_plan_workspace_size", "check_batch", "BatchError", "VerifyError", "library",
            "abi_version", "F32", "BF16"]
@@ -178,6 +182,11 @@ def library(path: Optional[str] = None):
     lib.verify_norm_rotary_append.argtypes = [P, RP, i32, vp, i64, vp, i64, vp, i64, vp, vp, f32, vp, vp, vp, vp, vp,
                                               vp, i64, vp, vp, vp]
     lib.verify_norm_rotary_append.restype = ctypes.c_int
+    lib.verify_attention_shared_workspace_size.argtypes = [P, i32, i32, i32, i32, i32, ctypes.POINTER(sz)]
+    lib.verify_attention_shared_workspace_size.restype = ctypes.c_int
+    lib.verify_attention_shared.argtypes = [P, i32, i32, i32, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz,
+                                            vp]
+    lib.verify_attention_shared.restype = ctypes.c_int
     lib.verify_adjust_logits.argtypes = [i32, i32, i64, i64, i32, vp, vp, vp, ctypes.POINTER(AdjustParams), vp, i64, vp]
     lib.verify_adjust_logits.restype = ctypes.c_int
     lib.verify_count_tokens.argtypes = [i32, i32, i64, i32, vp, vp, vp, vp, i32, vp, vp, vp]
@@ -1045,6 +1054,57 @@ def _workspace_size(where, params, *bounds):
     n = ctypes.c_size_t(0)
     _check(getattr(library(), where)(ctypes.byref(params), *bounds, ctypes.byref(n)), where)
     return int(n.value)
+
+
+def attention_shared_workspace_size(q, k_cache, block_tables, *, num_groups: int, max_q_len: int, max_seq_len: int,
+                                    max_prefix_len: int) -> int:
+    return _workspace_size("verify_attention_shared_workspace_size", _attn_params(q, k_cache, block_tables, 0, 0.0, 0),
+                           q.shape[0], int(max_q_len), int(max_seq_len), int(num_groups), int(max_prefix_len))
+
+
+def verify_attention_shared(q, k_cache, v_cache, block_tables, seq_lens, q_start, group_start, prefix_lens, *,
+                            max_q_len: int, max_seq_len: int, max_prefix_len: int, scale: float = 0.0, sinks=None,
+                            out=None, workspace=None, stream=None, check=None):
+    """verify_attention of a batch in which groups of requests begin with the same cached
+    tokens: the keys of a common prefix are read once for all rows of its group.
+
+    group_start [G + 1] int32: requests group_start[k] .. group_start[k + 1] - 1 form
+    group k; prefix_lens [G] int32: their first prefix_lens[k] // 16 block table entries
+    are the same; max_prefix_len bounds them.  k_cache, v_cache and workspace are 16-byte
+    aligned.  Other arguments and the result as for verify_attention without a window."""
+    import torch
+    if q.dim() != 3:
+        raise ValueError("q must be [T, Hq, D], got %s" % (tuple(q.shape),))
+    if group_start.dim() != 1 or group_start.shape[0] < 1:
+        raise ValueError("group_start must be [G + 1], got %s" % (tuple(group_start.shape),))
+    T, Hq, D = q.shape
+    dtype, dev, idx = q.dtype, q.device, q.get_device()
+    G = group_start.shape[0] - 1
+    p_q = _arg(q, "q", None, dtype, idx, dev)
+    layer, params = _layer_args(Hq, D, dtype, q.element_size(), idx, dev, k_cache, v_cache, block_tables, seq_lens,
+                                q_start)
+    p_gs = _arg(group_start, "group_start", None, torch.int32, idx, dev)
+    p_pl = _arg(prefix_lens, "prefix_lens", (G,), torch.int32, idx, dev)
+    p_sinks = None if sinks is None else _arg(sinks, "sinks", (Hq,), torch.float32, idx, dev)
+    p_ws, ws_have = _workspace_arg(workspace, idx, dev)
+    if check or check is None and CHECK_BY_DEFAULT:
+        _checked(check, "verify_attention_shared", q_start=q_start, total_q=T, max_q_len=max_q_len, seq_lens=seq_lens,
+                 block_tables=block_tables, num_blocks=k_cache.shape[0], max_seq_len=max_seq_len, stream=stream)
+    params.scale = float(scale)
+    bounds = T, int(max_q_len), int(max_seq_len), G, int(max_prefix_len)
+    if out is None:
+        out = _scratch((T, Hq, D), dtype, dev, stream)
+    p_out = _arg(out, "out", (T, Hq, D), dtype, idx, dev)
+    if workspace is None:
+        ws_have = _workspace_size("verify_attention_shared_workspace_size", params, *bounds)
+        if ws_have > 0:
+            workspace = _scratch(ws_have, torch.uint8, dev, stream)
+            p_ws = workspace.data_ptr()
+    if idx < 0:
+        _dev_ptr(q, "q")
+    _launch("verify_attention_shared", idx, ctypes.byref(params), *bounds, p_q, *layer, p_gs, p_pl, p_sinks, p_out,
+            p_ws, ws_have, _stream_ptr(stream, dev))
+    return out
 
 
 def key_weights_workspace_size(q, k_cache, block_tables, *, max_q_len: int, max_seq_len: int) -> int:

@@ -1,0 +1,939 @@
+// verify_shared.hip -- paged attention of a batch whose requests begin with the same
+// tokens: the keys of a common prefix are read once for all rows that see them.
+//
+// A segment is a run of packed query rows and a run of KV blocks that they see:
+//   prefix k   all rows of the requests of group k, the blocks of its prefix;
+//   own i      the rows of request i, its blocks behind the prefix.
+// A row's softmax runs over its prefix segment and its own one.  Both parts leave the
+// running maximum m (of the scores times scale log2 e), l = sum 2^(s - m) and the
+// output sum 2^(s - m) v, unnormalised and in fp32, and a last pass joins them:
+//     out = sum_k 2^(m_k - M) o_k / (sum_k 2^(m_k - M) l_k + 2^(sink log2 e - M)).
+//
+// Work.  A pair is (segment, KV head, row tile), a unit 128 keys of a pair.  Units are
+// numbered segment by segment, then head, tile and key; the prefixes' units are cut
+// into equal ranges for one part of the workgroups, the own ones' for the other, all of
+// them resident at once.  A range's piece of pair p in workgroup w leaves its partial
+// result in slot p + w, which no other piece has, since one of the two grows from each
+// piece to the next.
+//
+// Matrix products, per 16-row tile and 32 keys (two blocks), lane = 16 lg + l16:
+//   S^T = K Q^T    v_mfma_f32_16x16x32_bf16, A = K: row m of product t is key
+//                  8 ((m >> 2) & 1) + 4 t + (m & 3) of block m >> 3, so that lane lg's
+//                  results of both products are its eight keys 8 lg .. 8 lg + 7 of 32;
+//   O^T += V^T P^T the same instruction, A = V^T: a lane's 16 bytes are the eight keys
+//                  8 lg .. 8 lg + 7 of dim l16, B = P^T as the scores left it.
+// Nothing but the operands of several wavefronts goes through LDS.
+//
+// Few rows (flat): the four wavefronts of a workgroup take 32 of a unit's 128 keys each,
+// with all rows, straight from memory into operand registers, the next unit's keys
+// asked for as soon as this one's scores are done.  Bound by memory.
+// Many rows (tall): the wavefronts take the rows, and the keys pass through a ring of
+// LDS stages that all of them read.  Bound by the matrix units and the exponentials.
+#include <type_traits>
+
+#include "common.h"
+
+// m0 is set inside the global->LDS load sequence (see dma16_run); the compiler
+// reloads m0 before each of its own uses, so clobbering it there is safe.
+#pragma clang diagnostic ignored "-Winline-asm"
+
+namespace averify {
+namespace {
+
+constexpr int kWaves = 4;
+constexpr int kThreads = kWaves * kWave;
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr int kUnitBlocks = 8;      // KV blocks of a unit
+constexpr int kInlineSegs = 512;    // segments whose units every workgroup counts itself
+constexpr int kStages = 4;          // of the tall walk's ring
+constexpr float kNoMax = -3.0e38f;  // a maximum over no key
+// Softmax weights may exceed 1 by up to this factor (log2) before a row's maximum is
+// raised: with a maximum that need not be exact the raise is rare.
+constexpr float kSlackLog2 = 8.f;
+// 16-row tiles of a flat walk at most: those whose operands fit 256 registers
+constexpr int flat_tiles(int d, bool f32) { return !f32 && d == 64 ? 3 : 2; }
+constexpr int tall_tiles(int d) { return d == 64 ? 4 : 2; }  // per wavefront
+
+typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
+typedef float f32x4_t __attribute__((ext_vector_type(4)));
+// callers' tensors need only be aligned to an element
+typedef uint32_t u32x4h_t __attribute__((ext_vector_type(4), aligned(2)));
+typedef float f32x4u_t __attribute__((ext_vector_type(4), aligned(4)));
+
+struct SharedArgs {
+    const void* q;
+    const uint8_t* kc;
+    const uint8_t* vc;
+    const float* sinks;
+    void* out;
+    float* part_o;    // [slots][tile rows][D]
+    float2* part_ml;  // [slots][tile rows] maximum and sum
+    int64_t* unit_off;  // [segments + 1]
+    int32_t* pair_off;  // [segments + 1]
+    int32_t* masked;    // [groups] whether a row of the group stands inside the prefix
+    int num_seqs, num_groups, hq, hkv, group, max_blocks, num_blocks, max_seq_len, max_prefix, total_q;
+    int nwg;
+    int tile_a, tile_b;    // rows of a tile at most: prefix and own segments
+    int64_t slots_a, slots_b;
+    float scale_log2;
+};
+
+struct Index {  // device arrays that nothing writes
+    const int32_t* __restrict__ tables;
+    const int32_t* __restrict__ lens;
+    const int32_t* __restrict__ q_start;
+    const int32_t* __restrict__ group_start;
+    const int32_t* __restrict__ prefix;
+};
+
+struct Segment {
+    int q0, rows;    // first packed row, packed rows times query heads per KV head
+    int b_lo, b_hi;  // blocks
+    int tile, tiles; // rows of a tile, tiles
+    int table;       // the request whose block table lists the blocks
+    int S, n;        // own: cached keys and new ones
+};
+
+__device__ __forceinline__ int clamp_to(int v, int lo, int hi) { return max(lo, min(v, hi)); }
+
+__device__ __forceinline__ int prefix_blocks(const SharedArgs& a, const Index& x, int k) {
+    return clamp_to(x.prefix[k], 0, min(a.max_prefix, a.max_blocks * kBlockTokens)) / kBlockTokens;
+}
+
+// The group of request i: the last one that begins at or before it, if it holds i.
+__device__ __forceinline__ int group_of(const SharedArgs& a, const Index& x, int i) {
+    int lo = 0, hi = a.num_groups - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (x.group_start[mid] <= i) lo = mid; else hi = mid - 1;
+    }
+    return x.group_start[lo] <= i && i < x.group_start[lo + 1] ? lo : -1;
+}
+
+// Rows divided evenly over as few tiles of at most `most` rows as there need be.
+__device__ __forceinline__ void divide(Segment& g, int most) {
+    g.tiles = (g.rows + most - 1) / most;
+    g.tile = g.tiles ? ((g.rows + g.tiles - 1) / g.tiles + 15) / 16 * 16 : 16;
+}
+
+__device__ __forceinline__ int clamped_len(const SharedArgs& a, const Index& x, int i) {
+    return clamp_to(x.lens[i], 0, min(a.max_seq_len, a.max_blocks * kBlockTokens));
+}
+
+__device__ __forceinline__ Segment prefix_segment(const SharedArgs& a, const Index& x, int k) {
+    Segment g;
+    const int r0 = clamp_to(x.group_start[k], 0, a.num_seqs), r1 = clamp_to(x.group_start[k + 1], r0, a.num_seqs);
+    g.q0 = clamp_to(x.q_start[r0], 0, a.total_q);
+    g.rows = (clamp_to(x.q_start[r1], g.q0, a.total_q) - g.q0) * a.group;
+    g.b_lo = 0;
+    g.b_hi = prefix_blocks(a, x, k);
+    g.table = min(r0, a.num_seqs - 1);
+    g.S = g.b_hi * kBlockTokens;
+    g.n = 0;
+    divide(g, a.tile_a);
+    return g;
+}
+
+__device__ __forceinline__ Segment own_segment(const SharedArgs& a, const Index& x, int i) {
+    Segment g;
+    g.q0 = clamp_to(x.q_start[i], 0, a.total_q);
+    g.n = clamp_to(x.q_start[i + 1], g.q0, a.total_q) - g.q0;
+    g.rows = g.n * a.group;
+    const int k = group_of(a, x, i);
+    g.S = clamped_len(a, x, i);
+    g.b_lo = k >= 0 ? prefix_blocks(a, x, k) : 0;
+    g.b_hi = max(g.b_lo, (g.S + kBlockTokens - 1) / kBlockTokens);
+    g.table = i;
+    divide(g, a.tile_b);
+    return g;
+}
+
+__device__ __forceinline__ Segment segment_of(const SharedArgs& a, const Index& x, int s) {
+    return s < a.num_groups ? prefix_segment(a, x, s) : own_segment(a, x, s - a.num_groups);
+}
+
+__device__ __forceinline__ int units_of(const Segment& g) { return (g.b_hi - g.b_lo + kUnitBlocks - 1) / kUnitBlocks; }
+
+// Unit and pair offsets of all segments, by one workgroup of THREADS threads.
+template <int THREADS>
+__device__ void count_units(const SharedArgs& a, const Index& x, int64_t* unit_off, int32_t* pair_off, int32_t* masked) {
+    __shared__ int64_t s_units[THREADS / kWave];
+    __shared__ int s_pairs[THREADS / kWave];
+    const int tid = threadIdx.x, segs = a.num_groups + a.num_seqs;
+    for (int k = tid; k < a.num_groups; k += THREADS) masked[k] = 0;
+    __syncthreads();
+    int64_t units0 = 0;
+    int pairs0 = 0;
+    for (int base = 0; base < segs; base += THREADS) {
+        const int s = base + tid;
+        int pairs = 0, each = 0;
+        if (s < segs) {
+            const Segment g = segment_of(a, x, s);
+            each = units_of(g);
+            pairs = each > 0 ? g.tiles * a.hkv : 0;
+            // a row that stands in front of the prefix's last key sees a part of it
+            if (s >= a.num_groups && g.n > 0 && g.b_lo > 0 && g.S - g.n < g.b_lo * kBlockTokens - 1)
+                masked[group_of(a, x, s - a.num_groups)] = 1;
+        }
+        int64_t u = (int64_t)pairs * each;
+        int p = pairs;
+        const int64_t u_mine = u;
+        const int lane = tid % kWave;
+        for (int o = 1; o < kWave; o <<= 1) {
+            const int64_t uo = __shfl_up(u, o);
+            const int po = __shfl_up(p, o);
+            if (lane >= o) u += uo, p += po;
+        }
+        if (lane == kWave - 1) s_units[tid / kWave] = u, s_pairs[tid / kWave] = p;
+        __syncthreads();
+        int64_t u_all = 0;
+        int p_all = 0;
+        for (int w = 0; w < THREADS / kWave; ++w) {
+            if (w < tid / kWave) u += s_units[w], p += s_pairs[w];
+            u_all += s_units[w];
+            p_all += s_pairs[w];
+        }
+        if (s < segs) {
+            unit_off[s] = units0 + u - u_mine;
+            pair_off[s] = pairs0 + p - pairs;
+        }
+        units0 += u_all;
+        pairs0 += p_all;
+        __syncthreads();
+    }
+    if (tid == 0) unit_off[segs] = units0, pair_off[segs] = pairs0;
+    __syncthreads();
+}
+
+__global__ __launch_bounds__(1024) void shared_schedule(SharedArgs a, Index x) {
+    count_units<1024>(a, x, a.unit_off, a.pair_off, a.masked);
+}
+
+// How the workgroups are divided: na of them take the prefixes' ua units, the others the
+// ub own ones.  Where there are fewer units than workgroups, ca and cb of them have one.
+struct Share {
+    int64_t ua, ub;
+    int na, ca, cb, pa;
+};
+
+// A unit of a prefix costs about what an own one does: the one fills the matrix units
+// for 128 rows, the other waits for 64 KiB.
+__device__ __forceinline__ Share divide_workgroups(const SharedArgs& a, const int64_t* unit_off, const int32_t* pair_off) {
+    Share h;
+    h.ua = unit_off[a.num_groups];
+    h.ub = unit_off[a.num_groups + a.num_seqs] - h.ua;
+    h.pa = pair_off[a.num_groups];
+    if (h.ua == 0) h.na = 0;
+    else if (h.ub == 0) h.na = a.nwg;
+    else h.na = clamp_to((int)((double)h.ua / (double)(h.ua + h.ub) * a.nwg / 8 + 0.5) * 8, 8, a.nwg - 8);
+    h.ca = (int)min((int64_t)h.na, h.ua);
+    h.cb = (int)min((int64_t)(a.nwg - h.na), h.ub);
+    return h;
+}
+
+// One workgroup's piece of a pair.
+struct Piece {
+    int q0, row0, rows;  // the segment's first packed row; the tile's first row and rows
+    int head;
+    int b_lo, b_hi;      // the segment's blocks
+    int u0, u1;          // units
+    int min_pos, S;      // lowest position of a row; keys from S on are not the request's
+    int pos0;            // own: position of the segment's first row
+    bool prefix;
+    bool masked;         // prefix: some row stands inside it
+    const int32_t* table;
+    int64_t slot_row;    // first row of the partial result
+};
+
+// The position of the tile's row r; rows behind its last one see no key.
+__device__ __forceinline__ int row_position(const SharedArgs& a, const Index& x, const Piece& p, int r) {
+    if (r >= p.rows) return -1;
+    const int at = (p.row0 + r) / a.group;
+    if (!p.prefix) return p.pos0 + at;
+    if (!p.masked) return INT32_MAX;
+    int lo = 0, hi = a.num_seqs - 1;
+    const int row = p.q0 + at;
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (x.q_start[mid] <= row) lo = mid; else hi = mid - 1;
+    }
+    return clamped_len(a, x, lo) - (x.q_start[lo + 1] - row);
+}
+
+template <typename T, int D>
+__device__ __forceinline__ const T* query_row(const SharedArgs& a, const Piece& p, int r) {
+    const int e = p.row0 + min(r, p.rows - 1);
+    return static_cast<const T*>(a.q) + ((int64_t)(p.q0 + e / a.group) * a.hq + p.head * a.group + e % a.group) * D;
+}
+
+// Maximum and sum over lanes l, l ^ 16, l ^ 32, l ^ 48, which hold one row's keys.
+__device__ __forceinline__ float rows_max(float v) {
+    const auto s = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    const float m = fmaxf(__uint_as_float(s[0]), __uint_as_float(s[1]));
+    const auto t = __builtin_amdgcn_permlane16_swap(__float_as_uint(m), __float_as_uint(m), false, false);
+    return fmaxf(__uint_as_float(t[0]), __uint_as_float(t[1]));
+}
+__device__ __forceinline__ float rows_sum(float v) {
+    const auto s = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    const float m = __uint_as_float(s[0]) + __uint_as_float(s[1]);
+    const auto t = __builtin_amdgcn_permlane16_swap(__float_as_uint(m), __float_as_uint(m), false, false);
+    return __uint_as_float(t[0]) + __uint_as_float(t[1]);
+}
+
+// Raises the row's maximum where one of its scores exceeds it by more than the slack,
+// and rescales what has been summed.
+template <int DT>
+__device__ __forceinline__ void raise(float top, float scale, float& m, float& l, f32x4_t* o) {
+    const float mine = top * scale;
+    if (__any(mine > m + kSlackLog2)) {
+        const float next = fmaxf(m, rows_max(mine));
+        const float f = __builtin_amdgcn_exp2f(m - next);
+        m = next;
+        l *= f;
+#pragma unroll
+        for (int t = 0; t < DT; ++t) o[t] *= f;
+    }
+}
+
+// V^T of keys from `left` on (of the lane's eight) becomes zero: what a slot behind the
+// last key holds may be no number.
+__device__ __forceinline__ uint4 first_keys(uint4 v, int left) {
+    const uint32_t m[4] = {left > 1 ? ~0u : left > 0 ? 0xffffu : 0u, left > 3 ? ~0u : left > 2 ? 0xffffu : 0u,
+                           left > 5 ? ~0u : left > 4 ? 0xffffu : 0u, left > 7 ? ~0u : left > 6 ? 0xffffu : 0u};
+    return make_uint4(v.x & m[0], v.y & m[1], v.z & m[2], v.w & m[3]);
+}
+
+__device__ __forceinline__ bf16x8_t as_bf16x8(const uint4& v) { return __builtin_bit_cast(bf16x8_t, v); }
+
+// One step of 32 keys from block b0 on for RT row tiles.  load_k(t, c) and load_v(dt)
+// give the operands; ok: whether the block of the lane's keys is mapped.
+template <int D, int RT, typename LoadK, typename AfterK, typename LoadV>
+__device__ __forceinline__ void step32(const Piece& p, int b0, bool edge, bool ok, float scale, const bf16x8_t (*q)[D / 32],
+                                       const int* pos, float* m, float* l, f32x4_t (*o)[D / 16], LoadK load_k,
+                                       AfterK after_k, LoadV load_v) {
+    const int lg = (threadIdx.x % kWave) / 16;
+    f32x4_t s[RT][2];
+#pragma unroll
+    for (int r = 0; r < RT; ++r) s[r][0] = s[r][1] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int c = 0; c < D / 32; ++c)
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            const bf16x8_t k = load_k(t, c);
+#pragma unroll
+            for (int r = 0; r < RT; ++r) s[r][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, q[r][c], s[r][t], 0, 0, 0);
+        }
+    after_k();
+    const int key0 = b0 * kBlockTokens + 8 * lg;
+    bf16x8_t w[RT];
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+        if (edge) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (!ok || key0 + e > pos[r]) s[r][e / 4][e % 4] = -INFINITY;
+        }
+        const float top = fmaxf(fmaxf(fmaxf(s[r][0][0], s[r][0][1]), fmaxf(s[r][0][2], s[r][0][3])),
+                                fmaxf(fmaxf(s[r][1][0], s[r][1][1]), fmaxf(s[r][1][2], s[r][1][3])));
+        raise<D / 16>(top, scale, m[r], l[r], o[r]);
+        float e8[8], sum = 0.f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            e8[e] = __builtin_amdgcn_exp2f(fmaf(s[r][e / 4][e % 4], scale, -m[r]));
+            sum += e8[e];
+        }
+        l[r] += sum;
+        w[r] = as_bf16x8(make_uint4(pack_bf16x2(e8[0], e8[1]), pack_bf16x2(e8[2], e8[3]), pack_bf16x2(e8[4], e8[5]),
+                                    pack_bf16x2(e8[6], e8[7])));
+    }
+#pragma unroll
+    for (int t = 0; t < D / 16; ++t) {
+        uint4 v = load_v(t);
+        if (edge) v = first_keys(v, ok ? p.S - key0 : 0);
+#pragma unroll
+        for (int r = 0; r < RT; ++r) o[r][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(v), w[r], o[r][t], 0, 0, 0);
+    }
+}
+
+// Row r's dims 16 t + 4 lg .. + 3 of the partial result, and its maximum and sum.
+template <int D>
+__device__ __forceinline__ void store_partial(const SharedArgs& a, const Piece& p, int r, int t, const f32x4_t& v) {
+    const int lg = (threadIdx.x % kWave) / 16;
+    if (r < p.rows) *reinterpret_cast<f32x4_t*>(a.part_o + (p.slot_row + r) * D + 16 * t + 4 * lg) = v;
+}
+
+// The four wavefronts' states of the same rows, joined and stored.  smem: 4 D / 16 KiB.
+template <int D, int RT>
+__device__ __forceinline__ void join_waves(const SharedArgs& a, const Piece& p, float* m, float* l, f32x4_t (*o)[D / 16],
+                                           uint8_t* smem) {
+    constexpr int DT = D / 16;
+    __shared__ float s_ml[2][kWaves][16];
+    const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave, l16 = lane % 16;
+    f32x4_t* part = reinterpret_cast<f32x4_t*>(smem);
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+        const float sum = rows_sum(l[r]);
+        if (lane < 16) s_ml[0][wave][l16] = m[r], s_ml[1][wave][l16] = sum;
+#pragma unroll
+        for (int t = 0; t < DT; ++t) part[(wave * DT + t) * kWave + lane] = o[r][t];
+        __syncthreads();
+        float top = s_ml[0][0][l16];
+#pragma unroll
+        for (int w = 1; w < kWaves; ++w) top = fmaxf(top, s_ml[0][w][l16]);
+        float f[kWaves], all = 0.f;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+            f[w] = __builtin_amdgcn_exp2f(s_ml[0][w][l16] - top);
+            all = fmaf(s_ml[1][w][l16], f[w], all);
+        }
+#pragma unroll
+        for (int t = wave * (DT / kWaves); t < (wave + 1) * (DT / kWaves); ++t) {
+            f32x4_t v = part[t * kWave + lane] * f[0];
+#pragma unroll
+            for (int w = 1; w < kWaves; ++w) v += part[(w * DT + t) * kWave + lane] * f[w];
+            store_partial<D>(a, p, r * 16 + l16, t, v);
+        }
+        if (threadIdx.x < 16 && r * 16 + l16 < p.rows) a.part_ml[p.slot_row + r * 16 + l16] = make_float2(top, all);
+        __syncthreads();
+    }
+}
+
+// Few rows, bf16.
+template <int D, int RT>
+__device__ void walk_flat(const SharedArgs& a, const Index& x, const Piece& p, uint8_t* smem) {
+    constexpr int DT = D / 16, C = D / 32;
+    const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave, l16 = lane % 16, lg = lane / 16;
+    bf16x8_t q[RT][C];
+    f32x4_t o[RT][DT];
+    float m[RT], l[RT];
+    int pos[RT];
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+        const uint16_t* row = query_row<uint16_t, D>(a, p, r * 16 + l16);
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+            q[r][c] = __builtin_bit_cast(bf16x8_t, *reinterpret_cast<const u32x4h_t*>(row + 32 * c + 8 * lg));
+        pos[r] = row_position(a, x, p, r * 16 + l16);
+        m[r] = kNoMax;
+        l[r] = 0.f;
+#pragma unroll
+        for (int t = 0; t < DT; ++t) o[r][t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    }
+    constexpr int64_t kTile = (int64_t)D * kBlockTokens * 2;  // bytes of a block's keys of one head
+    // this wavefront's two blocks of unit u; a block behind the last one is unmapped
+    auto first = [&](int u) { return p.b_lo + u * kUnitBlocks + 2 * wave; };
+    auto id_of = [&](int b) {
+        if (b >= p.b_hi) return -1;
+        const int id = p.table[b];
+        return id >= 0 && id < a.num_blocks ? id : -1;
+    };
+    uint4 k[2][C], v[DT];
+    const int k_at = (l16 & 3) * 16 + ((l16 >> 2) & 1) * 128 + lg * 256, v_at = l16 * 32 + (lg & 1) * 16;
+    auto load_k = [&](int id0, int id1) {
+        const uint8_t* from = a.kc + ((int64_t)max(l16 >> 3 ? id1 : id0, 0) * a.hkv + p.head) * kTile + k_at;
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+#pragma unroll
+            for (int t = 0; t < 2; ++t) k[t][c] = ld16(from + c * 1024 + t * 64);
+    };
+    auto load_v = [&](int id0, int id1) {
+        const uint8_t* from = a.vc + ((int64_t)max(lg >> 1 ? id1 : id0, 0) * a.hkv + p.head) * kTile + v_at;
+#pragma unroll
+        for (int t = 0; t < DT; ++t) v[t] = ld16(from + t * 512);
+    };
+    int id0 = -1, id1 = -1, next0 = -1, next1 = -1;
+    if (p.u0 < p.u1) {
+        id0 = id_of(first(p.u0));
+        id1 = id_of(first(p.u0) + 1);
+        if (id0 >= 0 || id1 >= 0) {
+            load_k(id0, id1);
+            load_v(id0, id1);
+        }
+        if (p.u0 + 1 < p.u1) {
+            next0 = id_of(first(p.u0 + 1));
+            next1 = id_of(first(p.u0 + 1) + 1);
+        }
+    }
+    for (int u = p.u0; u < p.u1; ++u) {
+        const int b0 = first(u);
+        const bool more = next0 >= 0 || next1 >= 0;
+        int after0 = -1, after1 = -1;
+        if (u + 2 < p.u1) {
+            after0 = id_of(first(u + 2));
+            after1 = id_of(first(u + 2) + 1);
+        }
+        if (id0 >= 0 || id1 >= 0) {
+            const bool edge = (b0 + 2) * kBlockTokens - 1 > p.min_pos || id0 < 0 || id1 < 0;
+            const bool ok = (lg >> 1 ? id1 : id0) >= 0;
+            step32<D, RT>(p, b0, edge, ok, a.scale_log2, q, pos, m, l, o, [&](int t, int c) { return as_bf16x8(k[t][c]); },
+                          [&]() { if (more) load_k(next0, next1); }, [&](int t) { return v[t]; });
+        } else if (more) {
+            load_k(next0, next1);
+        }
+        if (more) load_v(next0, next1);
+        id0 = next0;
+        id1 = next1;
+        next0 = after0;
+        next1 = after1;
+    }
+    join_waves<D, RT>(a, p, m, l, o, smem);
+}
+
+// Few rows, fp32: fp32 products (v_mfma_f32_16x16x4_f32), a block of 16 keys at a time.
+// Lane 16 lg + l16 takes the 16-byte chunks lg, lg + 4, ... of key l16; product i of a
+// chunk multiplies its i-th dim.  A lane's 16 bytes of V^T are its keys 4 lg .. 4 lg + 3.
+template <int D, int RT>
+__device__ void walk_flat_f32(const SharedArgs& a, const Index& x, const Piece& p, uint8_t* smem) {
+    constexpr int DT = D / 16, C = D / 16;
+    const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave, l16 = lane % 16, lg = lane / 16;
+    f32x4_t q[RT][C], o[RT][DT];
+    float m[RT], l[RT];
+    int pos[RT];
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+        const float* row = query_row<float, D>(a, p, r * 16 + l16);
+#pragma unroll
+        for (int c = 0; c < C; ++c) q[r][c] = *reinterpret_cast<const f32x4u_t*>(row + 16 * c + 4 * lg);
+        pos[r] = row_position(a, x, p, r * 16 + l16);
+        m[r] = kNoMax;
+        l[r] = 0.f;
+#pragma unroll
+        for (int t = 0; t < DT; ++t) o[r][t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    }
+    constexpr int64_t kTile = (int64_t)D * kBlockTokens * 4;
+    // block e of this wavefront: two of every unit
+    auto block = [&](int e) { return p.b_lo + (p.u0 + (e >> 1)) * kUnitBlocks + 2 * wave + (e & 1); };
+    auto id_of = [&](int e) {
+        const int b = block(e);
+        if (e >= 2 * (p.u1 - p.u0) || b >= p.b_hi) return -1;
+        const int id = p.table[b];
+        return id >= 0 && id < a.num_blocks ? id : -1;
+    };
+    f32x4_t k[C], v[DT];
+    auto load_k = [&](int id) {
+        const uint8_t* from = a.kc + ((int64_t)id * a.hkv + p.head) * kTile + l16 * 16 + lg * 256;
+#pragma unroll
+        for (int c = 0; c < C; ++c) k[c] = *reinterpret_cast<const f32x4_t*>(from + c * 1024);
+    };
+    auto load_v = [&](int id) {
+        const uint8_t* from = a.vc + ((int64_t)id * a.hkv + p.head) * kTile + l16 * 64 + lg * 16;
+#pragma unroll
+        for (int t = 0; t < DT; ++t) v[t] = *reinterpret_cast<const f32x4_t*>(from + t * 1024);
+    };
+    int id = id_of(0), next = id_of(1);
+    if (id >= 0) {
+        load_k(id);
+        load_v(id);
+    }
+    for (int e = 0; e < 2 * (p.u1 - p.u0); ++e) {
+        const int after = id_of(e + 2);
+        if (id >= 0) {
+            const int key0 = block(e) * kBlockTokens + 4 * lg;
+            const bool edge = block(e) * kBlockTokens + kBlockTokens - 1 > p.min_pos;
+            f32x4_t s[RT];
+#pragma unroll
+            for (int r = 0; r < RT; ++r) {
+                // two chains of products: none waits for the one before it
+                f32x4_t s0{0.f, 0.f, 0.f, 0.f}, s1{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int c = 0; c < C; ++c)
+#pragma unroll
+                    for (int i = 0; i < 4; i += 2) {
+                        s0 = __builtin_amdgcn_mfma_f32_16x16x4f32(k[c][i], q[r][c][i], s0, 0, 0, 0);
+                        s1 = __builtin_amdgcn_mfma_f32_16x16x4f32(k[c][i + 1], q[r][c][i + 1], s1, 0, 0, 0);
+                    }
+                s[r] = s0 + s1;
+            }
+            if (next >= 0) load_k(next);
+#pragma unroll
+            for (int r = 0; r < RT; ++r) {
+                if (edge) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (key0 + i > pos[r]) s[r][i] = -INFINITY;
+                }
+                raise<DT>(fmaxf(fmaxf(s[r][0], s[r][1]), fmaxf(s[r][2], s[r][3])), a.scale_log2, m[r], l[r], o[r]);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    s[r][i] = exp2f(fmaf(s[r][i], a.scale_log2, -m[r]));
+                    l[r] += s[r][i];
+                }
+            }
+#pragma unroll
+            for (int t = 0; t < DT; ++t) {
+                if (edge) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (key0 + i >= p.S) v[t][i] = 0.f;
+                }
+#pragma unroll
+                for (int r = 0; r < RT; ++r)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) o[r][t] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[t][i], s[r][i], o[r][t], 0, 0, 0);
+            }
+        } else if (next >= 0) {
+            load_k(next);
+        }
+        if (next >= 0) load_v(next);
+        id = next;
+        next = after;
+    }
+    join_waves<D, RT>(a, p, m, l, o, smem);
+}
+
+// Many rows, bf16: wavefront w has RT tiles of the rows; the ring's stages hold two
+// blocks each, K and then V.
+template <int D, int RT>
+__device__ void walk_tall(const SharedArgs& a, const Index& x, const Piece& p, uint8_t* smem) {
+    constexpr int DT = D / 16, C = D / 32;
+    constexpr int kTile = D * kBlockTokens * 2;  // bytes of a block's keys of one head
+    constexpr int kStage = 4 * kTile, kRun = kTile / 1024;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave, l16 = lane % 16,
+              lg = lane / 16;
+    bf16x8_t q[RT][C];
+    f32x4_t o[RT][DT];
+    float m[RT], l[RT];
+    int pos[RT];
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+        const int row_at = (wave * RT + r) * 16 + l16;
+        const uint16_t* row = query_row<uint16_t, D>(a, p, row_at);
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+            q[r][c] = __builtin_bit_cast(bf16x8_t, *reinterpret_cast<const u32x4h_t*>(row + 32 * c + 8 * lg));
+        pos[r] = row_position(a, x, p, row_at);
+        m[r] = kNoMax;
+        l[r] = 0.f;
+#pragma unroll
+        for (int t = 0; t < DT; ++t) o[r][t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    }
+    const int b_first = p.b_lo + p.u0 * kUnitBlocks, b_end = min(p.b_hi, p.b_lo + p.u1 * kUnitBlocks);
+    const int steps = max(0, (b_end - b_first + 1) / 2);
+    auto id_of = [&](int b) {
+        if (b >= b_end) return -1;
+        const int id = p.table[b];
+        return id >= 0 && id < a.num_blocks ? id : -1;
+    };
+    const uint32_t ring = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)smem;
+    // wavefronts 0 and 1 fetch the K tiles of a step's two blocks, 2 and 3 the V tiles
+    auto fetch = [&](int e) {
+        const int id = max(0, id_of(b_first + 2 * e + (wave & 1)));
+        const uint8_t* from = (wave < 2 ? a.kc : a.vc) + ((int64_t)id * a.hkv + p.head) * kTile;
+        dma16_run<kRun>(ring + (e % kStages) * kStage + wave * kTile, from, lane * 16);
+    };
+    // the loads of Q are done before the ring's are counted
+    wait_vmcnt<0>();
+#pragma unroll
+    for (int e = 0; e < kStages - 1; ++e)
+        if (e < steps) fetch(e);
+    const int k_at = (l16 >> 3) * kTile + (l16 & 3) * 16 + ((l16 >> 2) & 1) * 128 + lg * 256;
+    const int v_at = 2 * kTile + (lg >> 1) * kTile + l16 * 32 + (lg & 1) * 16;
+    for (int e = 0; e < steps; ++e) {
+        // this wavefront's loads of stages e + 1 .. e + kStages - 2 may be under way
+        if (e + kStages - 2 < steps) wait_vmcnt<(kStages - 2) * kRun>();
+        else wait_vmcnt<0>();
+        // behind it stage e is whole, and nobody reads stage e - 1 any more
+        lds_barrier();
+        if (e + kStages - 1 < steps) fetch(e + kStages - 1);
+        const uint8_t* stage = smem + (e % kStages) * kStage;
+        const int b0 = b_first + 2 * e;
+        const int id0 = id_of(b0), id1 = id_of(b0 + 1);
+        const bool edge = (b0 + 2) * kBlockTokens - 1 > p.min_pos || id0 < 0 || id1 < 0;
+        const bool ok = (lg >> 1 ? id1 : id0) >= 0;
+        step32<D, RT>(p, b0, edge, ok, a.scale_log2, q, pos, m, l, o,
+                      [&](int t, int c) { return as_bf16x8(ld16(stage + k_at + c * 1024 + t * 64)); }, []() {},
+                      [&](int t) { return ld16(stage + v_at + t * 512); });
+    }
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+        const int row_at = (wave * RT + r) * 16 + l16;
+        const float sum = rows_sum(l[r]);
+#pragma unroll
+        for (int t = 0; t < DT; ++t) store_partial<D>(a, p, row_at, t, o[r][t]);
+        if (lg == 0 && row_at < p.rows) a.part_ml[p.slot_row + row_at] = make_float2(m[r], sum);
+    }
+    __syncthreads();  // the ring is free
+}
+
+template <typename T, int D>
+constexpr int smem_bytes() {
+    const int joined = kWaves * (D / 16) * 1024;
+    const int ring = sizeof(T) == 2 ? kStages * 4 * D * kBlockTokens * 2 : 0;
+    return joined > ring ? joined : ring;
+}
+
+template <typename T, int D, bool INLINE>
+__global__ __launch_bounds__(kThreads, 2) void shared_walk(SharedArgs a, Index x) {
+    __shared__ __attribute__((aligned(16))) uint8_t smem[smem_bytes<T, D>()];
+    __shared__ int64_t s_unit_off[INLINE ? kInlineSegs + 1 : 1];
+    __shared__ int32_t s_pair_off[INLINE ? kInlineSegs + 1 : 1];
+    __shared__ int32_t s_masked[INLINE ? kInlineSegs : 1];
+    const int64_t* unit_off = INLINE ? s_unit_off : a.unit_off;
+    const int32_t* pair_off = INLINE ? s_pair_off : a.pair_off;
+    const int32_t* masked = INLINE ? s_masked : a.masked;
+    const int segs = a.num_groups + a.num_seqs;
+    if constexpr (INLINE) {
+        count_units<kThreads>(a, x, s_unit_off, s_pair_off, s_masked);
+        if (blockIdx.x == 0)  // for the pass that joins
+            for (int s = threadIdx.x; s <= segs; s += kThreads) a.unit_off[s] = s_unit_off[s], a.pair_off[s] = s_pair_off[s];
+    }
+    const Share h = divide_workgroups(a, unit_off, pair_off);
+    const bool first = (int)blockIdx.x < h.na;
+    // workgroups go round the eight XCDs: each takes a run of a prefix's units, whose
+    // heads then stay in few of the L2 caches
+    const int b = blockIdx.x, w = !first ? b - h.na : h.ca == h.na ? b % 8 * (h.na / 8) + b / 8 : b;
+    const int64_t units = first ? h.ua : h.ub;
+    const int count = first ? h.ca : h.cb;
+    if (w >= count) return;
+    int64_t u = units * w / count;
+    const int64_t u_end = units * (w + 1) / count;
+    while (u < u_end) {
+        const int64_t at = first ? u : h.ua + u;
+        int lo = first ? 0 : a.num_groups, hi = (first ? a.num_groups : segs) - 1;
+        while (lo < hi) {
+            const int mid = (lo + hi + 1) >> 1;
+            if (unit_off[mid] <= at) lo = mid; else hi = mid - 1;
+        }
+        const int s = __builtin_amdgcn_readfirstlane(lo);
+        const Segment g = segment_of(a, x, s);
+        const int each = units_of(g);
+        const int64_t local = at - unit_off[s];
+        const int pair = (int)(local / each), tile = pair % g.tiles;
+        Piece p;
+        p.q0 = g.q0;
+        p.row0 = tile * g.tile;
+        p.rows = max(0, min(g.tile, g.rows - p.row0));
+        p.head = pair / g.tiles;
+        p.b_lo = g.b_lo;
+        p.b_hi = g.b_hi;
+        p.u0 = (int)(local - (int64_t)pair * each);
+        p.u1 = (int)min((int64_t)each, p.u0 + (u_end - u));
+        u += p.u1 - p.u0;
+        p.S = g.S;
+        p.table = x.tables + (int64_t)g.table * a.max_blocks;
+        p.prefix = first;
+        p.pos0 = g.S - g.n;
+        p.masked = first && masked[s];
+        p.min_pos = first ? (p.masked ? -1 : INT32_MAX) : p.pos0 + p.row0 / a.group;
+        const int64_t slot = first ? pair_off[s] + pair + w : (int64_t)(pair_off[s] - h.pa) + pair + w;
+        if (slot >= (first ? a.slots_a : a.slots_b) || p.rows == 0) continue;
+        p.slot_row = first ? slot * a.tile_a : a.slots_a * a.tile_a + slot * a.tile_b;
+        // keys that none of the tile's rows sees
+        if (!first) {
+            const int seen = p.pos0 + (p.row0 + p.rows - 1) / a.group + 1 - p.b_lo * kBlockTokens;
+            p.u1 = max(p.u0, min(p.u1, (max(0, seen) + kUnitBlocks * kBlockTokens - 1) / (kUnitBlocks * kBlockTokens)));
+        }
+        if constexpr (sizeof(T) == 4) {
+            if (p.rows <= 16) walk_flat_f32<D, 1>(a, x, p, smem);
+            else walk_flat_f32<D, 2>(a, x, p, smem);
+        } else {
+            constexpr int RT = tall_tiles(D), FT = flat_tiles(D, false);
+            if (p.rows <= 16) walk_flat<D, 1>(a, x, p, smem);
+            else if (p.rows <= 32) walk_flat<D, 2>(a, x, p, smem);
+            else if (p.rows <= 16 * FT) walk_flat<D, FT>(a, x, p, smem);
+            else if (p.rows <= 64 * RT / 2) walk_tall<D, RT / 2>(a, x, p, smem);
+            else walk_tall<D, RT>(a, x, p, smem);
+        }
+    }
+}
+
+// A row's parts joined.  32 lanes (D = 64: 16) per (row, query head), a workgroup per
+// row and run of heads.
+template <typename T, int D>
+__global__ __launch_bounds__(kThreads) void shared_join(SharedArgs a, Index x) {
+    constexpr int kLanes = D / 4, kHeads = kThreads / kLanes;
+    const int row = blockIdx.x, tid = threadIdx.x;
+    // the row's request: the last one that begins at or before it
+    int before = 0;
+    for (int base = 0; base < a.num_seqs; base += kThreads) {
+        const int at = base + tid;
+        const int c = __syncthreads_count(at < a.num_seqs && x.q_start[at] <= row);
+        before += c;
+        if (c < kThreads) break;
+    }
+    const int i = before - 1;
+    const int h = blockIdx.y * kHeads + tid / kLanes, d = tid % kLanes * 4;
+    if (h >= a.hq || i < 0 || row >= x.q_start[i + 1]) return;
+    const Share sh = divide_workgroups(a, a.unit_off, a.pair_off);
+    const int head = h / a.group;
+    const int k = group_of(a, x, i);
+    float top = kNoMax, sum = 0.f;
+    f32x4_t acc{0.f, 0.f, 0.f, 0.f};
+    auto part = [&](int s, bool first) {
+        const Segment g = segment_of(a, x, s);
+        const int each = units_of(g);
+        if (each == 0 || g.rows == 0) return;
+        const int e = (row - g.q0) * a.group + h % a.group;
+        const int tile = e / g.tile, pair = head * g.tiles + tile;
+        const int64_t units = first ? sh.ua : sh.ub, u0 = a.unit_off[s] - (first ? 0 : sh.ua) + (int64_t)pair * each;
+        const int count = first ? sh.ca : sh.cb;
+        // workgroup w owns units [units w / count, units (w + 1) / count)
+        const int w0 = (int)(((u0 + 1) * count - 1) / units), w1 = (int)(((u0 + each) * count - 1) / units);
+        const int64_t p = first ? a.pair_off[s] + pair : a.pair_off[s] - sh.pa + pair;
+        for (int w = w0; w <= w1; ++w) {
+            const int64_t slot = p + w;
+            if (slot >= (first ? a.slots_a : a.slots_b)) break;
+            const int64_t at = (first ? slot * a.tile_a : a.slots_a * a.tile_a + slot * a.tile_b) + e - tile * g.tile;
+            const float2 ml = a.part_ml[at];
+            const f32x4_t o = *reinterpret_cast<const f32x4_t*>(a.part_o + at * D + d);
+            const float next = fmaxf(top, ml.x);
+            const float f0 = exp2f(top - next), f1 = exp2f(ml.x - next);
+            top = next;
+            sum = fmaf(sum, f0, ml.y * f1);
+            acc = acc * f0 + o * f1;
+        }
+    };
+    if (k >= 0) part(k, true);
+    part(a.num_groups + i, false);
+    // a sink adds to the sum alone; a row without keys is zero
+    const float den = a.sinks ? sum + exp2f(fmaf(a.sinks[h], kLog2e, -top)) : sum;
+    const f32x4_t y = sum == 0.f ? f32x4_t{0.f, 0.f, 0.f, 0.f} : acc / den;
+    T* to = static_cast<T*>(a.out) + ((int64_t)row * a.hq + h) * D + d;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) Storage<T>::store(to, e, y[e]);
+}
+
+// ------------------------------------------------------------------ host side
+
+struct SharedPlan {
+    int nwg, tile_a, tile_b;
+    int64_t slots_a, slots_b, segs;
+    size_t o_bytes, ml_bytes, off_bytes, total;
+};
+
+// Row tiles and partial results.  A tile holds at most the rows that its segment may
+// have: few of them (flat) or 64 tall_tiles.
+int plan_shared(const verify_attn_params* p, int32_t total_q, int32_t max_q_len, int32_t num_groups, SharedPlan& s) {
+    const int group = p->num_q_heads / p->num_kv_heads, D = p->head_dim;
+    const bool f32 = p->dtype == VERIFY_F32;
+    auto tile = [&](int64_t rows) {
+        const int flat = 16 * flat_tiles(D, f32);
+        const int need = (int)std::max<int64_t>(16, (std::min<int64_t>(rows, flat) + 15) / 16 * 16);
+        return f32 || rows <= flat ? need : 64 * tall_tiles(D);
+    };
+    const int64_t rows = (int64_t)total_q * group;
+    s.nwg = 2 * device_cus() / 8 * 8;
+    s.tile_a = tile(rows);
+    s.tile_b = tile(std::min<int64_t>(rows, (int64_t)max_q_len * group));
+    const int64_t pairs_a = (rows / s.tile_a + num_groups) * p->num_kv_heads;
+    const int64_t pairs_b = (rows / s.tile_b + p->num_seqs) * p->num_kv_heads;
+    if (pairs_a + pairs_b >= (1 << 30)) return VERIFY_EUNSUPPORTED;
+    s.slots_a = pairs_a + s.nwg;
+    s.slots_b = pairs_b + s.nwg;
+    s.segs = (int64_t)num_groups + p->num_seqs;
+    const int64_t part_rows = s.slots_a * s.tile_a + s.slots_b * s.tile_b;
+    s.o_bytes = (size_t)part_rows * D * 4;
+    s.ml_bytes = align_up((size_t)part_rows * 8, 16);
+    s.off_bytes = align_up((size_t)(s.segs + 1) * 8, 16) + 2 * align_up((size_t)(s.segs + 1) * 4, 16);
+    s.total = s.o_bytes + s.ml_bytes + s.off_bytes;
+    return VERIFY_OK;
+}
+
+int check_shared(const verify_attn_params* p, int32_t total_q, int32_t max_q_len, int32_t max_seq_len, int32_t num_groups,
+                 int32_t max_prefix_len) {
+    const int rc = validate(p, total_q, max_q_len, max_seq_len);
+    if (rc != VERIFY_OK) return rc;
+    if (num_groups < 0 || max_prefix_len < 0) return VERIFY_EINVAL;
+    if (p->sliding_window > 0 || p->kv_split_blocks > 0) return VERIFY_EUNSUPPORTED;
+    if (num_groups > 65535) return VERIFY_EUNSUPPORTED;
+    const int64_t group = p->num_q_heads / p->num_kv_heads;
+    if ((int64_t)total_q * group >= (1 << 30)) return VERIFY_EUNSUPPORTED;
+    if (p->max_blocks_per_seq > (1 << 26)) return VERIFY_EUNSUPPORTED;
+    return VERIFY_OK;
+}
+
+// Nothing to share: the call is verify_attention.
+bool is_plain(const verify_attn_params* p, int32_t num_groups, int32_t max_prefix_len) {
+    return num_groups == 0 || max_prefix_len < kBlockTokens || p->num_blocks == 0;
+}
+
+template <typename T, int D>
+void launch_shared(const SharedArgs& a, const Index& x, hipStream_t stream) {
+    if (a.num_groups + a.num_seqs <= kInlineSegs) {
+        hipLaunchKernelGGL((shared_walk<T, D, true>), dim3(a.nwg), dim3(kThreads), 0, stream, a, x);
+    } else {
+        hipLaunchKernelGGL(shared_schedule, dim3(1), dim3(1024), 0, stream, a, x);
+        hipLaunchKernelGGL((shared_walk<T, D, false>), dim3(a.nwg), dim3(kThreads), 0, stream, a, x);
+    }
+    constexpr int kHeads = kThreads / (D / 4);
+    hipLaunchKernelGGL((shared_join<T, D>), dim3(a.total_q, (a.hq + kHeads - 1) / kHeads), dim3(kThreads), 0, stream, a, x);
+}
+
+}  // namespace
+}  // namespace averify
+
+using namespace averify;
+
+extern "C" int verify_attention_shared_workspace_size(const verify_attn_params* params, int32_t total_q,
+                                                      int32_t max_q_len, int32_t max_seq_len, int32_t num_groups,
+                                                      int32_t max_prefix_len, size_t* bytes) {
+    int rc = check_shared(params, total_q, max_q_len, max_seq_len, num_groups, max_prefix_len);
+    if (rc != VERIFY_OK) return rc;
+    if (!bytes) return VERIFY_EINVAL;
+    *bytes = 0;
+    if (params->num_seqs == 0 || total_q == 0) return VERIFY_OK;
+    if (is_plain(params, num_groups, max_prefix_len))
+        return verify_attention_workspace_size(params, total_q, max_q_len, max_seq_len, bytes);
+    SharedPlan s;
+    rc = plan_shared(params, total_q, max_q_len, num_groups, s);
+    if (rc == VERIFY_OK) *bytes = s.total;
+    return rc;
+}
+
+extern "C" int verify_attention_shared(const verify_attn_params* params, int32_t total_q, int32_t max_q_len,
+                                       int32_t max_seq_len, int32_t num_groups, int32_t max_prefix_len,
+                                       const void* q, const void* k_cache, const void* v_cache,
+                                       const int32_t* block_tables, const int32_t* seq_lens, const int32_t* q_start,
+                                       const int32_t* group_start, const int32_t* prefix_lens, const float* sinks,
+                                       void* out, void* workspace, size_t workspace_bytes, hipStream_t stream) {
+    int rc = check_shared(params, total_q, max_q_len, max_seq_len, num_groups, max_prefix_len);
+    if (rc != VERIFY_OK) return rc;
+    if (is_plain(params, num_groups, max_prefix_len))
+        return verify_attention(params, total_q, max_q_len, max_seq_len, q, k_cache, v_cache, block_tables, seq_lens,
+                                q_start, sinks, out, workspace, workspace_bytes, stream);
+    if (params->num_seqs == 0 || total_q == 0) return VERIFY_OK;
+    if (!q || !k_cache || !v_cache || !block_tables || !seq_lens || !q_start || !group_start || !prefix_lens || !out)
+        return VERIFY_EINVAL;
+    if (((uintptr_t)k_cache | (uintptr_t)v_cache | (uintptr_t)workspace) & 15) return VERIFY_EINVAL;
+    SharedPlan s;
+    rc = plan_shared(params, total_q, max_q_len, num_groups, s);
+    if (rc != VERIFY_OK) return rc;
+    if (!workspace || workspace_bytes < s.total) return VERIFY_EWORKSPACE;
+    uint8_t* ws = static_cast<uint8_t*>(workspace);
+    SharedArgs a{};
+    a.q = q;
+    a.kc = static_cast<const uint8_t*>(k_cache);
+    a.vc = static_cast<const uint8_t*>(v_cache);
+    a.sinks = sinks;
+    a.out = out;
+    a.part_o = reinterpret_cast<float*>(ws);
+    a.part_ml = reinterpret_cast<float2*>(ws + s.o_bytes);
+    ws += s.o_bytes + s.ml_bytes;
+    a.unit_off = reinterpret_cast<int64_t*>(ws);
+    ws += align_up((size_t)(s.segs + 1) * 8, 16);
+    a.pair_off = reinterpret_cast<int32_t*>(ws);
+    a.masked = reinterpret_cast<int32_t*>(ws + align_up((size_t)(s.segs + 1) * 4, 16));
+    a.num_seqs = params->num_seqs;
+    a.num_groups = num_groups;
+    a.hq = params->num_q_heads;
+    a.hkv = params->num_kv_heads;
+    a.group = a.hq / a.hkv;
+    a.max_blocks = params->max_blocks_per_seq;
+    a.num_blocks = params->num_blocks;
+    a.max_seq_len = max_seq_len;
+    a.max_prefix = max_prefix_len;
+    a.total_q = total_q;
+    a.nwg = s.nwg;
+    a.tile_a = s.tile_a;
+    a.tile_b = s.tile_b;
+    a.slots_a = s.slots_a;
+    a.slots_b = s.slots_b;
+    const float scale = params->scale > 0.f ? params->scale : 1.f / sqrtf((float)params->head_dim);
+    a.scale_log2 = scale * kLog2e;
+    const Index x{block_tables, seq_lens, q_start, group_start, prefix_lens};
+    if (params->dtype == VERIFY_BF16)
+        params->head_dim == 128 ? launch_shared<uint16_t, 128>(a, x, stream) : launch_shared<uint16_t, 64>(a, x, stream);
+    else
+        params->head_dim == 128 ? launch_shared<float, 128>(a, x, stream) : launch_shared<float, 64>(a, x, stream);
+    return check_launch();
+}

@@ -86,6 +86,42 @@ def test_count_tokens(kw, want):
     assert _count(**kw) == want
 
 
+def _shared(attn=None, T=5, mq=3, ms=100, G=1, mp=64, q=DUMMY, kc=DUMMY, vc=DUMMY, gs=DUMMY, pl=DUMMY, out=DUMMY, ws=DUMMY,
+            size=None):
+    params = attn or _attn()
+    if size is None:
+        n = ctypes.c_size_t(0)
+        rc = av.library().verify_attention_shared_workspace_size(ctypes.byref(params), T, mq, ms, G, mp, ctypes.byref(n))
+        size = n.value if rc == av.OK else 0
+    return av.library().verify_attention_shared(ctypes.byref(params), T, mq, ms, G, mp, q, kc, vc, DUMMY, DUMMY, DUMMY, gs,
+                                                pl, None, out, ws, size, None)
+
+
+@pytest.mark.parametrize("kw,want", [
+    (dict(attn=_attn(sliding_window=5)), av.EUNSUPPORTED), (dict(attn=_attn(kv_split_blocks=1)), av.EUNSUPPORTED),
+    (dict(attn=_attn(head_dim=96)), av.EUNSUPPORTED), (dict(attn=_attn(num_q_heads=7)), av.EINVAL),
+    (dict(G=-1), av.EINVAL), (dict(G=65536), av.EUNSUPPORTED), (dict(mp=-1), av.EINVAL), (dict(T=-1), av.EINVAL),
+    (dict(T=2 ** 29), av.EUNSUPPORTED), (dict(attn=_attn(max_blocks_per_seq=2 ** 27)), av.EUNSUPPORTED),
+    (dict(q=None), av.EINVAL), (dict(gs=None), av.EINVAL), (dict(pl=None), av.EINVAL), (dict(out=None), av.EINVAL),
+    (dict(kc=ctypes.c_void_p(0x1008)), av.EINVAL), (dict(vc=ctypes.c_void_p(0x1004)), av.EINVAL),
+    (dict(ws=ctypes.c_void_p(0x1008)), av.EINVAL), (dict(ws=None), av.EWORKSPACE), (dict(size=100), av.EWORKSPACE),
+    (dict(T=0, q=None), av.OK), (dict(attn=_attn(num_seqs=0), gs=None), av.OK),
+])
+def test_attention_shared(kw, want):
+    assert _shared(**kw) == want
+
+
+def test_attention_shared_without_a_prefix_is_verify_attention():
+    n, m = ctypes.c_size_t(0), ctypes.c_size_t(0)
+    p = _attn()
+    av.library().verify_attention_workspace_size(ctypes.byref(p), 5, 3, 100, ctypes.byref(m))
+    for groups, prefix in ((0, 64), (1, 15)):
+        assert av.library().verify_attention_shared_workspace_size(ctypes.byref(p), 5, 3, 100, groups, prefix,
+                                                                   ctypes.byref(n)) == av.OK
+        assert n.value == m.value
+        assert _shared(G=groups, mp=prefix, q=None) == av.EINVAL
+
+
 def test_the_binding_refuses():
     i32 = torch.int32
     x, tok, qs = torch.zeros((5, 100)), torch.zeros(5, dtype=i32), torch.zeros(3, dtype=i32)
@@ -120,6 +156,22 @@ def test_the_binding_refuses():
     for kw in (dict(q_weight=torch.ones(63)), dict(k_weight=torch.ones(64, dtype=torch.bfloat16)), {}):
         with pytest.raises((ValueError, TypeError)):
             av.verify_norm_rotary(q, None, pos, freq, **kw)
+
+
+def test_the_binding_refuses_shared_attention():
+    i32 = torch.int32
+    kc, vc = torch.zeros((4, 2, 8, 16, 8), dtype=torch.bfloat16), torch.zeros((4, 2, 64, 16), dtype=torch.bfloat16)
+    base = [torch.zeros((3, 4, 64), dtype=torch.bfloat16), kc, vc, torch.zeros((2, 2), dtype=i32), torch.zeros(2, dtype=i32),
+            torch.zeros(3, dtype=i32), torch.zeros(2, dtype=i32), torch.zeros(1, dtype=i32)]
+    bounds = dict(max_q_len=2, max_seq_len=32, max_prefix_len=16)
+    for at, t in [(0, base[0][0]), (1, kc[:, :1]), (2, vc.float()), (3, base[3][0]), (4, base[4][:1]), (5, base[5][:2]),
+                  (6, base[6][:0]), (6, base[6].long()), (7, base[6]), (0, base[0])]:
+        args = list(base)
+        args[at] = t
+        with pytest.raises((ValueError, TypeError)):
+            av.verify_attention_shared(*args, **bounds)
+    with pytest.raises(av.VerifyError):
+        av.attention_shared_workspace_size(base[0], kc, base[3], num_groups=-1, **bounds)
 
 
 def test_the_structs_agree_with_c():
