@@ -44,7 +44,7 @@ constexpr int kWaves = 4;
 constexpr int kThreads = kWaves * kWave;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kUnitBlocks = 8;      // KV blocks of a unit
-constexpr int kInlineSegs = 512;    // segments whose units every workgroup counts itself
+constexpr int kInlineSegs = 255;    // segments whose units every workgroup counts itself
 constexpr int kStages = 4;          // of the tall walk's ring
 constexpr float kNoMax = -3.0e38f;  // a maximum over no key
 // Softmax weights may exceed 1 by up to this factor (log2) before a row's maximum is
@@ -68,9 +68,7 @@ struct SharedArgs {
     void* out;
     float* part_o;    // [slots][tile rows][D]
     float2* part_ml;  // [slots][tile rows] maximum and sum
-    int64_t* unit_off;  // [segments + 1]
-    int32_t* pair_off;  // [segments + 1]
-    int32_t* masked;    // [groups] whether a row of the group stands inside the prefix
+    struct Segment* segments;  // [segments + 1], in memory for the pass that joins
     int num_seqs, num_groups, hq, hkv, group, max_blocks, num_blocks, max_seq_len, max_prefix, total_q;
     int nwg;
     int tile_a, tile_b;    // rows of a tile at most: prefix and own segments
@@ -86,12 +84,16 @@ struct Index {  // device arrays that nothing writes
     const int32_t* __restrict__ prefix;
 };
 
-struct Segment {
+struct __attribute__((aligned(16))) Segment {
+    int64_t unit0;   // number of its first unit; the last entry holds the counts of all
+    int pair0;       // and of its first pair
     int q0, rows;    // first packed row, packed rows times query heads per KV head
     int b_lo, b_hi;  // blocks
     int tile, tiles; // rows of a tile, tiles
     int table;       // the request whose block table lists the blocks
-    int S, n;        // own: cached keys and new ones
+    int S;           // keys from S on are not the request's
+    int pos0;        // own: position of the first row; prefix: whether a row stands inside
+    int group;       // own: the request's group, or -1
 };
 
 __device__ __forceinline__ int clamp_to(int v, int lo, int hi) { return max(lo, min(v, hi)); }
@@ -110,75 +112,66 @@ __device__ __forceinline__ int group_of(const SharedArgs& a, const Index& x, int
     return x.group_start[lo] <= i && i < x.group_start[lo + 1] ? lo : -1;
 }
 
-// Rows divided evenly over as few tiles of at most `most` rows as there need be.
-__device__ __forceinline__ void divide(Segment& g, int most) {
-    g.tiles = (g.rows + most - 1) / most;
-    g.tile = g.tiles ? ((g.rows + g.tiles - 1) / g.tiles + 15) / 16 * 16 : 16;
-}
-
 __device__ __forceinline__ int clamped_len(const SharedArgs& a, const Index& x, int i) {
     return clamp_to(x.lens[i], 0, min(a.max_seq_len, a.max_blocks * kBlockTokens));
 }
 
-__device__ __forceinline__ Segment prefix_segment(const SharedArgs& a, const Index& x, int k) {
-    Segment g;
-    const int r0 = clamp_to(x.group_start[k], 0, a.num_seqs), r1 = clamp_to(x.group_start[k + 1], r0, a.num_seqs);
-    g.q0 = clamp_to(x.q_start[r0], 0, a.total_q);
-    g.rows = (clamp_to(x.q_start[r1], g.q0, a.total_q) - g.q0) * a.group;
-    g.b_lo = 0;
-    g.b_hi = prefix_blocks(a, x, k);
-    g.table = min(r0, a.num_seqs - 1);
-    g.S = g.b_hi * kBlockTokens;
-    g.n = 0;
-    divide(g, a.tile_a);
-    return g;
-}
-
-__device__ __forceinline__ Segment own_segment(const SharedArgs& a, const Index& x, int i) {
-    Segment g;
-    g.q0 = clamp_to(x.q_start[i], 0, a.total_q);
-    g.n = clamp_to(x.q_start[i + 1], g.q0, a.total_q) - g.q0;
-    g.rows = g.n * a.group;
-    const int k = group_of(a, x, i);
-    g.S = clamped_len(a, x, i);
-    g.b_lo = k >= 0 ? prefix_blocks(a, x, k) : 0;
-    g.b_hi = max(g.b_lo, (g.S + kBlockTokens - 1) / kBlockTokens);
-    g.table = i;
-    divide(g, a.tile_b);
-    return g;
-}
-
+// Segment s, but for its first unit and pair.
 __device__ __forceinline__ Segment segment_of(const SharedArgs& a, const Index& x, int s) {
-    return s < a.num_groups ? prefix_segment(a, x, s) : own_segment(a, x, s - a.num_groups);
+    Segment g;
+    const bool first = s < a.num_groups;
+    if (first) {
+        const int r0 = clamp_to(x.group_start[s], 0, a.num_seqs), r1 = clamp_to(x.group_start[s + 1], r0, a.num_seqs);
+        g.q0 = clamp_to(x.q_start[r0], 0, a.total_q);
+        g.rows = (clamp_to(x.q_start[r1], g.q0, a.total_q) - g.q0) * a.group;
+        g.b_lo = 0;
+        g.b_hi = prefix_blocks(a, x, s);
+        g.table = min(r0, a.num_seqs - 1);
+        g.S = g.b_hi * kBlockTokens;
+        g.pos0 = 0;
+        g.group = s;
+    } else {
+        const int i = s - a.num_groups;
+        g.q0 = clamp_to(x.q_start[i], 0, a.total_q);
+        const int n = clamp_to(x.q_start[i + 1], g.q0, a.total_q) - g.q0;
+        g.rows = n * a.group;
+        g.group = group_of(a, x, i);
+        g.S = clamped_len(a, x, i);
+        g.b_lo = g.group >= 0 ? prefix_blocks(a, x, g.group) : 0;
+        g.b_hi = max(g.b_lo, (g.S + kBlockTokens - 1) / kBlockTokens);
+        g.table = i;
+        g.pos0 = g.S - n;
+    }
+    // rows divided evenly over as few tiles as there need be
+    const int most = first ? a.tile_a : a.tile_b;
+    g.tiles = (g.rows + most - 1) / most;
+    g.tile = g.tiles ? ((g.rows + g.tiles - 1) / g.tiles + 15) / 16 * 16 : 16;
+    return g;
 }
 
 __device__ __forceinline__ int units_of(const Segment& g) { return (g.b_hi - g.b_lo + kUnitBlocks - 1) / kUnitBlocks; }
 
-// Unit and pair offsets of all segments, by one workgroup of THREADS threads.
+// All segments, by one workgroup of THREADS threads, and behind them an entry with the
+// number of all units and pairs.
 template <int THREADS>
-__device__ void count_units(const SharedArgs& a, const Index& x, int64_t* unit_off, int32_t* pair_off, int32_t* masked) {
+__device__ void count_units(const SharedArgs& a, const Index& x, Segment* segments) {
     __shared__ int64_t s_units[THREADS / kWave];
     __shared__ int s_pairs[THREADS / kWave];
-    const int tid = threadIdx.x, segs = a.num_groups + a.num_seqs;
-    for (int k = tid; k < a.num_groups; k += THREADS) masked[k] = 0;
-    __syncthreads();
+    const int tid = threadIdx.x, lane = tid % kWave, segs = a.num_groups + a.num_seqs;
     int64_t units0 = 0;
     int pairs0 = 0;
     for (int base = 0; base < segs; base += THREADS) {
         const int s = base + tid;
+        Segment g;
         int pairs = 0, each = 0;
         if (s < segs) {
-            const Segment g = segment_of(a, x, s);
+            g = segment_of(a, x, s);
             each = units_of(g);
             pairs = each > 0 ? g.tiles * a.hkv : 0;
-            // a row that stands in front of the prefix's last key sees a part of it
-            if (s >= a.num_groups && g.n > 0 && g.b_lo > 0 && g.S - g.n < g.b_lo * kBlockTokens - 1)
-                masked[group_of(a, x, s - a.num_groups)] = 1;
         }
         int64_t u = (int64_t)pairs * each;
         int p = pairs;
         const int64_t u_mine = u;
-        const int lane = tid % kWave;
         for (int o = 1; o < kWave; o <<= 1) {
             const int64_t uo = __shfl_up(u, o);
             const int po = __shfl_up(p, o);
@@ -194,20 +187,24 @@ __device__ void count_units(const SharedArgs& a, const Index& x, int64_t* unit_o
             p_all += s_pairs[w];
         }
         if (s < segs) {
-            unit_off[s] = units0 + u - u_mine;
-            pair_off[s] = pairs0 + p - pairs;
+            g.unit0 = units0 + u - u_mine;
+            g.pair0 = pairs0 + p - pairs;
+            segments[s] = g;
         }
         units0 += u_all;
         pairs0 += p_all;
         __syncthreads();
     }
-    if (tid == 0) unit_off[segs] = units0, pair_off[segs] = pairs0;
+    // a row that stands in front of its prefix's last key sees a part of it
+    for (int i = tid; i < a.num_seqs; i += THREADS) {
+        const Segment& g = segments[a.num_groups + i];
+        if (g.group >= 0 && g.rows > 0 && g.pos0 < g.b_lo * kBlockTokens - 1) segments[g.group].pos0 = 1;
+    }
+    if (tid == 0) segments[segs].unit0 = units0, segments[segs].pair0 = pairs0;
     __syncthreads();
 }
 
-__global__ __launch_bounds__(1024) void shared_schedule(SharedArgs a, Index x) {
-    count_units<1024>(a, x, a.unit_off, a.pair_off, a.masked);
-}
+__global__ __launch_bounds__(1024) void shared_schedule(SharedArgs a, Index x) { count_units<1024>(a, x, a.segments); }
 
 // How the workgroups are divided: na of them take the prefixes' ua units, the others the
 // ub own ones.  Where there are fewer units than workgroups, ca and cb of them have one.
@@ -218,11 +215,11 @@ struct Share {
 
 // A unit of a prefix costs about what an own one does: the one fills the matrix units
 // for 128 rows, the other waits for 64 KiB.
-__device__ __forceinline__ Share divide_workgroups(const SharedArgs& a, const int64_t* unit_off, const int32_t* pair_off) {
+__device__ __forceinline__ Share divide_workgroups(const SharedArgs& a, const Segment* segments) {
     Share h;
-    h.ua = unit_off[a.num_groups];
-    h.ub = unit_off[a.num_groups + a.num_seqs] - h.ua;
-    h.pa = pair_off[a.num_groups];
+    h.ua = segments[a.num_groups].unit0;
+    h.ub = segments[a.num_groups + a.num_seqs].unit0 - h.ua;
+    h.pa = segments[a.num_groups].pair0;
     if (h.ua == 0) h.na = 0;
     else if (h.ub == 0) h.na = a.nwg;
     else h.na = clamp_to((int)((double)h.ua / (double)(h.ua + h.ub) * a.nwg / 8 + 0.5) * 8, 8, a.nwg - 8);
@@ -230,6 +227,10 @@ __device__ __forceinline__ Share divide_workgroups(const SharedArgs& a, const in
     h.cb = (int)min((int64_t)(a.nwg - h.na), h.ub);
     return h;
 }
+
+// a / b rounded down, 0 <= a < 2^52: a quotient in binary64 is not rounded up to the next
+// whole number.
+__device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) { return (int64_t)((double)a / (double)b); }
 
 // One workgroup's piece of a pair.
 struct Piece {
@@ -239,8 +240,7 @@ struct Piece {
     int u0, u1;          // units
     int min_pos, S;      // lowest position of a row; keys from S on are not the request's
     int pos0;            // own: position of the segment's first row
-    bool prefix;
-    bool masked;         // prefix: some row stands inside it
+    bool prefix, masked; // of a prefix, in which some row stands
     const int32_t* table;
     int64_t slot_row;    // first row of the partial result
 };
@@ -402,7 +402,8 @@ __device__ __forceinline__ void join_waves(const SharedArgs& a, const Piece& p, 
 template <int D, int RT>
 __device__ void walk_flat(const SharedArgs& a, const Index& x, const Piece& p, uint8_t* smem) {
     constexpr int DT = D / 16, C = D / 32;
-    const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave, l16 = lane % 16, lg = lane / 16;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave, l16 = lane % 16,
+              lg = lane / 16;
     bf16x8_t q[RT][C];
     f32x4_t o[RT][DT];
     float m[RT], l[RT];
@@ -420,11 +421,12 @@ __device__ void walk_flat(const SharedArgs& a, const Index& x, const Piece& p, u
         for (int t = 0; t < DT; ++t) o[r][t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     }
     constexpr int64_t kTile = (int64_t)D * kBlockTokens * 2;  // bytes of a block's keys of one head
-    // this wavefront's two blocks of unit u; a block behind the last one is unmapped
+    // This wavefront's two blocks of a unit.  The ids of 32 units lie in the lanes of a
+    // register, -1 where a block is unmapped or behind the last one.
     auto first = [&](int u) { return p.b_lo + u * kUnitBlocks + 2 * wave; };
-    auto id_of = [&](int b) {
-        if (b >= p.b_hi) return -1;
-        const int id = p.table[b];
+    auto read_ids = [&](int u) {
+        const int b = first(u + lane / 2) + lane % 2;
+        const int id = u + lane / 2 < p.u1 && b < p.b_hi ? p.table[b] : -1;
         return id >= 0 && id < a.num_blocks ? id : -1;
     };
     uint4 k[2][C], v[DT];
@@ -441,27 +443,17 @@ __device__ void walk_flat(const SharedArgs& a, const Index& x, const Piece& p, u
 #pragma unroll
         for (int t = 0; t < DT; ++t) v[t] = ld16(from + t * 512);
     };
-    int id0 = -1, id1 = -1, next0 = -1, next1 = -1;
-    if (p.u0 < p.u1) {
-        id0 = id_of(first(p.u0));
-        id1 = id_of(first(p.u0) + 1);
-        if (id0 >= 0 || id1 >= 0) {
-            load_k(id0, id1);
-            load_v(id0, id1);
-        }
-        if (p.u0 + 1 < p.u1) {
-            next0 = id_of(first(p.u0 + 1));
-            next1 = id_of(first(p.u0 + 1) + 1);
-        }
+    int ids = read_ids(p.u0);
+    int id0 = __builtin_amdgcn_readlane(ids, 0), id1 = __builtin_amdgcn_readlane(ids, 1);
+    if (id0 >= 0 || id1 >= 0) {
+        load_k(id0, id1);
+        load_v(id0, id1);
     }
     for (int u = p.u0; u < p.u1; ++u) {
-        const int b0 = first(u);
+        const int b0 = first(u), at = (u + 1 - p.u0) % 32;
+        if (at == 0) ids = read_ids(u + 1);
+        const int next0 = __builtin_amdgcn_readlane(ids, 2 * at), next1 = __builtin_amdgcn_readlane(ids, 2 * at + 1);
         const bool more = next0 >= 0 || next1 >= 0;
-        int after0 = -1, after1 = -1;
-        if (u + 2 < p.u1) {
-            after0 = id_of(first(u + 2));
-            after1 = id_of(first(u + 2) + 1);
-        }
         if (id0 >= 0 || id1 >= 0) {
             const bool edge = (b0 + 2) * kBlockTokens - 1 > p.min_pos || id0 < 0 || id1 < 0;
             const bool ok = (lg >> 1 ? id1 : id0) >= 0;
@@ -473,8 +465,6 @@ __device__ void walk_flat(const SharedArgs& a, const Index& x, const Piece& p, u
         if (more) load_v(next0, next1);
         id0 = next0;
         id1 = next1;
-        next0 = after0;
-        next1 = after1;
     }
     join_waves<D, RT>(a, p, m, l, o, smem);
 }
@@ -581,7 +571,7 @@ __device__ void walk_flat_f32(const SharedArgs& a, const Index& x, const Piece& 
     join_waves<D, RT>(a, p, m, l, o, smem);
 }
 
-// Many rows, bf16: wavefront w has RT tiles of the rows; the ring's stages hold two
+// Many rows, bf16: wavefront w has the rows' tiles w, w + 4, ...; the ring's stages hold two
 // blocks each, K and then V.
 template <int D, int RT>
 __device__ void walk_tall(const SharedArgs& a, const Index& x, const Piece& p, uint8_t* smem) {
@@ -596,7 +586,7 @@ __device__ void walk_tall(const SharedArgs& a, const Index& x, const Piece& p, u
     int pos[RT];
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
-        const int row_at = (wave * RT + r) * 16 + l16;
+        const int row_at = (r * kWaves + wave) * 16 + l16;
         const uint16_t* row = query_row<uint16_t, D>(a, p, row_at);
 #pragma unroll
         for (int c = 0; c < C; ++c)
@@ -609,20 +599,27 @@ __device__ void walk_tall(const SharedArgs& a, const Index& x, const Piece& p, u
     }
     const int b_first = p.b_lo + p.u0 * kUnitBlocks, b_end = min(p.b_hi, p.b_lo + p.u1 * kUnitBlocks);
     const int steps = max(0, (b_end - b_first + 1) / 2);
-    auto id_of = [&](int b) {
-        if (b >= b_end) return -1;
-        const int id = p.table[b];
+    // The ids of 64 blocks lie in the lanes of a register, two runs of them in turn; -1
+    // where a block is unmapped or behind the last one.  Each read is waited for where
+    // it is made: left pending, the compiler would have to wait in every step, for the
+    // ring's loads too.
+    auto read_ids = [&](int from) {
+        const int b = b_first + from + lane;
+        const int id = b < b_end ? p.table[b] : -1;
+        __builtin_amdgcn_s_waitcnt(kWaitVmcnt0);
         return id >= 0 && id < a.num_blocks ? id : -1;
     };
+    int even = read_ids(0), odd = steps > 32 ? read_ids(64) : -1;
+    auto id_of = [&](int at) { return __builtin_amdgcn_readlane(at & 64 ? odd : even, at & 63); };
     const uint32_t ring = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)smem;
     // wavefronts 0 and 1 fetch the K tiles of a step's two blocks, 2 and 3 the V tiles
     auto fetch = [&](int e) {
-        const int id = max(0, id_of(b_first + 2 * e + (wave & 1)));
+        const int id = max(0, id_of(2 * e + (wave & 1)));
         const uint8_t* from = (wave < 2 ? a.kc : a.vc) + ((int64_t)id * a.hkv + p.head) * kTile;
         dma16_run<kRun>(ring + (e % kStages) * kStage + wave * kTile, from, lane * 16);
     };
     // the loads of Q are done before the ring's are counted
-    wait_vmcnt<0>();
+    __builtin_amdgcn_s_waitcnt(kWaitVmcnt0);
 #pragma unroll
     for (int e = 0; e < kStages - 1; ++e)
         if (e < steps) fetch(e);
@@ -634,10 +631,12 @@ __device__ void walk_tall(const SharedArgs& a, const Index& x, const Piece& p, u
         else wait_vmcnt<0>();
         // behind it stage e is whole, and nobody reads stage e - 1 any more
         lds_barrier();
+        // the run before this step's is used up
+        if (e % 32 == 0 && e > 0 && 2 * e + 64 < 2 * steps) (e & 32 ? even : odd) = read_ids(2 * e + 64);
         if (e + kStages - 1 < steps) fetch(e + kStages - 1);
         const uint8_t* stage = smem + (e % kStages) * kStage;
         const int b0 = b_first + 2 * e;
-        const int id0 = id_of(b0), id1 = id_of(b0 + 1);
+        const int id0 = id_of(2 * e), id1 = id_of(2 * e + 1);
         const bool edge = (b0 + 2) * kBlockTokens - 1 > p.min_pos || id0 < 0 || id1 < 0;
         const bool ok = (lg >> 1 ? id1 : id0) >= 0;
         step32<D, RT>(p, b0, edge, ok, a.scale_log2, q, pos, m, l, o,
@@ -646,7 +645,7 @@ __device__ void walk_tall(const SharedArgs& a, const Index& x, const Piece& p, u
     }
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
-        const int row_at = (wave * RT + r) * 16 + l16;
+        const int row_at = (r * kWaves + wave) * 16 + l16;
         const float sum = rows_sum(l[r]);
 #pragma unroll
         for (int t = 0; t < DT; ++t) store_partial<D>(a, p, row_at, t, o[r][t]);
@@ -665,19 +664,15 @@ constexpr int smem_bytes() {
 template <typename T, int D, bool INLINE>
 __global__ __launch_bounds__(kThreads, 2) void shared_walk(SharedArgs a, Index x) {
     __shared__ __attribute__((aligned(16))) uint8_t smem[smem_bytes<T, D>()];
-    __shared__ int64_t s_unit_off[INLINE ? kInlineSegs + 1 : 1];
-    __shared__ int32_t s_pair_off[INLINE ? kInlineSegs + 1 : 1];
-    __shared__ int32_t s_masked[INLINE ? kInlineSegs : 1];
-    const int64_t* unit_off = INLINE ? s_unit_off : a.unit_off;
-    const int32_t* pair_off = INLINE ? s_pair_off : a.pair_off;
-    const int32_t* masked = INLINE ? s_masked : a.masked;
+    __shared__ Segment s_segments[INLINE ? kInlineSegs + 1 : 1];
+    const Segment* segments = INLINE ? s_segments : a.segments;
     const int segs = a.num_groups + a.num_seqs;
     if constexpr (INLINE) {
-        count_units<kThreads>(a, x, s_unit_off, s_pair_off, s_masked);
+        count_units<kThreads>(a, x, s_segments);
         if (blockIdx.x == 0)  // for the pass that joins
-            for (int s = threadIdx.x; s <= segs; s += kThreads) a.unit_off[s] = s_unit_off[s], a.pair_off[s] = s_pair_off[s];
+            for (int s = threadIdx.x; s <= segs; s += kThreads) a.segments[s] = s_segments[s];
     }
-    const Share h = divide_workgroups(a, unit_off, pair_off);
+    const Share h = divide_workgroups(a, segments);
     const bool first = (int)blockIdx.x < h.na;
     // workgroups go round the eight XCDs: each takes a run of a prefix's units, whose
     // heads then stay in few of the L2 caches
@@ -685,37 +680,37 @@ __global__ __launch_bounds__(kThreads, 2) void shared_walk(SharedArgs a, Index x
     const int64_t units = first ? h.ua : h.ub;
     const int count = first ? h.ca : h.cb;
     if (w >= count) return;
-    int64_t u = units * w / count;
-    const int64_t u_end = units * (w + 1) / count;
+    int64_t u = quotient(units * w, count);
+    const int64_t u_end = quotient(units * (w + 1), count);
     while (u < u_end) {
         const int64_t at = first ? u : h.ua + u;
         int lo = first ? 0 : a.num_groups, hi = (first ? a.num_groups : segs) - 1;
         while (lo < hi) {
             const int mid = (lo + hi + 1) >> 1;
-            if (unit_off[mid] <= at) lo = mid; else hi = mid - 1;
+            if (segments[mid].unit0 <= at) lo = mid; else hi = mid - 1;
         }
-        const int s = __builtin_amdgcn_readfirstlane(lo);
-        const Segment g = segment_of(a, x, s);
-        const int each = units_of(g);
-        const int64_t local = at - unit_off[s];
-        const int pair = (int)(local / each), tile = pair % g.tiles;
+        auto same = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
+        const Segment& g = segments[lo];
+        const int each = same(units_of(g)), tiles = same(g.tiles);
+        const int64_t local = at - g.unit0;
+        const int pair = same((int)quotient(local, each)), tile = pair % tiles;
         Piece p;
-        p.q0 = g.q0;
-        p.row0 = tile * g.tile;
-        p.rows = max(0, min(g.tile, g.rows - p.row0));
-        p.head = pair / g.tiles;
-        p.b_lo = g.b_lo;
-        p.b_hi = g.b_hi;
-        p.u0 = (int)(local - (int64_t)pair * each);
-        p.u1 = (int)min((int64_t)each, p.u0 + (u_end - u));
+        p.q0 = same(g.q0);
+        p.row0 = tile * same(g.tile);
+        p.rows = max(0, min(same(g.tile), same(g.rows) - p.row0));
+        p.head = pair / tiles;
+        p.b_lo = same(g.b_lo);
+        p.b_hi = same(g.b_hi);
+        p.u0 = same((int)(local - (int64_t)pair * each));
+        p.u1 = same((int)min((int64_t)each, p.u0 + (u_end - u)));
         u += p.u1 - p.u0;
-        p.S = g.S;
-        p.table = x.tables + (int64_t)g.table * a.max_blocks;
+        p.S = same(g.S);
+        p.table = x.tables + (int64_t)same(g.table) * a.max_blocks;
         p.prefix = first;
-        p.pos0 = g.S - g.n;
-        p.masked = first && masked[s];
+        p.pos0 = same(g.pos0);
+        p.masked = first && p.pos0;
         p.min_pos = first ? (p.masked ? -1 : INT32_MAX) : p.pos0 + p.row0 / a.group;
-        const int64_t slot = first ? pair_off[s] + pair + w : (int64_t)(pair_off[s] - h.pa) + pair + w;
+        const int64_t slot = same(g.pair0) - (first ? 0 : same(h.pa)) + pair + w;
         if (slot >= (first ? a.slots_a : a.slots_b) || p.rows == 0) continue;
         p.slot_row = first ? slot * a.tile_a : a.slots_a * a.tile_a + slot * a.tile_b;
         // keys that none of the tile's rows sees
@@ -723,25 +718,30 @@ __global__ __launch_bounds__(kThreads, 2) void shared_walk(SharedArgs a, Index x
             const int seen = p.pos0 + (p.row0 + p.rows - 1) / a.group + 1 - p.b_lo * kBlockTokens;
             p.u1 = max(p.u0, min(p.u1, (max(0, seen) + kUnitBlocks * kBlockTokens - 1) / (kUnitBlocks * kBlockTokens)));
         }
+        const int tiles16 = (p.rows + 15) / 16;
         if constexpr (sizeof(T) == 4) {
-            if (p.rows <= 16) walk_flat_f32<D, 1>(a, x, p, smem);
+            if (tiles16 == 1) walk_flat_f32<D, 1>(a, x, p, smem);
             else walk_flat_f32<D, 2>(a, x, p, smem);
         } else {
             constexpr int RT = tall_tiles(D), FT = flat_tiles(D, false);
-            if (p.rows <= 16) walk_flat<D, 1>(a, x, p, smem);
-            else if (p.rows <= 32) walk_flat<D, 2>(a, x, p, smem);
-            else if (p.rows <= 16 * FT) walk_flat<D, FT>(a, x, p, smem);
-            else if (p.rows <= 64 * RT / 2) walk_tall<D, RT / 2>(a, x, p, smem);
+            if (tiles16 == 1) walk_flat<D, 1>(a, x, p, smem);
+            else if (tiles16 == 2) walk_flat<D, 2>(a, x, p, smem);
+            else if (tiles16 <= FT) walk_flat<D, FT>(a, x, p, smem);
+            else if (tiles16 <= 4) walk_tall<D, 1>(a, x, p, smem);
+            else if (tiles16 <= 8) walk_tall<D, 2>(a, x, p, smem);
+            else if (RT > 2 && tiles16 <= 12) walk_tall<D, RT == 4 ? 3 : RT>(a, x, p, smem);
             else walk_tall<D, RT>(a, x, p, smem);
         }
     }
 }
 
-// A row's parts joined.  32 lanes (D = 64: 16) per (row, query head), a workgroup per
-// row and run of heads.
-template <typename T, int D>
+// A row's parts joined: kLanes lanes for the dims of a (row, query head), SPLIT groups of
+// them for its pieces, a workgroup per row and run of heads.
+template <typename T, int D, int SPLIT>
 __global__ __launch_bounds__(kThreads) void shared_join(SharedArgs a, Index x) {
-    constexpr int kLanes = D / 4, kHeads = kThreads / kLanes;
+    constexpr int kLanes = D / 4, kGroups = kThreads / kLanes, kHeads = kGroups / SPLIT, kBatch = 4;
+    __shared__ f32x4_t s_acc[SPLIT > 1 ? kThreads : 1];
+    __shared__ float2 s_ml[SPLIT > 1 ? kGroups : 1];
     const int row = blockIdx.x, tid = threadIdx.x;
     // the row's request: the last one that begins at or before it
     int before = 0;
@@ -752,39 +752,70 @@ __global__ __launch_bounds__(kThreads) void shared_join(SharedArgs a, Index x) {
         if (c < kThreads) break;
     }
     const int i = before - 1;
-    const int h = blockIdx.y * kHeads + tid / kLanes, d = tid % kLanes * 4;
-    if (h >= a.hq || i < 0 || row >= x.q_start[i + 1]) return;
-    const Share sh = divide_workgroups(a, a.unit_off, a.pair_off);
+    if (i < 0 || row >= x.q_start[i + 1]) return;
+    const int unit = tid / kLanes, part_of = unit % SPLIT, d = tid % kLanes * 4;
+    const int h = min((int)blockIdx.y * kHeads + unit / SPLIT, a.hq - 1);
     const int head = h / a.group;
-    const int k = group_of(a, x, i);
-    float top = kNoMax, sum = 0.f;
-    f32x4_t acc{0.f, 0.f, 0.f, 0.f};
-    auto part = [&](int s, bool first) {
-        const Segment g = segment_of(a, x, s);
-        const int each = units_of(g);
+    const Segment own = a.segments[a.num_groups + i];
+    const Share sh = divide_workgroups(a, a.segments);
+    const Segment common = a.segments[max(own.group, 0)];
+    // pieces of the two pairs, one after the other: piece e's row among the partial rows
+    int pieces[2] = {0, 0};
+    int64_t at[2] = {0, 0};
+    auto find = [&](const Segment& g, bool first) {
+        const int each = units_of(g), k = first ? 0 : 1;
         if (each == 0 || g.rows == 0) return;
         const int e = (row - g.q0) * a.group + h % a.group;
         const int tile = e / g.tile, pair = head * g.tiles + tile;
-        const int64_t units = first ? sh.ua : sh.ub, u0 = a.unit_off[s] - (first ? 0 : sh.ua) + (int64_t)pair * each;
+        const int64_t units = first ? sh.ua : sh.ub, u0 = g.unit0 - (first ? 0 : sh.ua) + (int64_t)pair * each;
         const int count = first ? sh.ca : sh.cb;
         // workgroup w owns units [units w / count, units (w + 1) / count)
-        const int w0 = (int)(((u0 + 1) * count - 1) / units), w1 = (int)(((u0 + each) * count - 1) / units);
-        const int64_t p = first ? a.pair_off[s] + pair : a.pair_off[s] - sh.pa + pair;
-        for (int w = w0; w <= w1; ++w) {
-            const int64_t slot = p + w;
-            if (slot >= (first ? a.slots_a : a.slots_b)) break;
-            const int64_t at = (first ? slot * a.tile_a : a.slots_a * a.tile_a + slot * a.tile_b) + e - tile * g.tile;
-            const float2 ml = a.part_ml[at];
-            const f32x4_t o = *reinterpret_cast<const f32x4_t*>(a.part_o + at * D + d);
+        const int w0 = (int)quotient((u0 + 1) * count - 1, units), w1 = (int)quotient((u0 + each) * count - 1, units);
+        const int64_t slot = g.pair0 - (first ? 0 : sh.pa) + pair + w0;
+        pieces[k] = (int)max((int64_t)0, min((int64_t)(w1 - w0 + 1), (first ? a.slots_a : a.slots_b) - slot));
+        at[k] = (first ? slot * a.tile_a : a.slots_a * a.tile_a + slot * a.tile_b) + e - tile * g.tile;
+    };
+    if (own.group >= 0) find(common, true);
+    find(own, false);
+    float top = kNoMax, sum = 0.f;
+    f32x4_t acc{0.f, 0.f, 0.f, 0.f};
+    const int all = pieces[0] + pieces[1];
+    for (int base = part_of; base < all; base += SPLIT * kBatch) {
+        float2 ml[kBatch];
+        f32x4_t o[kBatch];
+#pragma unroll
+        for (int z = 0; z < kBatch; ++z) {
+            const int e = min(base + z * SPLIT, all - 1), k = e < pieces[0] ? 0 : 1;
+            const int64_t r = at[k] + (int64_t)(k ? e - pieces[0] : e) * (k ? a.tile_b : a.tile_a);
+            ml[z] = a.part_ml[r];
+            o[z] = *reinterpret_cast<const f32x4_t*>(a.part_o + r * D + d);
+        }
+#pragma unroll
+        for (int z = 0; z < kBatch; ++z) {
+            if (base + z * SPLIT >= all) break;
+            const float next = fmaxf(top, ml[z].x);
+            const float f0 = exp2f(top - next), f1 = exp2f(ml[z].x - next);
+            top = next;
+            sum = fmaf(sum, f0, ml[z].y * f1);
+            acc = acc * f0 + o[z] * f1;
+        }
+    }
+    if constexpr (SPLIT > 1) {
+        s_acc[tid] = acc;
+        if (d == 0) s_ml[unit] = make_float2(top, sum);
+        __syncthreads();
+        if (part_of != 0) return;
+#pragma unroll
+        for (int z = 1; z < SPLIT; ++z) {
+            const float2 ml = s_ml[unit + z];
             const float next = fmaxf(top, ml.x);
             const float f0 = exp2f(top - next), f1 = exp2f(ml.x - next);
             top = next;
             sum = fmaf(sum, f0, ml.y * f1);
-            acc = acc * f0 + o * f1;
+            acc = acc * f0 + s_acc[tid + z * kLanes] * f1;
         }
-    };
-    if (k >= 0) part(k, true);
-    part(a.num_groups + i, false);
+    }
+    if ((int)blockIdx.y * kHeads + unit / SPLIT >= a.hq) return;
     // a sink adds to the sum alone; a row without keys is zero
     const float den = a.sinks ? sum + exp2f(fmaf(a.sinks[h], kLog2e, -top)) : sum;
     const f32x4_t y = sum == 0.f ? f32x4_t{0.f, 0.f, 0.f, 0.f} : acc / den;
@@ -798,7 +829,8 @@ __global__ __launch_bounds__(kThreads) void shared_join(SharedArgs a, Index x) {
 struct SharedPlan {
     int nwg, tile_a, tile_b;
     int64_t slots_a, slots_b, segs;
-    size_t o_bytes, ml_bytes, off_bytes, total;
+    int split;  // groups of threads that share a row's pieces in the pass that joins
+    size_t o_bytes, ml_bytes, total;
 };
 
 // Row tiles and partial results.  A tile holds at most the rows that its segment may
@@ -824,8 +856,8 @@ int plan_shared(const verify_attn_params* p, int32_t total_q, int32_t max_q_len,
     const int64_t part_rows = s.slots_a * s.tile_a + s.slots_b * s.tile_b;
     s.o_bytes = (size_t)part_rows * D * 4;
     s.ml_bytes = align_up((size_t)part_rows * 8, 16);
-    s.off_bytes = align_up((size_t)(s.segs + 1) * 8, 16) + 2 * align_up((size_t)(s.segs + 1) * 4, 16);
-    s.total = s.o_bytes + s.ml_bytes + s.off_bytes;
+    s.total = s.o_bytes + s.ml_bytes + (size_t)(s.segs + 1) * sizeof(Segment);
+    s.split = s.nwg >= 24 * pairs_a ? 8 : s.nwg >= 8 * pairs_a ? 4 : 1;
     return VERIFY_OK;
 }
 
@@ -848,15 +880,21 @@ bool is_plain(const verify_attn_params* p, int32_t num_groups, int32_t max_prefi
 }
 
 template <typename T, int D>
-void launch_shared(const SharedArgs& a, const Index& x, hipStream_t stream) {
+void launch_shared(const SharedArgs& a, const Index& x, int split, hipStream_t stream) {
     if (a.num_groups + a.num_seqs <= kInlineSegs) {
         hipLaunchKernelGGL((shared_walk<T, D, true>), dim3(a.nwg), dim3(kThreads), 0, stream, a, x);
     } else {
         hipLaunchKernelGGL(shared_schedule, dim3(1), dim3(1024), 0, stream, a, x);
         hipLaunchKernelGGL((shared_walk<T, D, false>), dim3(a.nwg), dim3(kThreads), 0, stream, a, x);
     }
-    constexpr int kHeads = kThreads / (D / 4);
-    hipLaunchKernelGGL((shared_join<T, D>), dim3(a.total_q, (a.hq + kHeads - 1) / kHeads), dim3(kThreads), 0, stream, a, x);
+    auto join = [&](auto n) {
+        constexpr int kHeads = kThreads / (D / 4) / decltype(n)::value;
+        hipLaunchKernelGGL((shared_join<T, D, decltype(n)::value>), dim3(a.total_q, (a.hq + kHeads - 1) / kHeads),
+                           dim3(kThreads), 0, stream, a, x);
+    };
+    if (split == 8) join(std::integral_constant<int, 8>{});
+    else if (split == 4) join(std::integral_constant<int, 4>{});
+    else join(std::integral_constant<int, 1>{});
 }
 
 }  // namespace
@@ -908,11 +946,7 @@ extern "C" int verify_attention_shared(const verify_attn_params* params, int32_t
     a.out = out;
     a.part_o = reinterpret_cast<float*>(ws);
     a.part_ml = reinterpret_cast<float2*>(ws + s.o_bytes);
-    ws += s.o_bytes + s.ml_bytes;
-    a.unit_off = reinterpret_cast<int64_t*>(ws);
-    ws += align_up((size_t)(s.segs + 1) * 8, 16);
-    a.pair_off = reinterpret_cast<int32_t*>(ws);
-    a.masked = reinterpret_cast<int32_t*>(ws + align_up((size_t)(s.segs + 1) * 4, 16));
+    a.segments = reinterpret_cast<Segment*>(ws + s.o_bytes + s.ml_bytes);
     a.num_seqs = params->num_seqs;
     a.num_groups = num_groups;
     a.hq = params->num_q_heads;
@@ -932,8 +966,10 @@ extern "C" int verify_attention_shared(const verify_attn_params* params, int32_t
     a.scale_log2 = scale * kLog2e;
     const Index x{block_tables, seq_lens, q_start, group_start, prefix_lens};
     if (params->dtype == VERIFY_BF16)
-        params->head_dim == 128 ? launch_shared<uint16_t, 128>(a, x, stream) : launch_shared<uint16_t, 64>(a, x, stream);
+        params->head_dim == 128 ? launch_shared<uint16_t, 128>(a, x, s.split, stream)
+                                : launch_shared<uint16_t, 64>(a, x, s.split, stream);
     else
-        params->head_dim == 128 ? launch_shared<float, 128>(a, x, stream) : launch_shared<float, 64>(a, x, stream);
+        params->head_dim == 128 ? launch_shared<float, 128>(a, x, s.split, stream)
+                                : launch_shared<float, 64>(a, x, s.split, stream);
     return check_launch();
 }
