@@ -44,15 +44,29 @@ constexpr int kWaves = 4;
 constexpr int kThreads = kWaves * kWave;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kUnitBlocks = 8;      // KV blocks of a unit
-constexpr int kInlineSegs = 255;    // segments whose units every workgroup counts itself
+// What a pair costs beside its blocks (its rows, the first blocks' latency, the join of
+// the wavefronts, the partial result), in units: it counts so many units more, without
+// blocks, in front of its own.
+constexpr int kPairUnits = 4;
+constexpr int kInlineSegs = 256;    // segments whose units every workgroup counts itself
 constexpr int kStages = 4;          // of the tall walk's ring
 constexpr float kNoMax = -3.0e38f;  // a maximum over no key
 // Softmax weights may exceed 1 by up to this factor (log2) before a row's maximum is
 // raised: with a maximum that need not be exact the raise is rare.
 constexpr float kSlackLog2 = 8.f;
-// 16-row tiles of a flat walk at most: those whose operands fit 256 registers
-constexpr int flat_tiles(int d, bool f32) { return !f32 && d == 64 ? 3 : 2; }
-constexpr int tall_tiles(int d) { return d == 64 ? 4 : 2; }  // per wavefront
+// 16-row tiles of a flat walk at most.  In bf16 two of them and the keys under way do not
+// fit 256 registers, and the ring serves 32 rows as well (5.1 TB/s; flat, with 16 rows, 5.8).
+constexpr int flat_tiles(bool f32) { return f32 ? 2 : 1; }
+constexpr int tall_tiles(int d) { return d == 64 ? 3 : 2; }  // per wavefront
+
+// The lane's number, of which the compiler does not know that it is the same in every
+// piece of a workgroup: what a walk derives from it is computed in that walk, instead of
+// taking registers from all others.
+__device__ __forceinline__ int own_lane() {
+    int lane = threadIdx.x % kWave;
+    asm volatile("" : "+v"(lane));
+    return lane;
+}
 
 typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
@@ -68,7 +82,8 @@ struct SharedArgs {
     void* out;
     float* part_o;    // [slots][tile rows][D]
     float2* part_ml;  // [slots][tile rows] maximum and sum
-    struct Segment* segments;  // [segments + 1], in memory for the pass that joins
+    struct Segment* segments;  // in memory for the pass that joins
+    struct Share* share;
     int num_seqs, num_groups, hq, hkv, group, max_blocks, num_blocks, max_seq_len, max_prefix, total_q;
     int nwg;
     int tile_a, tile_b;    // rows of a tile at most: prefix and own segments
@@ -85,11 +100,11 @@ struct Index {  // device arrays that nothing writes
 };
 
 struct __attribute__((aligned(16))) Segment {
-    int64_t unit0;   // number of its first unit; the last entry holds the counts of all
-    int pair0;       // and of its first pair
+    int64_t unit0;   // own: number of its first unit; prefix: of its first item.  The entry
+                     // behind the last prefix's and own one hold the numbers of all
+    int pair0;       // own: of its first pair; prefix: parts that each pair's keys are cut into
     int q0, rows;    // first packed row, packed rows times query heads per KV head
     int b_lo, b_hi;  // blocks
-    int tile, tiles; // rows of a tile, tiles
     int table;       // the request whose block table lists the blocks
     int S;           // keys from S on are not the request's
     int pos0;        // own: position of the first row; prefix: whether a row stands inside
@@ -142,24 +157,62 @@ __device__ __forceinline__ Segment segment_of(const SharedArgs& a, const Index& 
         g.table = i;
         g.pos0 = g.S - n;
     }
-    // rows divided evenly over as few tiles as there need be
-    const int most = first ? a.tile_a : a.tile_b;
-    g.tiles = (g.rows + most - 1) / most;
-    g.tile = g.tiles ? ((g.rows + g.tiles - 1) / g.tiles + 15) / 16 * 16 : 16;
     return g;
 }
 
-__device__ __forceinline__ int units_of(const Segment& g) { return (g.b_hi - g.b_lo + kUnitBlocks - 1) / kUnitBlocks; }
+// A segment's rows divided evenly over as few tiles of at most `most` rows as there need
+// be: their number, and the rows of one.
+__device__ __forceinline__ int tiles_of(const Segment& g, int most) { return (g.rows + most - 1) / most; }
+__device__ __forceinline__ int tile_rows(const Segment& g, int tiles) {
+    return tiles ? ((g.rows + tiles - 1) / tiles + 15) / 16 * 16 : 16;
+}
 
-// All segments, by one workgroup of THREADS threads, and behind them an entry with the
-// number of all units and pairs.
+__device__ __forceinline__ int units_of(const Segment& g) {
+    return g.b_hi > g.b_lo ? (g.b_hi - g.b_lo + kUnitBlocks - 1) / kUnitBlocks + kPairUnits : 0;
+}
+
+// v summed over all threads before this one, and over all (THREADS of them).
+template <int THREADS, typename V>
+__device__ __forceinline__ V scan_before(V v, V* s_wave, V& all) {
+    const int tid = threadIdx.x, lane = tid % kWave;
+    V x = v;
+    for (int o = 1; o < kWave; o <<= 1) {
+        const V y = __shfl_up(x, o);
+        if (lane >= o) x += y;
+    }
+    if (lane == kWave - 1) s_wave[tid / kWave] = x;
+    __syncthreads();
+    all = 0;
+    for (int w = 0; w < THREADS / kWave; ++w) {
+        if (w < tid / kWave) x += s_wave[w];
+        all += s_wave[w];
+    }
+    __syncthreads();
+    return x - v;
+}
+
+// How the workgroups are divided: na of them take the prefixes' items, the others the ub
+// own units.  Where there are fewer of these than workgroups, cb of them have one.
+struct __attribute__((aligned(16))) Share {
+    int64_t ub;
+    int items, na, cb;
+};
+
+// Cuts each prefix's pairs into parts of about `cost` units.
+__device__ __forceinline__ int parts_of(const Segment& g, int cost) {
+    return max(1, (units_of(g) - kPairUnits + cost - 1) / cost);
+}
+
+// All segments, by one workgroup of THREADS threads: the own ones' units and pairs are
+// counted, and the prefixes' pairs are cut into items.
 template <int THREADS>
-__device__ void count_units(const SharedArgs& a, const Index& x, Segment* segments) {
-    __shared__ int64_t s_units[THREADS / kWave];
-    __shared__ int s_pairs[THREADS / kWave];
-    const int tid = threadIdx.x, lane = tid % kWave, segs = a.num_groups + a.num_seqs;
-    int64_t units0 = 0;
-    int pairs0 = 0;
+__device__ void count_units(const SharedArgs& a, const Index& x, Segment* segments, Share* share) {
+    __shared__ int64_t s_long[THREADS / kWave];
+    __shared__ int s_int[THREADS / kWave];
+    __shared__ int64_t s_best;
+    const int tid = threadIdx.x, segs = a.num_groups + a.num_seqs;
+    int64_t prefix_units = 0, units = 0;
+    int pairs_all = 0;
     for (int base = 0; base < segs; base += THREADS) {
         const int s = base + tid;
         Segment g;
@@ -167,65 +220,87 @@ __device__ void count_units(const SharedArgs& a, const Index& x, Segment* segmen
         if (s < segs) {
             g = segment_of(a, x, s);
             each = units_of(g);
-            pairs = each > 0 ? g.tiles * a.hkv : 0;
+            pairs = each > 0 ? tiles_of(g, s < a.num_groups ? a.tile_a : a.tile_b) * a.hkv : 0;
         }
-        int64_t u = (int64_t)pairs * each;
-        int p = pairs;
-        const int64_t u_mine = u;
-        for (int o = 1; o < kWave; o <<= 1) {
-            const int64_t uo = __shfl_up(u, o);
-            const int po = __shfl_up(p, o);
-            if (lane >= o) u += uo, p += po;
-        }
-        if (lane == kWave - 1) s_units[tid / kWave] = u, s_pairs[tid / kWave] = p;
-        __syncthreads();
-        int64_t u_all = 0;
-        int p_all = 0;
-        for (int w = 0; w < THREADS / kWave; ++w) {
-            if (w < tid / kWave) u += s_units[w], p += s_pairs[w];
-            u_all += s_units[w];
-            p_all += s_pairs[w];
-        }
+        const bool own = s >= a.num_groups;
+        int64_t prefix_here, units_here;
+        int pairs_here;
+        scan_before<THREADS>((int64_t)(own ? 0 : pairs) * each, s_long, prefix_here);
+        const int64_t u = scan_before<THREADS>((int64_t)(own ? pairs : 0) * each, s_long, units_here);
+        const int p = scan_before<THREADS>(own ? pairs : 0, s_int, pairs_here);
         if (s < segs) {
-            g.unit0 = units0 + u - u_mine;
-            g.pair0 = pairs0 + p - pairs;
+            g.unit0 = units + u;
+            g.pair0 = own ? pairs_all + p : pairs;
             segments[s] = g;
         }
-        units0 += u_all;
-        pairs0 += p_all;
-        __syncthreads();
+        prefix_units += prefix_here;
+        units += units_here;
+        pairs_all += pairs_here;
     }
+    if (tid == 0) {
+        Share h;
+        h.ub = units;
+        if (prefix_units == 0) h.na = 0;
+        else if (units == 0) h.na = a.nwg;
+        else h.na = clamp_to((int)((double)prefix_units / (double)(prefix_units + units) * a.nwg / 8 + 0.5) * 8, 8, a.nwg - 8);
+        h.cb = (int)min((int64_t)(a.nwg - h.na), units);
+        h.items = 0;
+        *share = h;
+        s_best = INT64_MAX;
+    }
+    __syncthreads();
+    if (prefix_units > 0) {
+        // The parts' length with which the last of the na workgroups is done first, each
+        // taking its share of the items one after the other: candidates between a fourth
+        // of the mean share and four times it, 16 lanes to each.
+        constexpr int kLanes = 16, kCandidates = THREADS / kLanes;
+        const int64_t na = share->na;
+        const float mean = fmaxf(1.f, (float)prefix_units / (float)na);
+        auto length = [&](int c) { return (int)fminf(1.0e9f, ceilf(mean * 0.25f * exp2f(4.f / (kCandidates - 1) * c))); };
+        const int c = tid / kLanes, cost = length(c);
+        int64_t items = 0;
+        int longest = 0;
+        for (int k = tid % kLanes; k < a.num_groups; k += kLanes) {
+            const Segment& g = segments[k];
+            if (g.pair0 == 0) continue;
+            const int parts = parts_of(g, cost), u = units_of(g) - kPairUnits;
+            items += (int64_t)g.pair0 * parts;
+            longest = max(longest, (u + parts - 1) / parts);
+        }
+        for (int o = 1; o < kLanes; o <<= 1) {
+            items += __shfl_xor(items, o);
+            longest = max(longest, __shfl_xor(longest, o));
+        }
+        const bool fits = items <= a.slots_a;
+        const int64_t time = min((int64_t)1 << 40, ((items + na - 1) / na) * (longest + kPairUnits));
+        // the longest parts of equal candidates
+        if (tid % kLanes == 0 && fits) atomicMin((unsigned long long*)&s_best, (unsigned long long)(time << 8 | (kCandidates - 1 - c)));
+        __syncthreads();
+        // whole prefixes always fit
+        const int chosen = s_best == INT64_MAX ? INT32_MAX / 2 : length(kCandidates - 1 - (int)(s_best & 0xff));
+        int64_t before = 0;
+        for (int base = 0; base < a.num_groups; base += THREADS) {
+            const int k = base + tid;
+            const int pairs = k < a.num_groups ? segments[k].pair0 : 0;
+            const int parts = pairs ? parts_of(segments[k], chosen) : 0;
+            int64_t here;
+            const int64_t i0 = before + scan_before<THREADS>((int64_t)pairs * parts, s_long, here);
+            if (k < a.num_groups) segments[k].unit0 = i0, segments[k].pair0 = parts;
+            before += here;
+        }
+        if (tid == 0) share->items = (int)before;
+    }
+    __syncthreads();
     // a row that stands in front of its prefix's last key sees a part of it
     for (int i = tid; i < a.num_seqs; i += THREADS) {
         const Segment& g = segments[a.num_groups + i];
         if (g.group >= 0 && g.rows > 0 && g.pos0 < g.b_lo * kBlockTokens - 1) segments[g.group].pos0 = 1;
     }
-    if (tid == 0) segments[segs].unit0 = units0, segments[segs].pair0 = pairs0;
     __syncthreads();
 }
 
-__global__ __launch_bounds__(1024) void shared_schedule(SharedArgs a, Index x) { count_units<1024>(a, x, a.segments); }
-
-// How the workgroups are divided: na of them take the prefixes' ua units, the others the
-// ub own ones.  Where there are fewer units than workgroups, ca and cb of them have one.
-struct Share {
-    int64_t ua, ub;
-    int na, ca, cb, pa;
-};
-
-// A unit of a prefix costs about what an own one does: the one fills the matrix units
-// for 128 rows, the other waits for 64 KiB.
-__device__ __forceinline__ Share divide_workgroups(const SharedArgs& a, const Segment* segments) {
-    Share h;
-    h.ua = segments[a.num_groups].unit0;
-    h.ub = segments[a.num_groups + a.num_seqs].unit0 - h.ua;
-    h.pa = segments[a.num_groups].pair0;
-    if (h.ua == 0) h.na = 0;
-    else if (h.ub == 0) h.na = a.nwg;
-    else h.na = clamp_to((int)((double)h.ua / (double)(h.ua + h.ub) * a.nwg / 8 + 0.5) * 8, 8, a.nwg - 8);
-    h.ca = (int)min((int64_t)h.na, h.ua);
-    h.cb = (int)min((int64_t)(a.nwg - h.na), h.ub);
-    return h;
+__global__ __launch_bounds__(1024) void shared_schedule(SharedArgs a, Index x) {
+    count_units<1024>(a, x, a.segments, a.share);
 }
 
 // a / b rounded down, 0 <= a < 2^52: a quotient in binary64 is not rounded up to the next
@@ -280,19 +355,36 @@ __device__ __forceinline__ float rows_sum(float v) {
     return __uint_as_float(t[0]) + __uint_as_float(t[1]);
 }
 
-// Raises the row's maximum where one of its scores exceeds it by more than the slack,
-// and rescales what has been summed.
-template <int DT>
-__device__ __forceinline__ void raise(float top, float scale, float& m, float& l, f32x4_t* o) {
-    const float mine = top * scale;
-    if (__any(mine > m + kSlackLog2)) {
-        const float next = fmaxf(m, rows_max(mine));
-        const float f = __builtin_amdgcn_exp2f(m - next);
+// The scores of a lane's N keys of one row become weights 2^(scale s - m), whose sum joins
+// l.  Where a weight would exceed the slack the maximum is raised first, and what has
+// been summed is rescaled.
+template <int N, int DT>
+__device__ __forceinline__ void weigh(float* s, float scale, float& m, float& l, f32x4_t* o) {
+    float t[N];
+#pragma unroll
+    for (int e = 0; e < N; ++e) t[e] = fmaf(s[e], scale, -m);
+    float top = t[0];
+#pragma unroll
+    for (int e = 1; e < N; ++e) top = fmaxf(top, t[e]);
+    if (__any(top > kSlackLog2)) {
+        float high = s[0];
+#pragma unroll
+        for (int e = 1; e < N; ++e) high = fmaxf(high, s[e]);
+        const float next = fmaxf(m, rows_max(high * scale)), f = __builtin_amdgcn_exp2f(m - next);
         m = next;
         l *= f;
 #pragma unroll
-        for (int t = 0; t < DT; ++t) o[t] *= f;
+        for (int d = 0; d < DT; ++d) o[d] *= f;
+#pragma unroll
+        for (int e = 0; e < N; ++e) t[e] = fmaf(s[e], scale, -m);
     }
+    float sum = 0.f;
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+        s[e] = __builtin_amdgcn_exp2f(t[e]);
+        sum += s[e];
+    }
+    l += sum;
 }
 
 // V^T of keys from `left` on (of the lane's eight) becomes zero: what a slot behind the
@@ -306,12 +398,12 @@ __device__ __forceinline__ uint4 first_keys(uint4 v, int left) {
 __device__ __forceinline__ bf16x8_t as_bf16x8(const uint4& v) { return __builtin_bit_cast(bf16x8_t, v); }
 
 // One step of 32 keys from block b0 on for RT row tiles.  load_k(t, c) and load_v(dt)
-// give the operands; ok: whether the block of the lane's keys is mapped.
-template <int D, int RT, typename LoadK, typename AfterK, typename LoadV>
-__device__ __forceinline__ void step32(const Piece& p, int b0, bool edge, bool ok, float scale, const bf16x8_t (*q)[D / 32],
+// give the operands; EDGE: some row does not see some key, or a block is not mapped
+// (ok: whether the lane's keys' is).
+template <int D, int RT, bool EDGE, typename LoadK, typename AfterK, typename LoadV>
+__device__ __forceinline__ void step32(const Piece& p, int lg, int b0, bool ok, float scale, const bf16x8_t (*q)[D / 32],
                                        const int* pos, float* m, float* l, f32x4_t (*o)[D / 16], LoadK load_k,
                                        AfterK after_k, LoadV load_v) {
-    const int lg = (threadIdx.x % kWave) / 16;
     f32x4_t s[RT][2];
 #pragma unroll
     for (int r = 0; r < RT; ++r) s[r][0] = s[r][1] = f32x4_t{0.f, 0.f, 0.f, 0.f};
@@ -328,28 +420,20 @@ __device__ __forceinline__ void step32(const Piece& p, int b0, bool edge, bool o
     bf16x8_t w[RT];
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
-        if (edge) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-                if (!ok || key0 + e > pos[r]) s[r][e / 4][e % 4] = -INFINITY;
-        }
-        const float top = fmaxf(fmaxf(fmaxf(s[r][0][0], s[r][0][1]), fmaxf(s[r][0][2], s[r][0][3])),
-                                fmaxf(fmaxf(s[r][1][0], s[r][1][1]), fmaxf(s[r][1][2], s[r][1][3])));
-        raise<D / 16>(top, scale, m[r], l[r], o[r]);
-        float e8[8], sum = 0.f;
+        float e8[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            e8[e] = __builtin_amdgcn_exp2f(fmaf(s[r][e / 4][e % 4], scale, -m[r]));
-            sum += e8[e];
+            e8[e] = s[r][e / 4][e % 4];
+            if (EDGE && (!ok || key0 + e > pos[r])) e8[e] = -INFINITY;
         }
-        l[r] += sum;
+        weigh<8, D / 16>(e8, scale, m[r], l[r], o[r]);
         w[r] = as_bf16x8(make_uint4(pack_bf16x2(e8[0], e8[1]), pack_bf16x2(e8[2], e8[3]), pack_bf16x2(e8[4], e8[5]),
                                     pack_bf16x2(e8[6], e8[7])));
     }
 #pragma unroll
     for (int t = 0; t < D / 16; ++t) {
         uint4 v = load_v(t);
-        if (edge) v = first_keys(v, ok ? p.S - key0 : 0);
+        if (EDGE) v = first_keys(v, ok ? p.S - key0 : 0);
 #pragma unroll
         for (int r = 0; r < RT; ++r) o[r][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(v), w[r], o[r][t], 0, 0, 0);
     }
@@ -357,8 +441,7 @@ __device__ __forceinline__ void step32(const Piece& p, int b0, bool edge, bool o
 
 // Row r's dims 16 t + 4 lg .. + 3 of the partial result, and its maximum and sum.
 template <int D>
-__device__ __forceinline__ void store_partial(const SharedArgs& a, const Piece& p, int r, int t, const f32x4_t& v) {
-    const int lg = (threadIdx.x % kWave) / 16;
+__device__ __forceinline__ void store_partial(const SharedArgs& a, const Piece& p, int lg, int r, int t, const f32x4_t& v) {
     if (r < p.rows) *reinterpret_cast<f32x4_t*>(a.part_o + (p.slot_row + r) * D + 16 * t + 4 * lg) = v;
 }
 
@@ -368,7 +451,7 @@ __device__ __forceinline__ void join_waves(const SharedArgs& a, const Piece& p, 
                                            uint8_t* smem) {
     constexpr int DT = D / 16;
     __shared__ float s_ml[2][kWaves][16];
-    const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave, l16 = lane % 16;
+    const int wave = threadIdx.x / kWave, lane = own_lane(), l16 = lane % 16;
     f32x4_t* part = reinterpret_cast<f32x4_t*>(smem);
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
@@ -391,7 +474,7 @@ __device__ __forceinline__ void join_waves(const SharedArgs& a, const Piece& p, 
             f32x4_t v = part[t * kWave + lane] * f[0];
 #pragma unroll
             for (int w = 1; w < kWaves; ++w) v += part[(w * DT + t) * kWave + lane] * f[w];
-            store_partial<D>(a, p, r * 16 + l16, t, v);
+            store_partial<D>(a, p, lane / 16, r * 16 + l16, t, v);
         }
         if (threadIdx.x < 16 && r * 16 + l16 < p.rows) a.part_ml[p.slot_row + r * 16 + l16] = make_float2(top, all);
         __syncthreads();
@@ -399,10 +482,10 @@ __device__ __forceinline__ void join_waves(const SharedArgs& a, const Piece& p, 
 }
 
 // Few rows, bf16.
-template <int D, int RT>
+template <int D>
 __device__ void walk_flat(const SharedArgs& a, const Index& x, const Piece& p, uint8_t* smem) {
-    constexpr int DT = D / 16, C = D / 32;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave, l16 = lane % 16,
+    constexpr int RT = 1, DT = D / 16, C = D / 32;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = own_lane(), l16 = lane % 16,
               lg = lane / 16;
     bf16x8_t q[RT][C];
     f32x4_t o[RT][DT];
@@ -457,8 +540,13 @@ __device__ void walk_flat(const SharedArgs& a, const Index& x, const Piece& p, u
         if (id0 >= 0 || id1 >= 0) {
             const bool edge = (b0 + 2) * kBlockTokens - 1 > p.min_pos || id0 < 0 || id1 < 0;
             const bool ok = (lg >> 1 ? id1 : id0) >= 0;
-            step32<D, RT>(p, b0, edge, ok, a.scale_log2, q, pos, m, l, o, [&](int t, int c) { return as_bf16x8(k[t][c]); },
-                          [&]() { if (more) load_k(next0, next1); }, [&](int t) { return v[t]; });
+            auto step = [&](auto is_edge) {
+                step32<D, RT, decltype(is_edge)::value>(
+                    p, lg, b0, ok, a.scale_log2, q, pos, m, l, o, [&](int t, int c) { return as_bf16x8(k[t][c]); },
+                    [&]() { if (more) load_k(next0, next1); }, [&](int t) { return v[t]; });
+            };
+            if (edge) step(std::true_type{});
+            else step(std::false_type{});
         } else if (more) {
             load_k(next0, next1);
         }
@@ -475,7 +563,7 @@ __device__ void walk_flat(const SharedArgs& a, const Index& x, const Piece& p, u
 template <int D, int RT>
 __device__ void walk_flat_f32(const SharedArgs& a, const Index& x, const Piece& p, uint8_t* smem) {
     constexpr int DT = D / 16, C = D / 16;
-    const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave, l16 = lane % 16, lg = lane / 16;
+    const int wave = threadIdx.x / kWave, lane = own_lane(), l16 = lane % 16, lg = lane / 16;
     f32x4_t q[RT][C], o[RT][DT];
     float m[RT], l[RT];
     int pos[RT];
@@ -542,12 +630,9 @@ __device__ void walk_flat_f32(const SharedArgs& a, const Index& x, const Piece& 
                     for (int i = 0; i < 4; ++i)
                         if (key0 + i > pos[r]) s[r][i] = -INFINITY;
                 }
-                raise<DT>(fmaxf(fmaxf(s[r][0], s[r][1]), fmaxf(s[r][2], s[r][3])), a.scale_log2, m[r], l[r], o[r]);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    s[r][i] = exp2f(fmaf(s[r][i], a.scale_log2, -m[r]));
-                    l[r] += s[r][i];
-                }
+                float w[4] = {s[r][0], s[r][1], s[r][2], s[r][3]};
+                weigh<4, DT>(w, a.scale_log2, m[r], l[r], o[r]);
+                s[r] = f32x4_t{w[0], w[1], w[2], w[3]};
             }
 #pragma unroll
             for (int t = 0; t < DT; ++t) {
@@ -578,7 +663,7 @@ __device__ void walk_tall(const SharedArgs& a, const Index& x, const Piece& p, u
     constexpr int DT = D / 16, C = D / 32;
     constexpr int kTile = D * kBlockTokens * 2;  // bytes of a block's keys of one head
     constexpr int kStage = 4 * kTile, kRun = kTile / 1024;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave, l16 = lane % 16,
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = own_lane(), l16 = lane % 16,
               lg = lane / 16;
     bf16x8_t q[RT][C];
     f32x4_t o[RT][DT];
@@ -639,16 +724,21 @@ __device__ void walk_tall(const SharedArgs& a, const Index& x, const Piece& p, u
         const int id0 = id_of(2 * e), id1 = id_of(2 * e + 1);
         const bool edge = (b0 + 2) * kBlockTokens - 1 > p.min_pos || id0 < 0 || id1 < 0;
         const bool ok = (lg >> 1 ? id1 : id0) >= 0;
-        step32<D, RT>(p, b0, edge, ok, a.scale_log2, q, pos, m, l, o,
-                      [&](int t, int c) { return as_bf16x8(ld16(stage + k_at + c * 1024 + t * 64)); }, []() {},
-                      [&](int t) { return ld16(stage + v_at + t * 512); });
+        auto step = [&](auto is_edge) {
+            step32<D, RT, decltype(is_edge)::value>(
+                p, lg, b0, ok, a.scale_log2, q, pos, m, l, o,
+                [&](int t, int c) { return as_bf16x8(ld16(stage + k_at + c * 1024 + t * 64)); }, []() {},
+                [&](int t) { return ld16(stage + v_at + t * 512); });
+        };
+        if (edge) step(std::true_type{});
+        else step(std::false_type{});
     }
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
         const int row_at = (r * kWaves + wave) * 16 + l16;
         const float sum = rows_sum(l[r]);
 #pragma unroll
-        for (int t = 0; t < DT; ++t) store_partial<D>(a, p, row_at, t, o[r][t]);
+        for (int t = 0; t < DT; ++t) store_partial<D>(a, p, lg, row_at, t, o[r][t]);
         if (lg == 0 && row_at < p.rows) a.part_ml[p.slot_row + row_at] = make_float2(m[r], sum);
     }
     __syncthreads();  // the ring is free
@@ -664,53 +754,79 @@ constexpr int smem_bytes() {
 template <typename T, int D, bool INLINE>
 __global__ __launch_bounds__(kThreads, 2) void shared_walk(SharedArgs a, Index x) {
     __shared__ __attribute__((aligned(16))) uint8_t smem[smem_bytes<T, D>()];
-    __shared__ Segment s_segments[INLINE ? kInlineSegs + 1 : 1];
+    __shared__ Segment s_segments[INLINE ? kInlineSegs : 1];
+    __shared__ Share s_share;
     const Segment* segments = INLINE ? s_segments : a.segments;
     const int segs = a.num_groups + a.num_seqs;
     if constexpr (INLINE) {
-        count_units<kThreads>(a, x, s_segments);
-        if (blockIdx.x == 0)  // for the pass that joins
-            for (int s = threadIdx.x; s <= segs; s += kThreads) a.segments[s] = s_segments[s];
+        count_units<kThreads>(a, x, s_segments, &s_share);
+        if (blockIdx.x == 0) {  // for the pass that joins
+            for (int s = threadIdx.x; s < segs; s += kThreads) a.segments[s] = s_segments[s];
+            if (threadIdx.x == 0) *a.share = s_share;
+        }
     }
-    const Share h = divide_workgroups(a, segments);
-    const bool first = (int)blockIdx.x < h.na;
-    // workgroups go round the eight XCDs: each takes a run of a prefix's units, whose
-    // heads then stay in few of the L2 caches
-    const int b = blockIdx.x, w = !first ? b - h.na : h.ca == h.na ? b % 8 * (h.na / 8) + b / 8 : b;
-    const int64_t units = first ? h.ua : h.ub;
-    const int count = first ? h.ca : h.cb;
-    if (w >= count) return;
-    int64_t u = quotient(units * w, count);
-    const int64_t u_end = quotient(units * (w + 1), count);
-    while (u < u_end) {
-        const int64_t at = first ? u : h.ua + u;
+    const Share h = INLINE ? s_share : *a.share;
+    auto same = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
+    const int na = same(h.na), b = blockIdx.x;
+    const bool first = b < na;
+    // Workgroups go round the eight XCDs.  Each XCD takes a run of the items, its workgroups
+    // one after the other: the tiles of one part of the keys follow each other, so that
+    // they are walked at the same time and the keys come out of the XCD's L2.
+    const int xcd = b % 8, step = first ? na / 8 : 0;
+    int item = first ? (int)((int64_t)same(h.items) * xcd / 8) + b / 8 : 0;
+    const int items = first ? (int)((int64_t)same(h.items) * (xcd + 1) / 8) : 0;
+    const int w = b - na, count = same(h.cb);
+    int64_t u = 0, u_end = 0;
+    if (!first) {
+        if (w >= count) return;
+        u = quotient(h.ub * w, count);
+        u_end = quotient(h.ub * (w + 1), count);
+    }
+    while (first ? item < items : u < u_end) {
+        const int64_t at = first ? item : u;
         int lo = first ? 0 : a.num_groups, hi = (first ? a.num_groups : segs) - 1;
         while (lo < hi) {
             const int mid = (lo + hi + 1) >> 1;
             if (segments[mid].unit0 <= at) lo = mid; else hi = mid - 1;
         }
-        auto same = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
         const Segment& g = segments[lo];
-        const int each = same(units_of(g)), tiles = same(g.tiles);
+        const int each = same(units_of(g)), tiles = same(tiles_of(g, first ? a.tile_a : a.tile_b));
         const int64_t local = at - g.unit0;
-        const int pair = same((int)quotient(local, each)), tile = pair % tiles;
+        int tile;
+        int64_t slot;
         Piece p;
+        if (first) {
+            // item = (head * parts + part) * tiles + tile
+            const int parts = same(g.pair0), e = same((int)local), part = e / tiles % parts, real = each - kPairUnits;
+            tile = e % tiles;
+            p.head = e / tiles / parts;
+            p.u0 = (int)((int64_t)real * part / parts);
+            p.u1 = (int)((int64_t)real * (part + 1) / parts);
+            slot = item;
+            item += step;
+        } else {
+            const int pair = same((int)quotient(local, each));
+            tile = pair % tiles;
+            p.head = pair / tiles;
+            const int from = same((int)(local - (int64_t)pair * each)), to = same((int)min((int64_t)each, from + (u_end - u)));
+            u += to - from;
+            p.u0 = max(0, from - kPairUnits);
+            p.u1 = to - kPairUnits;
+            if (p.u1 <= 0) continue;
+            slot = same(g.pair0) + pair + w;
+        }
+        const int tile_height = same(tile_rows(g, tiles));
         p.q0 = same(g.q0);
-        p.row0 = tile * same(g.tile);
-        p.rows = max(0, min(same(g.tile), same(g.rows) - p.row0));
-        p.head = pair / tiles;
+        p.row0 = tile * tile_height;
+        p.rows = max(0, min(tile_height, same(g.rows) - p.row0));
         p.b_lo = same(g.b_lo);
         p.b_hi = same(g.b_hi);
-        p.u0 = same((int)(local - (int64_t)pair * each));
-        p.u1 = same((int)min((int64_t)each, p.u0 + (u_end - u)));
-        u += p.u1 - p.u0;
         p.S = same(g.S);
         p.table = x.tables + (int64_t)same(g.table) * a.max_blocks;
         p.prefix = first;
         p.pos0 = same(g.pos0);
         p.masked = first && p.pos0;
         p.min_pos = first ? (p.masked ? -1 : INT32_MAX) : p.pos0 + p.row0 / a.group;
-        const int64_t slot = same(g.pair0) - (first ? 0 : same(h.pa)) + pair + w;
         if (slot >= (first ? a.slots_a : a.slots_b) || p.rows == 0) continue;
         p.slot_row = first ? slot * a.tile_a : a.slots_a * a.tile_a + slot * a.tile_b;
         // keys that none of the tile's rows sees
@@ -723,13 +839,10 @@ __global__ __launch_bounds__(kThreads, 2) void shared_walk(SharedArgs a, Index x
             if (tiles16 == 1) walk_flat_f32<D, 1>(a, x, p, smem);
             else walk_flat_f32<D, 2>(a, x, p, smem);
         } else {
-            constexpr int RT = tall_tiles(D), FT = flat_tiles(D, false);
-            if (tiles16 == 1) walk_flat<D, 1>(a, x, p, smem);
-            else if (tiles16 == 2) walk_flat<D, 2>(a, x, p, smem);
-            else if (tiles16 <= FT) walk_flat<D, FT>(a, x, p, smem);
+            constexpr int RT = tall_tiles(D);
+            if (tiles16 == 1) walk_flat<D>(a, x, p, smem);
             else if (tiles16 <= 4) walk_tall<D, 1>(a, x, p, smem);
             else if (tiles16 <= 8) walk_tall<D, 2>(a, x, p, smem);
-            else if (RT > 2 && tiles16 <= 12) walk_tall<D, RT == 4 ? 3 : RT>(a, x, p, smem);
             else walk_tall<D, RT>(a, x, p, smem);
         }
     }
@@ -757,23 +870,32 @@ __global__ __launch_bounds__(kThreads) void shared_join(SharedArgs a, Index x) {
     const int h = min((int)blockIdx.y * kHeads + unit / SPLIT, a.hq - 1);
     const int head = h / a.group;
     const Segment own = a.segments[a.num_groups + i];
-    const Share sh = divide_workgroups(a, a.segments);
+    const Share sh = *a.share;
     const Segment common = a.segments[max(own.group, 0)];
-    // pieces of the two pairs, one after the other: piece e's row among the partial rows
+    // pieces of the two pairs, one after the other: the first one's row among the partial
+    // rows, and the distance to the next one's
     int pieces[2] = {0, 0};
-    int64_t at[2] = {0, 0};
+    int64_t at[2] = {0, 0}, next_at[2] = {0, a.tile_b};
     auto find = [&](const Segment& g, bool first) {
-        const int each = units_of(g), k = first ? 0 : 1;
+        const int each = units_of(g);
         if (each == 0 || g.rows == 0) return;
         const int e = (row - g.q0) * a.group + h % a.group;
-        const int tile = e / g.tile, pair = head * g.tiles + tile;
-        const int64_t units = first ? sh.ua : sh.ub, u0 = g.unit0 - (first ? 0 : sh.ua) + (int64_t)pair * each;
-        const int count = first ? sh.ca : sh.cb;
-        // workgroup w owns units [units w / count, units (w + 1) / count)
-        const int w0 = (int)quotient((u0 + 1) * count - 1, units), w1 = (int)quotient((u0 + each) * count - 1, units);
-        const int64_t slot = g.pair0 - (first ? 0 : sh.pa) + pair + w0;
-        pieces[k] = (int)max((int64_t)0, min((int64_t)(w1 - w0 + 1), (first ? a.slots_a : a.slots_b) - slot));
-        at[k] = (first ? slot * a.tile_a : a.slots_a * a.tile_a + slot * a.tile_b) + e - tile * g.tile;
+        const int tiles = tiles_of(g, first ? a.tile_a : a.tile_b), height = tile_rows(g, tiles);
+        const int tile = e / height;
+        if (first) {
+            const int64_t slot = g.unit0 + (int64_t)head * g.pair0 * tiles + tile;
+            pieces[0] = slot + (int64_t)(g.pair0 - 1) * tiles < a.slots_a ? g.pair0 : 0;
+            at[0] = slot * a.tile_a + e - tile * height;
+            next_at[0] = (int64_t)tiles * a.tile_a;
+        } else {
+            const int pair = head * tiles + tile;
+            const int64_t u0 = g.unit0 + (int64_t)pair * each;
+            // workgroup w owns units [ub w / cb, ub (w + 1) / cb)
+            const int w0 = (int)quotient((u0 + kPairUnits + 1) * sh.cb - 1, sh.ub), w1 = (int)quotient((u0 + each) * sh.cb - 1, sh.ub);
+            const int64_t slot = g.pair0 + pair + w0;
+            pieces[1] = (int)max((int64_t)0, min((int64_t)(w1 - w0 + 1), a.slots_b - slot));
+            at[1] = a.slots_a * a.tile_a + slot * a.tile_b + e - tile * height;
+        }
     };
     if (own.group >= 0) find(common, true);
     find(own, false);
@@ -786,7 +908,7 @@ __global__ __launch_bounds__(kThreads) void shared_join(SharedArgs a, Index x) {
 #pragma unroll
         for (int z = 0; z < kBatch; ++z) {
             const int e = min(base + z * SPLIT, all - 1), k = e < pieces[0] ? 0 : 1;
-            const int64_t r = at[k] + (int64_t)(k ? e - pieces[0] : e) * (k ? a.tile_b : a.tile_a);
+            const int64_t r = at[k] + (k ? e - pieces[0] : e) * next_at[k];
             ml[z] = a.part_ml[r];
             o[z] = *reinterpret_cast<const f32x4_t*>(a.part_o + r * D + d);
         }
@@ -839,7 +961,7 @@ int plan_shared(const verify_attn_params* p, int32_t total_q, int32_t max_q_len,
     const int group = p->num_q_heads / p->num_kv_heads, D = p->head_dim;
     const bool f32 = p->dtype == VERIFY_F32;
     auto tile = [&](int64_t rows) {
-        const int flat = 16 * flat_tiles(D, f32);
+        const int flat = 16 * flat_tiles(f32);
         const int need = (int)std::max<int64_t>(16, (std::min<int64_t>(rows, flat) + 15) / 16 * 16);
         return f32 || rows <= flat ? need : 64 * tall_tiles(D);
     };
@@ -850,13 +972,13 @@ int plan_shared(const verify_attn_params* p, int32_t total_q, int32_t max_q_len,
     const int64_t pairs_a = (rows / s.tile_a + num_groups) * p->num_kv_heads;
     const int64_t pairs_b = (rows / s.tile_b + p->num_seqs) * p->num_kv_heads;
     if (pairs_a + pairs_b >= (1 << 30)) return VERIFY_EUNSUPPORTED;
-    s.slots_a = pairs_a + s.nwg;
+    s.slots_a = pairs_a + 4 * s.nwg;
     s.slots_b = pairs_b + s.nwg;
     s.segs = (int64_t)num_groups + p->num_seqs;
     const int64_t part_rows = s.slots_a * s.tile_a + s.slots_b * s.tile_b;
     s.o_bytes = (size_t)part_rows * D * 4;
     s.ml_bytes = align_up((size_t)part_rows * 8, 16);
-    s.total = s.o_bytes + s.ml_bytes + (size_t)(s.segs + 1) * sizeof(Segment);
+    s.total = s.o_bytes + s.ml_bytes + sizeof(Share) + (size_t)s.segs * sizeof(Segment);
     s.split = s.nwg >= 24 * pairs_a ? 8 : s.nwg >= 8 * pairs_a ? 4 : 1;
     return VERIFY_OK;
 }
@@ -896,6 +1018,10 @@ void launch_shared(const SharedArgs& a, const Index& x, int split, hipStream_t s
     else if (split == 4) join(std::integral_constant<int, 4>{});
     else join(std::integral_constant<int, 1>{});
 }
+
+// two workgroups per compute unit
+static_assert(sizeof(Segment) == 48 && smem_bytes<uint16_t, 128>() + 48 * kInlineSegs + 1024 <= 80 * 1024 &&
+              sizeof(Share) % 8 == 0, "LDS and workspace");
 
 }  // namespace
 }  // namespace averify
@@ -946,7 +1072,8 @@ extern "C" int verify_attention_shared(const verify_attn_params* params, int32_t
     a.out = out;
     a.part_o = reinterpret_cast<float*>(ws);
     a.part_ml = reinterpret_cast<float2*>(ws + s.o_bytes);
-    a.segments = reinterpret_cast<Segment*>(ws + s.o_bytes + s.ml_bytes);
+    a.share = reinterpret_cast<Share*>(ws + s.o_bytes + s.ml_bytes);
+    a.segments = reinterpret_cast<Segment*>(a.share + 1);
     a.num_seqs = params->num_seqs;
     a.num_groups = num_groups;
     a.hq = params->num_q_heads;
