@@ -47,7 +47,7 @@ constexpr int kUnitBlocks = 8;      // KV blocks of a unit
 // What a pair costs beside its blocks (its rows, the first blocks' latency, the join of
 // the wavefronts, the partial result), in units: it counts so many units more, without
 // blocks, in front of its own.
-constexpr int kPairUnits = 4;
+constexpr int kPairUnits = 1;
 constexpr int kInlineSegs = 256;    // segments whose units every workgroup counts itself
 constexpr int kStages = 4;          // of the tall walk's ring
 constexpr float kNoMax = -3.0e38f;  // a maximum over no key
@@ -657,7 +657,8 @@ __device__ void walk_flat_f32(const SharedArgs& a, const Index& x, const Piece& 
 }
 
 // Many rows, bf16: wavefront w has the rows' tiles w, w + 4, ...; the ring's stages hold two
-// blocks each, K and then V.
+// blocks each, K and then V.  While a step's scores become weights on the vector units,
+// the next step's are on the matrix units, so that a wavefront keeps both at work.
 template <int D, int RT>
 __device__ void walk_tall(const SharedArgs& a, const Index& x, const Piece& p, uint8_t* smem) {
     constexpr int DT = D / 16, C = D / 32;
@@ -703,35 +704,115 @@ __device__ void walk_tall(const SharedArgs& a, const Index& x, const Piece& p, u
         const uint8_t* from = (wave < 2 ? a.kc : a.vc) + ((int64_t)id * a.hkv + p.head) * kTile;
         dma16_run<kRun>(ring + (e % kStages) * kStage + wave * kTile, from, lane * 16);
     };
+    const int k_at = (l16 >> 3) * kTile + (l16 & 3) * 16 + ((l16 >> 2) & 1) * 128 + lg * 256;
+    const int v_at = 2 * kTile + (lg >> 1) * kTile + l16 * 32 + (lg & 1) * 16;
+    f32x4_t s[RT][2];
+    auto products = [&](int e) {
+        const uint8_t* stage = smem + (e % kStages) * kStage + k_at;
+        uint4 k[C][2];
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+#pragma unroll
+            for (int t = 0; t < 2; ++t) k[c][t] = ld16(stage + c * 1024 + t * 64);
+#pragma unroll
+        for (int r = 0; r < RT; ++r) s[r][0] = s[r][1] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int r = 0; r < RT; ++r)
+                    s[r][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(k[c][t]), q[r][c], s[r][t], 0, 0, 0);
+    };
     // the loads of Q are done before the ring's are counted
     __builtin_amdgcn_s_waitcnt(kWaitVmcnt0);
 #pragma unroll
     for (int e = 0; e < kStages - 1; ++e)
         if (e < steps) fetch(e);
-    const int k_at = (l16 >> 3) * kTile + (l16 & 3) * 16 + ((l16 >> 2) & 1) * 128 + lg * 256;
-    const int v_at = 2 * kTile + (lg >> 1) * kTile + l16 * 32 + (lg & 1) * 16;
+    if (steps >= kStages - 1) wait_vmcnt<(kStages - 2) * kRun>();
+    else wait_vmcnt<0>();
+    lds_barrier();
+    products(0);
     for (int e = 0; e < steps; ++e) {
-        // this wavefront's loads of stages e + 1 .. e + kStages - 2 may be under way
-        if (e + kStages - 2 < steps) wait_vmcnt<(kStages - 2) * kRun>();
+        // this wavefront's loads of stage e + 2 may be under way
+        if (e + 2 < steps) wait_vmcnt<kRun>();
         else wait_vmcnt<0>();
-        // behind it stage e is whole, and nobody reads stage e - 1 any more
+        // behind it stage e + 1 is whole, and nobody reads stage e - 1 any more
         lds_barrier();
-        // the run before this step's is used up
+        // the run of ids before this step's is used up
         if (e % 32 == 0 && e > 0 && 2 * e + 64 < 2 * steps) (e & 32 ? even : odd) = read_ids(2 * e + 64);
         if (e + kStages - 1 < steps) fetch(e + kStages - 1);
-        const uint8_t* stage = smem + (e % kStages) * kStage;
-        const int b0 = b_first + 2 * e;
-        const int id0 = id_of(2 * e), id1 = id_of(2 * e + 1);
-        const bool edge = (b0 + 2) * kBlockTokens - 1 > p.min_pos || id0 < 0 || id1 < 0;
-        const bool ok = (lg >> 1 ? id1 : id0) >= 0;
-        auto step = [&](auto is_edge) {
-            step32<D, RT, decltype(is_edge)::value>(
-                p, lg, b0, ok, a.scale_log2, q, pos, m, l, o,
-                [&](int t, int c) { return as_bf16x8(ld16(stage + k_at + c * 1024 + t * 64)); }, []() {},
-                [&](int t) { return ld16(stage + v_at + t * 512); });
-        };
-        if (edge) step(std::true_type{});
-        else step(std::false_type{});
+        uint8_t* stage = smem + (e % kStages) * kStage;
+        const int b0 = b_first + 2 * e, id0 = id_of(2 * e), id1 = id_of(2 * e + 1);
+        if ((b0 + 2) * kBlockTokens - 1 > p.min_pos || id0 < 0 || id1 < 0) {
+            // some row does not see some key, or a block is not mapped
+            const int key0 = b0 * kBlockTokens + 8 * lg;
+            const bool ok = (lg >> 1 ? id1 : id0) >= 0;
+#pragma unroll
+            for (int r = 0; r < RT; ++r)
+#pragma unroll
+                for (int n = 0; n < 8; ++n)
+                    if (!ok || key0 + n > pos[r]) s[r][n / 4][n % 4] = -INFINITY;
+            // what a slot without a key holds may be no number: it becomes zero in V
+            if ((b0 + 2) * kBlockTokens > p.S || id0 < 0 || id1 < 0) {
+                const int block = threadIdx.x / D, left = p.S - (b0 + block) * kBlockTokens;
+                if (block < 2) {
+                    uint4* v = reinterpret_cast<uint4*>(stage + (2 + block) * kTile + threadIdx.x % D * 32);
+                    const bool mapped = (block ? id1 : id0) >= 0;
+                    v[0] = first_keys(v[0], mapped ? left : 0);
+                    v[1] = first_keys(v[1], mapped ? left - 8 : 0);
+                }
+                lds_barrier();
+            }
+        }
+        // the weights' exponents; where one exceeds the slack its row's maximum is raised
+        float t[RT][8];
+        bool high = false;
+#pragma unroll
+        for (int r = 0; r < RT; ++r) {
+            float top = kNoMax;
+#pragma unroll
+            for (int n = 0; n < 8; ++n) {
+                t[r][n] = fmaf(s[r][n / 4][n % 4], a.scale_log2, -m[r]);
+                top = fmaxf(top, t[r][n]);
+            }
+            high |= top > kSlackLog2;
+        }
+        if (__any(high)) {
+#pragma unroll
+            for (int r = 0; r < RT; ++r) {
+                float top = kNoMax;
+#pragma unroll
+                for (int n = 0; n < 8; ++n) top = fmaxf(top, s[r][n / 4][n % 4] * a.scale_log2);
+                const float next = fmaxf(m[r], rows_max(top)), f = __builtin_amdgcn_exp2f(m[r] - next);
+                m[r] = next;
+                l[r] *= f;
+#pragma unroll
+                for (int d = 0; d < DT; ++d) o[r][d] *= f;
+#pragma unroll
+                for (int n = 0; n < 8; ++n) t[r][n] = fmaf(s[r][n / 4][n % 4], a.scale_log2, -m[r]);
+            }
+        }
+        products(e + 1);  // behind the last step: of what lies there, for nothing
+        bf16x8_t w[RT];
+#pragma unroll
+        for (int r = 0; r < RT; ++r) {
+            float sum = 0.f;
+#pragma unroll
+            for (int n = 0; n < 8; ++n) {
+                t[r][n] = __builtin_amdgcn_exp2f(t[r][n]);
+                sum += t[r][n];
+            }
+            l[r] += sum;
+            w[r] = as_bf16x8(make_uint4(pack_bf16x2(t[r][0], t[r][1]), pack_bf16x2(t[r][2], t[r][3]),
+                                        pack_bf16x2(t[r][4], t[r][5]), pack_bf16x2(t[r][6], t[r][7])));
+        }
+#pragma unroll
+        for (int d = 0; d < DT; ++d) {
+            const bf16x8_t v = as_bf16x8(ld16(stage + v_at + d * 512));
+#pragma unroll
+            for (int r = 0; r < RT; ++r) o[r][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, w[r], o[r][d], 0, 0, 0);
+        }
     }
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
