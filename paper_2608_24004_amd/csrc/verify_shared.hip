@@ -74,6 +74,14 @@ typedef float f32x4_t __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4h_t __attribute__((ext_vector_type(4), aligned(2)));
 typedef float f32x4u_t __attribute__((ext_vector_type(4), aligned(4)));
 
+// Where a row's partial results lie.
+struct __attribute__((aligned(16))) RowParts {
+    int64_t unit0;  // own: the segment's first unit, and pair
+    int pair0, each, tiles, height, e0;  // units of a pair (0: none), tiles, rows of a tile, the row's first place
+    int item0, parts, prefix_tiles, prefix_height, prefix_e0;  // of a prefix: likewise (parts 0: none)
+};
+static_assert(sizeof(RowParts) == 48, "three loads");
+
 struct SharedArgs {
     const void* q;
     const uint8_t* kc;
@@ -82,8 +90,9 @@ struct SharedArgs {
     void* out;
     float* part_o;    // [slots][tile rows][D]
     float2* part_ml;  // [slots][tile rows] maximum and sum
-    struct Segment* segments;  // in memory for the pass that joins
+    RowParts* rows;  // [total_q]
     struct Share* share;
+    struct Segment* segments;  // where a workgroup does not count them itself
     int num_seqs, num_groups, hq, hkv, group, max_blocks, num_blocks, max_seq_len, max_prefix, total_q;
     int nwg;
     int tile_a, tile_b;    // rows of a tile at most: prefix and own segments
@@ -172,23 +181,30 @@ __device__ __forceinline__ int units_of(const Segment& g) {
 }
 
 // v summed over all threads before this one, and over all (THREADS of them).
-template <int THREADS, typename V>
-__device__ __forceinline__ V scan_before(V v, V* s_wave, V& all) {
+struct Sums {
+    int64_t prefix, own;
+    int pairs;
+};
+__device__ __forceinline__ Sums operator+(const Sums& a, const Sums& b) {
+    return Sums{a.prefix + b.prefix, a.own + b.own, a.pairs + b.pairs};
+}
+template <int THREADS>
+__device__ __forceinline__ Sums scan_before(const Sums& v, Sums* s_wave, Sums& all) {
     const int tid = threadIdx.x, lane = tid % kWave;
-    V x = v;
+    Sums x = v;
     for (int o = 1; o < kWave; o <<= 1) {
-        const V y = __shfl_up(x, o);
-        if (lane >= o) x += y;
+        const Sums y{__shfl_up(x.prefix, o), __shfl_up(x.own, o), __shfl_up(x.pairs, o)};
+        if (lane >= o) x = x + y;
     }
     if (lane == kWave - 1) s_wave[tid / kWave] = x;
     __syncthreads();
-    all = 0;
+    all = Sums{0, 0, 0};
     for (int w = 0; w < THREADS / kWave; ++w) {
-        if (w < tid / kWave) x += s_wave[w];
-        all += s_wave[w];
+        if (w < tid / kWave) x = x + s_wave[w];
+        all = all + s_wave[w];
     }
     __syncthreads();
-    return x - v;
+    return Sums{x.prefix - v.prefix, x.own - v.own, x.pairs - v.pairs};
 }
 
 // How the workgroups are divided: na of them take the prefixes' items, the others the ub
@@ -207,12 +223,10 @@ __device__ __forceinline__ int parts_of(const Segment& g, int cost) {
 // counted, and the prefixes' pairs are cut into items.
 template <int THREADS>
 __device__ void count_units(const SharedArgs& a, const Index& x, Segment* segments, Share* share) {
-    __shared__ int64_t s_long[THREADS / kWave];
-    __shared__ int s_int[THREADS / kWave];
+    __shared__ Sums s_wave[THREADS / kWave];
     __shared__ int64_t s_best;
     const int tid = threadIdx.x, segs = a.num_groups + a.num_seqs;
-    int64_t prefix_units = 0, units = 0;
-    int pairs_all = 0;
+    Sums sums{0, 0, 0};
     for (int base = 0; base < segs; base += THREADS) {
         const int s = base + tid;
         Segment g;
@@ -223,20 +237,17 @@ __device__ void count_units(const SharedArgs& a, const Index& x, Segment* segmen
             pairs = each > 0 ? tiles_of(g, s < a.num_groups ? a.tile_a : a.tile_b) * a.hkv : 0;
         }
         const bool own = s >= a.num_groups;
-        int64_t prefix_here, units_here;
-        int pairs_here;
-        scan_before<THREADS>((int64_t)(own ? 0 : pairs) * each, s_long, prefix_here);
-        const int64_t u = scan_before<THREADS>((int64_t)(own ? pairs : 0) * each, s_long, units_here);
-        const int p = scan_before<THREADS>(own ? pairs : 0, s_int, pairs_here);
+        const int64_t u = (int64_t)pairs * each;
+        Sums here;
+        const Sums before = sums + scan_before<THREADS>(Sums{own ? 0 : u, own ? u : 0, own ? pairs : 0}, s_wave, here);
         if (s < segs) {
-            g.unit0 = units + u;
-            g.pair0 = own ? pairs_all + p : pairs;
+            g.unit0 = before.own;
+            g.pair0 = own ? before.pairs : pairs;
             segments[s] = g;
         }
-        prefix_units += prefix_here;
-        units += units_here;
-        pairs_all += pairs_here;
+        sums = sums + here;
     }
+    const int64_t prefix_units = sums.prefix, units = sums.own;
     if (tid == 0) {
         Share h;
         h.ub = units;
@@ -283,10 +294,10 @@ __device__ void count_units(const SharedArgs& a, const Index& x, Segment* segmen
             const int k = base + tid;
             const int pairs = k < a.num_groups ? segments[k].pair0 : 0;
             const int parts = pairs ? parts_of(segments[k], chosen) : 0;
-            int64_t here;
-            const int64_t i0 = before + scan_before<THREADS>((int64_t)pairs * parts, s_long, here);
+            Sums here;
+            const int64_t i0 = before + scan_before<THREADS>(Sums{(int64_t)pairs * parts, 0, 0}, s_wave, here).prefix;
             if (k < a.num_groups) segments[k].unit0 = i0, segments[k].pair0 = parts;
-            before += here;
+            before += here.prefix;
         }
         if (tid == 0) share->items = (int)before;
     }
@@ -307,6 +318,43 @@ __global__ __launch_bounds__(1024) void shared_schedule(SharedArgs a, Index x) {
 // whole number.
 __device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) { return (int64_t)((double)a / (double)b); }
 
+// The request of a packed row: the last one that begins at or before it.
+__device__ __forceinline__ int request_of(const int32_t* q_start, int num_seqs, int row) {
+    int lo = 0, hi = num_seqs - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (q_start[mid] <= row) lo = mid; else hi = mid - 1;
+    }
+    return lo;
+}
+
+// The rows' records for the pass that joins, a row to a thread of the launch.
+__device__ __forceinline__ void describe_rows(const SharedArgs& a, const Index& x, const Segment* segments) {
+    for (int64_t row = (int64_t)blockIdx.x * kThreads + threadIdx.x; row < a.total_q; row += (int64_t)a.nwg * kThreads) {
+        const int i = request_of(x.q_start, a.num_seqs, (int)row);
+        RowParts r{};
+        r.e0 = -1;  // a row of no request
+        if (x.q_start[i] <= row && row < x.q_start[i + 1]) {
+            const Segment own = segments[a.num_groups + i];
+            r.unit0 = own.unit0;
+            r.pair0 = own.pair0;
+            r.each = units_of(own);
+            r.tiles = tiles_of(own, a.tile_b);
+            r.height = tile_rows(own, r.tiles);
+            r.e0 = max(0, (int)row - own.q0) * a.group;
+            if (own.group >= 0) {
+                const Segment common = segments[own.group];
+                r.item0 = (int)common.unit0;
+                r.parts = units_of(common) > 0 ? common.pair0 : 0;
+                r.prefix_tiles = tiles_of(common, a.tile_a);
+                r.prefix_height = tile_rows(common, r.prefix_tiles);
+                r.prefix_e0 = max(0, (int)row - common.q0) * a.group;
+            }
+        }
+        a.rows[row] = r;
+    }
+}
+
 // One workgroup's piece of a pair.
 struct Piece {
     int q0, row0, rows;  // the segment's first packed row; the tile's first row and rows
@@ -326,13 +374,8 @@ __device__ __forceinline__ int row_position(const SharedArgs& a, const Index& x,
     const int at = (p.row0 + r) / a.group;
     if (!p.prefix) return p.pos0 + at;
     if (!p.masked) return INT32_MAX;
-    int lo = 0, hi = a.num_seqs - 1;
-    const int row = p.q0 + at;
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (x.q_start[mid] <= row) lo = mid; else hi = mid - 1;
-    }
-    return clamped_len(a, x, lo) - (x.q_start[lo + 1] - row);
+    const int row = p.q0 + at, i = request_of(x.q_start, a.num_seqs, row);
+    return clamped_len(a, x, i) - (x.q_start[i + 1] - row);
 }
 
 template <typename T, int D>
@@ -840,11 +883,26 @@ __global__ __launch_bounds__(kThreads, 2) void shared_walk(SharedArgs a, Index x
     const Segment* segments = INLINE ? s_segments : a.segments;
     const int segs = a.num_groups + a.num_seqs;
     if constexpr (INLINE) {
-        count_units<kThreads>(a, x, s_segments, &s_share);
-        if (blockIdx.x == 0) {  // for the pass that joins
-            for (int s = threadIdx.x; s < segs; s += kThreads) a.segments[s] = s_segments[s];
-            if (threadIdx.x == 0) *a.share = s_share;
+        // the descriptor in LDS first, where the ring will be: one latency instead of one
+        // for each array that another one's entry leads to
+        int32_t* s_start = reinterpret_cast<int32_t*>(smem);
+        int32_t* s_lens = s_start + kInlineSegs + 1;
+        int32_t* s_groups = s_lens + kInlineSegs;
+        int32_t* s_prefix = s_groups + kInlineSegs + 1;
+        for (int i = threadIdx.x; i <= max(a.num_seqs, a.num_groups); i += kThreads) {
+            if (i <= a.num_seqs) s_start[i] = x.q_start[i];
+            if (i < a.num_seqs) s_lens[i] = x.lens[i];
+            if (i <= a.num_groups) s_groups[i] = x.group_start[i];
+            if (i < a.num_groups) s_prefix[i] = x.prefix[i];
         }
+        __syncthreads();
+        const Index y{x.tables, s_lens, s_start, s_groups, s_prefix};
+        count_units<kThreads>(a, y, s_segments, &s_share);
+        describe_rows(a, y, s_segments);
+        if (blockIdx.x == 0 && threadIdx.x == 0) *a.share = s_share;  // for the pass that joins
+        __syncthreads();
+    } else {
+        describe_rows(a, x, a.segments);
     }
     const Share h = INLINE ? s_share : *a.share;
     auto same = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
@@ -865,10 +923,20 @@ __global__ __launch_bounds__(kThreads, 2) void shared_walk(SharedArgs a, Index x
     }
     while (first ? item < items : u < u_end) {
         const int64_t at = first ? item : u;
+        // the last segment that begins at or before it
         int lo = first ? 0 : a.num_groups, hi = (first ? a.num_groups : segs) - 1;
-        while (lo < hi) {
-            const int mid = (lo + hi + 1) >> 1;
-            if (segments[mid].unit0 <= at) lo = mid; else hi = mid - 1;
+        if constexpr (INLINE) {
+            int found = 0;
+            for (int base = lo; base <= hi; base += kWave) {
+                const int k = base + (int)threadIdx.x % kWave;
+                found += __popcll(__ballot(k <= hi && segments[min(k, hi)].unit0 <= at));
+            }
+            lo += found - 1;
+        } else {
+            while (lo < hi) {
+                const int mid = (lo + hi + 1) >> 1;
+                if (segments[mid].unit0 <= at) lo = mid; else hi = mid - 1;
+            }
         }
         const Segment& g = segments[lo];
         const int each = same(units_of(g)), tiles = same(tiles_of(g, first ? a.tile_a : a.tile_b));
@@ -932,54 +1000,37 @@ __global__ __launch_bounds__(kThreads, 2) void shared_walk(SharedArgs a, Index x
 // A row's parts joined: kLanes lanes for the dims of a (row, query head), SPLIT groups of
 // them for its pieces, a workgroup per row and run of heads.
 template <typename T, int D, int SPLIT>
-__global__ __launch_bounds__(kThreads) void shared_join(SharedArgs a, Index x) {
+__global__ __launch_bounds__(kThreads) void shared_join(SharedArgs a) {
     constexpr int kLanes = D / 4, kGroups = kThreads / kLanes, kHeads = kGroups / SPLIT, kBatch = 4;
     __shared__ f32x4_t s_acc[SPLIT > 1 ? kThreads : 1];
     __shared__ float2 s_ml[SPLIT > 1 ? kGroups : 1];
     const int row = blockIdx.x, tid = threadIdx.x;
-    // the row's request: the last one that begins at or before it
-    int before = 0;
-    for (int base = 0; base < a.num_seqs; base += kThreads) {
-        const int at = base + tid;
-        const int c = __syncthreads_count(at < a.num_seqs && x.q_start[at] <= row);
-        before += c;
-        if (c < kThreads) break;
-    }
-    const int i = before - 1;
-    if (i < 0 || row >= x.q_start[i + 1]) return;
+    const RowParts r = a.rows[row];
+    const Share sh = *a.share;
+    if (r.e0 < 0) return;
     const int unit = tid / kLanes, part_of = unit % SPLIT, d = tid % kLanes * 4;
     const int h = min((int)blockIdx.y * kHeads + unit / SPLIT, a.hq - 1);
-    const int head = h / a.group;
-    const Segment own = a.segments[a.num_groups + i];
-    const Share sh = *a.share;
-    const Segment common = a.segments[max(own.group, 0)];
+    const int head = h / a.group, in_group = h % a.group;
     // pieces of the two pairs, one after the other: the first one's row among the partial
     // rows, and the distance to the next one's
     int pieces[2] = {0, 0};
     int64_t at[2] = {0, 0}, next_at[2] = {0, a.tile_b};
-    auto find = [&](const Segment& g, bool first) {
-        const int each = units_of(g);
-        if (each == 0 || g.rows == 0) return;
-        const int e = (row - g.q0) * a.group + h % a.group;
-        const int tiles = tiles_of(g, first ? a.tile_a : a.tile_b), height = tile_rows(g, tiles);
-        const int tile = e / height;
-        if (first) {
-            const int64_t slot = g.unit0 + (int64_t)head * g.pair0 * tiles + tile;
-            pieces[0] = slot + (int64_t)(g.pair0 - 1) * tiles < a.slots_a ? g.pair0 : 0;
-            at[0] = slot * a.tile_a + e - tile * height;
-            next_at[0] = (int64_t)tiles * a.tile_a;
-        } else {
-            const int pair = head * tiles + tile;
-            const int64_t u0 = g.unit0 + (int64_t)pair * each;
-            // workgroup w owns units [ub w / cb, ub (w + 1) / cb)
-            const int w0 = (int)quotient((u0 + kPairUnits + 1) * sh.cb - 1, sh.ub), w1 = (int)quotient((u0 + each) * sh.cb - 1, sh.ub);
-            const int64_t slot = g.pair0 + pair + w0;
-            pieces[1] = (int)max((int64_t)0, min((int64_t)(w1 - w0 + 1), a.slots_b - slot));
-            at[1] = a.slots_a * a.tile_a + slot * a.tile_b + e - tile * height;
-        }
-    };
-    if (own.group >= 0) find(common, true);
-    find(own, false);
+    if (r.parts > 0) {
+        const int e = r.prefix_e0 + in_group, tile = e / r.prefix_height;
+        const int64_t slot = r.item0 + (int64_t)head * r.parts * r.prefix_tiles + tile;
+        pieces[0] = slot + (int64_t)(r.parts - 1) * r.prefix_tiles < a.slots_a ? r.parts : 0;
+        at[0] = slot * a.tile_a + e - tile * r.prefix_height;
+        next_at[0] = (int64_t)r.prefix_tiles * a.tile_a;
+    }
+    if (r.each > 0) {
+        const int e = r.e0 + in_group, tile = e / r.height, pair = head * r.tiles + tile;
+        const int64_t u0 = r.unit0 + (int64_t)pair * r.each;
+        // workgroup w owns units [ub w / cb, ub (w + 1) / cb)
+        const int w0 = (int)quotient((u0 + kPairUnits + 1) * sh.cb - 1, sh.ub), w1 = (int)quotient((u0 + r.each) * sh.cb - 1, sh.ub);
+        const int64_t slot = r.pair0 + pair + w0;
+        pieces[1] = (int)max((int64_t)0, min((int64_t)(w1 - w0 + 1), a.slots_b - slot));
+        at[1] = a.slots_a * a.tile_a + slot * a.tile_b + e - tile * r.height;
+    }
     float top = kNoMax, sum = 0.f;
     f32x4_t acc{0.f, 0.f, 0.f, 0.f};
     const int all = pieces[0] + pieces[1];
@@ -989,9 +1040,9 @@ __global__ __launch_bounds__(kThreads) void shared_join(SharedArgs a, Index x) {
 #pragma unroll
         for (int z = 0; z < kBatch; ++z) {
             const int e = min(base + z * SPLIT, all - 1), k = e < pieces[0] ? 0 : 1;
-            const int64_t r = at[k] + (k ? e - pieces[0] : e) * next_at[k];
-            ml[z] = a.part_ml[r];
-            o[z] = *reinterpret_cast<const f32x4_t*>(a.part_o + r * D + d);
+            const int64_t from = at[k] + (k ? e - pieces[0] : e) * next_at[k];
+            ml[z] = a.part_ml[from];
+            o[z] = *reinterpret_cast<const f32x4_t*>(a.part_o + from * D + d);
         }
 #pragma unroll
         for (int z = 0; z < kBatch; ++z) {
@@ -1059,7 +1110,8 @@ int plan_shared(const verify_attn_params* p, int32_t total_q, int32_t max_q_len,
     const int64_t part_rows = s.slots_a * s.tile_a + s.slots_b * s.tile_b;
     s.o_bytes = (size_t)part_rows * D * 4;
     s.ml_bytes = align_up((size_t)part_rows * 8, 16);
-    s.total = s.o_bytes + s.ml_bytes + sizeof(Share) + (size_t)s.segs * sizeof(Segment);
+    s.total = s.o_bytes + s.ml_bytes + (size_t)total_q * sizeof(RowParts) + sizeof(Share) +
+              (size_t)s.segs * sizeof(Segment);
     s.split = s.nwg >= 24 * pairs_a ? 8 : s.nwg >= 8 * pairs_a ? 4 : 1;
     return VERIFY_OK;
 }
@@ -1093,7 +1145,7 @@ void launch_shared(const SharedArgs& a, const Index& x, int split, hipStream_t s
     auto join = [&](auto n) {
         constexpr int kHeads = kThreads / (D / 4) / decltype(n)::value;
         hipLaunchKernelGGL((shared_join<T, D, decltype(n)::value>), dim3(a.total_q, (a.hq + kHeads - 1) / kHeads),
-                           dim3(kThreads), 0, stream, a, x);
+                           dim3(kThreads), 0, stream, a);
     };
     if (split == 8) join(std::integral_constant<int, 8>{});
     else if (split == 4) join(std::integral_constant<int, 4>{});
@@ -1153,7 +1205,8 @@ extern "C" int verify_attention_shared(const verify_attn_params* params, int32_t
     a.out = out;
     a.part_o = reinterpret_cast<float*>(ws);
     a.part_ml = reinterpret_cast<float2*>(ws + s.o_bytes);
-    a.share = reinterpret_cast<Share*>(ws + s.o_bytes + s.ml_bytes);
+    a.rows = reinterpret_cast<RowParts*>(ws + s.o_bytes + s.ml_bytes);
+    a.share = reinterpret_cast<Share*>(a.rows + total_q);
     a.segments = reinterpret_cast<Segment*>(a.share + 1);
     a.num_seqs = params->num_seqs;
     a.num_groups = num_groups;
