@@ -48,6 +48,7 @@ constexpr int kUnitBlocks = 8;      // KV blocks of a unit
 // the wavefronts, the partial result), in units: it counts so many units more, without
 // blocks, in front of its own.
 constexpr int kPairUnits = 1;
+constexpr int kItemUnits = 4;  // likewise of a part of a prefix, with its way through the join
 constexpr int kInlineSegs = 256;    // segments whose units every workgroup counts itself
 constexpr int kStages = 4;          // of the tall walk's ring
 constexpr float kNoMax = -3.0e38f;  // a maximum over no key
@@ -283,7 +284,7 @@ __device__ void count_units(const SharedArgs& a, const Index& x, Segment* segmen
             longest = max(longest, __shfl_xor(longest, o));
         }
         const bool fits = items <= a.slots_a;
-        const int64_t time = min((int64_t)1 << 40, ((items + na - 1) / na) * (longest + kPairUnits));
+        const int64_t time = min((int64_t)1 << 40, ((items + na - 1) / na) * (longest + kItemUnits));
         // the longest parts of equal candidates
         if (tid % kLanes == 0 && fits) atomicMin((unsigned long long*)&s_best, (unsigned long long)(time << 8 | (kCandidates - 1 - c)));
         __syncthreads();
@@ -750,13 +751,15 @@ __device__ void walk_tall(const SharedArgs& a, const Index& x, const Piece& p, u
     const int k_at = (l16 >> 3) * kTile + (l16 & 3) * 16 + ((l16 >> 2) & 1) * 128 + lg * 256;
     const int v_at = 2 * kTile + (lg >> 1) * kTile + l16 * 32 + (lg & 1) * 16;
     f32x4_t s[RT][2];
-    auto products = [&](int e) {
+    uint4 k[C][2];
+    auto read_k = [&](int e) {
         const uint8_t* stage = smem + (e % kStages) * kStage + k_at;
-        uint4 k[C][2];
 #pragma unroll
         for (int c = 0; c < C; ++c)
 #pragma unroll
             for (int t = 0; t < 2; ++t) k[c][t] = ld16(stage + c * 1024 + t * 64);
+    };
+    auto products = [&]() {
 #pragma unroll
         for (int r = 0; r < RT; ++r) s[r][0] = s[r][1] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -775,7 +778,8 @@ __device__ void walk_tall(const SharedArgs& a, const Index& x, const Piece& p, u
     if (steps >= kStages - 1) wait_vmcnt<(kStages - 2) * kRun>();
     else wait_vmcnt<0>();
     lds_barrier();
-    products(0);
+    read_k(0);
+    products();
     for (int e = 0; e < steps; ++e) {
         // this wavefront's loads of stage e + 2 may be under way
         if (e + 2 < steps) wait_vmcnt<kRun>();
@@ -808,6 +812,7 @@ __device__ void walk_tall(const SharedArgs& a, const Index& x, const Piece& p, u
                 lds_barrier();
             }
         }
+        read_k(e + 1);  // behind the last step: what lies there, for nothing
         // the weights' exponents; where one exceeds the slack its row's maximum is raised
         float t[RT][8];
         bool high = false;
@@ -836,7 +841,7 @@ __device__ void walk_tall(const SharedArgs& a, const Index& x, const Piece& p, u
                 for (int n = 0; n < 8; ++n) t[r][n] = fmaf(s[r][n / 4][n % 4], a.scale_log2, -m[r]);
             }
         }
-        products(e + 1);  // behind the last step: of what lies there, for nothing
+        products();
         bf16x8_t w[RT];
 #pragma unroll
         for (int r = 0; r < RT; ++r) {
