@@ -94,6 +94,7 @@ struct SharedArgs {
     RowParts* rows;  // [total_q]
     struct Share* share;
     struct Segment* segments;  // where a workgroup does not count them itself
+    struct Items* items;
     int num_seqs, num_groups, hq, hkv, group, max_blocks, num_blocks, max_seq_len, max_prefix, total_q;
     int nwg;
     int tile_a, tile_b;    // rows of a tile at most: prefix and own segments
@@ -110,9 +111,8 @@ struct Index {  // device arrays that nothing writes
 };
 
 struct __attribute__((aligned(16))) Segment {
-    int64_t unit0;   // own: number of its first unit; prefix: of its first item.  The entry
-                     // behind the last prefix's and own one hold the numbers of all
-    int pair0;       // own: of its first pair; prefix: parts that each pair's keys are cut into
+    int64_t unit0;   // number of its first unit
+    int pair0;       // own: of its first pair; prefix: pairs
     int q0, rows;    // first packed row, packed rows times query heads per KV head
     int b_lo, b_hi;  // blocks
     int table;       // the request whose block table lists the blocks
@@ -172,147 +172,151 @@ __device__ __forceinline__ Segment segment_of(const SharedArgs& a, const Index& 
 
 // A segment's rows divided evenly over as few tiles of at most `most` rows as there need
 // be: their number, and the rows of one.
-__device__ __forceinline__ int tiles_of(const Segment& g, int most) { return (g.rows + most - 1) / most; }
+__device__ __forceinline__ int tiles_of(const Segment& g, int most) { return (uint32_t)(g.rows + most - 1) / (uint32_t)most; }
 __device__ __forceinline__ int tile_rows(const Segment& g, int tiles) {
-    return tiles ? ((g.rows + tiles - 1) / tiles + 15) / 16 * 16 : 16;
+    return tiles ? ((uint32_t)(g.rows + tiles - 1) / (uint32_t)tiles + 15) / 16 * 16 : 16;
 }
 
 __device__ __forceinline__ int units_of(const Segment& g) {
     return g.b_hi > g.b_lo ? (g.b_hi - g.b_lo + kUnitBlocks - 1) / kUnitBlocks + kPairUnits : 0;
 }
 
-// v summed over all threads before this one, and over all (THREADS of them).
-struct Sums {
-    int64_t prefix, own;
-    int pairs;
-};
-__device__ __forceinline__ Sums operator+(const Sums& a, const Sums& b) {
-    return Sums{a.prefix + b.prefix, a.own + b.own, a.pairs + b.pairs};
+// v of the lanes up to this one, summed.
+__device__ __forceinline__ int scan_lanes(int v) {
+    auto add = [&](auto ctrl, auto rows) {
+        v += __builtin_amdgcn_update_dpp(0, v, decltype(ctrl)::value, decltype(rows)::value, 0xf, false);
+    };
+    using std::integral_constant;
+    add(integral_constant<int, 0x111>{}, integral_constant<int, 0xf>{});  // the lane 1, 2, 4, 8 before it in its row of 16
+    add(integral_constant<int, 0x112>{}, integral_constant<int, 0xf>{});
+    add(integral_constant<int, 0x114>{}, integral_constant<int, 0xf>{});
+    add(integral_constant<int, 0x118>{}, integral_constant<int, 0xf>{});
+    add(integral_constant<int, 0x142>{}, integral_constant<int, 0xa>{});  // the last lane of the row before
+    add(integral_constant<int, 0x143>{}, integral_constant<int, 0xc>{});  // the last lane of the first half
+    return v;
 }
-template <int THREADS>
-__device__ __forceinline__ Sums scan_before(const Sums& v, Sums* s_wave, Sums& all) {
-    const int tid = threadIdx.x, lane = tid % kWave;
-    Sums x = v;
+__device__ __forceinline__ int64_t scan_lanes(int64_t v) {
     for (int o = 1; o < kWave; o <<= 1) {
-        const Sums y{__shfl_up(x.prefix, o), __shfl_up(x.own, o), __shfl_up(x.pairs, o)};
-        if (lane >= o) x = x + y;
+        const int64_t w = __shfl_up(v, o);
+        if ((int)threadIdx.x % kWave >= o) v += w;
     }
-    if (lane == kWave - 1) s_wave[tid / kWave] = x;
-    __syncthreads();
-    all = Sums{0, 0, 0};
-    for (int w = 0; w < THREADS / kWave; ++w) {
-        if (w < tid / kWave) x = x + s_wave[w];
-        all = all + s_wave[w];
-    }
-    __syncthreads();
-    return Sums{x.prefix - v.prefix, x.own - v.own, x.pairs - v.pairs};
+    return v;
 }
 
 // How the workgroups are divided: na of them take the prefixes' items, the others the ub
-// own units.  Where there are fewer of these than workgroups, cb of them have one.
+// own units behind unit ua.  Where there are fewer of these than workgroups, cb of them
+// have one.
 struct __attribute__((aligned(16))) Share {
-    int64_t ub;
+    int64_t ua, ub;
     int items, na, cb;
 };
 
-// Cuts each prefix's pairs into parts of about `cost` units.
-__device__ __forceinline__ int parts_of(const Segment& g, int cost) {
-    return max(1, (units_of(g) - kPairUnits + cost - 1) / cost);
-}
+// A prefix's items: the first one, and the parts that each of its pairs is cut into.
+struct Items {
+    int first, parts;
+};
 
-// All segments, by one workgroup of THREADS threads: the own ones' units and pairs are
-// counted, and the prefixes' pairs are cut into items.
-template <int THREADS>
-__device__ void count_units(const SharedArgs& a, const Index& x, Segment* segments, Share* share) {
-    __shared__ Sums s_wave[THREADS / kWave];
-    __shared__ int64_t s_best;
-    const int tid = threadIdx.x, segs = a.num_groups + a.num_seqs;
-    Sums sums{0, 0, 0};
+// Counts the units and pairs of all segments and cuts the prefixes' pairs into items, by
+// one workgroup of THREADS threads.  Count: of all units.
+template <int THREADS, typename Count>
+__device__ __forceinline__ Share count_units(const SharedArgs& a, const Index& x, Segment* segments, Items* items) {
+    __shared__ Count s_units[THREADS / kWave];
+    __shared__ int s_pairs[THREADS / kWave];
+    const int tid = threadIdx.x, lane = tid % kWave, segs = a.num_groups + a.num_seqs;
+    Count units = 0;
+    int pairs = 0;
     for (int base = 0; base < segs; base += THREADS) {
         const int s = base + tid;
         Segment g;
-        int pairs = 0, each = 0;
+        int p = 0, each = 0;
         if (s < segs) {
             g = segment_of(a, x, s);
             each = units_of(g);
-            pairs = each > 0 ? tiles_of(g, s < a.num_groups ? a.tile_a : a.tile_b) * a.hkv : 0;
+            p = each > 0 ? tiles_of(g, s < a.num_groups ? a.tile_a : a.tile_b) * a.hkv : 0;
         }
-        const bool own = s >= a.num_groups;
-        const int64_t u = (int64_t)pairs * each;
-        Sums here;
-        const Sums before = sums + scan_before<THREADS>(Sums{own ? 0 : u, own ? u : 0, own ? pairs : 0}, s_wave, here);
+        const Count u = (Count)p * each, u_lanes = scan_lanes(u);
+        const int p_lanes = scan_lanes(p);
+        if (lane == kWave - 1) s_units[tid / kWave] = u_lanes, s_pairs[tid / kWave] = p_lanes;
+        __syncthreads();
+        Count u_all = 0, u_before = units + u_lanes - u;
+        int p_all = 0, p_before = pairs + p_lanes - p;
+#pragma unroll
+        for (int w = 0; w < THREADS / kWave; ++w) {
+            if (w < tid / kWave) u_before += s_units[w], p_before += s_pairs[w];
+            u_all += s_units[w];
+            p_all += s_pairs[w];
+        }
         if (s < segs) {
-            g.unit0 = before.own;
-            g.pair0 = own ? before.pairs : pairs;
+            g.unit0 = u_before;
+            g.pair0 = s < a.num_groups ? p : p_before;
             segments[s] = g;
         }
-        sums = sums + here;
-    }
-    const int64_t prefix_units = sums.prefix, units = sums.own;
-    if (tid == 0) {
-        Share h;
-        h.ub = units;
-        if (prefix_units == 0) h.na = 0;
-        else if (units == 0) h.na = a.nwg;
-        else h.na = clamp_to((int)((double)prefix_units / (double)(prefix_units + units) * a.nwg / 8 + 0.5) * 8, 8, a.nwg - 8);
-        h.cb = (int)min((int64_t)(a.nwg - h.na), units);
-        h.items = 0;
-        *share = h;
-        s_best = INT64_MAX;
-    }
-    __syncthreads();
-    if (prefix_units > 0) {
-        // The parts' length with which the last of the na workgroups is done first, each
-        // taking its share of the items one after the other: candidates between a fourth
-        // of the mean share and four times it, 16 lanes to each.
-        constexpr int kLanes = 16, kCandidates = THREADS / kLanes;
-        const int64_t na = share->na;
-        const float mean = fmaxf(1.f, (float)prefix_units / (float)na);
-        auto length = [&](int c) { return (int)fminf(1.0e9f, ceilf(mean * 0.25f * exp2f(4.f / (kCandidates - 1) * c))); };
-        const int c = tid / kLanes, cost = length(c);
-        int64_t items = 0;
-        int longest = 0;
-        for (int k = tid % kLanes; k < a.num_groups; k += kLanes) {
-            const Segment& g = segments[k];
-            if (g.pair0 == 0) continue;
-            const int parts = parts_of(g, cost), u = units_of(g) - kPairUnits;
-            items += (int64_t)g.pair0 * parts;
-            longest = max(longest, (u + parts - 1) / parts);
-        }
-        for (int o = 1; o < kLanes; o <<= 1) {
-            items += __shfl_xor(items, o);
-            longest = max(longest, __shfl_xor(longest, o));
-        }
-        const bool fits = items <= a.slots_a;
-        const int64_t time = min((int64_t)1 << 40, ((items + na - 1) / na) * (longest + kItemUnits));
-        // the longest parts of equal candidates
-        if (tid % kLanes == 0 && fits) atomicMin((unsigned long long*)&s_best, (unsigned long long)(time << 8 | (kCandidates - 1 - c)));
+        units += u_all;
+        pairs += p_all;
         __syncthreads();
-        // whole prefixes always fit
-        const int chosen = s_best == INT64_MAX ? INT32_MAX / 2 : length(kCandidates - 1 - (int)(s_best & 0xff));
-        int64_t before = 0;
-        for (int base = 0; base < a.num_groups; base += THREADS) {
-            const int k = base + tid;
-            const int pairs = k < a.num_groups ? segments[k].pair0 : 0;
-            const int parts = pairs ? parts_of(segments[k], chosen) : 0;
-            Sums here;
-            const int64_t i0 = before + scan_before<THREADS>(Sums{(int64_t)pairs * parts, 0, 0}, s_wave, here).prefix;
-            if (k < a.num_groups) segments[k].unit0 = i0, segments[k].pair0 = parts;
-            before += here.prefix;
-        }
-        if (tid == 0) share->items = (int)before;
     }
-    __syncthreads();
+    Share h;
+    h.ua = a.num_seqs > 0 ? segments[a.num_groups].unit0 : units;
+    h.ub = units - h.ua;
+    if (h.ua == 0) h.na = 0;
+    else if (h.ub == 0) h.na = a.nwg;
+    else h.na = clamp_to((int)((float)h.ua / (float)units * (a.nwg / 8) + 0.5f) * 8, 8, a.nwg - 8);
+    h.cb = (int)min((int64_t)(a.nwg - h.na), h.ub);
+    h.items = 0;
     // a row that stands in front of its prefix's last key sees a part of it
     for (int i = tid; i < a.num_seqs; i += THREADS) {
         const Segment& g = segments[a.num_groups + i];
         if (g.group >= 0 && g.rows > 0 && g.pos0 < g.b_lo * kBlockTokens - 1) segments[g.group].pos0 = 1;
     }
+    if (h.ua > 0) {
+        // The parts' length with which the last of the na workgroups is done first, each
+        // taking its share of the items one after the other: 16 candidates between a
+        // fourth of the mean share and four times it, four lanes to each, in every
+        // wavefront for itself.
+        const float mean = fmaxf(1.f, (float)h.ua / (float)h.na);
+        auto length = [&](int c) { return fminf(1.0e9f, ceilf(mean * 0.25f * __builtin_amdgcn_exp2f(4.f / 15 * c))); };
+        auto parts_of = [&](const Segment& g, float cost) {
+            return max(1, (int)ceilf((float)(units_of(g) - kPairUnits) * __builtin_amdgcn_rcpf(cost) - 0.001f));
+        };
+        const int c = lane / 4;
+        const float cost = length(c);
+        float all = 0.f;
+        int longest = 0;
+        for (int k = lane % 4; k < a.num_groups; k += 4) {
+            const Segment& g = segments[k];
+            if (g.pair0 == 0) continue;
+            const int parts = parts_of(g, cost);
+            all += (float)g.pair0 * (float)parts;
+            longest = max(longest, (units_of(g) - kPairUnits + parts - 1) / parts);
+        }
+        for (int o = 1; o < 4; o <<= 1) {
+            all += __shfl_xor(all, o);
+            longest = max(longest, __shfl_xor(longest, o));
+        }
+        // (rounded sums: items that would not fit are cut off well before the last slot)
+        float time = all < 0.99f * (float)a.slots_a ? ceilf(all * __builtin_amdgcn_rcpf((float)h.na) - 0.001f) * (float)(longest + kItemUnits)
+                                                    : INFINITY;
+        float best = time;
+        for (int o = 4; o < kWave; o <<= 1) best = fminf(best, __shfl_xor(best, o));
+        // the longest parts of equal candidates; whole prefixes always fit
+        const uint64_t equal = __ballot(time == best);
+        const float chosen = best < INFINITY ? length((63 - __clzll((long long)equal)) / 4) : 1.0e9f;
+        for (int base = 0; base < a.num_groups; base += kWave) {
+            const int k = base + lane;
+            const Segment* g = segments + min(k, a.num_groups - 1);
+            const int parts = k < a.num_groups && g->pair0 > 0 ? parts_of(*g, chosen) : 0;
+            const int here = scan_lanes(parts * g->pair0);
+            if (tid < kWave && k < a.num_groups) items[k] = Items{h.items + here - parts * g->pair0, parts};
+            h.items += __builtin_amdgcn_readlane(here, kWave - 1);
+        }
+    }
     __syncthreads();
+    return h;
 }
 
 __global__ __launch_bounds__(1024) void shared_schedule(SharedArgs a, Index x) {
-    count_units<1024>(a, x, a.segments, a.share);
+    const Share h = count_units<1024, int64_t>(a, x, a.segments, a.items);
+    if (threadIdx.x == 0) *a.share = h;
 }
 
 // a / b rounded down, 0 <= a < 2^52: a quotient in binary64 is not rounded up to the next
@@ -330,14 +334,15 @@ __device__ __forceinline__ int request_of(const int32_t* q_start, int num_seqs, 
 }
 
 // The rows' records for the pass that joins, a row to a thread of the launch.
-__device__ __forceinline__ void describe_rows(const SharedArgs& a, const Index& x, const Segment* segments) {
+__device__ __forceinline__ void describe_rows(const SharedArgs& a, const Index& x, const Segment* segments, const Items* items,
+                                              int64_t ua) {
     for (int64_t row = (int64_t)blockIdx.x * kThreads + threadIdx.x; row < a.total_q; row += (int64_t)a.nwg * kThreads) {
         const int i = request_of(x.q_start, a.num_seqs, (int)row);
         RowParts r{};
         r.e0 = -1;  // a row of no request
         if (x.q_start[i] <= row && row < x.q_start[i + 1]) {
             const Segment own = segments[a.num_groups + i];
-            r.unit0 = own.unit0;
+            r.unit0 = own.unit0 - ua;
             r.pair0 = own.pair0;
             r.each = units_of(own);
             r.tiles = tiles_of(own, a.tile_b);
@@ -345,8 +350,8 @@ __device__ __forceinline__ void describe_rows(const SharedArgs& a, const Index& 
             r.e0 = max(0, (int)row - own.q0) * a.group;
             if (own.group >= 0) {
                 const Segment common = segments[own.group];
-                r.item0 = (int)common.unit0;
-                r.parts = units_of(common) > 0 ? common.pair0 : 0;
+                r.item0 = items[own.group].first;
+                r.parts = common.pair0 > 0 ? items[own.group].parts : 0;
                 r.prefix_tiles = tiles_of(common, a.tile_a);
                 r.prefix_height = tile_rows(common, r.prefix_tiles);
                 r.prefix_e0 = max(0, (int)row - common.q0) * a.group;
@@ -884,8 +889,10 @@ template <typename T, int D, bool INLINE>
 __global__ __launch_bounds__(kThreads, 2) void shared_walk(SharedArgs a, Index x) {
     __shared__ __attribute__((aligned(16))) uint8_t smem[smem_bytes<T, D>()];
     __shared__ Segment s_segments[INLINE ? kInlineSegs : 1];
-    __shared__ Share s_share;
+    __shared__ Items s_items[INLINE ? kInlineSegs : 1];
     const Segment* segments = INLINE ? s_segments : a.segments;
+    const Items* prefix_items = INLINE ? s_items : a.items;
+    Share h;
     const int segs = a.num_groups + a.num_seqs;
     if constexpr (INLINE) {
         // the descriptor in LDS first, where the ring will be: one latency instead of one
@@ -902,14 +909,14 @@ __global__ __launch_bounds__(kThreads, 2) void shared_walk(SharedArgs a, Index x
         }
         __syncthreads();
         const Index y{x.tables, s_lens, s_start, s_groups, s_prefix};
-        count_units<kThreads>(a, y, s_segments, &s_share);
-        describe_rows(a, y, s_segments);
-        if (blockIdx.x == 0 && threadIdx.x == 0) *a.share = s_share;  // for the pass that joins
+        h = count_units<kThreads, int>(a, y, s_segments, s_items);
+        describe_rows(a, y, s_segments, s_items, h.ua);
+        if (blockIdx.x == 0 && threadIdx.x == 0) *a.share = h;  // for the pass that joins
         __syncthreads();
     } else {
-        describe_rows(a, x, a.segments);
+        h = *a.share;
+        describe_rows(a, x, a.segments, a.items, h.ua);
     }
-    const Share h = INLINE ? s_share : *a.share;
     auto same = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
     const int na = same(h.na), b = blockIdx.x;
     const bool first = b < na;
@@ -927,41 +934,43 @@ __global__ __launch_bounds__(kThreads, 2) void shared_walk(SharedArgs a, Index x
         u_end = quotient(h.ub * (w + 1), count);
     }
     while (first ? item < items : u < u_end) {
-        const int64_t at = first ? item : u;
+        const int64_t at = first ? item : h.ua + u;
+        auto begin = [&](int k) { return first ? (int64_t)prefix_items[k].first : segments[k].unit0; };
         // the last segment that begins at or before it
         int lo = first ? 0 : a.num_groups, hi = (first ? a.num_groups : segs) - 1;
         if constexpr (INLINE) {
             int found = 0;
             for (int base = lo; base <= hi; base += kWave) {
                 const int k = base + (int)threadIdx.x % kWave;
-                found += __popcll(__ballot(k <= hi && segments[min(k, hi)].unit0 <= at));
+                found += __popcll(__ballot(k <= hi && begin(min(k, hi)) <= at));
             }
             lo += found - 1;
         } else {
             while (lo < hi) {
                 const int mid = (lo + hi + 1) >> 1;
-                if (segments[mid].unit0 <= at) lo = mid; else hi = mid - 1;
+                if (begin(mid) <= at) lo = mid; else hi = mid - 1;
             }
         }
         const Segment& g = segments[lo];
         const int each = same(units_of(g)), tiles = same(tiles_of(g, first ? a.tile_a : a.tile_b));
-        const int64_t local = at - g.unit0;
+        const int64_t local = at - begin(lo);
         int tile;
         int64_t slot;
         Piece p;
         if (first) {
             // item = (head * parts + part) * tiles + tile
-            const int parts = same(g.pair0), e = same((int)local), part = e / tiles % parts, real = each - kPairUnits;
-            tile = e % tiles;
-            p.head = e / tiles / parts;
-            p.u0 = (int)((int64_t)real * part / parts);
-            p.u1 = (int)((int64_t)real * (part + 1) / parts);
+            const uint32_t parts = same(prefix_items[lo].parts), e = same((int)local), row = e / (uint32_t)tiles, real = each - kPairUnits;
+            p.head = row / parts;
+            const uint32_t part = row - p.head * parts;
+            tile = e - row * tiles;
+            p.u0 = (int)quotient((int64_t)real * part, parts);
+            p.u1 = (int)quotient((int64_t)real * (part + 1), parts);
             slot = item;
             item += step;
         } else {
             const int pair = same((int)quotient(local, each));
-            tile = pair % tiles;
-            p.head = pair / tiles;
+            p.head = (uint32_t)pair / (uint32_t)tiles;
+            tile = pair - p.head * tiles;
             const int from = same((int)(local - (int64_t)pair * each)), to = same((int)min((int64_t)each, from + (u_end - u)));
             u += to - from;
             p.u0 = max(0, from - kPairUnits);
@@ -1088,13 +1097,15 @@ __global__ __launch_bounds__(kThreads) void shared_join(SharedArgs a) {
 struct SharedPlan {
     int nwg, tile_a, tile_b;
     int64_t slots_a, slots_b, segs;
+    bool inlined;
     int split;  // groups of threads that share a row's pieces in the pass that joins
     size_t o_bytes, ml_bytes, total;
 };
 
 // Row tiles and partial results.  A tile holds at most the rows that its segment may
 // have: few of them (flat) or 64 tall_tiles.
-int plan_shared(const verify_attn_params* p, int32_t total_q, int32_t max_q_len, int32_t num_groups, SharedPlan& s) {
+int plan_shared(const verify_attn_params* p, int32_t total_q, int32_t max_q_len, int32_t max_seq_len, int32_t num_groups,
+                int32_t max_prefix_len, SharedPlan& s) {
     const int group = p->num_q_heads / p->num_kv_heads, D = p->head_dim;
     const bool f32 = p->dtype == VERIFY_F32;
     auto tile = [&](int64_t rows) {
@@ -1116,7 +1127,12 @@ int plan_shared(const verify_attn_params* p, int32_t total_q, int32_t max_q_len,
     s.o_bytes = (size_t)part_rows * D * 4;
     s.ml_bytes = align_up((size_t)part_rows * 8, 16);
     s.total = s.o_bytes + s.ml_bytes + (size_t)total_q * sizeof(RowParts) + sizeof(Share) +
-              (size_t)s.segs * sizeof(Segment);
+              (size_t)s.segs * sizeof(Segment) + (size_t)num_groups * sizeof(Items);
+    // the units of all pairs in 32 bits: then every workgroup can count them itself
+    const int64_t most_units = std::min<int64_t>(std::max(max_seq_len, max_prefix_len), (int64_t)p->max_blocks_per_seq * kBlockTokens) /
+                                   (kUnitBlocks * kBlockTokens) + 2 + kPairUnits;
+    s.inlined = s.segs <= kInlineSegs && (pairs_a + pairs_b) * most_units < (1LL << 31) && s.slots_a < (1LL << 30);
+
     s.split = s.nwg >= 24 * pairs_a ? 8 : s.nwg >= 8 * pairs_a ? 4 : 1;
     return VERIFY_OK;
 }
@@ -1140,8 +1156,9 @@ bool is_plain(const verify_attn_params* p, int32_t num_groups, int32_t max_prefi
 }
 
 template <typename T, int D>
-void launch_shared(const SharedArgs& a, const Index& x, int split, hipStream_t stream) {
-    if (a.num_groups + a.num_seqs <= kInlineSegs) {
+void launch_shared(const SharedArgs& a, const Index& x, const SharedPlan& plan, hipStream_t stream) {
+    const int split = plan.split;
+    if (plan.inlined) {
         hipLaunchKernelGGL((shared_walk<T, D, true>), dim3(a.nwg), dim3(kThreads), 0, stream, a, x);
     } else {
         hipLaunchKernelGGL(shared_schedule, dim3(1), dim3(1024), 0, stream, a, x);
@@ -1158,8 +1175,8 @@ void launch_shared(const SharedArgs& a, const Index& x, int split, hipStream_t s
 }
 
 // two workgroups per compute unit
-static_assert(sizeof(Segment) == 48 && smem_bytes<uint16_t, 128>() + 48 * kInlineSegs + 1024 <= 80 * 1024 &&
-              sizeof(Share) % 8 == 0, "LDS and workspace");
+static_assert(sizeof(Segment) == 48 && smem_bytes<uint16_t, 128>() + (48 + 8) * kInlineSegs + 1024 <= 80 * 1024 &&
+              sizeof(Share) % 16 == 0, "LDS and workspace");
 
 }  // namespace
 }  // namespace averify
@@ -1177,7 +1194,7 @@ extern "C" int verify_attention_shared_workspace_size(const verify_attn_params* 
     if (is_plain(params, num_groups, max_prefix_len))
         return verify_attention_workspace_size(params, total_q, max_q_len, max_seq_len, bytes);
     SharedPlan s;
-    rc = plan_shared(params, total_q, max_q_len, num_groups, s);
+    rc = plan_shared(params, total_q, max_q_len, max_seq_len, num_groups, max_prefix_len, s);
     if (rc == VERIFY_OK) *bytes = s.total;
     return rc;
 }
@@ -1198,7 +1215,7 @@ extern "C" int verify_attention_shared(const verify_attn_params* params, int32_t
         return VERIFY_EINVAL;
     if (((uintptr_t)k_cache | (uintptr_t)v_cache | (uintptr_t)workspace) & 15) return VERIFY_EINVAL;
     SharedPlan s;
-    rc = plan_shared(params, total_q, max_q_len, num_groups, s);
+    rc = plan_shared(params, total_q, max_q_len, max_seq_len, num_groups, max_prefix_len, s);
     if (rc != VERIFY_OK) return rc;
     if (!workspace || workspace_bytes < s.total) return VERIFY_EWORKSPACE;
     uint8_t* ws = static_cast<uint8_t*>(workspace);
@@ -1213,6 +1230,7 @@ extern "C" int verify_attention_shared(const verify_attn_params* params, int32_t
     a.rows = reinterpret_cast<RowParts*>(ws + s.o_bytes + s.ml_bytes);
     a.share = reinterpret_cast<Share*>(a.rows + total_q);
     a.segments = reinterpret_cast<Segment*>(a.share + 1);
+    a.items = reinterpret_cast<Items*>(a.segments + s.segs);
     a.num_seqs = params->num_seqs;
     a.num_groups = num_groups;
     a.hq = params->num_q_heads;
@@ -1232,10 +1250,10 @@ extern "C" int verify_attention_shared(const verify_attn_params* params, int32_t
     a.scale_log2 = scale * kLog2e;
     const Index x{block_tables, seq_lens, q_start, group_start, prefix_lens};
     if (params->dtype == VERIFY_BF16)
-        params->head_dim == 128 ? launch_shared<uint16_t, 128>(a, x, s.split, stream)
-                                : launch_shared<uint16_t, 64>(a, x, s.split, stream);
+        params->head_dim == 128 ? launch_shared<uint16_t, 128>(a, x, s, stream)
+                                : launch_shared<uint16_t, 64>(a, x, s, stream);
     else
-        params->head_dim == 128 ? launch_shared<float, 128>(a, x, s.split, stream)
-                                : launch_shared<float, 64>(a, x, s.split, stream);
+        params->head_dim == 128 ? launch_shared<float, 128>(a, x, s, stream)
+                                : launch_shared<float, 64>(a, x, s, stream);
     return check_launch();
 }
