@@ -48,8 +48,11 @@ constexpr int kUnitBlocks = 8;      // KV blocks of a unit
 // the wavefronts, the partial result), in units: it counts so many units more, without
 // blocks, in front of its own.
 constexpr int kPairUnits = 1;
-constexpr int kItemUnits = 4;  // likewise of a part of a prefix, with its way through the join
+constexpr float kItemUnits = 2.f;  // likewise of a part of a prefix, with its way through the join
 constexpr int kInlineSegs = 256;    // segments whose units every workgroup counts itself
+// A prefix's unit of 128 rows beside one of few rows: 3.5 us where 4.3 (the one fills the
+// matrix units, the other waits for 64 KiB; 32 requests of nine rows, 8192 common keys).
+constexpr float kTallUnit = 0.8f;
 constexpr int kStages = 4;          // of the tall walk's ring
 constexpr float kNoMax = -3.0e38f;  // a maximum over no key
 // Softmax weights may exceed 1 by up to this factor (log2) before a row's maximum is
@@ -258,28 +261,25 @@ __device__ __forceinline__ Share count_units(const SharedArgs& a, const Index& x
     Share h;
     h.ua = a.num_seqs > 0 ? segments[a.num_groups].unit0 : units;
     h.ub = units - h.ua;
-    if (h.ua == 0) h.na = 0;
-    else if (h.ub == 0) h.na = a.nwg;
-    else h.na = clamp_to((int)((float)h.ua / (float)units * (a.nwg / 8) + 0.5f) * 8, 8, a.nwg - 8);
-    h.cb = (int)min((int64_t)(a.nwg - h.na), h.ub);
-    h.items = 0;
     // a row that stands in front of its prefix's last key sees a part of it
     for (int i = tid; i < a.num_seqs; i += THREADS) {
         const Segment& g = segments[a.num_groups + i];
         if (g.group >= 0 && g.rows > 0 && g.pos0 < g.b_lo * kBlockTokens - 1) segments[g.group].pos0 = 1;
     }
+    h.na = h.items = 0;
     if (h.ua > 0) {
-        // The parts' length with which the last of the na workgroups is done first, each
-        // taking its share of the items one after the other: 16 candidates between a
-        // fourth of the mean share and four times it, four lanes to each, in every
-        // wavefront for itself.
-        const float mean = fmaxf(1.f, (float)h.ua / (float)h.na);
-        auto length = [&](int c) { return fminf(1.0e9f, ceilf(mean * 0.25f * __builtin_amdgcn_exp2f(4.f / 15 * c))); };
+        // The parts' length and the number of workgroups with which the last of all is
+        // done first: 16 lengths between an eighth of a workgroup's mean share and four
+        // times it, each with as many workgroups as there are items, with a half and a
+        // third of that, and with their share of the work.  Four lanes to a length, in
+        // every wavefront for itself.
+        const float unit = a.tile_a >= 128 ? kTallUnit : 1.f;
+        const float mean = fmaxf(1.f, ((float)h.ua * unit + (float)h.ub) * __builtin_amdgcn_rcpf(unit * a.nwg));
+        auto length = [&](int c) { return fminf(1.0e9f, ceilf(mean * 0.125f * __builtin_amdgcn_exp2f(5.f / 15 * c))); };
         auto parts_of = [&](const Segment& g, float cost) {
             return max(1, (int)ceilf((float)(units_of(g) - kPairUnits) * __builtin_amdgcn_rcpf(cost) - 0.001f));
         };
-        const int c = lane / 4;
-        const float cost = length(c);
+        const float cost = length(lane / 4);
         float all = 0.f;
         int longest = 0;
         for (int k = lane % 4; k < a.num_groups; k += 4) {
@@ -293,14 +293,24 @@ __device__ __forceinline__ Share count_units(const SharedArgs& a, const Index& x
             all += __shfl_xor(all, o);
             longest = max(longest, __shfl_xor(longest, o));
         }
+        // the workgroups of this candidate, eight at least for each kind of work
+        const int most = h.ub > 0 ? a.nwg - 8 : a.nwg;
+        const float share = (float)h.ua * unit * a.nwg * __builtin_amdgcn_rcpf((float)h.ua * unit + (float)h.ub);
+        const float want = ceilf((lane % 4 == 3 ? share : all * __builtin_amdgcn_rcpf(1.f + lane % 4)) * 0.125f - 0.001f) * 8.f;
+        const float na = fminf(fmaxf(want, 8.f), (float)most);
+        const float rounds = ceilf(all * __builtin_amdgcn_rcpf(na) - 0.001f);
         // (rounded sums: items that would not fit are cut off well before the last slot)
-        float time = all < 0.99f * (float)a.slots_a ? ceilf(all * __builtin_amdgcn_rcpf((float)h.na) - 0.001f) * (float)(longest + kItemUnits)
-                                                    : INFINITY;
+        const float time = all < 0.99f * (float)a.slots_a
+                               ? fmaxf(rounds * ((float)longest + kItemUnits) * unit, (float)h.ub * __builtin_amdgcn_rcpf(fmaxf(a.nwg - na, 1.f)))
+                               : INFINITY;
         float best = time;
-        for (int o = 4; o < kWave; o <<= 1) best = fminf(best, __shfl_xor(best, o));
+        for (int o = 1; o < kWave; o <<= 1) best = fminf(best, __shfl_xor(best, o));
         // the longest parts of equal candidates; whole prefixes always fit
         const uint64_t equal = __ballot(time == best);
-        const float chosen = best < INFINITY ? length((63 - __clzll((long long)equal)) / 4) : 1.0e9f;
+        const int winner = 63 - __clzll((long long)equal);
+        const bool fits = best < INFINITY;
+        const float chosen = fits ? length(winner / 4) : 1.0e9f;
+        h.na = fits ? __shfl((int)na, winner) : h.ub > 0 ? a.nwg / 2 : a.nwg;
         for (int base = 0; base < a.num_groups; base += kWave) {
             const int k = base + lane;
             const Segment* g = segments + min(k, a.num_groups - 1);
@@ -310,6 +320,7 @@ __device__ __forceinline__ Share count_units(const SharedArgs& a, const Index& x
             h.items += __builtin_amdgcn_readlane(here, kWave - 1);
         }
     }
+    h.cb = (int)min((int64_t)(a.nwg - h.na), h.ub);
     __syncthreads();
     return h;
 }
