@@ -12,10 +12,12 @@
 // What bounds it: memory, 2 V bytes in and out per row.  The request's state is small
 // beside them: a bit per token tells whether a count need be read at all, so V / 4
 // bytes of bits and the counts of the few tokens that were had.  A workgroup takes
-// kSpan tokens of one request and all of its rows: state and biases become a factor
-// and a summand per token in registers, eight tokens to a thread, and a row costs a
-// compare, a select and a fused multiply-add per element; a draft changes one token's
-// summand on the way to the next row.
+// kSpan tokens of one request and all of its rows: state and biases become a bit and a
+// summand per token in registers, eight tokens to a thread; a draft changes those of
+// one token on the way to the next row.  What hides the memory's latency is the number
+// of wavefronts: counts and biases, which only a draft needs again, lie in LDS (with them
+// and the next rows in registers, four wavefronts per SIMD instead of eight, 288 rows of
+// 151936 took 60 us).  Wavefronts whose tokens nothing changes move bits.
 #include <type_traits>
 
 #include "common.h"
@@ -46,6 +48,7 @@ struct AdjustArgs {
     const int32_t* mask_rows;
     int64_t row_stride, out_stride;
     int vocab, words, total_q, num_slots, num_biases, num_masks;
+    int penal;
 };
 
 // A thread's eight logits.  WIDE: neighbours, in 16-byte loads; otherwise kThreads
@@ -110,17 +113,61 @@ template <typename T, bool WIDE> struct Group {
     }
 };
 
+// -inf where a bit of `allowed` is 0, the others' bits as they are.
+template <bool WIDE>
+__device__ __forceinline__ void mask_bits(Group<uint16_t, WIDE>& g, uint32_t allowed) {
+    auto all = [&](int e) { return (uint32_t)((int32_t)(allowed << (31 - e)) >> 31); };
+    if constexpr (WIDE) {
+        auto pair = [&](uint32_t w, int e) {
+            const uint32_t m = (all(e) & 0xffffu) | (all(e + 1) & 0xffff0000u);
+            return (w & m) | (0xff80ff80u & ~m);
+        };
+        g.v[0] = make_uint4(pair(g.v[0].x, 0), pair(g.v[0].y, 2), pair(g.v[0].z, 4), pair(g.v[0].w, 6));
+    } else {
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) g.s[e] = allowed >> e & 1u ? g.s[e] : (uint16_t)0xff80u;
+    }
+}
+template <bool WIDE>
+__device__ __forceinline__ void mask_bits(Group<float, WIDE>& g, uint32_t allowed) {
+    float v[kPer];
+    g.get(v);
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) v[e] = allowed >> e & 1u ? v[e] : -INFINITY;
+    g.set(v);
+}
+
 // Workgroup (x, i, z): tokens x kSpan .. of request i, the z-th part of its rows.
 template <typename T, bool WIDE, bool IN_PLACE>
 __global__ __launch_bounds__(kThreads) void adjust_rows(AdjustArgs a) {
     __shared__ int s_token[kThreads];
     __shared__ float s_value[kThreads];
     __shared__ int s_found[kThreads / kWave];
+    __shared__ int s_draft[kThreads];
+    __shared__ int s_mask[kThreads];
+    __shared__ int s_count[kPer][kThreads];
+    __shared__ float s_bias[kPer][kThreads];
     const int tid = threadIdx.x, i = blockIdx.y;
     const int q0 = max(0, min(a.q_start[i], a.total_q)), n = max(0, min(a.q_start[i + 1], a.total_q) - q0);
     const int part = (n + (int)gridDim.z - 1) / (int)gridDim.z;
     const int j0 = min(n, (int)blockIdx.z * part), j1 = min(n, j0 + part);
     if (j0 >= j1) return;
+    const bool penal = a.penal;
+    // the rows' drafts and masks, kThreads of them at a time
+    auto read_rows = [&](int from) {
+        const int j = from + tid;
+        s_draft[tid] = penal && j > 0 && j < n ? a.tokens[q0 + j] : -1;
+        s_mask[tid] = a.mask_rows && j < n ? a.mask_rows[q0 + j] : -1;
+    };
+    const int slot = penal ? a.slots ? a.slots[i] : i : -1;
+    const float rep = a.repetition ? a.repetition[i] : 1.f, freq = a.frequency ? a.frequency[i] : 0.f,
+                pres = a.presence ? a.presence[i] : 0.f;
+    const int b0 = a.bias_start ? max(0, min(a.bias_start[i], a.num_biases)) : 0;
+    const int b1 = a.bias_start ? min(a.bias_start[i + 1], a.num_biases) : 0;
+    int rows0 = j0;  // the row of the first entry in s_draft
+    read_rows(rows0);
+    __syncthreads();
+    const float inv = 1.f / rep;
     const int span0 = blockIdx.x * kSpan;
     const int tok0 = span0 + (WIDE ? tid * kPer : tid);
     auto token = [&](int e) { return tok0 + (WIDE ? e : e * kThreads); };
@@ -137,39 +184,49 @@ __global__ __launch_bounds__(kThreads) void adjust_rows(AdjustArgs a) {
         return b;
     };
 
+    const T* in = static_cast<const T*>(a.logits) + (int64_t)q0 * a.row_stride;
+    T* to = static_cast<T*>(a.out) + (int64_t)q0 * a.out_stride;
+    // The next rows' masks and logits.  What a mask lacks whole need not be read; in
+    // place, neither need what nothing changes (`touched`, a bit per row).
+    Group<T, WIDE> g[kRows];
+    uint32_t allowed[kRows];
+    auto load_masks = [&](int base) {
+#pragma unroll
+        for (int x = 0; x < kRows; ++x) {
+            allowed[x] = 0xffu;
+            if (a.mask_rows && base + x < j1) {
+                const int m = s_mask[base + x - rows0];
+                if (m >= 0 && m < a.num_masks) allowed[x] = bits_of(a.mask + (int64_t)m * a.words * 4);
+            }
+        }
+    };
+    auto load_rows = [&](int base, uint32_t touched) {
+#pragma unroll
+        for (int x = 0; x < kRows; ++x)
+            if (base + x < j1 && live && allowed[x] && (!IN_PLACE || (touched >> x & 1u) || allowed[x] != 0xffu))
+                g[x].load(in + (int64_t)(base + x) * a.row_stride, tok0, room);
+    };
+    // Out of place the first rows are under way before the state that changes them is
+    // read: a chain of four or five memory latencies.
+    load_masks(j0);
+    if (!IN_PLACE) load_rows(j0, 0);
+
+    // a token of this span: its thread, and its place among that thread's
+    auto owner = [&](int d) { return WIDE ? (d - span0) / kPer : (d - span0) % kThreads; };
+    auto place = [&](int d) { return WIDE ? (d - span0) % kPer : (d - span0) / kThreads; };
     // the request's state: tokens had (a bit each), their counts, biases
     uint32_t had = 0, biased = 0;
-    int32_t c[kPer];
-    float bias[kPer];
+    float add[kPer];  // -0: a sum's neutral element
 #pragma unroll
-    for (int e = 0; e < kPer; ++e) c[e] = 0, bias[e] = -0.f;  // -0: a sum's neutral element
-    const bool penal = a.counts != nullptr;
-    float rep = 1.f, inv = 1.f, freq = 0.f, pres = 0.f;
-    if (penal) {
-        if (a.repetition) rep = a.repetition[i], inv = 1.f / rep;
-        if (a.frequency) freq = a.frequency[i];
-        if (a.presence) pres = a.presence[i];
-        const int slot = a.slots ? a.slots[i] : i;
-        if (slot >= 0 && slot < a.num_slots) {
-            const uint8_t* seen = a.seen + (int64_t)slot * 2 * a.words * 4;
-            const uint32_t prompt = bits_of(seen), out = bits_of(seen + (int64_t)a.words * 4);
-            if (out) {
-                const int32_t* counts = a.counts + (int64_t)slot * a.vocab;
+    for (int e = 0; e < kPer; ++e) add[e] = -0.f;
+    if (b1 > b0) {
 #pragma unroll
-                for (int e = 0; e < kPer; ++e)
-                    if ((out >> e & 1u) && token(e) < a.vocab) c[e] = max(0, counts[token(e)]);
-            }
-            had = prompt;
-#pragma unroll
-            for (int e = 0; e < kPer; ++e) had |= (uint32_t)(c[e] > 0) << e;
-        }
-    }
-    if (a.bias_start) {
+        for (int e = 0; e < kPer; ++e) s_bias[e][tid] = -0.f;
         // the list's entries of this span, kThreads of the list at a time, in its order
-        const int b0 = max(0, min(a.bias_start[i], a.num_biases)), b1 = min(a.bias_start[i + 1], a.num_biases);
         for (int base = b0; base < b1; base += kThreads) {
             const int at = base + tid, tok = at < b1 ? a.bias_tokens[at] : -1;
             const bool here = tok >= span0 && tok - span0 < kSpan && tok < a.vocab;
+            if (!__syncthreads_or(here)) continue;
             const uint64_t vote = __ballot(here);
             if (tid % kWave == 0) s_found[tid / kWave] = __popcll(vote);
             __syncthreads();
@@ -187,90 +244,105 @@ __global__ __launch_bounds__(kThreads) void adjust_rows(AdjustArgs a) {
             __syncthreads();
             for (int p = 0; p < all; ++p) {
                 const int d = s_token[p];
-#pragma unroll
-                for (int e = 0; e < kPer; ++e)
-                    if (d == token(e)) bias[e] += s_value[p], biased |= 1u << e;
+                if (owner(d) == tid) s_bias[place(d)][tid] += s_value[p], biased |= 1u << place(d);
             }
-            __syncthreads();
+        }
+        if (biased) {
+#pragma unroll
+            for (int e = 0; e < kPer; ++e) add[e] = s_bias[e][tid];
         }
     }
-    // token e: x becomes fma(x, x > 0 ? up[e] : down[e], add[e])
-    float up[kPer], down[kPer], add[kPer];
-    auto settle = [&](int e) {
-        up[e] = had >> e & 1u ? inv : 1.f;
-        down[e] = had >> e & 1u ? rep : 1.f;
-        add[e] = bias[e];
-        if (c[e] > 0) add[e] -= fmaf(freq, (float)c[e], pres);
-    };
+    if (penal) {
+        uint32_t prompt = 0, out = 0;
+        const int32_t* counts = nullptr;
+        if (slot >= 0 && slot < a.num_slots) {
+            const uint8_t* seen = a.seen + (int64_t)slot * 2 * a.words * 4;
+            counts = a.counts + (int64_t)slot * a.vocab;
+            prompt = bits_of(seen);
+            out = bits_of(seen + (int64_t)a.words * 4);
+        }
+        had = prompt;
 #pragma unroll
-    for (int e = 0; e < kPer; ++e) settle(e);
-    // the draft that row j stands behind (no draft: -1)
-    auto draft = [&](int j) {
-        const int d = j > 0 ? a.tokens[q0 + j] : -1;
-        if (d < span0 || d - span0 >= kSpan || d >= a.vocab) return;
+        for (int e = 0; e < kPer; ++e) s_count[e][tid] = 0;
+        if (out) {
+            int c[kPer];
 #pragma unroll
-        for (int e = 0; e < kPer; ++e)
-            if (d == token(e)) {
-                ++c[e];
-                had |= 1u << e;
-                settle(e);
+            for (int e = 0; e < kPer; ++e) c[e] = (out >> e & 1u) && token(e) < a.vocab ? max(0, counts[token(e)]) : 0;
+#pragma unroll
+            for (int e = 0; e < kPer; ++e) {
+                s_count[e][tid] = c[e];
+                had |= (uint32_t)(c[e] > 0) << e;
+                if (c[e] > 0) add[e] -= fmaf(freq, (float)c[e], pres);
             }
+        }
+    }
+    // the draft that row j stands behind, or -1 where it is none of this span's tokens
+    auto in_span = [&](int d) { return d >= span0 && d - span0 < kSpan && d < a.vocab ? d : -1; };
+    auto draft_of = [&](int j) {
+        const int d = __builtin_amdgcn_readfirstlane(j < j1 ? s_draft[j - rows0] : -1);
+        return in_span(d);
     };
-    if (penal)
-        for (int j = 1; j < j0; ++j) draft(j);
+    auto count_draft = [&](int d) {
+        if (d < 0 || owner(d) != tid) return;
+        const int e = place(d), c = ++s_count[e][tid];
+        const float bias = biased >> e & 1u ? s_bias[e][tid] : -0.f, sum = bias - fmaf(freq, (float)c, pres);
+        had |= 1u << e;
+#pragma unroll
+        for (int n = 0; n < kPer; ++n) add[n] = n == e ? sum : add[n];
+    };
+    if (penal) {
+        // the drafts in front of this part's rows
+        for (int from = 1; from < j0; from += kThreads) {
+            const int d = from + tid < j0 ? a.tokens[q0 + from + tid] : -1;
+            __syncthreads();
+            s_token[tid] = d;
+            __syncthreads();
+            for (int j = 0; j < min(kThreads, j0 - from); ++j) count_draft(in_span(s_token[j]));
+        }
+    }
 
-    const T* in = static_cast<const T*>(a.logits) + (int64_t)q0 * a.row_stride;
-    T* to = static_cast<T*>(a.out) + (int64_t)q0 * a.out_stride;
     for (int base = j0; base < j1; base += kRows) {
-        Group<T, WIDE> g[kRows];
-        uint32_t allowed[kRows];
-        // In place a group that nothing changes is neither read nor written.  The
-        // drafts of these rows may change it: those rows' groups are read too.
-        uint32_t coming = 0;
-        if (IN_PLACE && penal) {
-            uint32_t had_by = 0;
+        int draft[kRows];
+#pragma unroll
+        for (int x = 0; x < kRows; ++x) draft[x] = draft_of(base + x);
+        if (IN_PLACE || base > j0) {
+            uint32_t touched = had | biased ? ~0u : 0u, mine = 0;
 #pragma unroll
             for (int x = 0; x < kRows; ++x) {
-                const int j = base + x, d = j > 0 && j < j1 ? a.tokens[q0 + j] : -1;
-#pragma unroll
-                for (int e = 0; e < kPer; ++e) had_by |= d == token(e) && d < a.vocab;
-                coming |= had_by << x;
+                if (IN_PLACE && draft[x] >= 0) mine |= owner(draft[x]) == tid;
+                touched |= mine << x;
             }
-        }
-#pragma unroll
-        for (int x = 0; x < kRows; ++x) {
-            const int j = base + x;
-            allowed[x] = 0xffu;
-            if (a.mask_rows && j < j1) {
-                const int m = a.mask_rows[q0 + j];
-                if (m >= 0 && m < a.num_masks) allowed[x] = bits_of(a.mask + (int64_t)m * a.words * 4);
-            }
-        }
-#pragma unroll
-        for (int x = 0; x < kRows; ++x) {
-            const int j = base + x;
-            // what is masked whole need not be read
-            const bool changed = !IN_PLACE || had || biased || allowed[x] != 0xffu || (coming >> x & 1u);
-            if (j < j1 && live && allowed[x] && changed) g[x].load(in + (int64_t)j * a.row_stride, tok0, room);
+            load_rows(base, touched);
         }
 #pragma unroll
         for (int x = 0; x < kRows; ++x) {
             const int j = base + x;
             if (j >= j1) break;
-            if (penal) draft(j);
-            const bool changed = had || biased || allowed[x] != 0xffu;
-            if (changed) {
-                float v[kPer];
-                if (allowed[x]) g[x].get(v);
+            count_draft(draft[x]);
+            const bool change = had || biased, masked = allowed[x] != 0xffu;
+            if (__any(change)) {
+                if (change && allowed[x]) {
+                    float v[kPer];
+                    g[x].get(v);
 #pragma unroll
-                for (int e = 0; e < kPer; ++e) {
-                    const float y = fmaf(v[e], v[e] > 0.f ? up[e] : down[e], add[e]);
-                    v[e] = allowed[x] >> e & 1u ? y : -INFINITY;
+                    for (int e = 0; e < kPer; ++e) {
+                        const float f = v[e] > 0.f ? inv : rep;
+                        v[e] = fmaf(v[e], had >> e & 1u ? f : 1.f, add[e]);
+                    }
+                    g[x].set(v);
                 }
-                g[x].set(v);
             }
-            if (live && (!IN_PLACE || changed)) g[x].store(to + (int64_t)j * a.out_stride, tok0, room);
+            if (masked) mask_bits(g[x], allowed[x]);
+            if (live && (!IN_PLACE || change || masked)) g[x].store(to + (int64_t)j * a.out_stride, tok0, room);
         }
+        if (base + kRows >= j1) break;
+        if (base + 2 * kRows > rows0 + kThreads) {  // the next rows' entries are not all here
+            __syncthreads();
+            rows0 = base + kRows;
+            read_rows(rows0);
+            __syncthreads();
+        }
+        load_masks(base + kRows);
     }
 }
 
@@ -341,6 +413,7 @@ extern "C" int verify_adjust_logits(int32_t num_seqs, int32_t total_q, int64_t v
     a.tokens = tokens;
     a.q_start = q_start;
     if (penal) {
+        a.penal = 1;
         a.repetition = params->repetition;
         a.frequency = params->frequency;
         a.presence = params->presence;

@@ -85,6 +85,7 @@ CASES = [
     ([2, 2], 4104, dict(penalties="", biases=600)),
     ([17, 1, 2, 6], 20000, dict(penalties="f", special=True)),
     ([70], 6000, dict(penalties="rp", history=2000, masks=True)),   # rows divided over workgroups
+    ([700, 3], 2500, dict(penalties="rfp", biases=4, masks=True)),  # more rows than a workgroup keeps entries of
     ([1] * 40, 2056, dict(biases=5)),
     ([4, 3], 30000, dict(penalties="r", history=0)),
 ]
