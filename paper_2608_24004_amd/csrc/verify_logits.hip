@@ -51,85 +51,64 @@ struct AdjustArgs {
     int penal;
 };
 
-// A thread's eight logits.  WIDE: neighbours, in 16-byte loads; otherwise kThreads
-// apart, so that a wavefront's lanes are neighbours whatever a row's alignment.
-template <typename T, bool WIDE> struct Group {
-    static constexpr int kVecs = kPer * (int)sizeof(T) / 16;
-    uint4 v[WIDE ? kVecs : 1];
-    T s[WIDE ? 1 : kPer];
+// A thread's eight logits, neighbours, in 16-byte accesses that need only be aligned to
+// an element (rows of an odd vocabulary).
+typedef uint32_t u32x4_2 __attribute__((ext_vector_type(4), aligned(2)));
+typedef uint32_t u32x4_4 __attribute__((ext_vector_type(4), aligned(4)));
+template <typename T> struct Group {
+    using Vec = std::conditional_t<sizeof(T) == 2, u32x4_2, u32x4_4>;
+    static constexpr int kVecs = kPer * (int)sizeof(T) / 16, kIn = 16 / (int)sizeof(T);
+    uint4 v[kVecs];
 
-    // tokens from `room` on are behind the vocabulary
-    __device__ __forceinline__ void load(const T* row, int tok, int room) {
-        if constexpr (WIDE) {
-            if (room >= kPer) {
+    // `room` of the eight are in the vocabulary
+    __device__ __forceinline__ void load(const T* at, int room) {
+        if (room >= kPer) {
 #pragma unroll
-                for (int k = 0; k < kVecs; ++k) v[k] = ld16_stream(row + tok + k * (16 / (int)sizeof(T)));
-            } else {
-                T t[kPer] = {};
-#pragma unroll
-                for (int e = 0; e < kPer; ++e) if (e < room) t[e] = row[tok + e];
-                __builtin_memcpy(v, t, sizeof(t));
+            for (int k = 0; k < kVecs; ++k) {
+                const Vec x = __builtin_nontemporal_load(reinterpret_cast<const Vec*>(at + k * kIn));
+                v[k] = make_uint4(x.x, x.y, x.z, x.w);
             }
         } else {
+            T t[kPer] = {};
 #pragma unroll
-            for (int e = 0; e < kPer; ++e) if (tok + e * kThreads < room) s[e] = row[tok + e * kThreads];
+            for (int e = 0; e < kPer; ++e) if (e < room) t[e] = at[e];
+            __builtin_memcpy(v, t, sizeof(t));
         }
     }
-    __device__ __forceinline__ void store(T* row, int tok, int room) const {
-        if constexpr (WIDE) {
-            if (room >= kPer) {
+    __device__ __forceinline__ void store(T* at, int room) const {
+        if (room >= kPer) {
 #pragma unroll
-                for (int k = 0; k < kVecs; ++k) reinterpret_cast<uint4*>(row + tok)[k] = v[k];
-            } else {
-                T t[kPer];
-                __builtin_memcpy(t, v, sizeof(t));
-#pragma unroll
-                for (int e = 0; e < kPer; ++e) if (e < room) row[tok + e] = t[e];
-            }
+            for (int k = 0; k < kVecs; ++k) *reinterpret_cast<Vec*>(at + k * kIn) = Vec{v[k].x, v[k].y, v[k].z, v[k].w};
         } else {
+            T t[kPer];
+            __builtin_memcpy(t, v, sizeof(t));
 #pragma unroll
-            for (int e = 0; e < kPer; ++e) if (tok + e * kThreads < room) row[tok + e * kThreads] = s[e];
+            for (int e = 0; e < kPer; ++e) if (e < room) at[e] = t[e];
         }
     }
     __device__ __forceinline__ void get(float* x) const {
-        if constexpr (WIDE) {
 #pragma unroll
-            for (int k = 0; k < kVecs; ++k) unpack16(v[k], x + k * (16 / (int)sizeof(T)), T{});
-        } else {
-#pragma unroll
-            for (int e = 0; e < kPer; ++e) x[e] = Storage<T>::load(s, e);
-        }
+        for (int k = 0; k < kVecs; ++k) unpack16(v[k], x + k * kIn, T{});
     }
     __device__ __forceinline__ void set(const float* x) {
-        if constexpr (WIDE && sizeof(T) == 2) {
+        if constexpr (sizeof(T) == 2)
             v[0] = make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]),
                               pack_bf16x2(x[6], x[7]));
-        } else if constexpr (WIDE) {
+        else
             __builtin_memcpy(v, x, kPer * sizeof(float));
-        } else {
-#pragma unroll
-            for (int e = 0; e < kPer; ++e) Storage<T>::store(s, e, x[e]);
-        }
     }
 };
 
 // -inf where a bit of `allowed` is 0, the others' bits as they are.
-template <bool WIDE>
-__device__ __forceinline__ void mask_bits(Group<uint16_t, WIDE>& g, uint32_t allowed) {
+__device__ __forceinline__ void mask_bits(Group<uint16_t>& g, uint32_t allowed) {
     auto all = [&](int e) { return (uint32_t)((int32_t)(allowed << (31 - e)) >> 31); };
-    if constexpr (WIDE) {
-        auto pair = [&](uint32_t w, int e) {
-            const uint32_t m = (all(e) & 0xffffu) | (all(e + 1) & 0xffff0000u);
-            return (w & m) | (0xff80ff80u & ~m);
-        };
-        g.v[0] = make_uint4(pair(g.v[0].x, 0), pair(g.v[0].y, 2), pair(g.v[0].z, 4), pair(g.v[0].w, 6));
-    } else {
-#pragma unroll
-        for (int e = 0; e < kPer; ++e) g.s[e] = allowed >> e & 1u ? g.s[e] : (uint16_t)0xff80u;
-    }
+    auto pair = [&](uint32_t w, int e) {
+        const uint32_t m = (all(e) & 0xffffu) | (all(e + 1) & 0xffff0000u);
+        return (w & m) | (0xff80ff80u & ~m);
+    };
+    g.v[0] = make_uint4(pair(g.v[0].x, 0), pair(g.v[0].y, 2), pair(g.v[0].z, 4), pair(g.v[0].w, 6));
 }
-template <bool WIDE>
-__device__ __forceinline__ void mask_bits(Group<float, WIDE>& g, uint32_t allowed) {
+__device__ __forceinline__ void mask_bits(Group<float>& g, uint32_t allowed) {
     float v[kPer];
     g.get(v);
 #pragma unroll
@@ -138,7 +117,7 @@ __device__ __forceinline__ void mask_bits(Group<float, WIDE>& g, uint32_t allowe
 }
 
 // Workgroup (x, i, z): tokens x kSpan .. of request i, the z-th part of its rows.
-template <typename T, bool WIDE, bool IN_PLACE>
+template <typename T, bool IN_PLACE>
 __global__ __launch_bounds__(kThreads) void adjust_rows(AdjustArgs a) {
     __shared__ int s_token[kThreads];
     __shared__ float s_value[kThreads];
@@ -169,26 +148,16 @@ __global__ __launch_bounds__(kThreads) void adjust_rows(AdjustArgs a) {
     __syncthreads();
     const float inv = 1.f / rep;
     const int span0 = blockIdx.x * kSpan;
-    const int tok0 = span0 + (WIDE ? tid * kPer : tid);
-    auto token = [&](int e) { return tok0 + (WIDE ? e : e * kThreads); };
-    const int room = WIDE ? a.vocab - tok0 : a.vocab;  // Group's bound
-    const bool live = tok0 < a.vocab;
-    // eight bits of a bit array, bit e for token(e); bits behind the vocabulary are 0
-    auto bits_of = [&](const uint8_t* bits) -> uint32_t {
-        if (!live) return 0;
-        if constexpr (WIDE) return bits[tok0 >> 3];
-        uint32_t b = 0;
-#pragma unroll
-        for (int e = 0; e < kPer; ++e)
-            if (token(e) < a.vocab) b |= (bits[token(e) >> 3] >> (token(e) & 7) & 1u) << e;
-        return b;
-    };
+    const int tok0 = span0 + tid * kPer, room = a.vocab - tok0;
+    const bool live = room > 0;
+    // the eight bits of a bit array
+    auto bits_of = [&](const uint8_t* bits) -> uint32_t { return live ? bits[tok0 >> 3] : 0; };
 
     const T* in = static_cast<const T*>(a.logits) + (int64_t)q0 * a.row_stride;
     T* to = static_cast<T*>(a.out) + (int64_t)q0 * a.out_stride;
     // The next rows' masks and logits.  What a mask lacks whole need not be read; in
     // place, neither need what nothing changes (`touched`, a bit per row).
-    Group<T, WIDE> g[kRows];
+    Group<T> g[kRows];
     uint32_t allowed[kRows];
     auto load_masks = [&](int base) {
 #pragma unroll
@@ -204,7 +173,7 @@ __global__ __launch_bounds__(kThreads) void adjust_rows(AdjustArgs a) {
 #pragma unroll
         for (int x = 0; x < kRows; ++x)
             if (base + x < j1 && live && allowed[x] && (!IN_PLACE || (touched >> x & 1u) || allowed[x] != 0xffu))
-                g[x].load(in + (int64_t)(base + x) * a.row_stride, tok0, room);
+                g[x].load(in + (int64_t)(base + x) * a.row_stride + tok0, room);
     };
     // Out of place the first rows are under way before the state that changes them is
     // read: a chain of four or five memory latencies.
@@ -212,8 +181,8 @@ __global__ __launch_bounds__(kThreads) void adjust_rows(AdjustArgs a) {
     if (!IN_PLACE) load_rows(j0, 0);
 
     // a token of this span: its thread, and its place among that thread's
-    auto owner = [&](int d) { return WIDE ? (d - span0) / kPer : (d - span0) % kThreads; };
-    auto place = [&](int d) { return WIDE ? (d - span0) % kPer : (d - span0) / kThreads; };
+    auto owner = [&](int d) { return (d - span0) / kPer; };
+    auto place = [&](int d) { return (d - span0) % kPer; };
     // the request's state: tokens had (a bit each), their counts, biases
     uint32_t had = 0, biased = 0;
     float add[kPer];  // -0: a sum's neutral element
@@ -267,7 +236,7 @@ __global__ __launch_bounds__(kThreads) void adjust_rows(AdjustArgs a) {
         if (out) {
             int c[kPer];
 #pragma unroll
-            for (int e = 0; e < kPer; ++e) c[e] = (out >> e & 1u) && token(e) < a.vocab ? max(0, counts[token(e)]) : 0;
+            for (int e = 0; e < kPer; ++e) c[e] = (out >> e & 1u) && e < room ? max(0, counts[tok0 + e]) : 0;
 #pragma unroll
             for (int e = 0; e < kPer; ++e) {
                 s_count[e][tid] = c[e];
@@ -333,7 +302,7 @@ __global__ __launch_bounds__(kThreads) void adjust_rows(AdjustArgs a) {
                 }
             }
             if (masked) mask_bits(g[x], allowed[x]);
-            if (live && (!IN_PLACE || change || masked)) g[x].store(to + (int64_t)j * a.out_stride, tok0, room);
+            if (live && (!IN_PLACE || change || masked)) g[x].store(to + (int64_t)j * a.out_stride + tok0, room);
         }
         if (base + kRows >= j1) break;
         if (base + 2 * kRows > rows0 + kThreads) {  // the next rows' entries are not all here
@@ -375,10 +344,10 @@ __global__ __launch_bounds__(kThreads) void count_tokens(CountArgs a) {
     }
 }
 
-template <typename T, bool IN_PLACE>
-void launch_adjust(const AdjustArgs& a, const dim3& grid, bool wide, hipStream_t stream) {
-    if (wide) hipLaunchKernelGGL((adjust_rows<T, true, IN_PLACE>), grid, dim3(kThreads), 0, stream, a);
-    else hipLaunchKernelGGL((adjust_rows<T, false, IN_PLACE>), grid, dim3(kThreads), 0, stream, a);
+template <typename T>
+void launch_adjust(const AdjustArgs& a, const dim3& grid, hipStream_t stream) {
+    if (a.logits == a.out) hipLaunchKernelGGL((adjust_rows<T, true>), grid, dim3(kThreads), 0, stream, a);
+    else hipLaunchKernelGGL((adjust_rows<T, false>), grid, dim3(kThreads), 0, stream, a);
 }
 
 }  // namespace
@@ -405,8 +374,7 @@ extern "C" int verify_adjust_logits(int32_t num_seqs, int32_t total_q, int64_t v
     if (params->num_slots < 0 || params->num_biases < 0 || params->num_masks < 0) return VERIFY_EINVAL;
     if (num_seqs == 0 || total_q == 0) return VERIFY_OK;
     if (!logits || !out || !q_start) return VERIFY_EINVAL;
-    const bool in_place = logits == out;
-    if (in_place && row_stride != out_stride) return VERIFY_EINVAL;
+    if (logits == out && row_stride != out_stride) return VERIFY_EINVAL;
     AdjustArgs a{};
     a.logits = logits;
     a.out = out;
@@ -442,12 +410,8 @@ extern "C" int verify_adjust_logits(int32_t num_seqs, int32_t total_q, int64_t v
     const int64_t spans = (vocab + kSpan - 1) / kSpan, wgs = spans * num_seqs, rows = (total_q + num_seqs - 1) / num_seqs;
     const int64_t parts = std::max<int64_t>(1, std::min<int64_t>({(1024 + wgs - 1) / wgs, rows, 65535}));
     const dim3 grid((unsigned)spans, (unsigned)num_seqs, (unsigned)parts);
-    const int esize = logits_dtype == VERIFY_BF16 ? 2 : 4, n = 16 / esize;
-    const bool wide = (((uintptr_t)logits | (uintptr_t)out) & 15) == 0 && row_stride % n == 0 && out_stride % n == 0;
-    if (logits_dtype == VERIFY_BF16)
-        in_place ? launch_adjust<uint16_t, true>(a, grid, wide, stream) : launch_adjust<uint16_t, false>(a, grid, wide, stream);
-    else
-        in_place ? launch_adjust<float, true>(a, grid, wide, stream) : launch_adjust<float, false>(a, grid, wide, stream);
+    if (logits_dtype == VERIFY_BF16) launch_adjust<uint16_t>(a, grid, stream);
+    else launch_adjust<float>(a, grid, stream);
     return check_launch();
 }
 
