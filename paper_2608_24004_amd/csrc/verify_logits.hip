@@ -325,8 +325,9 @@ struct CountArgs {
     int vocab, words, total, num_slots, prompt;
 };
 
-// Workgroup (x, i): request i's tokens, kThreads at a time.  Integer sums and bits:
-// the order in which they arrive changes nothing.
+// Integer sums and bits: the order in which they arrive changes nothing.
+//
+// Workgroup (x, i): request i's tokens, kThreads at a time.
 __global__ __launch_bounds__(kThreads) void count_tokens(CountArgs a) {
     const int i = blockIdx.y;
     const int slot = a.slots ? a.slots[i] : i;
@@ -342,6 +343,46 @@ __global__ __launch_bounds__(kThreads) void count_tokens(CountArgs a) {
         if (!a.prompt) atomicAdd(counts + tok, 1);
         atomicOr(seen + (tok >> 5), 1u << (tok & 31));
     }
+}
+
+// The same for many tokens of a request, kPart at a time: text has the same few words of
+// bits again and again, and thousands of atomic operations on one word of memory come
+// one after the other (64 thousand tokens of eight prompts: 58 us).  So the bits are
+// gathered in LDS, where a set bit costs a read, and each word that got some leaves once.
+constexpr int kManyThreads = 512;
+constexpr int kPart = 4096;
+constexpr int kManyWords = 16384;  // LDS: a vocabulary of 524288
+__global__ __launch_bounds__(kManyThreads) void count_many(CountArgs a) {
+    extern __shared__ uint32_t s_bits[];
+    const int i = blockIdx.y, tid = threadIdx.x;
+    const int slot = a.slots ? a.slots[i] : i;
+    const int t0 = max(0, min(a.start[i], a.total));
+    int n = max(0, min(a.start[i + 1], a.total) - t0);
+    if (a.num) n = min(n, a.num[i]);
+    if (slot < 0 || slot >= a.num_slots || (int64_t)blockIdx.x * kPart >= n) return;
+    for (int w = tid; w < a.words; w += kManyThreads) s_bits[w] = 0;
+    __syncthreads();
+    int32_t* counts = a.counts + (int64_t)slot * a.vocab;
+    for (int64_t part = (int64_t)blockIdx.x * kPart; part < n; part += (int64_t)gridDim.x * kPart) {
+        int tok[kPart / kManyThreads];
+#pragma unroll
+        for (int x = 0; x < kPart / kManyThreads; ++x) {
+            const int64_t j = part + x * kManyThreads + tid;
+            tok[x] = j < n ? a.tokens[t0 + j] : -1;
+        }
+#pragma unroll
+        for (int x = 0; x < kPart / kManyThreads; ++x) {
+            if (tok[x] < 0 || tok[x] >= a.vocab) continue;
+            if (!a.prompt) atomicAdd(counts + tok[x], 1);
+            const uint32_t bit = 1u << (tok[x] & 31);
+            volatile uint32_t* word = s_bits + (tok[x] >> 5);
+            if (!(*word & bit)) atomicOr(s_bits + (tok[x] >> 5), bit);
+        }
+    }
+    __syncthreads();
+    uint32_t* seen = a.seen + ((int64_t)slot * 2 + (a.prompt ? 0 : 1)) * a.words;
+    for (int w = tid; w < a.words; w += kManyThreads)
+        if (s_bits[w]) atomicOr(seen + w, s_bits[w]);
 }
 
 template <typename T>
@@ -426,7 +467,14 @@ extern "C" int verify_count_tokens(int32_t num_seqs, int32_t total_tokens, int64
     const CountArgs a{counts, seen, tokens, token_start, num_tokens, slots, (int)vocab, (int)((vocab + 31) / 32),
                       total_tokens, num_slots, prompt};
     const int64_t per = ((int64_t)total_tokens + num_seqs - 1) / num_seqs;
-    const dim3 grid((unsigned)std::min<int64_t>((per + kThreads - 1) / kThreads, 256), (unsigned)num_seqs);
-    hipLaunchKernelGGL(count_tokens, grid, dim3(kThreads), 0, stream, a);
+    // from where clearing and reading the words costs less than the atomic operations
+    if (per >= 512 && a.words <= kManyWords) {
+        const dim3 grid((unsigned)std::min<int64_t>((total_tokens + kPart - 1) / kPart, std::max(1, 1024 / num_seqs)),
+                        (unsigned)num_seqs);
+        hipLaunchKernelGGL(count_many, grid, dim3(kManyThreads), a.words * 4, stream, a);
+    } else {
+        const dim3 grid((unsigned)std::min<int64_t>((per + kThreads - 1) / kThreads, 256), (unsigned)num_seqs);
+        hipLaunchKernelGGL(count_tokens, grid, dim3(kThreads), 0, stream, a);
+    }
     return check_launch();
 }
