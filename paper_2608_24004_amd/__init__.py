@@ -807,7 +807,13 @@ def _rotary_args(q, positions, inv_freq, axes, interleaved, scale, idx, dev):
         raise ValueError("axes must name the axis of each of the %d frequencies" % F)
     p_pos = _arg(positions, "positions", (T,) if positions.dim() == 1 else (num_axes, T), torch.int32, idx, dev)
     p_freq = _arg(inv_freq, "inv_freq", None, torch.float64, idx, dev)
-    key = (D, F, num_axes, bool(interleaved), float(scale), q.dtype, None if axes is None else tuple(axes))
+    try:
+        # of the usual 64 small numbers a string of bytes is made, hashed and compared in
+        # half of a tuple's time
+        turned = None if axes is None else bytes(axes)
+    except (TypeError, ValueError):
+        turned = tuple(axes)
+    key = (D, F, num_axes, bool(interleaved), float(scale), q.dtype, turned)
     params = _rotary_params.get(key)
     if params is None:
         axes = (0,) * F if axes is None else axes
@@ -981,33 +987,28 @@ def verify_adjust_logits(logits, tokens, q_start, *, counts=None, seen=None, slo
     p_logits, stride = _row_matrix(logits, "logits", (T, V), dtype, idx, dev)
     p_qs = _arg(q_start, "q_start", None, i32, idx, dev)
     p_tok = None if tokens is None else _arg(tokens, "tokens", (T,), i32, idx, dev)
-    params = AdjustParams()
+    state, bias, masks = (None,) * 6 + (0,), (None,) * 3 + (0,), (0, None, None)
     if repetition is not None or frequency is not None or presence is not None:
         if counts is None or seen is None or tokens is None:
             raise ValueError("a penalty needs counts, seen and tokens")
-        if repetition is not None:
-            params.repetition = _arg(repetition, "repetition", (B,), f32, idx, dev)
-        if frequency is not None:
-            params.frequency = _arg(frequency, "frequency", (B,), f32, idx, dev)
-        if presence is not None:
-            params.presence = _arg(presence, "presence", (B,), f32, idx, dev)
-        params.counts, params.seen, params.slots, params.num_slots = _token_state(counts, seen, slots, V, B, idx, dev)
+        state = (None if repetition is None else _arg(repetition, "repetition", (B,), f32, idx, dev),
+                 None if frequency is None else _arg(frequency, "frequency", (B,), f32, idx, dev),
+                 None if presence is None else _arg(presence, "presence", (B,), f32, idx, dev),
+                 *_token_state(counts, seen, slots, V, B, idx, dev))
     if bias_start is not None:
-        params.bias_start = _arg(bias_start, "bias_start", (B + 1,), i32, idx, dev)
         if bias_tokens is None or bias_values is None or bias_tokens.dim() != 1:
             raise ValueError("bias_start needs bias_tokens and bias_values of one dim")
         m = bias_tokens.shape[0]
-        params.bias_tokens = _arg(bias_tokens, "bias_tokens", None, i32, idx, dev)
-        params.bias_values = _arg(bias_values, "bias_values", (m,), f32, idx, dev)
-        params.num_biases = m
+        bias = (_arg(bias_start, "bias_start", (B + 1,), i32, idx, dev),
+                _arg(bias_tokens, "bias_tokens", None, i32, idx, dev),
+                _arg(bias_values, "bias_values", (m,), f32, idx, dev), m)
     elif bias_tokens is not None or bias_values is not None:
         raise ValueError("bias_tokens and bias_values need bias_start")
     if mask_rows is not None:
         if mask is None or mask.dim() != 2:
             raise ValueError("mask_rows needs mask [M, ceil(V / 32)]")
-        params.mask_rows = _arg(mask_rows, "mask_rows", (T,), i32, idx, dev)
-        params.mask = _arg(mask, "mask", (mask.shape[0], (V + 31) // 32), i32, idx, dev)
-        params.num_masks = mask.shape[0]
+        masks = (mask.shape[0], _arg(mask, "mask", (mask.shape[0], (V + 31) // 32), i32, idx, dev),
+                 _arg(mask_rows, "mask_rows", (T,), i32, idx, dev))
     elif mask is not None:
         raise ValueError("mask needs mask_rows")
     if check or check is None and CHECK_BY_DEFAULT:
@@ -1017,8 +1018,8 @@ def verify_adjust_logits(logits, tokens, q_start, *, counts=None, seen=None, slo
     p_out, out_stride = _row_matrix(out, "out", (T, V), dtype, idx, dev)
     if idx < 0:
         _dev_ptr(logits, "logits")
-    _launch("verify_adjust_logits", idx, B, T, V, stride, code, p_logits, p_tok, p_qs, ctypes.byref(params), p_out,
-            out_stride, _stream_ptr(stream, dev))
+    _launch("verify_adjust_logits", idx, B, T, V, stride, code, p_logits, p_tok, p_qs,
+            ctypes.byref(AdjustParams(*state, *bias, *masks)), p_out, out_stride, _stream_ptr(stream, dev))
     return out
 
 
@@ -1090,7 +1091,7 @@ def verify_attention_shared(q, k_cache, v_cache, block_tables, seq_lens, q_start
     if check or check is None and CHECK_BY_DEFAULT:
         _checked(check, "verify_attention_shared", q_start=q_start, total_q=T, max_q_len=max_q_len, seq_lens=seq_lens,
                  block_tables=block_tables, num_blocks=k_cache.shape[0], max_seq_len=max_seq_len, stream=stream)
-    params.scale = float(scale)
+    params.scale = scale
     bounds = T, int(max_q_len), int(max_seq_len), G, int(max_prefix_len)
     if out is None:
         out = _scratch((T, Hq, D), dtype, dev, stream)

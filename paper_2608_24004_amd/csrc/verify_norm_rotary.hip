@@ -9,10 +9,14 @@
 // The threads of a head are neighbours in a wavefront, each with a chunk of 16 bytes and
 // the chunk of its dims' partners, so that a head's sum of squares takes a few exchanges
 // between lanes and no memory.  A thread keeps the weights of its dims for all the heads
-// that it takes.  Loads leave before the angles are computed.
+// that it takes, multiplied into the sine and cosine of its row: a matrix per pair that
+// is the same for all heads.  Loads leave before the angles are computed.
 //
-// What bounds it: memory above a few thousand rows; below, a launch and the latencies of
-// positions, rows and, for the append, of q_start, the request's length and block ids.
+// What bounds it: memory above a few thousand rows (5461 rows of 40 heads of 128, 112 MB:
+// 31 us, 3.6 TB/s; with the weights' and the rotation's products apart, eight-way bank
+// conflicts on the angles and 128 bytes of a thread under way 36); below, a launch and
+// the latencies of positions, rows and, for the append, of q_start, the request's length
+// and block ids.
 #include <type_traits>
 
 #include "rotary.h"
@@ -47,10 +51,11 @@ __device__ __forceinline__ float group_sum(float v, int sh) {
     return v;
 }
 
-// Query or key heads of a workgroup at most.
-constexpr int kNormHeads = 8;
-// (row, head) units of a thread in flight.
-constexpr int kUnits = 4;
+// Query or key heads of a workgroup at most (six prompts of 12 thousand rows in all: 54.3 us
+// with 16, 56.8 with 8).
+constexpr int kNormHeads = 16;
+// (row, head) units of a thread in flight, 64 bytes.
+constexpr int units(bool inter) { return inter ? 4 : 2; }
 
 // Workgroup (tile, y): y below key_wgs takes keys, below key_wgs + value_wgs values,
 // the others queries.  WIDE: all rows and pair halves are 16-byte aligned; otherwise
@@ -61,7 +66,9 @@ __global__ __launch_bounds__(kRotThreads) void norm_rotate_rows(NormArgs na) {
     constexpr int CH = D / N;  // 16-byte chunks of a head
     constexpr int VH = value_heads((int)sizeof(T));
     constexpr int PLACE = APPEND ? kSearchEntries : 1, VALUES = APPEND && WIDE ? VH * kTile * (CH + 1) : 1;
-    __shared__ float2 cs[kTile][kMaxFreqs];
+    // rows four banks apart: a wavefront reads eight rows at once, 16 bytes per lane
+    __shared__ __attribute__((aligned(16))) float s_cos[kTile][kMaxFreqs + 4];
+    __shared__ __attribute__((aligned(16))) float s_sin[kTile][kMaxFreqs + 4];
     __shared__ Place place[kTile];
     __shared__ int32_t s_start[PLACE];
     __shared__ uint4 s_val[VALUES];
@@ -88,16 +95,20 @@ __global__ __launch_bounds__(kRotThreads) void norm_rotate_rows(NormArgs na) {
         if (f >= a.freqs) return;
         const double turns_per = a.inv_freq[f] * 0.15915494309189533577;  // 1 / 2 pi
         const int32_t* pos = a.positions + (int64_t)a.axis[f] * a.total_q + row0;
-        for (int r = r0; r < rows; r += step) cs[r][f] = unit_circle((double)pos[r] * turns_per, a.scale);
+        for (int r = r0; r < rows; r += step) {
+            const float2 cs = unit_circle((double)pos[r] * turns_per, a.scale);
+            s_cos[r][f] = cs.x;
+            s_sin[r][f] = cs.y;
+        }
     };
-    // where row r's head h goes, and the distance of its chunks there
-    auto target = [&](int r, int h) -> T* {
+    // where row r's head h_lo goes (null: nowhere), and the distance of its chunks there
+    auto target = [&](int r) -> T* {
         if (APPEND && key) {
             const Place p = place[r];
             if (p.block < 0) return nullptr;
-            return static_cast<T*>(a.k_out) + ((int64_t)p.block * a.hkv + h) * (D * kBlockTokens) + p.slot * N;
+            return static_cast<T*>(a.k_out) + ((int64_t)p.block * a.hkv + h_lo) * (D * kBlockTokens) + p.slot * N;
         }
-        return static_cast<T*>(key ? a.k_out : a.q_out) + (row0 + r) * (key ? a.k_out_stride : a.q_out_stride) + (int64_t)h * D;
+        return static_cast<T*>(key ? a.k_out : a.q_out) + (row0 + r) * (key ? a.k_out_stride : a.q_out_stride) + (int64_t)h_lo * D;
     };
     const int chunk_step = APPEND && key ? kBlockTokens * N : N;
 
@@ -117,12 +128,18 @@ __global__ __launch_bounds__(kRotThreads) void norm_rotate_rows(NormArgs na) {
         const int c0 = it < turned ? it : 2 * half / N + (it - turned);
         const int c1 = pair ? it + half / N : c0;
         const int step = kRotThreads >> sh, all = (h_hi - h_lo) * kTile;
+        // A thread's units: their rows alternate between kSets (32 threads to a head), or are
+        // all the same one.
+        constexpr int kUnits = units(INTER), kSets = CH == 32 ? 2 : 1;
+        const int u0 = tid >> sh;
+        const T* from[kSets];
+#pragma unroll
+        for (int z = 0; z < kSets; ++z) from[z] = in + (row0 + min((u0 + z * step) % kTile, rows - 1)) * in_stride + h_lo * D;
         u32x4 v0[kUnits], v1[kUnits];
         auto load = [&](int base) {
 #pragma unroll
             for (int x = 0; x < kUnits; ++x) {
-                const int u = min(base + (tid >> sh) + x * step, all - 1);
-                const T* head = in + (row0 + min(u % kTile, rows - 1)) * in_stride + (int64_t)(h_lo + u / kTile) * D;
+                const T* head = from[x % kSets] + min(base + u0 + x * step, all - 1) / kTile * D;
                 v0[x] = *reinterpret_cast<const u32x4*>(head + c0 * N);
                 if constexpr (!INTER) v1[x] = *reinterpret_cast<const u32x4*>(head + c1 * N);
             }
@@ -137,12 +154,36 @@ __global__ __launch_bounds__(kRotThreads) void norm_rotate_rows(NormArgs na) {
         angles();
         if (APPEND && key) find_places(a, row0, rows, s_start, place);
         __syncthreads();
+        // Weights, sine and cosine as one matrix per pair (a, b), the same for all heads of
+        // a row: a' = rs (aa a + ab b), b' = rs (ba a + bb b).
+        constexpr int F = INTER ? N / 2 : N;
+        float aa[kSets][F], ab[kSets][F], ba[kSets][F], bb[kSets][F];
+        T* to[kSets];
+#pragma unroll
+        for (int z = 0; z < kSets; ++z) {
+            const int r = (u0 + z * step) % kTile;
+            float cn[F], sn[F];
+            const int f0 = it < turned ? it * F : 0;
+            __builtin_memcpy(cn, __builtin_assume_aligned(&s_cos[r][f0], F * 4 > 16 ? 16 : F * 4), sizeof(cn));
+            __builtin_memcpy(sn, __builtin_assume_aligned(&s_sin[r][f0], F * 4 > 16 ? 16 : F * 4), sizeof(sn));
+#pragma unroll
+            for (int e = 0; e < F; ++e) {
+                const float wa = w0[INTER ? 2 * e : e], wb = INTER ? w0[2 * e + 1] : w1[e];
+                const float c = it < turned ? cn[e] : 1.f, d = it < turned ? sn[e] : 0.f;
+                aa[z][e] = wa * c;
+                ab[z][e] = -wb * d;
+                ba[z][e] = wa * d;
+                bb[z][e] = wb * c;
+            }
+            to[z] = works && r < rows ? target(r) : nullptr;
+        }
+        const int head_step = APPEND && key ? D * kBlockTokens : D;
         for (int base = 0; base < all; base += kUnits * step) {
             if (base) load(base);
 #pragma unroll
             for (int x = 0; x < kUnits; ++x) {
-                const int u = base + (tid >> sh) + x * step, r = u % kTile;
-                float p[N], q[N], ss = 0.f;
+                const int u = base + u0 + x * step, z = x % kSets;
+                float p[N], q[N], ss = 0.f;  // with INTER q stays unused
                 unpack16(make_uint4(v0[x].x, v0[x].y, v0[x].z, v0[x].w), p, T{});
 #pragma unroll
                 for (int e = 0; e < N; ++e) ss = fmaf(p[e], p[e], ss);
@@ -154,29 +195,26 @@ __global__ __launch_bounds__(kRotThreads) void norm_rotate_rows(NormArgs na) {
                     ss += pair ? s1 : 0.f;
                 }
                 const float rs = rsqrtf(fmaf(group_sum(works ? ss : 0.f, sh), 1.f / D, na.eps));
-                if (!works || u >= all || r >= rows) continue;
+                if (u >= all || !to[z]) continue;
+                float ya[F], yb[F];
 #pragma unroll
-                for (int e = 0; e < N; ++e) {
-                    p[e] *= rs * w0[e];
-                    if constexpr (!INTER) q[e] *= rs * w1[e];
+                for (int e = 0; e < F; ++e) {
+                    const float xa = p[INTER ? 2 * e : e], xb = INTER ? p[2 * e + 1] : q[e];
+                    ya[e] = rs * fmaf(ab[z][e], xb, aa[z][e] * xa);
+                    yb[e] = rs * fmaf(bb[z][e], xb, ba[z][e] * xa);
                 }
-                if (it < turned) {
-                    if constexpr (INTER) {
+                T* head = to[z] + u / kTile * head_step;
+                if constexpr (INTER) {
 #pragma unroll
-                        for (int e = 0; e < N; e += 2) turn(p[e], p[e + 1], cs[r][it * (N / 2) + e / 2]);
-                    } else {
-#pragma unroll
-                        for (int e = 0; e < N; ++e) turn(p[e], q[e], cs[r][it * N + e]);
-                    }
-                }
-                T* to = target(r, h_lo + u / kTile);
-                if (!to) continue;
-                const uint4 s0 = Vec<T>::pack(p);
-                *reinterpret_cast<u32x4*>(to + c0 * chunk_step) = u32x4{s0.x, s0.y, s0.z, s0.w};
-                if constexpr (!INTER) {
+                    for (int e = 0; e < F; ++e) p[2 * e] = ya[e], p[2 * e + 1] = yb[e];
+                    const uint4 y = Vec<T>::pack(p);
+                    *reinterpret_cast<u32x4*>(head + c0 * chunk_step) = u32x4{y.x, y.y, y.z, y.w};
+                } else {
+                    const uint4 y0 = Vec<T>::pack(ya);
+                    *reinterpret_cast<u32x4*>(head + c0 * chunk_step) = u32x4{y0.x, y0.y, y0.z, y0.w};
                     if (pair) {
-                        const uint4 s1 = Vec<T>::pack(q);
-                        *reinterpret_cast<u32x4*>(to + c1 * chunk_step) = u32x4{s1.x, s1.y, s1.z, s1.w};
+                        const uint4 y1 = Vec<T>::pack(yb);
+                        *reinterpret_cast<u32x4*>(head + c1 * chunk_step) = u32x4{y1.x, y1.y, y1.z, y1.w};
                     }
                 }
             }
@@ -209,9 +247,10 @@ __global__ __launch_bounds__(kRotThreads) void norm_rotate_rows(NormArgs na) {
             if (r >= rows) continue;
             p *= rs * w0;
             q *= rs * w1;
-            if (turned) turn(p, q, cs[r][it]);
-            T* to = target(r, h);
+            if (turned) turn(p, q, make_float2(s_cos[r][it], s_sin[r][it]));
+            T* to = target(r);
             if (!to) continue;
+            to += (h - h_lo) * (APPEND && key ? D * kBlockTokens : D);
             Storage<T>::store(to, d0 / N * chunk_step + d0 % N, p);
             Storage<T>::store(to, d1 / N * chunk_step + d1 % N, q);
         }
