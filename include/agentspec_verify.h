@@ -574,10 +574,10 @@ int verify_norm_rotary_append(const verify_attn_params *attn, const verify_rotar
  *   group_start  [num_groups + 1] int32, non-decreasing: requests group_start[k] ..
  *                group_start[k + 1] - 1 form group k.  Requests in front of the first
  *                and behind the last group share nothing.
- *   prefix_lens  [num_groups] int32 (clamped to [0, max_prefix_len]): the requests of
- *                group k have the same first prefix_lens[k] / 16 (rounded down) entries
- *                in block_tables, and that many blocks of cached keys at least.  Those of
- *                the group's first request are read.
+ *   prefix_lens  [num_groups] int32 (clamped to [0, max_prefix_len] and to the cached
+ *                keys of the group's first request): the requests of group k have the
+ *                same first prefix_lens[k] / 16 (rounded down) entries in block_tables.
+ *                Those of the group's first request are read.
  *   max_prefix_len   host upper bound on prefix_lens; below 16, or with no group, the
  *                call is verify_attention (with its workspace)
  *   max_q_len    host upper bound on n_i (sizes the launch; a request may exceed it)
@@ -587,10 +587,12 @@ int verify_norm_rotary_append(const verify_attn_params *attn, const verify_rotar
  *                prefix (a prompt that is still being read): it sees the keys up to its
  *                own.
  *   workspace    16-byte aligned (VERIFY_EINVAL otherwise), at least
- *                verify_attention_shared_workspace_size() bytes for the same arguments;
- *                its contents on entry are ignored
+ *                verify_attention_shared_workspace_size() bytes for the same arguments, or
+ *                for those of a batch of more requests and rows with the same other
+ *                arguments; its contents on entry are ignored
  * VERIFY_EUNSUPPORTED for params with sliding_window > 0 (a window does not see a long
- * prefix) or kv_split_blocks > 0, and where total_q Hq / Hkv reaches 2^30.
+ * prefix) or kv_split_blocks > 0, from 2^24 rows or 65536 query heads on, and where
+ * total_q Hq / Hkv reaches 2^30.
  */
 int verify_attention_shared_workspace_size(const verify_attn_params *params, int32_t total_q,
                                            int32_t max_q_len, int32_t max_seq_len,

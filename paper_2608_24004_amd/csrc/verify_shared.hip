@@ -126,8 +126,15 @@ struct __attribute__((aligned(16))) Segment {
 
 __device__ __forceinline__ int clamp_to(int v, int lo, int hi) { return max(lo, min(v, hi)); }
 
+__device__ __forceinline__ int clamped_len(const SharedArgs& a, const Index& x, int i) {
+    return clamp_to(x.lens[i], 0, min(a.max_seq_len, a.max_blocks * kBlockTokens));
+}
+
+// Whole blocks of group k's prefix, as far as its first request has cached them: their ids
+// are read from that request's row.
 __device__ __forceinline__ int prefix_blocks(const SharedArgs& a, const Index& x, int k) {
-    return clamp_to(x.prefix[k], 0, min(a.max_prefix, a.max_blocks * kBlockTokens)) / kBlockTokens;
+    const int cached = clamped_len(a, x, clamp_to(x.group_start[k], 0, a.num_seqs - 1));
+    return clamp_to(x.prefix[k], 0, min(a.max_prefix, cached)) / kBlockTokens;
 }
 
 // The group of request i: the last one that begins at or before it, if it holds i.
@@ -138,10 +145,6 @@ __device__ __forceinline__ int group_of(const SharedArgs& a, const Index& x, int
         if (x.group_start[mid] <= i) lo = mid; else hi = mid - 1;
     }
     return x.group_start[lo] <= i && i < x.group_start[lo + 1] ? lo : -1;
-}
-
-__device__ __forceinline__ int clamped_len(const SharedArgs& a, const Index& x, int i) {
-    return clamp_to(x.lens[i], 0, min(a.max_seq_len, a.max_blocks * kBlockTokens));
 }
 
 // Segment s, but for its first unit and pair.
@@ -1165,6 +1168,8 @@ int check_shared(const verify_attn_params* p, int32_t total_q, int32_t max_q_len
     if (num_groups > 65535) return VERIFY_EUNSUPPORTED;
     const int64_t group = p->num_q_heads / p->num_kv_heads;
     if ((int64_t)total_q * group >= (1 << 30)) return VERIFY_EUNSUPPORTED;
+    // the launch that joins: fewer than 2^32 threads in x, 65536 workgroups in y
+    if (total_q >= (1 << 24) || p->num_q_heads > 65535) return VERIFY_EUNSUPPORTED;
     if (p->max_blocks_per_seq > (1 << 26)) return VERIFY_EUNSUPPORTED;
     return VERIFY_OK;
 }

@@ -101,7 +101,8 @@ def _shared(attn=None, T=5, mq=3, ms=100, G=1, mp=64, q=DUMMY, kc=DUMMY, vc=DUMM
     (dict(attn=_attn(sliding_window=5)), av.EUNSUPPORTED), (dict(attn=_attn(kv_split_blocks=1)), av.EUNSUPPORTED),
     (dict(attn=_attn(head_dim=96)), av.EUNSUPPORTED), (dict(attn=_attn(num_q_heads=7)), av.EINVAL),
     (dict(G=-1), av.EINVAL), (dict(G=65536), av.EUNSUPPORTED), (dict(mp=-1), av.EINVAL), (dict(T=-1), av.EINVAL),
-    (dict(T=2 ** 29), av.EUNSUPPORTED), (dict(attn=_attn(max_blocks_per_seq=2 ** 27)), av.EUNSUPPORTED),
+    (dict(T=2 ** 29), av.EUNSUPPORTED), (dict(T=2 ** 24), av.EUNSUPPORTED),
+    (dict(attn=_attn(num_q_heads=65536, num_kv_heads=65536)), av.EUNSUPPORTED), (dict(attn=_attn(max_blocks_per_seq=2 ** 27)), av.EUNSUPPORTED),
     (dict(q=None), av.EINVAL), (dict(gs=None), av.EINVAL), (dict(pl=None), av.EINVAL), (dict(out=None), av.EINVAL),
     (dict(kc=ctypes.c_void_p(0x1008)), av.EINVAL), (dict(vc=ctypes.c_void_p(0x1004)), av.EINVAL),
     (dict(ws=ctypes.c_void_p(0x1008)), av.EINVAL), (dict(ws=None), av.EWORKSPACE), (dict(size=100), av.EWORKSPACE),
@@ -109,6 +110,25 @@ def _shared(attn=None, T=5, mq=3, ms=100, G=1, mp=64, q=DUMMY, kc=DUMMY, vc=DUMM
 ])
 def test_attention_shared(kw, want):
     assert _shared(**kw) == want
+
+
+def _shared_size(params, T, mq, ms, G, mp):
+    n = ctypes.c_size_t(0)
+    assert av.library().verify_attention_shared_workspace_size(ctypes.byref(params), T, mq, ms, G, mp, ctypes.byref(n)) == av.OK
+    return n.value
+
+
+@pytest.mark.parametrize("dtype", [av.BF16, av.F32])
+@pytest.mark.parametrize("heads", [(8, 8), (32, 8), (5, 1), (64, 1)])
+def test_shared_workspace_covers_smaller_batches(heads, dtype):
+    sizes = {}
+    for B in (1, 2, 7, 40, 300):
+        for T in (1, 3, 4, 9, 10, 33, 40, 130, 300, 1000, 5000):
+            for mq in (1, 9, 300):
+                p = _attn(num_seqs=B, num_q_heads=heads[0], num_kv_heads=heads[1], head_dim=64, dtype=dtype)
+                sizes[B, T, mq] = _shared_size(p, T, mq, 1000, 2, 64)
+    for (B, T, mq), size in sizes.items():
+        assert all(other <= size for (b, t, m), other in sizes.items() if b <= B and t <= T and m == mq)
 
 
 def test_attention_shared_without_a_prefix_is_verify_attention():

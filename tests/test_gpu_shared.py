@@ -26,6 +26,7 @@ CASES = [
     ("prompts", [(3, 512)], [512 + 100, 512 + 333, 512 + 1], [100, 333, 1], {}),  # prompts behind the prefix
     ("rows", [(5, 96)], [120, 111, 130, 140, 100], [3, 7, 2, 5, 4], {}),
     ("unmapped", [(3, 160)], [200, 180, 260], [4, 9, 2], dict(unmapped=[(0, 2), (1, 2), (2, 2), (2, 12), (1, 11)])),
+    ("longer than cached", [(2, 400), (2, 90)], [130, 120, 50, 95], [3, 40, 2, 5], {}),  # prefixes beyond the keys
     ("spikes", [(4, 1000)], [1100, 1030, 2000, 1001], [2, 3, 4, 1], dict(spike=True)),
     ("no prefix", [(2, 0), (2, 40)], [70, 30, 50, 90], [2, 3, 1, 4], {}),
 ]
