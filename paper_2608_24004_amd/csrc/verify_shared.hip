@@ -81,7 +81,7 @@ typedef float f32x4u_t __attribute__((ext_vector_type(4), aligned(4)));
 // Where a row's partial results lie.
 struct __attribute__((aligned(16))) RowParts {
     int64_t unit0;  // own: the segment's first unit, and pair
-    int pair0, each, tiles, height, e0;  // units of a pair (0: none), tiles, rows of a tile, the row's first place
+    int pair0, real, tiles, height, e0;  // units of a pair (0: none), tiles, rows of a tile, the row's first place
     int item0, parts, prefix_tiles, prefix_height, prefix_e0;  // of a prefix: likewise (parts 0: none)
 };
 static_assert(sizeof(RowParts) == 48, "three loads");
@@ -101,6 +101,7 @@ struct SharedArgs {
     int num_seqs, num_groups, hq, hkv, group, max_blocks, num_blocks, max_seq_len, max_prefix, total_q;
     int nwg;
     int tile_a, tile_b;    // rows of a tile at most: prefix and own segments
+    int weighted;          // own units are counted by the rows of their tiles
     int64_t slots_a, slots_b;
     float scale_log2;
 };
@@ -184,7 +185,19 @@ __device__ __forceinline__ int tile_rows(const Segment& g, int tiles) {
 }
 
 __device__ __forceinline__ int units_of(const Segment& g) {
-    return g.b_hi > g.b_lo ? (g.b_hi - g.b_lo + kUnitBlocks - 1) / kUnitBlocks + kPairUnits : 0;
+    return g.b_hi > g.b_lo ? (g.b_hi - g.b_lo + kUnitBlocks - 1) / kUnitBlocks : 0;
+}
+
+// Where the requests' rows may differ by several 16-row tiles per wavefront, a unit does
+// not cost the same in all of them (128 keys of head dim 64 take a workgroup 3.1 us with
+// 16 rows, 3.7 with 64, 4.3 with 128, 5.9 with 192): a unit then counts `each` and a
+// pair `extra` more; otherwise 1 and kPairUnits.
+constexpr int kMostEach = 6;
+struct Cost {
+    int extra, each;
+};
+__device__ __forceinline__ Cost cost_of(const SharedArgs& a, int height) {
+    return a.weighted ? Cost{4 * kPairUnits, height <= 16 ? 3 : height <= 128 ? 4 : kMostEach} : Cost{kPairUnits, 1};
 }
 
 // v of the lanes up to this one, summed.
@@ -237,8 +250,10 @@ __device__ __forceinline__ Share count_units(const SharedArgs& a, const Index& x
         int p = 0, each = 0;
         if (s < segs) {
             g = segment_of(a, x, s);
-            each = units_of(g);
-            p = each > 0 ? tiles_of(g, s < a.num_groups ? a.tile_a : a.tile_b) * a.hkv : 0;
+            const int tiles = tiles_of(g, s < a.num_groups ? a.tile_a : a.tile_b), real = units_of(g);
+            const Cost c = s < a.num_groups ? Cost{kPairUnits, 1} : cost_of(a, tile_rows(g, tiles));
+            each = real > 0 ? c.extra + real * c.each : 0;
+            p = each > 0 ? tiles * a.hkv : 0;
         }
         const Count u = (Count)p * each, u_lanes = scan_lanes(u);
         const int p_lanes = scan_lanes(p);
@@ -276,11 +291,11 @@ __device__ __forceinline__ Share count_units(const SharedArgs& a, const Index& x
         // times it, each with as many workgroups as there are items, with a half and a
         // third of that, and with their share of the work.  Four lanes to a length, in
         // every wavefront for itself.
-        const float unit = a.tile_a >= 128 ? kTallUnit : 1.f;
-        const float mean = fmaxf(1.f, ((float)h.ua * unit + (float)h.ub) * __builtin_amdgcn_rcpf(unit * a.nwg));
+        const float unit = a.tile_a >= 128 ? kTallUnit : 1.f, own = (float)h.ub * (a.weighted ? 0.25f : 1.f);
+        const float mean = fmaxf(1.f, ((float)h.ua * unit + own) * __builtin_amdgcn_rcpf(unit * a.nwg));
         auto length = [&](int c) { return fminf(1.0e9f, ceilf(mean * 0.125f * __builtin_amdgcn_exp2f(5.f / 15 * c))); };
         auto parts_of = [&](const Segment& g, float cost) {
-            return max(1, (int)ceilf((float)(units_of(g) - kPairUnits) * __builtin_amdgcn_rcpf(cost) - 0.001f));
+            return max(1, (int)ceilf((float)units_of(g) * __builtin_amdgcn_rcpf(cost) - 0.001f));
         };
         const float cost = length(lane / 4);
         float all = 0.f;
@@ -290,7 +305,7 @@ __device__ __forceinline__ Share count_units(const SharedArgs& a, const Index& x
             if (g.pair0 == 0) continue;
             const int parts = parts_of(g, cost);
             all += (float)g.pair0 * (float)parts;
-            longest = max(longest, (units_of(g) - kPairUnits + parts - 1) / parts);
+            longest = max(longest, (units_of(g) + parts - 1) / parts);
         }
         for (int o = 1; o < 4; o <<= 1) {
             all += __shfl_xor(all, o);
@@ -298,13 +313,13 @@ __device__ __forceinline__ Share count_units(const SharedArgs& a, const Index& x
         }
         // the workgroups of this candidate, eight at least for each kind of work
         const int most = h.ub > 0 ? a.nwg - 8 : a.nwg;
-        const float share = (float)h.ua * unit * a.nwg * __builtin_amdgcn_rcpf((float)h.ua * unit + (float)h.ub);
+        const float share = (float)h.ua * unit * a.nwg * __builtin_amdgcn_rcpf((float)h.ua * unit + own);
         const float want = ceilf((lane % 4 == 3 ? share : all * __builtin_amdgcn_rcpf(1.f + lane % 4)) * 0.125f - 0.001f) * 8.f;
         const float na = fminf(fmaxf(want, 8.f), (float)most);
         const float rounds = ceilf(all * __builtin_amdgcn_rcpf(na) - 0.001f);
         // (rounded sums: items that would not fit are cut off well before the last slot)
         const float time = all < 0.99f * (float)a.slots_a
-                               ? fmaxf(rounds * ((float)longest + kItemUnits) * unit, (float)h.ub * __builtin_amdgcn_rcpf(fmaxf(a.nwg - na, 1.f)))
+                               ? fmaxf(rounds * ((float)longest + kItemUnits) * unit, own * __builtin_amdgcn_rcpf(fmaxf(a.nwg - na, 1.f)))
                                : INFINITY;
         float best = time;
         for (int o = 1; o < kWave; o <<= 1) best = fminf(best, __shfl_xor(best, o));
@@ -323,7 +338,8 @@ __device__ __forceinline__ Share count_units(const SharedArgs& a, const Index& x
             h.items += __builtin_amdgcn_readlane(here, kWave - 1);
         }
     }
-    h.cb = (int)min((int64_t)(a.nwg - h.na), h.ub);
+    // (weighted: a range that lies within a pair holds a unit's beginning)
+    h.cb = (int)min((int64_t)(a.nwg - h.na), a.weighted && h.ub > 0 ? max((int64_t)1, h.ub / kMostEach) : h.ub);
     __syncthreads();
     return h;
 }
@@ -358,7 +374,7 @@ __device__ __forceinline__ void describe_rows(const SharedArgs& a, const Index& 
             const Segment own = segments[a.num_groups + i];
             r.unit0 = own.unit0 - ua;
             r.pair0 = own.pair0;
-            r.each = units_of(own);
+            r.real = units_of(own);
             r.tiles = tiles_of(own, a.tile_b);
             r.height = tile_rows(own, r.tiles);
             r.e0 = max(0, (int)row - own.q0) * a.group;
@@ -974,14 +990,15 @@ __global__ __launch_bounds__(kThreads, 2) void shared_walk(SharedArgs a, Index x
             }
         }
         const Segment& g = segments[lo];
-        const int each = same(units_of(g)), tiles = same(tiles_of(g, first ? a.tile_a : a.tile_b));
+        const int real = same(units_of(g)), tiles = same(tiles_of(g, first ? a.tile_a : a.tile_b));
+        const int tile_height = same(tile_rows(g, tiles));
         const int64_t local = at - begin(lo);
         int tile;
         int64_t slot;
         Piece p;
         if (first) {
             // item = (head * parts + part) * tiles + tile
-            const uint32_t parts = same(prefix_items[lo].parts), e = same((int)local), row = e / (uint32_t)tiles, real = each - kPairUnits;
+            const uint32_t parts = same(prefix_items[lo].parts), e = same((int)local), row = e / (uint32_t)tiles;
             p.head = row / parts;
             const uint32_t part = row - p.head * parts;
             tile = e - row * tiles;
@@ -990,17 +1007,18 @@ __global__ __launch_bounds__(kThreads, 2) void shared_walk(SharedArgs a, Index x
             slot = item;
             item += step;
         } else {
-            const int pair = same((int)quotient(local, each));
+            const Cost c = cost_of(a, tile_height);
+            const int each = c.extra + real * c.each, pair = same((int)quotient(local, each));
             p.head = (uint32_t)pair / (uint32_t)tiles;
             tile = pair - p.head * tiles;
             const int from = same((int)(local - (int64_t)pair * each)), to = same((int)min((int64_t)each, from + (u_end - u)));
             u += to - from;
-            p.u0 = max(0, from - kPairUnits);
-            p.u1 = to - kPairUnits;
-            if (p.u1 <= 0) continue;
+            // the units that begin in this range
+            p.u0 = (int)((uint32_t)(max(0, from - c.extra) + c.each - 1) / (uint32_t)c.each);
+            p.u1 = (int)((uint32_t)(max(0, to - c.extra) + c.each - 1) / (uint32_t)c.each);
+            if (p.u1 <= p.u0) continue;
             slot = same(g.pair0) + pair + w;
         }
-        const int tile_height = same(tile_rows(g, tiles));
         p.q0 = same(g.q0);
         p.row0 = tile * tile_height;
         p.rows = max(0, min(tile_height, same(g.rows) - p.row0));
@@ -1037,7 +1055,7 @@ __global__ __launch_bounds__(kThreads, 2) void shared_walk(SharedArgs a, Index x
 // them for its pieces, a workgroup per row and run of heads.
 template <typename T, int D, int SPLIT>
 __global__ __launch_bounds__(kThreads) void shared_join(SharedArgs a) {
-    constexpr int kLanes = D / 4, kGroups = kThreads / kLanes, kHeads = kGroups / SPLIT, kBatch = 4;
+    constexpr int kLanes = D / 4, kGroups = kThreads / kLanes, kHeads = kGroups / SPLIT, kBatch = 8;
     __shared__ f32x4_t s_acc[SPLIT > 1 ? kThreads : 1];
     __shared__ float2 s_ml[SPLIT > 1 ? kGroups : 1];
     const int row = blockIdx.x, tid = threadIdx.x;
@@ -1058,11 +1076,13 @@ __global__ __launch_bounds__(kThreads) void shared_join(SharedArgs a) {
         at[0] = slot * a.tile_a + e - tile * r.prefix_height;
         next_at[0] = (int64_t)r.prefix_tiles * a.tile_a;
     }
-    if (r.each > 0) {
+    if (r.real > 0) {
         const int e = r.e0 + in_group, tile = e / r.height, pair = head * r.tiles + tile;
-        const int64_t u0 = r.unit0 + (int64_t)pair * r.each;
+        const Cost c = cost_of(a, r.height);
+        const int64_t u0 = r.unit0 + (int64_t)pair * (c.extra + r.real * c.each) + c.extra;  // where its first unit begins
         // workgroup w owns units [ub w / cb, ub (w + 1) / cb)
-        const int w0 = (int)quotient((u0 + kPairUnits + 1) * sh.cb - 1, sh.ub), w1 = (int)quotient((u0 + r.each) * sh.cb - 1, sh.ub);
+        const int w0 = (int)quotient((u0 + 1) * sh.cb - 1, sh.ub);
+        const int w1 = (int)quotient((u0 + (r.real - 1) * c.each + 1) * sh.cb - 1, sh.ub);
         const int64_t slot = r.pair0 + pair + w0;
         pieces[1] = (int)max((int64_t)0, min((int64_t)(w1 - w0 + 1), a.slots_b - slot));
         at[1] = a.slots_a * a.tile_a + slot * a.tile_b + e - tile * r.height;
@@ -1119,7 +1139,7 @@ __global__ __launch_bounds__(kThreads) void shared_join(SharedArgs a) {
 struct SharedPlan {
     int nwg, tile_a, tile_b;
     int64_t slots_a, slots_b, segs;
-    bool inlined;
+    bool inlined, weighted;
     int split;  // groups of threads that share a row's pieces in the pass that joins
     size_t o_bytes, ml_bytes, total;
 };
@@ -1138,7 +1158,9 @@ int plan_shared(const verify_attn_params* p, int32_t total_q, int32_t max_q_len,
     const int64_t rows = (int64_t)total_q * group;
     s.nwg = 2 * device_cus() / 8 * 8;
     s.tile_a = tile(rows);
-    s.tile_b = tile(std::min<int64_t>(rows, (int64_t)max_q_len * group));
+    const int64_t own_rows = std::min<int64_t>(rows, (int64_t)max_q_len * group);
+    s.tile_b = tile(own_rows);
+    s.weighted = own_rows > 128 && s.tile_b > 128;
     const int64_t pairs_a = (rows / s.tile_a + num_groups) * p->num_kv_heads;
     const int64_t pairs_b = (rows / s.tile_b + p->num_seqs) * p->num_kv_heads;
     if (pairs_a + pairs_b >= (1 << 30)) return VERIFY_EUNSUPPORTED;
@@ -1152,8 +1174,8 @@ int plan_shared(const verify_attn_params* p, int32_t total_q, int32_t max_q_len,
               (size_t)s.segs * sizeof(Segment) + (size_t)num_groups * sizeof(Items);
     // the units of all pairs in 32 bits: then every workgroup can count them itself
     const int64_t most_units = std::min<int64_t>(std::max(max_seq_len, max_prefix_len), (int64_t)p->max_blocks_per_seq * kBlockTokens) /
-                                   (kUnitBlocks * kBlockTokens) + 2 + kPairUnits;
-    s.inlined = s.segs <= kInlineSegs && (pairs_a + pairs_b) * most_units < (1LL << 31) && s.slots_a < (1LL << 30);
+                                   (kUnitBlocks * kBlockTokens) + 2 + kPairUnits;  // times kMostEach
+    s.inlined = s.segs <= kInlineSegs && (pairs_a + pairs_b) * most_units * kMostEach < (1LL << 31) && s.slots_a < (1LL << 30);
 
     s.split = s.nwg >= 24 * pairs_a ? 8 : s.nwg >= 8 * pairs_a ? 4 : 1;
     return VERIFY_OK;
@@ -1268,6 +1290,7 @@ extern "C" int verify_attention_shared(const verify_attn_params* params, int32_t
     a.nwg = s.nwg;
     a.tile_a = s.tile_a;
     a.tile_b = s.tile_b;
+    a.weighted = s.weighted;
     a.slots_a = s.slots_a;
     a.slots_b = s.slots_b;
     const float scale = params->scale > 0.f ? params->scale : 1.f / sqrtf((float)params->head_dim);

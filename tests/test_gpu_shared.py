@@ -51,6 +51,16 @@ def test_shared(name, groups, S, n, opt, hq, hkv, d, dtype):
     np.testing.assert_array_equal(bits(out), bits(got))
 
 
+@pytest.mark.parametrize("short,long", [(1, 18), (1, 24), (3, 50), (17, 20)])
+@pytest.mark.parametrize("keys", [1, 20, 140, 500, 1300])
+def test_rows_of_very_different_numbers_share_few_units(short, long, keys):
+    """Ranges of a few units, in which the rows' tiles weigh differently."""
+    n = [short, long, short]
+    b = SharedBatch(keys + long, [(3, 32)], [32 + keys + long, 32 + keys + long, 40 + short], n, hq=8, hkv=1, d=64,
+                    dtype="bf16")
+    b.check(b.call(DEV))
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_a_long_prefix_and_long_requests(dtype):
     n = [1 + i % 6 for i in range(24)]
