@@ -222,6 +222,20 @@ __device__ __forceinline__ int64_t scan_lanes(int64_t v) {
     return v;
 }
 
+// Maximum and sum over lanes l, l ^ 16, l ^ 32, l ^ 48, which hold one row's keys.
+__device__ __forceinline__ float rows_max(float v) {
+    const auto s = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    const float m = fmaxf(__uint_as_float(s[0]), __uint_as_float(s[1]));
+    const auto t = __builtin_amdgcn_permlane16_swap(__float_as_uint(m), __float_as_uint(m), false, false);
+    return fmaxf(__uint_as_float(t[0]), __uint_as_float(t[1]));
+}
+__device__ __forceinline__ float rows_sum(float v) {
+    const auto s = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    const float m = __uint_as_float(s[0]) + __uint_as_float(s[1]);
+    const auto t = __builtin_amdgcn_permlane16_swap(__float_as_uint(m), __float_as_uint(m), false, false);
+    return __uint_as_float(t[0]) + __uint_as_float(t[1]);
+}
+
 // How the workgroups are divided: na of them take the prefixes' items, the others the ub
 // own units behind unit ua.  Where there are fewer of these than workgroups, cb of them
 // have one.
@@ -307,10 +321,14 @@ __device__ __forceinline__ Share count_units(const SharedArgs& a, const Index& x
             all += (float)g.pair0 * (float)parts;
             longest = max(longest, (units_of(g) + parts - 1) / parts);
         }
-        for (int o = 1; o < 4; o <<= 1) {
-            all += __shfl_xor(all, o);
-            longest = max(longest, __shfl_xor(longest, o));
-        }
+        // over the four lanes
+        auto lane_xor = [](int v, auto ctrl) { return __builtin_amdgcn_update_dpp(0, v, decltype(ctrl)::value, 0xf, 0xf, true); };
+        using One = std::integral_constant<int, 0xB1>;
+        using Two = std::integral_constant<int, 0x4E>;
+        all += __int_as_float(lane_xor(__float_as_int(all), One{}));
+        all += __int_as_float(lane_xor(__float_as_int(all), Two{}));
+        longest = max(longest, lane_xor(longest, One{}));
+        longest = max(longest, lane_xor(longest, Two{}));
         // the workgroups of this candidate, eight at least for each kind of work
         const int most = h.ub > 0 ? a.nwg - 8 : a.nwg;
         const float share = (float)h.ua * unit * a.nwg * __builtin_amdgcn_rcpf((float)h.ua * unit + own);
@@ -321,14 +339,21 @@ __device__ __forceinline__ Share count_units(const SharedArgs& a, const Index& x
         const float time = all < 0.99f * (float)a.slots_a
                                ? fmaxf(rounds * ((float)longest + kItemUnits) * unit, own * __builtin_amdgcn_rcpf(fmaxf(a.nwg - na, 1.f)))
                                : INFINITY;
-        float best = time;
-        for (int o = 1; o < kWave; o <<= 1) best = fminf(best, __shfl_xor(best, o));
+        float best = time;  // over all lanes: rows of 16 by rotations, then their four results
+        auto least = [&](auto ctrl) {
+            best = fminf(best, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(best), decltype(ctrl)::value, 0xf, 0xf, true)));
+        };
+        least(std::integral_constant<int, 0x121>{});
+        least(std::integral_constant<int, 0x122>{});
+        least(std::integral_constant<int, 0x124>{});
+        least(std::integral_constant<int, 0x128>{});
+        best = -rows_max(-best);
         // the longest parts of equal candidates; whole prefixes always fit
         const uint64_t equal = __ballot(time == best);
         const int winner = 63 - __clzll((long long)equal);
         const bool fits = best < INFINITY;
         const float chosen = fits ? length(winner / 4) : 1.0e9f;
-        h.na = fits ? __shfl((int)na, winner) : h.ub > 0 ? a.nwg / 2 : a.nwg;
+        h.na = fits ? __builtin_amdgcn_readlane((int)na, winner) : h.ub > 0 ? a.nwg / 2 : a.nwg;
         for (int base = 0; base < a.num_groups; base += kWave) {
             const int k = base + lane;
             const Segment* g = segments + min(k, a.num_groups - 1);
@@ -418,20 +443,6 @@ template <typename T, int D>
 __device__ __forceinline__ const T* query_row(const SharedArgs& a, const Piece& p, int r) {
     const int e = p.row0 + min(r, p.rows - 1);
     return static_cast<const T*>(a.q) + ((int64_t)(p.q0 + e / a.group) * a.hq + p.head * a.group + e % a.group) * D;
-}
-
-// Maximum and sum over lanes l, l ^ 16, l ^ 32, l ^ 48, which hold one row's keys.
-__device__ __forceinline__ float rows_max(float v) {
-    const auto s = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-    const float m = fmaxf(__uint_as_float(s[0]), __uint_as_float(s[1]));
-    const auto t = __builtin_amdgcn_permlane16_swap(__float_as_uint(m), __float_as_uint(m), false, false);
-    return fmaxf(__uint_as_float(t[0]), __uint_as_float(t[1]));
-}
-__device__ __forceinline__ float rows_sum(float v) {
-    const auto s = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-    const float m = __uint_as_float(s[0]) + __uint_as_float(s[1]);
-    const auto t = __builtin_amdgcn_permlane16_swap(__float_as_uint(m), __float_as_uint(m), false, false);
-    return __uint_as_float(t[0]) + __uint_as_float(t[1]);
 }
 
 // The scores of a lane's N keys of one row become weights 2^(scale s - m), whose sum joins
@@ -813,8 +824,11 @@ __device__ void walk_tall(const SharedArgs& a, const Index& x, const Piece& p, u
     if (steps >= kStages - 1) wait_vmcnt<(kStages - 2) * kRun>();
     else wait_vmcnt<0>();
     lds_barrier();
-    read_k(0);
-    products();
+    const bool works = wave * 16 < p.rows;  // a wavefront without rows fetches and waits
+    if (works) {
+        read_k(0);
+        products();
+    }
     for (int e = 0; e < steps; ++e) {
         // this wavefront's loads of stage e + 2 may be under way
         if (e + 2 < steps) wait_vmcnt<kRun>();
@@ -847,6 +861,7 @@ __device__ void walk_tall(const SharedArgs& a, const Index& x, const Piece& p, u
                 lds_barrier();
             }
         }
+        if (!works) continue;
         read_k(e + 1);  // behind the last step: what lies there, for nothing
         // the weights' exponents; where one exceeds the slack its row's maximum is raised
         float t[RT][8];
