@@ -794,6 +794,9 @@ __device__ void walk_tall(const SharedArgs& a, const Index& x, const Piece& p, u
         const uint8_t* from = (wave < 2 ? a.kc : a.vc) + ((int64_t)id * a.hkv + p.head) * kTile;
         dma16_run<kRun>(ring + (e % kStages) * kStage + wave * kTile, from, lane * 16);
     };
+    // (K's reads take twice the cycles they would with the second block's keys 0-3 and 4-7
+    // exchanged between the two products; putting the weights back in order before the
+    // second contraction then costs more than LDS, a third busy, gains: 295 -> 304 us.)
     const int k_at = (l16 >> 3) * kTile + (l16 & 3) * 16 + ((l16 >> 2) & 1) * 128 + lg * 256;
     const int v_at = 2 * kTile + (lg >> 1) * kTile + l16 * 32 + (lg & 1) * 16;
     f32x4_t s[RT][2];
