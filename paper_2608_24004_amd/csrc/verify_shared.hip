@@ -378,6 +378,21 @@ __global__ __launch_bounds__(1024) void shared_schedule(SharedArgs a, Index x) {
 // whole number.
 __device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) { return (int64_t)((double)a / (double)b); }
 
+// The last k in lo .. hi with begin(k) <= at (begin(lo) is), by a whole wavefront: 64 places
+// at once, so that thousands of entries in memory are two latencies deep.
+template <typename Begin, typename At>
+__device__ __forceinline__ int find_last(Begin begin, int lo, int hi, At at) {
+    const int lane = threadIdx.x % kWave;
+    for (;;) {
+        const int step = (hi - lo) / kWave + 1;
+        const int k = lo + lane * step;
+        const int found = __popcll(__ballot(k <= hi && begin(min(k, hi)) <= at));
+        lo += max(0, found - 1) * step;
+        if (step == 1) return lo;
+        hi = min(hi, lo + step - 1);
+    }
+}
+
 // The request of a packed row: the last one that begins at or before it.
 __device__ __forceinline__ int request_of(const int32_t* q_start, int num_seqs, int row) {
     int lo = 0, hi = num_seqs - 1;
@@ -388,11 +403,16 @@ __device__ __forceinline__ int request_of(const int32_t* q_start, int num_seqs, 
     return lo;
 }
 
-// The rows' records for the pass that joins, a row to a thread of the launch.
+// The rows' records for the pass that joins: a row to a thread of the launch where the
+// descriptor is in LDS, to a wavefront where it is in memory.
+template <bool INLINE>
 __device__ __forceinline__ void describe_rows(const SharedArgs& a, const Index& x, const Segment* segments, const Items* items,
                                               int64_t ua) {
-    for (int64_t row = (int64_t)blockIdx.x * kThreads + threadIdx.x; row < a.total_q; row += (int64_t)a.nwg * kThreads) {
-        const int i = request_of(x.q_start, a.num_seqs, (int)row);
+    constexpr int kRows = INLINE ? kThreads : kWaves;  // of a workgroup at a time
+    const int mine = INLINE ? threadIdx.x : threadIdx.x / kWave;
+    for (int64_t row = (int64_t)blockIdx.x * kRows + mine; row < a.total_q; row += (int64_t)a.nwg * kRows) {
+        const int i = INLINE ? request_of(x.q_start, a.num_seqs, (int)row)
+                             : find_last([&](int k) { return x.q_start[k]; }, 0, a.num_seqs - 1, (int)row);
         RowParts r{};
         r.e0 = -1;  // a row of no request
         if (x.q_start[i] <= row && row < x.q_start[i + 1]) {
@@ -966,12 +986,12 @@ __global__ __launch_bounds__(kThreads, 2) void shared_walk(SharedArgs a, Index x
         __syncthreads();
         const Index y{x.tables, s_lens, s_start, s_groups, s_prefix};
         h = count_units<kThreads, int>(a, y, s_segments, s_items);
-        describe_rows(a, y, s_segments, s_items, h.ua);
+        describe_rows<INLINE>(a, y, s_segments, s_items, h.ua);
         if (blockIdx.x == 0 && threadIdx.x == 0) *a.share = h;  // for the pass that joins
         __syncthreads();
     } else {
         h = *a.share;
-        describe_rows(a, x, a.segments, a.items, h.ua);
+        describe_rows<INLINE>(a, x, a.segments, a.items, h.ua);
     }
     auto same = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
     const int na = same(h.na), b = blockIdx.x;
@@ -993,20 +1013,7 @@ __global__ __launch_bounds__(kThreads, 2) void shared_walk(SharedArgs a, Index x
         const int64_t at = first ? item : h.ua + u;
         auto begin = [&](int k) { return first ? (int64_t)prefix_items[k].first : segments[k].unit0; };
         // the last segment that begins at or before it
-        int lo = first ? 0 : a.num_groups, hi = (first ? a.num_groups : segs) - 1;
-        if constexpr (INLINE) {
-            int found = 0;
-            for (int base = lo; base <= hi; base += kWave) {
-                const int k = base + (int)threadIdx.x % kWave;
-                found += __popcll(__ballot(k <= hi && begin(min(k, hi)) <= at));
-            }
-            lo += found - 1;
-        } else {
-            while (lo < hi) {
-                const int mid = (lo + hi + 1) >> 1;
-                if (begin(mid) <= at) lo = mid; else hi = mid - 1;
-            }
-        }
+        const int lo = find_last(begin, first ? 0 : a.num_groups, (first ? a.num_groups : segs) - 1, at);
         const Segment& g = segments[lo];
         const int real = same(units_of(g)), tiles = same(tiles_of(g, first ? a.tile_a : a.tile_b));
         const int tile_height = same(tile_rows(g, tiles));
