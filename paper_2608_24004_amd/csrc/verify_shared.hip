@@ -184,9 +184,15 @@ __device__ __forceinline__ Segment segment_of(const SharedArgs& a, const Index& 
 
 // A segment's rows divided evenly over as few tiles of at most `most` rows as there need
 // be: their number, and the rows of one.
-__device__ __forceinline__ int tiles_of(const Segment& g, int most) { return (uint32_t)(g.rows + most - 1) / (uint32_t)most; }
+__device__ __forceinline__ int tiles_of(const Segment& g, int most) {
+    // most is 16, 32 or 64 tall_tiles
+    static_assert(64 * tall_tiles(128) == 128 && 64 * tall_tiles(64) == 192 && flat_tiles(true) == 2, "powers of two and 192");
+    const uint32_t n = (uint32_t)(g.rows + most - 1);
+    return most == 192 ? __umulhi(n >> 6, 0xaaaaaaabu) >> 1 : n >> (31 - __clz(most));
+}
 __device__ __forceinline__ int tile_rows(const Segment& g, int tiles) {
-    return tiles ? ((uint32_t)(g.rows + tiles - 1) / (uint32_t)tiles + 15) / 16 * 16 : 16;
+    if (tiles <= 1) return max(16, (g.rows + 15) / 16 * 16);
+    return ((uint32_t)(g.rows + tiles - 1) / (uint32_t)tiles + 15) / 16 * 16;
 }
 
 __device__ __forceinline__ int units_of(const Segment& g) {
@@ -241,6 +247,10 @@ __device__ __forceinline__ float rows_sum(float v) {
     return __uint_as_float(t[0]) + __uint_as_float(t[1]);
 }
 
+// a / b rounded down, 0 <= a < 2^52: a quotient in binary64 is not rounded up to the next
+// whole number.
+__device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) { return (int64_t)((double)a / (double)b); }
+
 // How the workgroups are divided: na of them take the prefixes' items, the others the ub
 // own units behind unit ua.  Where there are fewer of these than workgroups, cb of them
 // have one.
@@ -270,7 +280,7 @@ __device__ __forceinline__ Share count_units(const SharedArgs& a, const Index& x
         if (s < segs) {
             g = segment_of(a, x, s);
             const int tiles = tiles_of(g, s < a.num_groups ? a.tile_a : a.tile_b), real = units_of(g);
-            const Cost c = s < a.num_groups ? Cost{kPairUnits, 1} : cost_of(a, tile_rows(g, tiles));
+            const Cost c = s >= a.num_groups && a.weighted ? cost_of(a, tile_rows(g, tiles)) : Cost{kPairUnits, 1};
             each = real > 0 ? c.extra + real * c.each : 0;
             p = each > 0 ? tiles * a.hkv : 0;
         }
@@ -378,10 +388,6 @@ __global__ __launch_bounds__(1024) void shared_schedule(SharedArgs a, Index x) {
     const Share h = count_units<1024, int64_t>(a, x, a.segments, a.items);
     if (threadIdx.x == 0) *a.share = h;
 }
-
-// a / b rounded down, 0 <= a < 2^52: a quotient in binary64 is not rounded up to the next
-// whole number.
-__device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) { return (int64_t)((double)a / (double)b); }
 
 // The last k in lo .. hi with begin(k) <= at (begin(lo) is), by a whole wavefront: 64 places
 // at once, so that thousands of entries in memory are two latencies deep.
@@ -983,10 +989,15 @@ __global__ __launch_bounds__(kThreads, 2) void shared_walk(SharedArgs a, Index x
         int32_t* s_groups = s_lens + kInlineSegs;
         int32_t* s_prefix = s_groups + kInlineSegs + 1;
         for (int i = threadIdx.x; i <= max(a.num_seqs, a.num_groups); i += kThreads) {
-            if (i <= a.num_seqs) s_start[i] = x.q_start[i];
-            if (i < a.num_seqs) s_lens[i] = x.lens[i];
-            if (i <= a.num_groups) s_groups[i] = x.group_start[i];
-            if (i < a.num_groups) s_prefix[i] = x.prefix[i];
+            // all four on their way before the first is waited for (places behind an
+            // array's last entry take that again)
+            const int seq = min(i, a.num_seqs), group = min(i, a.num_groups);
+            const int start = x.q_start[seq], len = x.lens[min(i, a.num_seqs - 1)];
+            const int begin = x.group_start[group], prefix = x.prefix[min(i, a.num_groups - 1)];
+            s_start[seq] = start;
+            s_lens[min(i, a.num_seqs - 1)] = len;
+            s_groups[group] = begin;
+            s_prefix[min(i, a.num_groups - 1)] = prefix;
         }
         __syncthreads();
         const Index y{x.tables, s_lens, s_start, s_groups, s_prefix};
@@ -1100,14 +1111,14 @@ __global__ __launch_bounds__(kThreads) void shared_join(SharedArgs a) {
     int pieces[2] = {0, 0};
     int64_t at[2] = {0, 0}, next_at[2] = {0, a.tile_b};
     if (r.parts > 0) {
-        const int e = r.prefix_e0 + in_group, tile = e / r.prefix_height;
+        const int e = r.prefix_e0 + in_group, tile = r.prefix_tiles > 1 ? (uint32_t)e / (uint32_t)r.prefix_height : 0;
         const int64_t slot = r.item0 + (int64_t)head * r.parts * r.prefix_tiles + tile;
         pieces[0] = slot + (int64_t)(r.parts - 1) * r.prefix_tiles < a.slots_a ? r.parts : 0;
         at[0] = slot * a.tile_a + e - tile * r.prefix_height;
         next_at[0] = (int64_t)r.prefix_tiles * a.tile_a;
     }
     if (r.real > 0) {
-        const int e = r.e0 + in_group, tile = e / r.height, pair = head * r.tiles + tile;
+        const int e = r.e0 + in_group, tile = r.tiles > 1 ? (uint32_t)e / (uint32_t)r.height : 0, pair = head * r.tiles + tile;
         const Cost c = cost_of(a, r.height);
         const int64_t u0 = r.unit0 + (int64_t)pair * (c.extra + r.real * c.each) + c.extra;  // where its first unit begins
         // workgroup w owns units [ub w / cb, ub (w + 1) / cb)
