@@ -591,8 +591,9 @@ int verify_norm_rotary_append(const verify_attn_params *attn, const verify_rotar
  *                for those of a batch of more requests and rows with the same other
  *                arguments; its contents on entry are ignored
  * VERIFY_EUNSUPPORTED for params with sliding_window > 0 (a window does not see a long
- * prefix) or kv_split_blocks > 0, from 2^24 rows or 65536 query heads on, and where
- * total_q Hq / Hkv reaches 2^30.
+ * prefix) or kv_split_blocks > 0, from 2^24 rows, 65536 query heads or 65536 groups on,
+ * for block tables of more than 2^26 entries, where total_q Hq / Hkv reaches 2^30, and
+ * where Hkv times the row tiles of all prefixes and requests could reach it.
  */
 int verify_attention_shared_workspace_size(const verify_attn_params *params, int32_t total_q,
                                            int32_t max_q_len, int32_t max_seq_len,
@@ -661,7 +662,7 @@ typedef struct verify_adjust_params {
  *             otherwise.  Rows outside the requests' are not written.
  * No workspace.  VERIFY_EINVAL where a penalty is given without counts, seen or tokens,
  * entries without their list, masks without mask; VERIFY_EUNSUPPORTED for vocab from
- * 2^31 - 2049 on.
+ * 2^31 - 2049, total_q from 2^30 and num_seqs from 65536 on.
  */
 int verify_adjust_logits(int32_t num_seqs, int32_t total_q, int64_t vocab, int64_t row_stride,
                          int32_t logits_dtype, const void *logits, const int32_t *tokens,
@@ -680,7 +681,7 @@ int verify_adjust_logits(int32_t num_seqs, int32_t total_q, int64_t vocab, int64
  *
  *   total_tokens  entries of tokens (token_start is clamped to [0, total_tokens])
  *   counts        may be NULL with prompt = 1
- * No workspace.
+ * No workspace.  VERIFY_EUNSUPPORTED for vocab from 2^31 - 32 and num_seqs from 65536 on.
  */
 int verify_count_tokens(int32_t num_seqs, int32_t total_tokens, int64_t vocab, int32_t num_slots,
                         const int32_t *tokens, const int32_t *token_start,

@@ -402,8 +402,8 @@ extern "C" int verify_adjust_logits(int32_t num_seqs, int32_t total_q, int64_t v
                                     int64_t out_stride, hipStream_t stream) {
     if (!params || num_seqs < 0 || total_q < 0 || vocab < 1) return VERIFY_EINVAL;
     if (logits_dtype != VERIFY_F32 && logits_dtype != VERIFY_BF16) return VERIFY_EUNSUPPORTED;
-    // a span's tokens are counted in 32 bits
-    if (vocab >= (int64_t)INT32_MAX - kSpan || num_seqs > 65535) return VERIFY_EUNSUPPORTED;
+    // a span's tokens and a part's rows are counted in 32 bits
+    if (vocab >= (int64_t)INT32_MAX - kSpan || total_q >= (1 << 30) || num_seqs > 65535) return VERIFY_EUNSUPPORTED;
     if (row_stride == 0) row_stride = vocab;
     if (out_stride == 0) out_stride = vocab;
     if (row_stride < vocab || out_stride < vocab) return VERIFY_EINVAL;
@@ -448,7 +448,7 @@ extern "C" int verify_adjust_logits(int32_t num_seqs, int32_t total_q, int64_t v
     a.words = (int)((vocab + 31) / 32);
     a.total_q = total_q;
     // a request's rows are divided where there would be few workgroups otherwise
-    const int64_t spans = (vocab + kSpan - 1) / kSpan, wgs = spans * num_seqs, rows = (total_q + num_seqs - 1) / num_seqs;
+    const int64_t spans = (vocab + kSpan - 1) / kSpan, wgs = spans * num_seqs, rows = ((int64_t)total_q + num_seqs - 1) / num_seqs;
     const int64_t parts = std::max<int64_t>(1, std::min<int64_t>({(1024 + wgs - 1) / wgs, rows, 65535}));
     const dim3 grid((unsigned)spans, (unsigned)num_seqs, (unsigned)parts);
     if (logits_dtype == VERIFY_BF16) launch_adjust<uint16_t>(a, grid, stream);
@@ -469,7 +469,7 @@ extern "C" int verify_count_tokens(int32_t num_seqs, int32_t total_tokens, int64
     const int64_t per = ((int64_t)total_tokens + num_seqs - 1) / num_seqs;
     // from where clearing and reading the words costs less than the atomic operations
     if (per >= 512 && a.words <= kManyWords) {
-        const dim3 grid((unsigned)std::min<int64_t>((total_tokens + kPart - 1) / kPart, std::max(1, 1024 / num_seqs)),
+        const dim3 grid((unsigned)std::min<int64_t>(((int64_t)total_tokens + kPart - 1) / kPart, std::max(1, 1024 / num_seqs)),
                         (unsigned)num_seqs);
         hipLaunchKernelGGL(count_many, grid, dim3(kManyThreads), a.words * 4, stream, a);
     } else {

@@ -72,6 +72,11 @@ def test_adjust_logits(kw, want):
     assert _adjust(**kw) == want
 
 
+def test_adjust_logits_refuses_more_rows_than_its_parts_count():
+    assert _adjust(T=2 ** 30) == av.EUNSUPPORTED and _adjust(T=2 ** 31 - 1) == av.EUNSUPPORTED
+    assert _adjust(T=2 ** 30 - 1, out=None) == av.EINVAL
+
+
 def _count(B=2, total=5, V=100, slots_n=3, tokens=DUMMY, start=DUMMY, prompt=0, counts=DUMMY, seen=DUMMY):
     return av.library().verify_count_tokens(B, total, V, slots_n, tokens, start, None, None, prompt, counts, seen, None)
 

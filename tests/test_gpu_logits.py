@@ -1,6 +1,8 @@
 """verify_adjust_logits and verify_count_tokens against the oracle."""
 from __future__ import annotations
 
+import ctypes
+
 import numpy as np
 import pytest
 import torch
@@ -163,6 +165,36 @@ def test_count_tokens(V, prompt):
                                prompt=prompt)
         np.testing.assert_array_equal(c.cpu().numpy(), want[0])
         np.testing.assert_array_equal(s.cpu().numpy(), want[1])
+
+
+def test_a_total_near_the_largest_bounds_the_requests_alone():
+    """total_tokens and total_q only clamp where requests begin and end: no memory behind
+    the last request is touched, and the launch is as large as any."""
+    V, B = 1000, 2
+    counts = torch.zeros(B, V, dtype=torch.int32, device=DEV)
+    seen = torch.zeros(B, 2, (V + 31) // 32, dtype=torch.int32, device=DEV)
+    tokens = torch.tensor([7, 7, 999, 3], dtype=torch.int32, device=DEV)
+    start = torch.tensor([0, 3, 4], dtype=torch.int32, device=DEV)
+    rc = av.library().verify_count_tokens(B, 2 ** 31 - 1, V, B, tokens.data_ptr(), start.data_ptr(), None, None, 0,
+                                          counts.data_ptr(), seen.data_ptr(), None)
+    assert rc == av.OK
+    torch.cuda.synchronize()
+    want = torch.zeros(B, V, dtype=torch.int32)
+    want[0, 7], want[0, 999], want[1, 3] = 2, 1, 1
+    assert torch.equal(counts.cpu(), want)
+    x = torch.randn(4, V, device=DEV)
+    out = torch.full_like(x, 5.0)
+    pen = torch.ones(B, device=DEV)
+    p = av.AdjustParams(presence=pen.data_ptr(), counts=counts.data_ptr(), seen=seen.data_ptr(), num_slots=B)
+    rc = av.library().verify_adjust_logits(B, 2 ** 30 - 1, V, 0, av.F32, x.data_ptr(), tokens.data_ptr(),
+                                           start.data_ptr(), ctypes.byref(p), out.data_ptr(), 0, None)
+    assert rc == av.OK
+    torch.cuda.synchronize()
+    got, y = out.cpu(), x.cpu()
+    for row, had in enumerate([{7, 999}, {7, 999}, {7, 999}, {3}]):
+        for v in had:
+            y[row, v] -= 1
+    assert torch.equal(got, y)
 
 
 def test_the_calls_of_decoding_captured_and_replayed():
