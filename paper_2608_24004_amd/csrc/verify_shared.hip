@@ -64,8 +64,11 @@ constexpr float kNoMax = -3.0e38f;  // a maximum over no key
 // raised: with a maximum that need not be exact the raise is rare.
 constexpr float kSlackLog2 = 8.f;
 // 16-row tiles of a flat walk at most.  In bf16 two of them and the keys under way do not
-// fit 256 registers, and the ring serves 32 rows as well (5.1 TB/s; flat, with 16 rows, 5.8).
-constexpr int flat_tiles(bool f32) { return f32 ? 2 : 1; }
+// fit 256 registers, and the ring serves 32 rows as well (5.1 TB/s; flat, with 16 rows, 5.8;
+// with Q in LDS three fit, but 32 requests of nine rows take 71 us instead of 65).  In fp32
+// more rows read the keys less often: 288 rows behind 65536 common keys, 309 GFLOP, take
+// 2.55 ms (121 TFLOP/s) with three tiles, 2.81 with two.
+constexpr int flat_tiles(bool f32, int d) { return !f32 ? 1 : d == 64 ? 4 : 3; }
 constexpr int tall_tiles(int d) { return d == 64 ? 3 : 2; }  // per wavefront
 
 // The lane's number, of which the compiler does not know that it is the same in every
@@ -185,10 +188,9 @@ __device__ __forceinline__ Segment segment_of(const SharedArgs& a, const Index& 
 // A segment's rows divided evenly over as few tiles of at most `most` rows as there need
 // be: their number, and the rows of one.
 __device__ __forceinline__ int tiles_of(const Segment& g, int most) {
-    // most is 16, 32 or 64 tall_tiles
-    static_assert(64 * tall_tiles(128) == 128 && 64 * tall_tiles(64) == 192 && flat_tiles(true) == 2, "powers of two and 192");
-    const uint32_t n = (uint32_t)(g.rows + most - 1);
-    return most == 192 ? __umulhi(n >> 6, 0xaaaaaaabu) >> 1 : n >> (31 - __clz(most));
+    // most is a power of two, or three times one
+    const uint32_t n = (uint32_t)(g.rows + most - 1) >> __builtin_ctz(most);
+    return most % 3 == 0 ? __umulhi(n, 0xaaaaaaabu) >> 1 : n;
 }
 __device__ __forceinline__ int tile_rows(const Segment& g, int tiles) {
     if (tiles <= 1) return max(16, (g.rows + 15) / 16 * 16);
@@ -681,18 +683,26 @@ __device__ void walk_flat(const SharedArgs& a, const Index& x, const Piece& p, u
 // Few rows, fp32: fp32 products (v_mfma_f32_16x16x4_f32), a block of 16 keys at a time.
 // Lane 16 lg + l16 takes the 16-byte chunks lg, lg + 4, ... of key l16; product i of a
 // chunk multiplies its i-th dim.  A lane's 16 bytes of V^T are its keys 4 lg .. 4 lg + 3.
+// Bound by the matrix units where there are several tiles, by memory with one.
 template <int D, int RT>
 __device__ void walk_flat_f32(const SharedArgs& a, const Index& x, const Piece& p, uint8_t* smem) {
     constexpr int DT = D / 16, C = D / 16;
-    const int wave = threadIdx.x / kWave, lane = own_lane(), l16 = lane % 16, lg = lane / 16;
-    f32x4_t q[RT][C], o[RT][DT];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = own_lane(), l16 = lane % 16,
+              lg = lane / 16;
+    // Q as its operands: of one tile in registers, of more in LDS
+    constexpr bool kInLds = RT > 1;
+    f32x4_t q[kInLds ? 1 : C], o[RT][DT];
+    f32x4_t* s_q = reinterpret_cast<f32x4_t*>(smem);
     float m[RT], l[RT];
     int pos[RT];
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
-        const float* row = query_row<float, D>(a, p, r * 16 + l16);
+        const float* row = query_row<float, D>(a, p, r * 16 + l16) + 4 * lg;
 #pragma unroll
-        for (int c = 0; c < C; ++c) q[r][c] = *reinterpret_cast<const f32x4u_t*>(row + 16 * c + 4 * lg);
+        for (int c = 0; c < C; ++c) {
+            if constexpr (!kInLds) q[c] = *reinterpret_cast<const f32x4u_t*>(row + 16 * c);
+            else if (c % kWaves == wave) s_q[(r * C + c) * kWave + lane] = *reinterpret_cast<const f32x4u_t*>(row + 16 * c);
+        }
         pos[r] = row_position(a, x, p, r * 16 + l16);
         m[r] = kNoMax;
         l[r] = 0.f;
@@ -702,12 +712,12 @@ __device__ void walk_flat_f32(const SharedArgs& a, const Index& x, const Piece& 
     constexpr int64_t kTile = (int64_t)D * kBlockTokens * 4;
     // block e of this wavefront: two of every unit
     auto block = [&](int e) { return p.b_lo + (p.u0 + (e >> 1)) * kUnitBlocks + 2 * wave + (e & 1); };
-    auto id_of = [&](int e) {
-        const int b = block(e);
-        if (e >= 2 * (p.u1 - p.u0) || b >= p.b_hi) return -1;
-        const int id = p.table[b];
+    // the ids of 64 of them in the lanes of a register, as in walk_flat
+    auto read_ids = [&](int e) {
+        const int b = block(e + lane), id = e + lane < 2 * (p.u1 - p.u0) && b < p.b_hi ? p.table[b] : -1;
         return id >= 0 && id < a.num_blocks ? id : -1;
     };
+    int ids = read_ids(0);
     f32x4_t k[C], v[DT];
     auto load_k = [&](int id) {
         const uint8_t* from = a.kc + ((int64_t)id * a.hkv + p.head) * kTile + l16 * 16 + lg * 256;
@@ -719,30 +729,35 @@ __device__ void walk_flat_f32(const SharedArgs& a, const Index& x, const Piece& 
 #pragma unroll
         for (int t = 0; t < DT; ++t) v[t] = *reinterpret_cast<const f32x4_t*>(from + t * 1024);
     };
-    int id = id_of(0), next = id_of(1);
+    int id = __builtin_amdgcn_readlane(ids, 0);
     if (id >= 0) {
         load_k(id);
         load_v(id);
     }
+    if (kInLds) __syncthreads();
     for (int e = 0; e < 2 * (p.u1 - p.u0); ++e) {
-        const int after = id_of(e + 2);
+        if ((e + 1) % kWave == 0) ids = read_ids(e + 1);
+        const int next = __builtin_amdgcn_readlane(ids, (e + 1) % kWave);
         if (id >= 0) {
             const int key0 = block(e) * kBlockTokens + 4 * lg;
             const bool edge = block(e) * kBlockTokens + kBlockTokens - 1 > p.min_pos;
-            f32x4_t s[RT];
+            // several chains of products: none waits for the one before it
+            constexpr int kChains = RT > 1 ? 1 : 2;
+            f32x4_t s[RT * kChains];
 #pragma unroll
-            for (int r = 0; r < RT; ++r) {
-                // two chains of products: none waits for the one before it
-                f32x4_t s0{0.f, 0.f, 0.f, 0.f}, s1{0.f, 0.f, 0.f, 0.f};
+            for (int r = 0; r < RT * kChains; ++r) s[r] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int c = 0; c < C; ++c)
+            for (int c = 0; c < C; ++c)
 #pragma unroll
-                    for (int i = 0; i < 4; i += 2) {
-                        s0 = __builtin_amdgcn_mfma_f32_16x16x4f32(k[c][i], q[r][c][i], s0, 0, 0, 0);
-                        s1 = __builtin_amdgcn_mfma_f32_16x16x4f32(k[c][i + 1], q[r][c][i + 1], s1, 0, 0, 0);
+                for (int r = 0; r < RT; ++r) {
+                    const f32x4_t y = kInLds ? s_q[(r * C + c) * kWave + lane] : q[c];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        f32x4_t& sum = s[r * kChains + i % kChains];
+                        sum = __builtin_amdgcn_mfma_f32_16x16x4f32(k[c][i], y[i], sum, 0, 0, 0);
                     }
-                s[r] = s0 + s1;
-            }
+                }
+            if (kChains > 1) s[0] += s[1];
             if (next >= 0) load_k(next);
 #pragma unroll
             for (int r = 0; r < RT; ++r) {
@@ -772,8 +787,8 @@ __device__ void walk_flat_f32(const SharedArgs& a, const Index& x, const Piece& 
         }
         if (next >= 0) load_v(next);
         id = next;
-        next = after;
     }
+    if (kInLds) __syncthreads();  // Q is used up
     join_waves<D, RT>(a, p, m, l, o, smem);
 }
 
@@ -967,7 +982,8 @@ __device__ void walk_tall(const SharedArgs& a, const Index& x, const Piece& p, u
 
 template <typename T, int D>
 constexpr int smem_bytes() {
-    const int joined = kWaves * (D / 16) * 1024;
+    const int joined = kWaves * (D / 16) * 1024;  // or fp32's Q
+    static_assert(sizeof(T) == 2 || flat_tiles(true, D) * 16 * D * 4 <= joined, "Q");
     const int ring = sizeof(T) == 2 ? kStages * 4 * D * kBlockTokens * 2 : 0;
     return joined > ring ? joined : ring;
 }
@@ -1081,7 +1097,9 @@ __global__ __launch_bounds__(kThreads, 2) void shared_walk(SharedArgs a, Index x
         const int tiles16 = (p.rows + 15) / 16;
         if constexpr (sizeof(T) == 4) {
             if (tiles16 == 1) walk_flat_f32<D, 1>(a, x, p, smem);
-            else walk_flat_f32<D, 2>(a, x, p, smem);
+            else if (tiles16 == 2) walk_flat_f32<D, 2>(a, x, p, smem);
+            else if (tiles16 == 3) walk_flat_f32<D, 3>(a, x, p, smem);
+            else walk_flat_f32<D, flat_tiles(true, D)>(a, x, p, smem);
         } else {
             constexpr int RT = tall_tiles(D);
             if (tiles16 == 1) walk_flat<D>(a, x, p, smem);
@@ -1192,9 +1210,9 @@ int plan_shared(const verify_attn_params* p, int32_t total_q, int32_t max_q_len,
     const int group = p->num_q_heads / p->num_kv_heads, D = p->head_dim;
     const bool f32 = p->dtype == VERIFY_F32;
     auto tile = [&](int64_t rows) {
-        const int flat = 16 * flat_tiles(f32);
-        const int need = (int)std::max<int64_t>(16, (std::min<int64_t>(rows, flat) + 15) / 16 * 16);
-        return f32 || rows <= flat ? need : 64 * tall_tiles(D);
+        const int flat = 16 * flat_tiles(f32, D);
+        if (!f32 && rows > flat) return 64 * tall_tiles(D);
+        return rows <= 16 ? 16 : rows <= 32 ? 32 : flat;
     };
     const int64_t rows = (int64_t)total_q * group;
     s.nwg = 2 * device_cus() / 8 * 8;
@@ -1202,8 +1220,9 @@ int plan_shared(const verify_attn_params* p, int32_t total_q, int32_t max_q_len,
     const int64_t own_rows = std::min<int64_t>(rows, (int64_t)max_q_len * group);
     s.tile_b = tile(own_rows);
     s.weighted = own_rows > 128 && s.tile_b > 128;
-    const int64_t pairs_a = (rows / s.tile_a + num_groups) * p->num_kv_heads;
-    const int64_t pairs_b = (rows / s.tile_b + p->num_seqs) * p->num_kv_heads;
+    // (rounded up, so that fewer rows in smaller tiles never need more)
+    const int64_t pairs_a = ((rows + s.tile_a - 1) / s.tile_a + num_groups) * p->num_kv_heads;
+    const int64_t pairs_b = ((rows + s.tile_b - 1) / s.tile_b + p->num_seqs) * p->num_kv_heads;
     if (pairs_a + pairs_b >= (1 << 30)) return VERIFY_EUNSUPPORTED;
     s.slots_a = pairs_a + 4 * s.nwg;
     s.slots_b = pairs_b + s.nwg;

@@ -136,6 +136,15 @@ def test_shared_workspace_covers_smaller_batches(heads, dtype):
         assert all(other <= size for (b, t, m), other in sizes.items() if b <= B and t <= T and m == mq)
 
 
+@pytest.mark.parametrize("dtype,d", [(av.BF16, 128), (av.F32, 128), (av.F32, 64)])
+def test_shared_workspace_covers_smaller_batches_of_many_heads(dtype, d):
+    """One row more may mean larger tiles, of every head."""
+    for heads, mq in (((4096, 4096), 10 ** 6), ((4096, 4096), 20), ((8192, 4096), 33)):
+        sizes = [_shared_size(_attn(num_seqs=2, num_q_heads=heads[0], num_kv_heads=heads[1], head_dim=d, dtype=dtype),
+                              T, mq, 1000, 1, 64) for T in range(1, 200)]
+        assert sizes == sorted(sizes)
+
+
 def test_attention_shared_without_a_prefix_is_verify_attention():
     n, m = ctypes.c_size_t(0), ctypes.c_size_t(0)
     p = _attn()
