@@ -9,7 +9,7 @@
 // output sum 2^(s - m) v, unnormalised and in fp32, and a last pass joins them:
 //     out = sum_k 2^(m_k - M) o_k / (sum_k 2^(m_k - M) l_k + 2^(sink log2 e - M)).
 //
-// Work.  A pair is (segment, KV head, row tile), a unit 128 keys of a pair.  The workgroups
+// Work.  A pair is (segment, KV head, row tile), a unit 128 keys of a pair (fp32: 64).  The workgroups
 // are all resident at once.  Some take the prefixes: each pair's keys are cut into parts
 // of the same length, an item is one part of one pair, and the items of a part's tiles
 // follow each other.  The others take the own units, numbered segment by segment, then
@@ -48,12 +48,15 @@ namespace {
 constexpr int kWaves = 4;
 constexpr int kThreads = kWaves * kWave;
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr int kUnitBlocks = 8;      // KV blocks of a unit
+// KV blocks of a unit: two for each wavefront in bf16, one in fp32, whose products take
+// eight times as long (two requests of three rows, 130 keys behind 64 common ones: 14.5 us,
+// with two 16.3).
+constexpr int unit_shift(bool f32) { return f32 ? 2 : 3; }
+constexpr int kUnitBlocks = 1 << unit_shift(false);
 // What a pair costs beside its blocks (its rows, the first blocks' latency, the join of
 // the wavefronts, the partial result), in units: it counts so many units more, without
 // blocks, in front of its own.
 constexpr int kPairUnits = 1;
-constexpr float kItemUnits = 2.f;  // likewise of a part of a prefix, with its way through the join
 constexpr int kInlineSegs = 256;    // segments whose units every workgroup counts itself
 // A prefix's unit of 128 rows beside one of few rows: 3.5 us where 4.3 (the one fills the
 // matrix units, the other waits for 64 KiB; 32 requests of nine rows, 8192 common keys).
@@ -109,6 +112,7 @@ struct SharedArgs {
     int num_seqs, num_groups, hq, hkv, group, max_blocks, num_blocks, max_seq_len, max_prefix, total_q;
     int nwg;
     int tile_a, tile_b;    // rows of a tile at most: prefix and own segments
+    int unit_shift;        // KV blocks of a unit, log2
     int weighted;          // own units are counted by the rows of their tiles
     int64_t slots_a, slots_b;
     float scale_log2;
@@ -197,8 +201,8 @@ __device__ __forceinline__ int tile_rows(const Segment& g, int tiles) {
     return ((uint32_t)(g.rows + tiles - 1) / (uint32_t)tiles + 15) / 16 * 16;
 }
 
-__device__ __forceinline__ int units_of(const Segment& g) {
-    return g.b_hi > g.b_lo ? (g.b_hi - g.b_lo + kUnitBlocks - 1) / kUnitBlocks : 0;
+__device__ __forceinline__ int units_of(const SharedArgs& a, const Segment& g) {
+    return g.b_hi > g.b_lo ? (g.b_hi - g.b_lo + (1 << a.unit_shift) - 1) >> a.unit_shift : 0;
 }
 
 // Where the requests' rows may differ by several 16-row tiles per wavefront, a unit does
@@ -266,6 +270,11 @@ struct Items {
     int first, parts;
 };
 
+// What a part of a prefix costs beside its units, in units, with its way through the join.
+__device__ __forceinline__ float item_units(const SharedArgs& a) {
+    return a.unit_shift == unit_shift(true) && a.tile_a > 16 ? 1.f : 2.f;
+}
+
 // Counts the units and pairs of all segments and cuts the prefixes' pairs into items, by
 // one workgroup of THREADS threads.  Count: of all units.
 template <int THREADS, typename Count>
@@ -281,7 +290,7 @@ __device__ __forceinline__ Share count_units(const SharedArgs& a, const Index& x
         int p = 0, each = 0;
         if (s < segs) {
             g = segment_of(a, x, s);
-            const int tiles = tiles_of(g, s < a.num_groups ? a.tile_a : a.tile_b), real = units_of(g);
+            const int tiles = tiles_of(g, s < a.num_groups ? a.tile_a : a.tile_b), real = units_of(a, g);
             const Cost c = s >= a.num_groups && a.weighted ? cost_of(a, tile_rows(g, tiles)) : Cost{kPairUnits, 1};
             each = real > 0 ? c.extra + real * c.each : 0;
             p = each > 0 ? tiles * a.hkv : 0;
@@ -318,44 +327,40 @@ __device__ __forceinline__ Share count_units(const SharedArgs& a, const Index& x
     h.na = h.items = 0;
     if (h.ua > 0) {
         // The parts' length and the number of workgroups with which the last of all is
-        // done first: 16 lengths between an eighth of a workgroup's mean share and four
-        // times it, each with as many workgroups as there are items, with a half and a
-        // third of that, and with their share of the work.  Four lanes to a length, in
-        // every wavefront for itself.
+        // done first: 64 lengths between an eighth of a workgroup's mean share and four
+        // times it, one to a lane, each with as many workgroups as there are items, with
+        // a half and a third of that, and with their share of the work.  Every wavefront
+        // does it for itself.
         const float unit = a.tile_a >= 128 ? kTallUnit : 1.f, own = (float)h.ub * (a.weighted ? 0.25f : 1.f);
         const float mean = fmaxf(1.f, ((float)h.ua * unit + own) * __builtin_amdgcn_rcpf(unit * a.nwg));
-        auto length = [&](int c) { return fminf(1.0e9f, ceilf(mean * 0.125f * __builtin_amdgcn_exp2f(5.f / 15 * c))); };
+        auto length = [&](int c) { return fminf(1.0e9f, ceilf(mean * 0.125f * __builtin_amdgcn_exp2f(5.f / 63 * c))); };
         auto parts_of = [&](const Segment& g, float cost) {
-            return max(1, (int)ceilf((float)units_of(g) * __builtin_amdgcn_rcpf(cost) - 0.001f));
+            return max(1, (int)ceilf((float)units_of(a, g) * __builtin_amdgcn_rcpf(cost) - 0.001f));
         };
-        const float cost = length(lane / 4);
+        const float cost = length(lane);
         float all = 0.f;
         int longest = 0;
-        for (int k = lane % 4; k < a.num_groups; k += 4) {
+        for (int k = 0; k < a.num_groups; ++k) {
             const Segment& g = segments[k];
-            if (g.pair0 == 0) continue;
-            const int parts = parts_of(g, cost);
+            const int units = units_of(a, g), parts = parts_of(g, cost);
             all += (float)g.pair0 * (float)parts;
-            longest = max(longest, (units_of(g) + parts - 1) / parts);
+            longest = max(longest, g.pair0 ? (int)ceilf((float)units * __builtin_amdgcn_rcpf((float)parts) - 0.001f) : 0);
         }
-        // over the four lanes
-        auto lane_xor = [](int v, auto ctrl) { return __builtin_amdgcn_update_dpp(0, v, decltype(ctrl)::value, 0xf, 0xf, true); };
-        using One = std::integral_constant<int, 0xB1>;
-        using Two = std::integral_constant<int, 0x4E>;
-        all += __int_as_float(lane_xor(__float_as_int(all), One{}));
-        all += __int_as_float(lane_xor(__float_as_int(all), Two{}));
-        longest = max(longest, lane_xor(longest, One{}));
-        longest = max(longest, lane_xor(longest, Two{}));
-        // the workgroups of this candidate, eight at least for each kind of work
-        const int most = h.ub > 0 ? a.nwg - 8 : a.nwg;
+        // the workgroups of this length, eight at least for each kind of work
+        const float most = h.ub > 0 ? a.nwg - 8 : a.nwg;
         const float share = (float)h.ua * unit * a.nwg * __builtin_amdgcn_rcpf((float)h.ua * unit + own);
-        const float want = ceilf((lane % 4 == 3 ? share : all * __builtin_amdgcn_rcpf(1.f + lane % 4)) * 0.125f - 0.001f) * 8.f;
-        const float na = fminf(fmaxf(want, 8.f), (float)most);
-        const float rounds = ceilf(all * __builtin_amdgcn_rcpf(na) - 0.001f);
+        float time = INFINITY, na = 0.f;
+#pragma unroll
+        for (int n = 0; n < 4; ++n) {
+            const float want = ceilf((n == 3 ? share : all * (n == 2 ? 1.f / 3 : n == 1 ? 0.5f : 1.f)) * 0.125f - 0.001f) * 8.f;
+            const float wgs = fminf(fmaxf(want, 8.f), most);
+            const float rounds = ceilf(all * __builtin_amdgcn_rcpf(wgs) - 0.001f);
+            const float t = fmaxf(rounds * ((float)longest + item_units(a)) * unit, own * __builtin_amdgcn_rcpf(fmaxf(a.nwg - wgs, 1.f)));
+            na = t <= time ? wgs : na;
+            time = fminf(t, time);
+        }
         // (rounded sums: items that would not fit are cut off well before the last slot)
-        const float time = all < 0.99f * (float)a.slots_a
-                               ? fmaxf(rounds * ((float)longest + kItemUnits) * unit, own * __builtin_amdgcn_rcpf(fmaxf(a.nwg - na, 1.f)))
-                               : INFINITY;
+        if (!(all < 0.99f * (float)a.slots_a)) time = INFINITY;
         float best = time;  // over all lanes: rows of 16 by rotations, then their four results
         auto least = [&](auto ctrl) {
             best = fminf(best, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(best), decltype(ctrl)::value, 0xf, 0xf, true)));
@@ -369,7 +374,7 @@ __device__ __forceinline__ Share count_units(const SharedArgs& a, const Index& x
         const uint64_t equal = __ballot(time == best);
         const int winner = 63 - __clzll((long long)equal);
         const bool fits = best < INFINITY;
-        const float chosen = fits ? length(winner / 4) : 1.0e9f;
+        const float chosen = fits ? length(winner) : 1.0e9f;
         h.na = fits ? __builtin_amdgcn_readlane((int)na, winner) : h.ub > 0 ? a.nwg / 2 : a.nwg;
         for (int base = 0; base < a.num_groups; base += kWave) {
             const int k = base + lane;
@@ -432,7 +437,7 @@ __device__ __forceinline__ void describe_rows(const SharedArgs& a, const Index& 
             const Segment own = segments[a.num_groups + i];
             r.unit0 = own.unit0 - ua;
             r.pair0 = own.pair0;
-            r.real = units_of(own);
+            r.real = units_of(a, own);
             r.tiles = tiles_of(own, a.tile_b);
             r.height = tile_rows(own, r.tiles);
             r.e0 = max(0, (int)row - own.q0) * a.group;
@@ -710,11 +715,11 @@ __device__ void walk_flat_f32(const SharedArgs& a, const Index& x, const Piece& 
         for (int t = 0; t < DT; ++t) o[r][t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     }
     constexpr int64_t kTile = (int64_t)D * kBlockTokens * 4;
-    // block e of this wavefront: two of every unit
-    auto block = [&](int e) { return p.b_lo + (p.u0 + (e >> 1)) * kUnitBlocks + 2 * wave + (e & 1); };
+    const int blocks = p.u1 - p.u0;  // of this wavefront: one of every unit
+    auto block = [&](int e) { return p.b_lo + ((p.u0 + e) << unit_shift(true)) + wave; };
     // the ids of 64 of them in the lanes of a register, as in walk_flat
     auto read_ids = [&](int e) {
-        const int b = block(e + lane), id = e + lane < 2 * (p.u1 - p.u0) && b < p.b_hi ? p.table[b] : -1;
+        const int b = block(e + lane), id = e + lane < blocks && b < p.b_hi ? p.table[b] : -1;
         return id >= 0 && id < a.num_blocks ? id : -1;
     };
     int ids = read_ids(0);
@@ -735,7 +740,7 @@ __device__ void walk_flat_f32(const SharedArgs& a, const Index& x, const Piece& 
         load_v(id);
     }
     if (kInLds) __syncthreads();
-    for (int e = 0; e < 2 * (p.u1 - p.u0); ++e) {
+    for (int e = 0; e < blocks; ++e) {
         if ((e + 1) % kWave == 0) ids = read_ids(e + 1);
         const int next = __builtin_amdgcn_readlane(ids, (e + 1) % kWave);
         if (id >= 0) {
@@ -1047,7 +1052,7 @@ __global__ __launch_bounds__(kThreads, 2) void shared_walk(SharedArgs a, Index x
         // the last segment that begins at or before it
         const int lo = find_last(begin, first ? 0 : a.num_groups, (first ? a.num_groups : segs) - 1, at);
         const Segment& g = segments[lo];
-        const int real = same(units_of(g)), tiles = same(tiles_of(g, first ? a.tile_a : a.tile_b));
+        const int real = same(units_of(a, g)), tiles = same(tiles_of(g, first ? a.tile_a : a.tile_b));
         const int tile_height = same(tile_rows(g, tiles));
         const int64_t local = at - begin(lo);
         int tile;
@@ -1092,7 +1097,7 @@ __global__ __launch_bounds__(kThreads, 2) void shared_walk(SharedArgs a, Index x
         // keys that none of the tile's rows sees
         if (!first) {
             const int seen = p.pos0 + (p.row0 + p.rows - 1) / a.group + 1 - p.b_lo * kBlockTokens;
-            p.u1 = max(p.u0, min(p.u1, (max(0, seen) + kUnitBlocks * kBlockTokens - 1) / (kUnitBlocks * kBlockTokens)));
+            p.u1 = max(p.u0, min(p.u1, (max(0, seen) + (kBlockTokens << a.unit_shift) - 1) / kBlockTokens >> a.unit_shift));
         }
         const int tiles16 = (p.rows + 15) / 16;
         if constexpr (sizeof(T) == 4) {
@@ -1234,7 +1239,7 @@ int plan_shared(const verify_attn_params* p, int32_t total_q, int32_t max_q_len,
               (size_t)s.segs * sizeof(Segment) + (size_t)num_groups * sizeof(Items);
     // the units of all pairs in 32 bits: then every workgroup can count them itself
     const int64_t most_units = std::min<int64_t>(std::max(max_seq_len, max_prefix_len), (int64_t)p->max_blocks_per_seq * kBlockTokens) /
-                                   (kUnitBlocks * kBlockTokens) + 2 + kPairUnits;  // times kMostEach
+                                   (kBlockTokens << unit_shift(f32)) + 2 + kPairUnits;  // times kMostEach
     s.inlined = s.segs <= kInlineSegs && (pairs_a + pairs_b) * most_units * kMostEach < (1LL << 31) && s.slots_a < (1LL << 30);
 
     s.split = s.nwg >= 24 * pairs_a ? 8 : s.nwg >= 8 * pairs_a ? 4 : 1;
@@ -1351,6 +1356,7 @@ extern "C" int verify_attention_shared(const verify_attn_params* params, int32_t
     a.tile_a = s.tile_a;
     a.tile_b = s.tile_b;
     a.weighted = s.weighted;
+    a.unit_shift = unit_shift(params->dtype == VERIFY_F32);
     a.slots_a = s.slots_a;
     a.slots_b = s.slots_b;
     const float scale = params->scale > 0.f ? params->scale : 1.f / sqrtf((float)params->head_dim);
