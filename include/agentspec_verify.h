@@ -577,7 +577,7 @@ int verify_norm_rotary_append(const verify_attn_params *attn, const verify_rotar
  *   prefix_lens  [num_groups] int32 (clamped to [0, max_prefix_len] and to the cached
  *                keys of the group's first request): the requests of group k have the
  *                same first prefix_lens[k] / 16 (rounded down) entries in block_tables.
- *                Those of the group's first request are read.
+ *                Those of the group's first request are read, or each request's own.
  *   max_prefix_len   host upper bound on prefix_lens; below 16, or with no group, the
  *                call is verify_attention (with its workspace)
  *   max_q_len    host upper bound on n_i (sizes the launch; a request may exceed it)
@@ -586,7 +586,8 @@ int verify_norm_rotary_append(const verify_attn_params *attn, const verify_rotar
  *   sinks and all other arguments as for verify_attention.  A row may stand inside the
  *                prefix (a prompt that is still being read): it sees the keys up to its
  *                own.
- *   workspace    16-byte aligned (VERIFY_EINVAL otherwise), at least
+ *   workspace    16-byte aligned (VERIFY_EINVAL otherwise; may be NULL where the size is 0:
+ *                few and short requests), at least
  *                verify_attention_shared_workspace_size() bytes for the same arguments, or
  *                for those of a batch of more requests and rows with the same other
  *                arguments; its contents on entry are ignored

@@ -62,6 +62,7 @@ constexpr int kInlineSegs = 256;    // segments whose units every workgroup coun
 // matrix units, the other waits for 64 KiB; 32 requests of nine rows, 8192 common keys).
 constexpr float kTallUnit = 0.8f;
 constexpr int kStages = 4;          // of the tall walk's ring
+constexpr int kShort = 1024, kShortF32 = 448;  // keys of a short request at most (see shared_short)
 constexpr float kNoMax = -3.0e38f;  // a maximum over no key
 // Softmax weights may exceed 1 by up to this factor (log2) before a row's maximum is
 // raised: with a maximum that need not be exact the raise is rare.
@@ -573,8 +574,21 @@ __device__ __forceinline__ void store_partial(const SharedArgs& a, const Piece& 
     if (r < p.rows) *reinterpret_cast<f32x4_t*>(a.part_o + (p.slot_row + r) * D + 16 * t + 4 * lg) = v;
 }
 
-// The four wavefronts' states of the same rows, joined and stored.  smem: 4 D / 16 KiB.
-template <int D, int RT>
+// A row's output: its sum joined by its sink, which adds to nothing else.  A row without
+// keys is zero.
+template <typename T>
+__device__ __forceinline__ void store_out(const SharedArgs& a, int64_t row, int h, int D, int d, float top, float sum,
+                                          const f32x4_t& acc) {
+    const float den = a.sinks ? sum + exp2f(fmaf(a.sinks[h], kLog2e, -top)) : sum;
+    const f32x4_t y = sum == 0.f ? f32x4_t{0.f, 0.f, 0.f, 0.f} : acc / den;
+    T* to = static_cast<T*>(a.out) + (row * a.hq + h) * D + d;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) Storage<T>::store(to, e, y[e]);
+}
+
+// The four wavefronts' states of the same rows, joined and stored: as a partial result, or
+// where the piece is all that its rows see (WHOLE) as the output.  smem: 4 D / 16 KiB.
+template <typename T, int D, int RT, bool WHOLE>
 __device__ __forceinline__ void join_waves(const SharedArgs& a, const Piece& p, float* m, float* l, f32x4_t (*o)[D / 16],
                                            uint8_t* smem) {
     constexpr int DT = D / 16;
@@ -602,15 +616,21 @@ __device__ __forceinline__ void join_waves(const SharedArgs& a, const Piece& p, 
             f32x4_t v = part[t * kWave + lane] * f[0];
 #pragma unroll
             for (int w = 1; w < kWaves; ++w) v += part[(w * DT + t) * kWave + lane] * f[w];
-            store_partial<D>(a, p, lane / 16, r * 16 + l16, t, v);
+            if constexpr (WHOLE) {
+                const int e = p.row0 + r * 16 + l16;
+                if (r * 16 + l16 < p.rows)
+                    store_out<T>(a, p.q0 + e / a.group, p.head * a.group + e % a.group, D, 16 * t + 4 * (lane / 16), top, all, v);
+            } else {
+                store_partial<D>(a, p, lane / 16, r * 16 + l16, t, v);
+            }
         }
-        if (threadIdx.x < 16 && r * 16 + l16 < p.rows) a.part_ml[p.slot_row + r * 16 + l16] = make_float2(top, all);
+        if (!WHOLE && threadIdx.x < 16 && r * 16 + l16 < p.rows) a.part_ml[p.slot_row + r * 16 + l16] = make_float2(top, all);
         __syncthreads();
     }
 }
 
 // Few rows, bf16.
-template <int D>
+template <int D, bool WHOLE = false>
 __device__ void walk_flat(const SharedArgs& a, const Index& x, const Piece& p, uint8_t* smem) {
     constexpr int RT = 1, DT = D / 16, C = D / 32;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = own_lane(), l16 = lane % 16,
@@ -682,14 +702,14 @@ __device__ void walk_flat(const SharedArgs& a, const Index& x, const Piece& p, u
         id0 = next0;
         id1 = next1;
     }
-    join_waves<D, RT>(a, p, m, l, o, smem);
+    join_waves<uint16_t, D, RT, WHOLE>(a, p, m, l, o, smem);
 }
 
 // Few rows, fp32: fp32 products (v_mfma_f32_16x16x4_f32), a block of 16 keys at a time.
 // Lane 16 lg + l16 takes the 16-byte chunks lg, lg + 4, ... of key l16; product i of a
 // chunk multiplies its i-th dim.  A lane's 16 bytes of V^T are its keys 4 lg .. 4 lg + 3.
 // Bound by the matrix units where there are several tiles, by memory with one.
-template <int D, int RT>
+template <int D, int RT, bool WHOLE = false>
 __device__ void walk_flat_f32(const SharedArgs& a, const Index& x, const Piece& p, uint8_t* smem) {
     constexpr int DT = D / 16, C = D / 16;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = own_lane(), l16 = lane % 16,
@@ -794,7 +814,7 @@ __device__ void walk_flat_f32(const SharedArgs& a, const Index& x, const Piece& 
         id = next;
     }
     if (kInLds) __syncthreads();  // Q is used up
-    join_waves<D, RT>(a, p, m, l, o, smem);
+    join_waves<float, D, RT, WHOLE>(a, p, m, l, o, smem);
 }
 
 // Many rows, bf16: wavefront w has the rows' tiles w, w + 4, ...; the ring's stages hold two
@@ -1115,6 +1135,38 @@ __global__ __launch_bounds__(kThreads, 2) void shared_walk(SharedArgs a, Index x
     }
 }
 
+// Few and short requests, whose 16-row tiles the card holds all at once: a workgroup walks
+// all that a tile's rows see, the prefix as the request's own table names it, with nothing
+// to divide before and nothing to join behind it.  Bound by the chain of lengths, block ids
+// and keys, then by 0.6 us per unit of bf16, 1.0 of fp32.  Replayed, divided and like this:
+// 8 requests of a row and 1024 keys 12.9 and 8.3 us, of 2048 keys 16.2 and 18.1; 16 of three
+// rows and 128 keys 13.9 and 4.6, 1024 keys 18.0 and 11.7; fp32, 8 of 256 keys 14.2 and 9.1,
+// of 512 16.2 and 14.1, but 2 of 512 11.8 and 14.2.
+//
+// Workgroup (head, request, tile).
+template <typename T, int D>
+__global__ __launch_bounds__(kThreads, 2) void shared_short(SharedArgs a, Index x) {
+    __shared__ __attribute__((aligned(16))) uint8_t smem[kWaves * (D / 16) * 1024];
+    const int i = blockIdx.y;
+    const int q0 = clamp_to(x.q_start[i], 0, a.total_q), n = clamp_to(x.q_start[i + 1], q0, a.total_q) - q0;
+    Piece p{};
+    p.q0 = q0;
+    p.head = blockIdx.x;
+    p.S = clamped_len(a, x, i);
+    p.b_hi = (p.S + kBlockTokens - 1) / kBlockTokens;
+    p.pos0 = p.S - n;
+    p.table = x.tables + (int64_t)i * a.max_blocks;
+    const int rows = n * a.group;
+    for (p.row0 = blockIdx.z * 16; p.row0 < rows; p.row0 += gridDim.z * 16) {
+        p.rows = min(16, rows - p.row0);
+        p.min_pos = p.pos0 + p.row0 / a.group;
+        const int seen = p.pos0 + (p.row0 + p.rows - 1) / a.group + 1, unit = kBlockTokens << a.unit_shift;
+        p.u1 = (max(0, seen) + unit - 1) / unit;
+        if constexpr (sizeof(T) == 2) walk_flat<D, true>(a, x, p, smem);
+        else walk_flat_f32<D, 1, true>(a, x, p, smem);
+    }
+}
+
 // A row's parts joined: kLanes lanes for the dims of a (row, query head), SPLIT groups of
 // them for its pieces, a workgroup per row and run of heads.
 template <typename T, int D, int SPLIT>
@@ -1190,12 +1242,7 @@ __global__ __launch_bounds__(kThreads) void shared_join(SharedArgs a) {
         }
     }
     if ((int)blockIdx.y * kHeads + unit / SPLIT >= a.hq) return;
-    // a sink adds to the sum alone; a row without keys is zero
-    const float den = a.sinks ? sum + exp2f(fmaf(a.sinks[h], kLog2e, -top)) : sum;
-    const f32x4_t y = sum == 0.f ? f32x4_t{0.f, 0.f, 0.f, 0.f} : acc / den;
-    T* to = static_cast<T*>(a.out) + ((int64_t)row * a.hq + h) * D + d;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) Storage<T>::store(to, e, y[e]);
+    store_out<T>(a, row, h, D, d, top, sum, acc);
 }
 
 // ------------------------------------------------------------------ host side
@@ -1204,6 +1251,7 @@ struct SharedPlan {
     int nwg, tile_a, tile_b;
     int64_t slots_a, slots_b, segs;
     bool inlined, weighted;
+    int short_tiles;  // row tiles of a request where all are short (shared_short), or 0
     int split;  // groups of threads that share a row's pieces in the pass that joins
     size_t o_bytes, ml_bytes, total;
 };
@@ -1226,6 +1274,13 @@ int plan_shared(const verify_attn_params* p, int32_t total_q, int32_t max_q_len,
     s.tile_b = tile(own_rows);
     s.weighted = own_rows > 128 && s.tile_b > 128;
     // (rounded up, so that fewer rows in smaller tiles never need more)
+    const int64_t keys = std::min<int64_t>(max_seq_len, (int64_t)p->max_blocks_per_seq * kBlockTokens);
+    const int64_t tiles16 = (own_rows + 15) / 16, pairs16 = tiles16 * p->num_seqs * p->num_kv_heads;
+    s.short_tiles = keys <= (f32 ? kShortF32 : kShort) && pairs16 <= s.nwg && p->num_seqs <= 65535 ? (int)tiles16 : 0;
+    if (s.short_tiles) {
+        s.total = 0;
+        return VERIFY_OK;
+    }
     const int64_t pairs_a = ((rows + s.tile_a - 1) / s.tile_a + num_groups) * p->num_kv_heads;
     const int64_t pairs_b = ((rows + s.tile_b - 1) / s.tile_b + p->num_seqs) * p->num_kv_heads;
     if (pairs_a + pairs_b >= (1 << 30)) return VERIFY_EUNSUPPORTED;
@@ -1268,6 +1323,10 @@ bool is_plain(const verify_attn_params* p, int32_t num_groups, int32_t max_prefi
 
 template <typename T, int D>
 void launch_shared(const SharedArgs& a, const Index& x, const SharedPlan& plan, hipStream_t stream) {
+    if (plan.short_tiles) {
+        hipLaunchKernelGGL((shared_short<T, D>), dim3(a.hkv, a.num_seqs, plan.short_tiles), dim3(kThreads), 0, stream, a, x);
+        return;
+    }
     const int split = plan.split;
     if (plan.inlined) {
         hipLaunchKernelGGL((shared_walk<T, D, true>), dim3(a.nwg), dim3(kThreads), 0, stream, a, x);
@@ -1304,7 +1363,7 @@ extern "C" int verify_attention_shared_workspace_size(const verify_attn_params* 
     if (params->num_seqs == 0 || total_q == 0) return VERIFY_OK;
     if (is_plain(params, num_groups, max_prefix_len))
         return verify_attention_workspace_size(params, total_q, max_q_len, max_seq_len, bytes);
-    SharedPlan s;
+    SharedPlan s{};
     rc = plan_shared(params, total_q, max_q_len, max_seq_len, num_groups, max_prefix_len, s);
     if (rc == VERIFY_OK) *bytes = s.total;
     return rc;
@@ -1325,10 +1384,10 @@ extern "C" int verify_attention_shared(const verify_attn_params* params, int32_t
     if (!q || !k_cache || !v_cache || !block_tables || !seq_lens || !q_start || !group_start || !prefix_lens || !out)
         return VERIFY_EINVAL;
     if (((uintptr_t)k_cache | (uintptr_t)v_cache | (uintptr_t)workspace) & 15) return VERIFY_EINVAL;
-    SharedPlan s;
+    SharedPlan s{};
     rc = plan_shared(params, total_q, max_q_len, max_seq_len, num_groups, max_prefix_len, s);
     if (rc != VERIFY_OK) return rc;
-    if (!workspace || workspace_bytes < s.total) return VERIFY_EWORKSPACE;
+    if (s.total > 0 && (!workspace || workspace_bytes < s.total)) return VERIFY_EWORKSPACE;
     uint8_t* ws = static_cast<uint8_t*>(workspace);
     SharedArgs a{};
     a.q = q;

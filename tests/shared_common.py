@@ -13,9 +13,10 @@ from bounded_common import BLOCK, q_start_of
 class SharedBatch:
     """groups: [(requests, prefix length)]; S, n: cached keys (with the prefix) and new
     tokens of each request.  Requests in front of and behind the groups: `lead` and the
-    rest.  Slots behind a request's keys and spare blocks hold NaN."""
+    rest.  Slots behind a request's keys and spare blocks hold NaN.  wide: block tables
+    and bounds of longer requests, so that none counts as short."""
 
-    def __init__(self, seed, groups, S, n, *, hq, hkv, d, dtype, lead=0, sinks=False, spike=False, unmapped=()):
+    def __init__(self, seed, groups, S, n, *, hq, hkv, d, dtype, lead=0, sinks=False, spike=False, unmapped=(), wide=False):
         rng = np.random.default_rng(seed)
         self.S, self.n = np.asarray(S, dtype=np.int32), np.asarray(n, dtype=np.int32)
         self.hq, self.hkv, self.d, self.dtype = hq, hkv, d, dtype
@@ -51,11 +52,14 @@ class SharedBatch:
         self.q, self.k, self.v = q.to(tdt), k_cache.to(tdt), v_cache.to(tdt)
         for i, b in unmapped:
             self.table[i, b] = [-1, total, 2 ** 31 - 1][b % 3]
+        if wide:
+            self.table = np.pad(self.table, ((0, 0), (0, max(0, 100 - self.table.shape[1]))), constant_values=-1)
+        self.max_seq_len = 16 * self.table.shape[1] if wide else int(self.S.max(initial=0))
         self.sinks = torch.as_tensor(rng.standard_normal(hq), dtype=torch.float32) if sinks else None
 
     @property
     def bounds(self):
-        return dict(max_q_len=int(self.n.max(initial=0)), max_seq_len=int(self.S.max(initial=0)),
+        return dict(max_q_len=int(self.n.max(initial=0)), max_seq_len=self.max_seq_len,
                     max_prefix_len=int(self.prefix.max(initial=0)))
 
     def to(self, device):

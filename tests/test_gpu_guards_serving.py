@@ -22,14 +22,15 @@ def _dev(x, dtype=None):
 
 
 @pytest.mark.parametrize("dtype,hq,hkv,d", [("bf16", 8, 2, 128), ("bf16", 8, 1, 64), ("f32", 6, 3, 128)])
+@pytest.mark.parametrize("wide", [False, True], ids=["", "wide"])
 @pytest.mark.parametrize("name,groups,S,n", [
     ("tall", [(6, 400)], [420 + 31 * i for i in range(6)], [9] * 6),
     ("flat", [(2, 1000), (0, 30), (1, 64)], [1001, 1010, 70, 33], [1, 2, 1, 1]),
     ("prompts", [(2, 96)], [400, 96], [300, 50]),
     ("many", [(200, 32), (90, 48)], [49 + i % 31 for i in range(300)], [1 + i % 3 for i in range(300)]),
 ])
-def test_shared_attention(name, groups, S, n, dtype, hq, hkv, d):
-    b = SharedBatch(11, groups, S, n, hq=hq, hkv=hkv, d=d, dtype=dtype, sinks=True)
+def test_shared_attention(name, groups, S, n, dtype, hq, hkv, d, wide):
+    b = SharedBatch(11, groups, S, n, hq=hq, hkv=hkv, d=d, dtype=dtype, sinks=True, wide=wide)
     args = b.to(DEV)
     sinks = b.sinks.to(DEV)
     size = av.attention_shared_workspace_size(args[0], args[1], args[3], num_groups=len(groups), **b.bounds)

@@ -34,9 +34,10 @@ HEADS = [(8, 2, 128, "bf16"), (8, 1, 64, "bf16"), (10, 2, 128, "bf16"), (8, 2, 1
 
 
 @pytest.mark.parametrize("hq,hkv,d,dtype", HEADS)
+@pytest.mark.parametrize("wide", [False, True], ids=["", "wide"])
 @pytest.mark.parametrize("name,groups,S,n,opt", CASES, ids=[c[0] for c in CASES])
-def test_shared(name, groups, S, n, opt, hq, hkv, d, dtype):
-    b = SharedBatch(len(S) + hq, groups, S, n, hq=hq, hkv=hkv, d=d, dtype=dtype, **opt)
+def test_shared(name, groups, S, n, opt, wide, hq, hkv, d, dtype):
+    b = SharedBatch(len(S) + hq, groups, S, n, hq=hq, hkv=hkv, d=d, dtype=dtype, wide=wide, **opt)
     args = b.to(DEV)
     before = [t.clone() for t in args]
     got = b.call(DEV, args)
@@ -57,7 +58,7 @@ def test_rows_of_very_different_numbers_share_few_units(short, long, keys):
     """Ranges of a few units, in which the rows' tiles weigh differently."""
     n = [short, long, short]
     b = SharedBatch(keys + long, [(3, 32)], [32 + keys + long, 32 + keys + long, 40 + short], n, hq=8, hkv=1, d=64,
-                    dtype="bf16")
+                    dtype="bf16", wide=True)
     b.check(b.call(DEV))
 
 
@@ -78,8 +79,21 @@ def test_more_requests_than_a_workgroup_counts_itself(batch):
     b.check(b.call(DEV))
 
 
-def test_bounds_that_are_not_tight_and_a_request_beyond_max_q_len():
-    b = SharedBatch(3, [(3, 200)], [260, 300, 210], [3, 70, 2], hq=8, hkv=2, d=128, dtype="bf16")
+@pytest.mark.parametrize("keys,dtype,short", [(1024, "bf16", True), (1025, "bf16", False), (448, "f32", True), (449, "f32", False)])
+def test_short_requests_need_no_workspace(keys, dtype, short):
+    """On both sides of the longest short request, with more rows than one tile and than
+    max_q_len."""
+    n = [1, 9, 30]
+    b = SharedBatch(keys, [(2, 333)], [keys, 340, keys - 50], n, hq=10, hkv=2, d=64, dtype=dtype, sinks=True)
+    args = b.to(DEV)
+    assert (av.attention_shared_workspace_size(args[0], args[1], args[3], num_groups=1, **b.bounds) == 0) == short
+    b.check(b.call(DEV, args))
+    b.check(b.call(DEV, args, max_q_len=2))
+
+
+@pytest.mark.parametrize("wide", [False, True])
+def test_bounds_that_are_not_tight_and_a_request_beyond_max_q_len(wide):
+    b = SharedBatch(3, [(3, 200)], [260, 300, 210], [3, 70, 2], hq=8, hkv=2, d=128, dtype="bf16", wide=wide)
     for kw in (dict(max_q_len=1), dict(max_q_len=500), dict(max_seq_len=16 * b.table.shape[1]), dict(max_prefix_len=5000)):
         b.check(b.call(DEV, **kw), str(kw))
     # a smaller bound cuts the shared part, not the result
@@ -95,8 +109,9 @@ def test_bounds_that_are_not_tight_and_a_request_beyond_max_q_len():
         np.testing.assert_array_equal(bits(got), bits(want))
 
 
-def test_rows_behind_the_last_request_stay_as_they_were():
-    b = SharedBatch(9, [(2, 64)], [80, 90], [2, 3], hq=4, hkv=2, d=64, dtype="bf16")
+@pytest.mark.parametrize("wide", [False, True])
+def test_rows_behind_the_last_request_stay_as_they_were(wide):
+    b = SharedBatch(9, [(2, 64)], [80, 90], [2, 3], hq=4, hkv=2, d=64, dtype="bf16", wide=wide)
     q, *rest = b.to(DEV)
     q = torch.cat([q, q[:2]])
     out = torch.full_like(q, 7.0)
@@ -105,9 +120,11 @@ def test_rows_behind_the_last_request_stay_as_they_were():
     assert (out[5:] == 7).all()
 
 
-def test_operands_at_odd_addresses():
+@pytest.mark.parametrize("wide", [False, True])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_operands_at_odd_addresses(dtype, wide):
     """q and out need only be aligned to an element."""
-    b = SharedBatch(2, [(3, 100)], [150, 120, 300], [4, 1, 9], hq=8, hkv=2, d=128, dtype="bf16")
+    b = SharedBatch(2, [(3, 100)], [150, 120, 300], [4, 1, 9], hq=8, hkv=2, d=128, dtype=dtype, wide=wide)
     args = b.to(DEV)
     want = b.call(DEV, args)
     flat = torch.zeros(args[0].numel() + 3, dtype=args[0].dtype, device=DEV)
@@ -116,12 +133,13 @@ def test_operands_at_odd_addresses():
     np.testing.assert_array_equal(bits(b.call(DEV, [q] + args[1:], out=out)), bits(want))
 
 
-def test_captured_and_replayed_on_new_lengths():
+@pytest.mark.parametrize("wide", [False, True])
+def test_captured_and_replayed_on_new_lengths(wide):
     """A graph's launch holds for any lengths within its bounds."""
-    b = SharedBatch(4, [(3, 320)], [500, 400, 350], [4, 2, 9], hq=8, hkv=2, d=64, dtype="bf16", sinks=True)
+    b = SharedBatch(4, [(3, 320)], [500, 400, 350], [4, 2, 9], hq=8, hkv=2, d=64, dtype="bf16", sinks=True, wide=wide)
     args = b.to(DEV)
     sinks = b.sinks.to(DEV)
-    bounds = dict(max_q_len=9, max_seq_len=600, max_prefix_len=400)
+    bounds = dict(max_q_len=9, max_seq_len=1600 if wide else 600, max_prefix_len=400)
     ws = torch.empty(av.attention_shared_workspace_size(args[0], args[1], args[3], num_groups=1, **bounds),
                      dtype=torch.uint8, device=DEV)
     out = torch.empty_like(args[0])
@@ -139,8 +157,10 @@ def test_captured_and_replayed_on_new_lengths():
         np.testing.assert_array_equal(bits(out), bits(run(None, None)))
 
 
-def test_two_calls_at_once_on_streams_of_their_own():
-    b = [SharedBatch(s, [(6, 640)], [700 + 50 * i for i in range(6)], [5] * 6, hq=8, hkv=2, d=128, dtype="bf16") for s in (1, 2)]
+@pytest.mark.parametrize("wide", [False, True])
+def test_two_calls_at_once_on_streams_of_their_own(wide):
+    b = [SharedBatch(s, [(6, 640)], [700 + 50 * i for i in range(6)], [5] * 6, hq=8, hkv=2, d=128, dtype="bf16", wide=wide)
+         for s in (1, 2)]
     args = [x.to(DEV) for x in b]
     want = [bits(x.call(DEV, a)) for x, a in zip(b, args)]
     streams = [torch.cuda.Stream() for _ in b]
