@@ -100,6 +100,7 @@ def test_adjust_logits(n, V, opt, dtype):
     x_t = torch.as_tensor(x).to(workload.torch_dtype(dtype))
     ref, size, touched = serving.adjust_logits(x_t.double().numpy(), c["tokens"], c["q_start"], **kw)
     dev = {k: _dev(v) for k, v in kw.items()}
+    before = [v.clone() for v in dev.values()]
     tok, qs = _dev(c["tokens"]), _dev(c["q_start"])
     logits = x_t.to(DEV)
     got = av.verify_adjust_logits(logits, tok, qs, **dev)
@@ -117,7 +118,6 @@ def test_adjust_logits(n, V, opt, dtype):
         av.verify_adjust_logits(part, tok, qs, out=part, **dev)
         np.testing.assert_array_equal(bits(part), bits(got))
         assert (wide[:, :off] == 9).all() and (wide[:, off + V:] == 9).all()
-    before = [v.clone() for v in dev.values()]
     for a, b in zip(before, dev.values()):
         assert torch.equal(a, b)
 
