@@ -1135,13 +1135,16 @@ __global__ __launch_bounds__(kThreads, 2) void shared_walk(SharedArgs a, Index x
     }
 }
 
-// Few and short requests, whose 16-row tiles the card holds all at once: a workgroup walks
-// all that a tile's rows see, the prefix as the request's own table names it, with nothing
-// to divide before and nothing to join behind it.  Bound by the chain of lengths, block ids
-// and keys, then by 0.6 us per unit of bf16, 1.0 of fp32.  Replayed, divided and like this:
-// 8 requests of a row and 1024 keys 12.9 and 8.3 us, of 2048 keys 16.2 and 18.1; 16 of three
-// rows and 128 keys 13.9 and 4.6, 1024 keys 18.0 and 11.7; fp32, 8 of 256 keys 14.2 and 9.1,
-// of 512 16.2 and 14.1, but 2 of 512 11.8 and 14.2.
+// Few and short requests: a workgroup walks all that 16 rows of a request and head see, the
+// prefix as the request's own table names it, with nothing to divide before and nothing to
+// join behind it.  Bound by the chain of lengths, block ids and keys, then by 0.6 us per
+// unit of bf16, 1.0 of fp32, and with many requests by the keys, prefixes out of L2.
+// Replayed, divided and like this: 8 requests of a row and 1024 keys 12.9 and 8.3 us, of
+// 2048 keys 16.2 and 18.1; fp32, 8 of 256 keys 14.2 and 9.1, of 512 16.2 and 14.1, but 2 of
+// 512 11.8 and 14.2.  All tiles' keys together: 128 requests of eight heads, 1000 keys, 141 of
+// them common, 101 and 84, 875 common 31 and 29; 250 such 42 and 52.  With several tiles,
+// which read the same keys: 64 requests of nine rows, 256 keys, 31 and 28, 512 keys 37 and 52
+// (fp32, where the divided walk takes few rows too: 256 keys 64 and 58).
 //
 // Workgroup (head, request, tile).
 template <typename T, int D>
@@ -1276,7 +1279,8 @@ int plan_shared(const verify_attn_params* p, int32_t total_q, int32_t max_q_len,
     // (rounded up, so that fewer rows in smaller tiles never need more)
     const int64_t keys = std::min<int64_t>(max_seq_len, (int64_t)p->max_blocks_per_seq * kBlockTokens);
     const int64_t tiles16 = (own_rows + 15) / 16, pairs16 = tiles16 * p->num_seqs * p->num_kv_heads;
-    s.short_tiles = keys <= (f32 ? kShortF32 : kShort) && pairs16 <= s.nwg && p->num_seqs <= 65535 ? (int)tiles16 : 0;
+    const int64_t most = f32 ? kShortF32 : kShort, rounds = f32 || tiles16 == 1 ? 2 : 1;
+    s.short_tiles = keys <= most && pairs16 * keys <= rounds * s.nwg * most && p->num_seqs <= 65535 ? (int)tiles16 : 0;
     if (s.short_tiles) {
         s.total = 0;
         return VERIFY_OK;

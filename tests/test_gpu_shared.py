@@ -69,13 +69,14 @@ def test_a_long_prefix_and_long_requests(dtype):
     b.check(b.call(DEV))
 
 
+@pytest.mark.parametrize("wide", [False, True])
 @pytest.mark.parametrize("batch", [511, 512, 700])
-def test_more_requests_than_a_workgroup_counts_itself(batch):
+def test_more_requests_than_a_workgroup_counts_itself(batch, wide):
     rng = np.random.default_rng(batch)
     sizes = [batch // 3, 0, batch // 2]
     lens = [int(x) for x in rng.integers(49, 120, size=batch)]
     n = [int(x) for x in rng.integers(0, 4, size=batch)]
-    b = SharedBatch(batch, list(zip(sizes, [32, 10, 48])), lens, n, hq=4, hkv=2, d=64, dtype="bf16", lead=2)
+    b = SharedBatch(batch, list(zip(sizes, [32, 10, 48])), lens, n, hq=4, hkv=2, d=64, dtype="bf16", lead=2, wide=wide)
     b.check(b.call(DEV))
 
 
