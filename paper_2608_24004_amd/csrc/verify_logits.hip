@@ -127,22 +127,22 @@ __global__ __launch_bounds__(kThreads) void adjust_rows(AdjustArgs a) {
     __shared__ int s_count[kPer][kThreads];
     __shared__ float s_bias[kPer][kThreads];
     const int tid = threadIdx.x, i = blockIdx.y;
+    const bool penal = a.penal;
+    const int slot = penal ? a.slots ? a.slots[i] : i : -1;
+    const float rep = a.repetition ? a.repetition[i] : 1.f, freq = a.frequency ? a.frequency[i] : 0.f,
+                pres = a.presence ? a.presence[i] : 0.f;
+    const int b0 = a.bias_start ? max(0, min(a.bias_start[i], a.num_biases)) : 0;
+    const int b1 = a.bias_start ? min(a.bias_start[i + 1], a.num_biases) : 0;
     const int q0 = max(0, min(a.q_start[i], a.total_q)), n = max(0, min(a.q_start[i + 1], a.total_q) - q0);
     const int part = (n + (int)gridDim.z - 1) / (int)gridDim.z;
     const int j0 = min(n, (int)blockIdx.z * part), j1 = min(n, j0 + part);
     if (j0 >= j1) return;
-    const bool penal = a.penal;
     // the rows' drafts and masks, kThreads of them at a time
     auto read_rows = [&](int from) {
         const int j = from + tid;
         s_draft[tid] = penal && j > 0 && j < n ? a.tokens[q0 + j] : -1;
         s_mask[tid] = a.mask_rows && j < n ? a.mask_rows[q0 + j] : -1;
     };
-    const int slot = penal ? a.slots ? a.slots[i] : i : -1;
-    const float rep = a.repetition ? a.repetition[i] : 1.f, freq = a.frequency ? a.frequency[i] : 0.f,
-                pres = a.presence ? a.presence[i] : 0.f;
-    const int b0 = a.bias_start ? max(0, min(a.bias_start[i], a.num_biases)) : 0;
-    const int b1 = a.bias_start ? min(a.bias_start[i + 1], a.num_biases) : 0;
     int rows0 = j0;  // the row of the first entry in s_draft
     read_rows(rows0);
     __syncthreads();
@@ -175,10 +175,23 @@ __global__ __launch_bounds__(kThreads) void adjust_rows(AdjustArgs a) {
             if (base + x < j1 && live && allowed[x] && (!IN_PLACE || (touched >> x & 1u) || allowed[x] != 0xffu))
                 g[x].load(in + (int64_t)(base + x) * a.row_stride + tok0, room);
     };
-    // Out of place the first rows are under way before the state that changes them is
-    // read: a chain of four or five memory latencies.
+    // The state's bits and the first masks, then out of place the first rows, are under way
+    // before anything is waited for that does not lead to them.
+    uint32_t prompt = 0, out = 0;
+    const int32_t* counts = nullptr;
+    if (penal && slot >= 0 && slot < a.num_slots) {
+        const uint8_t* seen = a.seen + (int64_t)slot * 2 * a.words * 4;
+        counts = a.counts + (int64_t)slot * a.vocab;
+        prompt = bits_of(seen);
+        out = bits_of(seen + (int64_t)a.words * 4);
+    }
     load_masks(j0);
     if (!IN_PLACE) load_rows(j0, 0);
+    int c[kPer] = {};
+    if (out) {
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) c[e] = (out >> e & 1u) && e < room ? counts[tok0 + e] : 0;
+    }
 
     // a token of this span: its thread, and its place among that thread's
     auto owner = [&](int d) { return (d - span0) / kPer; };
@@ -189,13 +202,17 @@ __global__ __launch_bounds__(kThreads) void adjust_rows(AdjustArgs a) {
 #pragma unroll
     for (int e = 0; e < kPer; ++e) add[e] = -0.f;
     if (b1 > b0) {
-#pragma unroll
-        for (int e = 0; e < kPer; ++e) s_bias[e][tid] = -0.f;
+        bool found = false;
         // the list's entries of this span, kThreads of the list at a time, in its order
         for (int base = b0; base < b1; base += kThreads) {
             const int at = base + tid, tok = at < b1 ? a.bias_tokens[at] : -1;
             const bool here = tok >= span0 && tok - span0 < kSpan && tok < a.vocab;
             if (!__syncthreads_or(here)) continue;
+            if (!found) {
+#pragma unroll
+                for (int e = 0; e < kPer; ++e) s_bias[e][tid] = -0.f;
+                found = true;
+            }
             const uint64_t vote = __ballot(here);
             if (tid % kWave == 0) s_found[tid / kWave] = __popcll(vote);
             __syncthreads();
@@ -222,27 +239,18 @@ __global__ __launch_bounds__(kThreads) void adjust_rows(AdjustArgs a) {
         }
     }
     if (penal) {
-        uint32_t prompt = 0, out = 0;
-        const int32_t* counts = nullptr;
-        if (slot >= 0 && slot < a.num_slots) {
-            const uint8_t* seen = a.seen + (int64_t)slot * 2 * a.words * 4;
-            counts = a.counts + (int64_t)slot * a.vocab;
-            prompt = bits_of(seen);
-            out = bits_of(seen + (int64_t)a.words * 4);
-        }
         had = prompt;
-#pragma unroll
-        for (int e = 0; e < kPer; ++e) s_count[e][tid] = 0;
         if (out) {
-            int c[kPer];
-#pragma unroll
-            for (int e = 0; e < kPer; ++e) c[e] = (out >> e & 1u) && e < room ? max(0, counts[tok0 + e]) : 0;
 #pragma unroll
             for (int e = 0; e < kPer; ++e) {
-                s_count[e][tid] = c[e];
+                c[e] = max(0, c[e]);
                 had |= (uint32_t)(c[e] > 0) << e;
                 if (c[e] > 0) add[e] -= fmaf(freq, (float)c[e], pres);
             }
+        }
+        if (n > 1) {  // there are drafts
+#pragma unroll
+            for (int e = 0; e < kPer; ++e) s_count[e][tid] = c[e];
         }
     }
     // the draft that row j stands behind, or -1 where it is none of this span's tokens
