@@ -54,8 +54,8 @@ __device__ __forceinline__ float group_sum(float v, int sh) {
 // Query or key heads of a workgroup at most (six prompts of 12 thousand rows in all: 54.3 us
 // with 16, 56.8 with 8).
 constexpr int kNormHeads = 16;
-// Workgroups that a compute unit holds, by their registers.
-constexpr int resident(bool append, bool inter) { return !inter ? 5 : append ? 6 : 8; }
+// Workgroups that a compute unit holds, by their registers or their wavefronts.
+constexpr int resident(bool append, bool wide, bool inter) { return !wide ? 8 : !inter ? 5 : append ? 6 : 8; }
 // (row, head) units of a thread in flight, 64 bytes.
 constexpr int units(bool inter) { return inter ? 4 : 2; }
 
@@ -280,12 +280,16 @@ int norm_call(NormArgs& na, const verify_rotary_params& p, hipStream_t stream) {
     for (int f = 0; f < a.freqs; ++f) a.axis[f] = p.axis[f];
     const int esize = p.dtype == VERIFY_BF16 ? 2 : 4, n = 16 / esize;
     if (APPEND) a.value_wgs = (a.hkv + value_heads(esize) - 1) / value_heads(esize);
+    const uint64_t bits = (uint64_t)(uintptr_t)a.q | (uintptr_t)a.k | (uintptr_t)a.v | (uintptr_t)a.q_out | (uintptr_t)a.k_out;
+    const int64_t strides = a.q_stride | a.k_stride | a.v_stride | a.q_out_stride | a.k_out_stride;
+    const int step = p.interleaved ? p.rotary_dim : a.freqs;
+    const bool wide = (bits & 15) == 0 && strides % n == 0 && step % n == 0;
     // Heads per workgroup, two at least.  Each costs its heads and some four more for its
     // tile's angles; what counts is the mean of all of them and of the rounds that they
     // take (2500 rows of 40 heads: eight, in one round, 14.0 us; three, in not quite two, 18.2;
     // 8000 rows: eight, in two, 39.4; 16, in one and a sixth, 41.5).  Of long inputs all
     // that a workgroup takes.
-    const int64_t tiles = ((int64_t)a.total_q + kTile - 1) / kTile, fit = (int64_t)resident(APPEND, p.interleaved) * device_cus();
+    const int64_t tiles = ((int64_t)a.total_q + kTile - 1) / kTile, fit = (int64_t)resident(APPEND, wide, p.interleaved) * device_cus();
     auto groups = [&](int64_t heads, int h) { return (heads + h - 1) / h; };
     auto wgs = [&](int h) { return tiles * (groups(a.hq, h) + groups(a.hkv, h) + a.value_wgs); };
     auto cost = [&](int h) { return ((wgs(h) + fit - 1) / fit * fit + wgs(h)) * (h + 4); };
@@ -294,10 +298,6 @@ int norm_call(NormArgs& na, const verify_rotary_params& p, hipStream_t stream) {
         for (int h = a.heads_per_wg - 1; h >= 2; --h)
             if (cost(h) < cost(a.heads_per_wg)) a.heads_per_wg = h;
     a.key_wgs = (int)groups(a.hkv, a.heads_per_wg);
-    const uint64_t bits = (uint64_t)(uintptr_t)a.q | (uintptr_t)a.k | (uintptr_t)a.v | (uintptr_t)a.q_out | (uintptr_t)a.k_out;
-    const int64_t strides = a.q_stride | a.k_stride | a.v_stride | a.q_out_stride | a.k_out_stride;
-    const int step = p.interleaved ? p.rotary_dim : a.freqs;
-    const bool wide = (bits & 15) == 0 && strides % n == 0 && step % n == 0;
     if (p.dtype == VERIFY_BF16)
         p.head_dim == 128 ? launch_norm<uint16_t, 128, APPEND>(na, p, wide, stream)
                           : launch_norm<uint16_t, 64, APPEND>(na, p, wide, stream);
