@@ -579,7 +579,8 @@ int verify_norm_rotary_append(const verify_attn_params *attn, const verify_rotar
  *                same first prefix_lens[k] / 16 (rounded down) entries in block_tables.
  *                Those of the group's first request are read, or each request's own.
  *   max_prefix_len   host upper bound on prefix_lens; below 16, or with no group, the
- *                call is verify_attention (with its workspace)
+ *                call is verify_attention: with its workspace, its max_q_len and its
+ *                condition on unused slots
  *   max_q_len    host upper bound on n_i (sizes the launch; a request may exceed it)
  *   k_cache, v_cache   16-byte aligned (VERIFY_EINVAL otherwise).  Slots behind a
  *                request's last key may hold anything.
