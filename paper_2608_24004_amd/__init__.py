@@ -937,17 +937,17 @@ def _row_matrix(t, name, shape, dtype, idx, device):
     """Address and row stride of a matrix whose rows are contiguous."""
     if not (t is not None and t.dtype is dtype and t.get_device() == idx >= 0 and t.shape == shape):
         _expect(t, name, shape, dtype, device)
-    stride = t.stride(0) if t.shape[0] > 1 else t.shape[1]
-    if t.shape[1] > 1 and t.stride(1) != 1 or stride < t.shape[1]:
-        raise ValueError("%s must have rows of %d adjacent elements, got strides %s" % (name, t.shape[1], tuple(t.stride())))
-    return t.data_ptr(), stride
+    if t.is_contiguous():
+        return t.data_ptr(), shape[1]
+    rows, stride = shape[0], t.stride()
+    if shape[1] > 1 and stride[1] != 1 or rows > 1 and stride[0] < shape[1]:
+        raise ValueError("%s must have rows of %d adjacent elements, got strides %s" % (name, shape[1], tuple(stride)))
+    return t.data_ptr(), stride[0] if rows > 1 else shape[1]
 
 
-def _token_state(counts, seen, slots, vocab, B, idx, dev):
+def _token_state(counts, seen, slots, vocab, B, idx, dev, i32):
     """Addresses of a state of token counts and bits and of the requests' slots in it,
     and its number of slots."""
-    import torch
-    i32 = torch.int32
     if counts.dim() != 2:
         raise ValueError("counts must be [slots, V], got %s" % (tuple(counts.shape),))
     n = counts.shape[0]
@@ -980,9 +980,9 @@ def verify_adjust_logits(logits, tokens, q_start, *, counts=None, seen=None, slo
         raise ValueError("logits must be [T, V], got %s" % (tuple(logits.shape),))
     T, V = logits.shape
     dev, dtype, idx = logits.device, logits.dtype, logits.get_device()
-    if q_start.dim() != 1 or q_start.shape[0] < 1:
+    if q_start.dim() != 1 or q_start.numel() < 1:
         raise ValueError("q_start must be [B + 1], got %s" % (tuple(q_start.shape),))
-    B = q_start.shape[0] - 1
+    B = q_start.numel() - 1
     code = _dtype_code(logits)
     p_logits, stride = _row_matrix(logits, "logits", (T, V), dtype, idx, dev)
     p_qs = _arg(q_start, "q_start", None, i32, idx, dev)
@@ -994,11 +994,11 @@ def verify_adjust_logits(logits, tokens, q_start, *, counts=None, seen=None, slo
         state = (None if repetition is None else _arg(repetition, "repetition", (B,), f32, idx, dev),
                  None if frequency is None else _arg(frequency, "frequency", (B,), f32, idx, dev),
                  None if presence is None else _arg(presence, "presence", (B,), f32, idx, dev),
-                 *_token_state(counts, seen, slots, V, B, idx, dev))
+                 *_token_state(counts, seen, slots, V, B, idx, dev, i32))
     if bias_start is not None:
         if bias_tokens is None or bias_values is None or bias_tokens.dim() != 1:
             raise ValueError("bias_start needs bias_tokens and bias_values of one dim")
-        m = bias_tokens.shape[0]
+        m = bias_tokens.numel()
         bias = (_arg(bias_start, "bias_start", (B + 1,), i32, idx, dev),
                 _arg(bias_tokens, "bias_tokens", None, i32, idx, dev),
                 _arg(bias_values, "bias_values", (m,), f32, idx, dev), m)
@@ -1035,18 +1035,18 @@ def verify_count_tokens(counts, seen, tokens, token_start, *, num_tokens=None, s
     over.  slots [B] int32: the requests' rows of the state (None: 0 .. B-1)."""
     import torch
     i32 = torch.int32
-    if token_start.dim() != 1 or token_start.shape[0] < 1:
+    if token_start.dim() != 1 or token_start.numel() < 1:
         raise ValueError("token_start must be [B + 1], got %s" % (tuple(token_start.shape),))
     if tokens.dim() != 1:
         raise ValueError("tokens must be packed in one dim, got %s" % (tuple(tokens.shape),))
-    B, dev, idx = token_start.shape[0] - 1, counts.device, counts.get_device()
-    p_counts, p_seen, p_slots, n = _token_state(counts, seen, slots, counts.shape[-1], B, idx, dev)
+    B, V, dev, idx = token_start.numel() - 1, counts.shape[-1], counts.device, counts.get_device()
+    p_counts, p_seen, p_slots, n = _token_state(counts, seen, slots, V, B, idx, dev, i32)
     p_tok = _arg(tokens, "tokens", None, i32, idx, dev)
     p_start = _arg(token_start, "token_start", None, i32, idx, dev)
     p_num = None if num_tokens is None else _arg(num_tokens, "num_tokens", (B,), i32, idx, dev)
     if idx < 0:
         _dev_ptr(counts, "counts")
-    _launch("verify_count_tokens", idx, B, tokens.shape[0], counts.shape[1], n, p_tok, p_start, p_num, p_slots,
+    _launch("verify_count_tokens", idx, B, tokens.numel(), V, n, p_tok, p_start, p_num, p_slots,
             int(bool(prompt)), p_counts, p_seen, _stream_ptr(stream, dev))
 
 
