@@ -226,13 +226,18 @@ def _check(status: int, where: str):
         raise VerifyError(status, where)
 
 
+_dtype_codes = {}
+
+
 def _dtype_code(t) -> int:
+    code = _dtype_codes.get(t.dtype)
+    if code is not None:
+        return code
     import torch
-    if t.dtype == torch.bfloat16:
-        return BF16
-    if t.dtype == torch.float32:
-        return F32
-    raise TypeError("unsupported storage dtype %s (bf16 or fp32)" % t.dtype)
+    _dtype_codes.update({torch.bfloat16: BF16, torch.float32: F32})
+    if t.dtype not in _dtype_codes:
+        raise TypeError("unsupported storage dtype %s (bf16 or fp32)" % t.dtype)
+    return _dtype_codes[t.dtype]
 
 
 def _dev_ptr(t, name, dtype=None):
@@ -287,9 +292,13 @@ def _workspace_arg(workspace, idx, device):
             workspace.numel() * workspace.element_size())
 
 
-def _layer_args(Hq, D, dtype, esize, idx, dev, k_cache, v_cache, block_tables, seq_lens, q_start):
+_attn_kept = {}
+
+
+def _layer_args(Hq, D, dtype, esize, idx, dev, k_cache, v_cache, block_tables, seq_lens, q_start, own=True):
     """Addresses of a layer's cache and batch descriptor, and its AttnParams
-    (sliding_window, scale and kv_split_blocks 0).  A batch of no requests may
+    (sliding_window, scale and kv_split_blocks 0): the caller's own, or one kept for
+    every call of the same sizes, which nobody may change.  A batch of no requests may
     come without seq_lens and q_start; the call refuses their absence otherwise."""
     import torch
     i32 = torch.int32
@@ -305,7 +314,15 @@ def _layer_args(Hq, D, dtype, esize, idx, dev, k_cache, v_cache, block_tables, s
     ptrs += [_arg(block_tables, "block_tables", None, i32, idx, dev),
              None if seq_lens is None else _arg(seq_lens, "seq_lens", (B,), i32, idx, dev),
              None if q_start is None else _arg(q_start, "q_start", (B + 1,), i32, idx, dev)]
-    return ptrs, AttnParams(B, Hq, hkv, D, 16, max_blocks, nb, 0, 0.0, _dtype_code(k_cache), 0)
+    key = (B, Hq, hkv, D, 16, max_blocks, nb, 0, 0.0, _dtype_code(k_cache), 0)
+    if own:
+        return ptrs, AttnParams(*key)
+    params = _attn_kept.get(key)
+    if params is None:
+        if len(_attn_kept) > 64:
+            _attn_kept.clear()
+        params = _attn_kept[key] = AttnParams(*key)
+    return ptrs, params
 
 
 # torch.cuda.current_stream builds a Stream object per call (2 us)
@@ -795,17 +812,17 @@ def _rows_arg(t, name, heads, D, dtype, idx, device, T):
 _rotary_params = {}
 
 
-def _rotary_args(q, positions, inv_freq, axes, interleaved, scale, idx, dev):
+def _rotary_args(q, T, D, positions, inv_freq, axes, interleaved, scale, idx, dev):
     """RotaryParams of a call, and the addresses of positions and inv_freq."""
     import torch
-    T, _, D = q.shape
     if inv_freq.dim() != 1:
         raise ValueError("inv_freq must be [rotary_dim / 2], got %s" % (tuple(inv_freq.shape),))
-    F = inv_freq.shape[0]
-    num_axes = 1 if positions.dim() == 1 else positions.shape[0]
+    F = inv_freq.numel()
+    one = positions.dim() == 1
+    num_axes = 1 if one else positions.shape[0]
     if num_axes != 1 if axes is None else len(axes) != F:
         raise ValueError("axes must name the axis of each of the %d frequencies" % F)
-    p_pos = _arg(positions, "positions", (T,) if positions.dim() == 1 else (num_axes, T), torch.int32, idx, dev)
+    p_pos = _arg(positions, "positions", (T,) if one else (num_axes, T), torch.int32, idx, dev)
     p_freq = _arg(inv_freq, "inv_freq", None, torch.float64, idx, dev)
     try:
         # of the usual 64 small numbers a string of bytes is made, hashed and compared in
@@ -869,7 +886,7 @@ def _rotary_call(where, norm, q, k, positions, inv_freq, axes, interleaved, scal
     Hkv = 0 if k is None else k.shape[1]
     p_q, s_q = _rows_arg(q, "q", Hq, D, dtype, idx, dev, T)
     p_k, s_k = (None, 0) if k is None else _rows_arg(k, "k", Hkv, D, dtype, idx, dev, T)
-    params, p_pos, p_freq = _rotary_args(q, positions, inv_freq, axes, interleaved, scale, idx, dev)
+    params, p_pos, p_freq = _rotary_args(q, T, D, positions, inv_freq, axes, interleaved, scale, idx, dev)
     norm = _norm_args(norm, D, idx, dev)
     if q_out is None:
         q_out = _scratch((T, Hq, D), dtype, dev, stream)
@@ -913,11 +930,11 @@ def _rotary_append_call(where, norm, q, k_new, v_new, positions, inv_freq, k_cac
     dtype, dev, idx = q.dtype, q.device, q.get_device()
     p_q, s_q = _rows_arg(q, "q", Hq, D, dtype, idx, dev, T)
     (p_kc, p_vc, *desc), attn = _layer_args(Hq, D, dtype, q.element_size(), idx, dev, k_cache, v_cache, block_tables,
-                                            seq_lens, q_start)
-    Hkv = k_cache.shape[1]
+                                            seq_lens, q_start, own=False)
+    Hkv = attn.num_kv_heads
     p_k, s_k = _rows_arg(k_new, "k_new", Hkv, D, dtype, idx, dev, T)
     p_v, s_v = _rows_arg(v_new, "v_new", Hkv, D, dtype, idx, dev, T)
-    params, p_pos, p_freq = _rotary_args(q, positions, inv_freq, axes, interleaved, scale, idx, dev)
+    params, p_pos, p_freq = _rotary_args(q, T, D, positions, inv_freq, axes, interleaved, scale, idx, dev)
     norm = _norm_args(norm, D, idx, dev)
     if check or check is None and CHECK_BY_DEFAULT:
         _checked(check, where, q_start=q_start, total_q=T, seq_lens=seq_lens,
@@ -1076,14 +1093,14 @@ def verify_attention_shared(q, k_cache, v_cache, block_tables, seq_lens, q_start
     import torch
     if q.dim() != 3:
         raise ValueError("q must be [T, Hq, D], got %s" % (tuple(q.shape),))
-    if group_start.dim() != 1 or group_start.shape[0] < 1:
+    if group_start.dim() != 1 or group_start.numel() < 1:
         raise ValueError("group_start must be [G + 1], got %s" % (tuple(group_start.shape),))
     T, Hq, D = q.shape
     dtype, dev, idx = q.dtype, q.device, q.get_device()
-    G = group_start.shape[0] - 1
+    G = group_start.numel() - 1
     p_q = _arg(q, "q", None, dtype, idx, dev)
     layer, params = _layer_args(Hq, D, dtype, q.element_size(), idx, dev, k_cache, v_cache, block_tables, seq_lens,
-                                q_start)
+                                q_start, own=scale != 0.0)
     p_gs = _arg(group_start, "group_start", None, torch.int32, idx, dev)
     p_pl = _arg(prefix_lens, "prefix_lens", (G,), torch.int32, idx, dev)
     p_sinks = None if sinks is None else _arg(sinks, "sinks", (Hq,), torch.float32, idx, dev)
@@ -1091,7 +1108,8 @@ def verify_attention_shared(q, k_cache, v_cache, block_tables, seq_lens, q_start
     if check or check is None and CHECK_BY_DEFAULT:
         _checked(check, "verify_attention_shared", q_start=q_start, total_q=T, max_q_len=max_q_len, seq_lens=seq_lens,
                  block_tables=block_tables, num_blocks=k_cache.shape[0], max_seq_len=max_seq_len, stream=stream)
-    params.scale = scale
+    if scale != 0.0:
+        params.scale = scale
     bounds = T, int(max_q_len), int(max_seq_len), G, int(max_prefix_len)
     if out is None:
         out = _scratch((T, Hq, D), dtype, dev, stream)
