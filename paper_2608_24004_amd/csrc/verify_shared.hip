@@ -335,17 +335,22 @@ __device__ __forceinline__ Share count_units(const SharedArgs& a, const Index& x
         const float unit = a.tile_a >= 128 ? kTallUnit : 1.f, own = (float)h.ub * (a.weighted ? 0.25f : 1.f);
         const float mean = fmaxf(1.f, ((float)h.ua * unit + own) * __builtin_amdgcn_rcpf(unit * a.nwg));
         auto length = [&](int c) { return fminf(1.0e9f, ceilf(mean * 0.125f * __builtin_amdgcn_exp2f(5.f / 63 * c))); };
-        auto parts_of = [&](const Segment& g, float cost) {
-            return max(1, (int)ceilf((float)units_of(a, g) * __builtin_amdgcn_rcpf(cost) - 0.001f));
+        auto parts_of = [&](int units, float cost) {
+            return max(1, (int)ceilf((float)units * __builtin_amdgcn_rcpf(cost) - 0.001f));
         };
         const float cost = length(lane);
         float all = 0.f;
         int longest = 0;
-        for (int k = 0; k < a.num_groups; ++k) {
-            const Segment& g = segments[k];
-            const int units = units_of(a, g), parts = parts_of(g, cost);
-            all += (float)g.pair0 * (float)parts;
-            longest = max(longest, g.pair0 ? (int)ceilf((float)units * __builtin_amdgcn_rcpf((float)parts) - 0.001f) : 0);
+        for (int base = 0; base < a.num_groups; base += kWave) {
+            // a group to a lane, handed to all lanes one after the other
+            const Segment* mine = segments + min(base + lane, a.num_groups - 1);
+            const int my_units = units_of(a, *mine), my_pairs = mine->pair0;
+            for (int k = 0; k < min(kWave, a.num_groups - base); ++k) {
+                const int units = __builtin_amdgcn_readlane(my_units, k), pairs = __builtin_amdgcn_readlane(my_pairs, k);
+                const int parts = parts_of(units, cost);
+                all += (float)pairs * (float)parts;
+                longest = max(longest, pairs ? (int)ceilf((float)units * __builtin_amdgcn_rcpf((float)parts) - 0.001f) : 0);
+            }
         }
         // the workgroups of this length, eight at least for each kind of work
         const float most = h.ub > 0 ? a.nwg - 8 : a.nwg;
@@ -380,7 +385,7 @@ __device__ __forceinline__ Share count_units(const SharedArgs& a, const Index& x
         for (int base = 0; base < a.num_groups; base += kWave) {
             const int k = base + lane;
             const Segment* g = segments + min(k, a.num_groups - 1);
-            const int parts = k < a.num_groups && g->pair0 > 0 ? parts_of(*g, chosen) : 0;
+            const int parts = k < a.num_groups && g->pair0 > 0 ? parts_of(units_of(a, *g), chosen) : 0;
             const int here = scan_lanes(parts * g->pair0);
             if (tid < kWave && k < a.num_groups) items[k] = Items{h.items + here - parts * g->pair0, parts};
             h.items += __builtin_amdgcn_readlane(here, kWave - 1);
@@ -392,7 +397,19 @@ __device__ __forceinline__ Share count_units(const SharedArgs& a, const Index& x
     return h;
 }
 
+constexpr int kScheduleGroups = 2048;  // that a schedule's workgroup keeps in LDS
 __global__ __launch_bounds__(1024) void shared_schedule(SharedArgs a, Index x) {
+    // every request looks for its group among them
+    __shared__ int32_t s_start[kScheduleGroups + 1], s_prefix[kScheduleGroups];
+    if (a.num_groups <= kScheduleGroups) {
+        for (int k = threadIdx.x; k <= a.num_groups; k += 1024) {
+            s_start[k] = x.group_start[k];
+            if (k < a.num_groups) s_prefix[k] = x.prefix[k];
+        }
+        __syncthreads();
+        x.group_start = s_start;
+        x.prefix = s_prefix;
+    }
     const Share h = count_units<1024, int64_t>(a, x, a.segments, a.items);
     if (threadIdx.x == 0) *a.share = h;
 }
