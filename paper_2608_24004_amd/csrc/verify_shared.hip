@@ -297,11 +297,12 @@ __device__ __forceinline__ Share count_units(const SharedArgs& a, const Index& x
             p = each > 0 ? tiles * a.hkv : 0;
         }
         const Count u = (Count)p * each, u_lanes = scan_lanes(u);
-        const int p_lanes = scan_lanes(p);
+        const int own = s < a.num_groups ? 0 : p;  // prefixes' pairs have slots of their own
+        const int p_lanes = scan_lanes(own);
         if (lane == kWave - 1) s_units[tid / kWave] = u_lanes, s_pairs[tid / kWave] = p_lanes;
         __syncthreads();
         Count u_all = 0, u_before = units + u_lanes - u;
-        int p_all = 0, p_before = pairs + p_lanes - p;
+        int p_all = 0, p_before = pairs + p_lanes - own;
 #pragma unroll
         for (int w = 0; w < THREADS / kWave; ++w) {
             if (w < tid / kWave) u_before += s_units[w], p_before += s_pairs[w];

@@ -62,6 +62,14 @@ def test_rows_of_very_different_numbers_share_few_units(short, long, keys):
     b.check(b.call(DEV))
 
 
+@pytest.mark.parametrize("dtype,d,n", [("f32", 128, [130] * 3), ("bf16", 128, [700, 650]), ("bf16", 64, [900, 850])])
+def test_a_prefix_of_more_row_tiles_than_workgroups_are_left_for_the_requests(dtype, d, n):
+    """The requests' partial results are numbered without the prefixes'."""
+    S = [p + 16 + 20 * i for i, p in enumerate(n)]
+    b = SharedBatch(7, [(len(n), 16)], S, n, hq=32, hkv=4, d=d, dtype=dtype)
+    b.check(b.call(DEV, max_seq_len=16 * b.table.shape[1]))
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_a_long_prefix_and_long_requests(dtype):
     n = [1 + i % 6 for i in range(24)]
