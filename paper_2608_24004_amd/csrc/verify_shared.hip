@@ -53,6 +53,7 @@ constexpr float kLog2e = 1.4426950408889634f;
 // with two 16.3).
 constexpr int unit_shift(bool f32) { return f32 ? 2 : 3; }
 constexpr int kUnitBlocks = 1 << unit_shift(false);
+static_assert(kUnitBlocks == 2 * kWaves && 1 << unit_shift(true) == kWaves, "the flat walks' blocks");
 // What a pair costs beside its blocks (its rows, the first blocks' latency, the join of
 // the wavefronts, the partial result), in units: it counts so many units more, without
 // blocks, in front of its own.
@@ -62,7 +63,10 @@ constexpr int kInlineSegs = 256;    // segments whose units every workgroup coun
 // matrix units, the other waits for 64 KiB; 32 requests of nine rows, 8192 common keys).
 constexpr float kTallUnit = 0.8f;
 constexpr int kStages = 4;          // of the tall walk's ring
-constexpr int kShort = 1024, kShortF32 = 448;  // keys of a short request at most (see shared_short)
+// Keys of a short request, and of all tiles of a workgroup's share of them, at most (see
+// shared_short).
+constexpr int short_keys(bool f32, int d) { return f32 ? d == 64 ? 704 : 448 : d == 64 ? 4096 : 2048; }
+constexpr int short_share(bool f32, int d) { return f32 ? 896 : d == 64 ? 2560 : 2048; }
 constexpr float kNoMax = -3.0e38f;  // a maximum over no key
 // Softmax weights may exceed 1 by up to this factor (log2) before a row's maximum is
 // raised: with a maximum that need not be exact the raise is rare.
@@ -604,13 +608,13 @@ __device__ __forceinline__ void store_out(const SharedArgs& a, int64_t row, int 
     for (int e = 0; e < 4; ++e) Storage<T>::store(to, e, y[e]);
 }
 
-// The four wavefronts' states of the same rows, joined and stored: as a partial result, or
-// where the piece is all that its rows see (WHOLE) as the output.  smem: 4 D / 16 KiB.
-template <typename T, int D, int RT, bool WHOLE>
+// The W wavefronts' states of the same rows, joined and stored: as a partial result, or
+// where the piece is all that its rows see (WHOLE) as the output.  smem: W D / 16 KiB.
+template <typename T, int D, int RT, bool WHOLE, int W>
 __device__ __forceinline__ void join_waves(const SharedArgs& a, const Piece& p, float* m, float* l, f32x4_t (*o)[D / 16],
                                            uint8_t* smem) {
     constexpr int DT = D / 16;
-    __shared__ float s_ml[2][kWaves][16];
+    __shared__ float s_ml[2][W][16];
     const int wave = threadIdx.x / kWave, lane = own_lane(), l16 = lane % 16;
     f32x4_t* part = reinterpret_cast<f32x4_t*>(smem);
 #pragma unroll
@@ -622,18 +626,20 @@ __device__ __forceinline__ void join_waves(const SharedArgs& a, const Piece& p, 
         __syncthreads();
         float top = s_ml[0][0][l16];
 #pragma unroll
-        for (int w = 1; w < kWaves; ++w) top = fmaxf(top, s_ml[0][w][l16]);
-        float f[kWaves], all = 0.f;
+        for (int w = 1; w < W; ++w) top = fmaxf(top, s_ml[0][w][l16]);
+        float f[W], all = 0.f;
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) {
+        for (int w = 0; w < W; ++w) {
             f[w] = __builtin_amdgcn_exp2f(s_ml[0][w][l16] - top);
             all = fmaf(s_ml[1][w][l16], f[w], all);
         }
 #pragma unroll
-        for (int t = wave * (DT / kWaves); t < (wave + 1) * (DT / kWaves); ++t) {
+        for (int t0 = 0; t0 < DT; t0 += W) {
+            const int t = t0 + wave;
+            if (DT % W != 0 && t >= DT) break;
             f32x4_t v = part[t * kWave + lane] * f[0];
 #pragma unroll
-            for (int w = 1; w < kWaves; ++w) v += part[(w * DT + t) * kWave + lane] * f[w];
+            for (int w = 1; w < W; ++w) v += part[(w * DT + t) * kWave + lane] * f[w];
             if constexpr (WHOLE) {
                 const int e = p.row0 + r * 16 + l16;
                 if (r * 16 + l16 < p.rows)
@@ -648,7 +654,7 @@ __device__ __forceinline__ void join_waves(const SharedArgs& a, const Piece& p, 
 }
 
 // Few rows, bf16.
-template <int D, bool WHOLE = false>
+template <int D, bool WHOLE = false, int W = kWaves>
 __device__ void walk_flat(const SharedArgs& a, const Index& x, const Piece& p, uint8_t* smem) {
     constexpr int RT = 1, DT = D / 16, C = D / 32;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = own_lane(), l16 = lane % 16,
@@ -672,7 +678,7 @@ __device__ void walk_flat(const SharedArgs& a, const Index& x, const Piece& p, u
     constexpr int64_t kTile = (int64_t)D * kBlockTokens * 2;  // bytes of a block's keys of one head
     // This wavefront's two blocks of a unit.  The ids of 32 units lie in the lanes of a
     // register, -1 where a block is unmapped or behind the last one.
-    auto first = [&](int u) { return p.b_lo + u * kUnitBlocks + 2 * wave; };
+    auto first = [&](int u) { return p.b_lo + 2 * (u * W + wave); };
     auto read_ids = [&](int u) {
         const int b = first(u + lane / 2) + lane % 2;
         const int id = u + lane / 2 < p.u1 && b < p.b_hi ? p.table[b] : -1;
@@ -720,14 +726,14 @@ __device__ void walk_flat(const SharedArgs& a, const Index& x, const Piece& p, u
         id0 = next0;
         id1 = next1;
     }
-    join_waves<uint16_t, D, RT, WHOLE>(a, p, m, l, o, smem);
+    join_waves<uint16_t, D, RT, WHOLE, W>(a, p, m, l, o, smem);
 }
 
 // Few rows, fp32: fp32 products (v_mfma_f32_16x16x4_f32), a block of 16 keys at a time.
 // Lane 16 lg + l16 takes the 16-byte chunks lg, lg + 4, ... of key l16; product i of a
 // chunk multiplies its i-th dim.  A lane's 16 bytes of V^T are its keys 4 lg .. 4 lg + 3.
 // Bound by the matrix units where there are several tiles, by memory with one.
-template <int D, int RT, bool WHOLE = false>
+template <int D, int RT, bool WHOLE = false, int W = kWaves>
 __device__ void walk_flat_f32(const SharedArgs& a, const Index& x, const Piece& p, uint8_t* smem) {
     constexpr int DT = D / 16, C = D / 16;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = own_lane(), l16 = lane % 16,
@@ -744,7 +750,7 @@ __device__ void walk_flat_f32(const SharedArgs& a, const Index& x, const Piece& 
 #pragma unroll
         for (int c = 0; c < C; ++c) {
             if constexpr (!kInLds) q[c] = *reinterpret_cast<const f32x4u_t*>(row + 16 * c);
-            else if (c % kWaves == wave) s_q[(r * C + c) * kWave + lane] = *reinterpret_cast<const f32x4u_t*>(row + 16 * c);
+            else if (c % W == wave) s_q[(r * C + c) * kWave + lane] = *reinterpret_cast<const f32x4u_t*>(row + 16 * c);
         }
         pos[r] = row_position(a, x, p, r * 16 + l16);
         m[r] = kNoMax;
@@ -754,7 +760,7 @@ __device__ void walk_flat_f32(const SharedArgs& a, const Index& x, const Piece& 
     }
     constexpr int64_t kTile = (int64_t)D * kBlockTokens * 4;
     const int blocks = p.u1 - p.u0;  // of this wavefront: one of every unit
-    auto block = [&](int e) { return p.b_lo + ((p.u0 + e) << unit_shift(true)) + wave; };
+    auto block = [&](int e) { return p.b_lo + (p.u0 + e) * W + wave; };
     // the ids of 64 of them in the lanes of a register, as in walk_flat
     auto read_ids = [&](int e) {
         const int b = block(e + lane), id = e + lane < blocks && b < p.b_hi ? p.table[b] : -1;
@@ -832,7 +838,7 @@ __device__ void walk_flat_f32(const SharedArgs& a, const Index& x, const Piece& 
         id = next;
     }
     if (kInLds) __syncthreads();  // Q is used up
-    join_waves<float, D, RT, WHOLE>(a, p, m, l, o, smem);
+    join_waves<float, D, RT, WHOLE, W>(a, p, m, l, o, smem);
 }
 
 // Many rows, bf16: wavefront w has the rows' tiles w, w + 4, ...; the ring's stages hold two
@@ -1155,19 +1161,22 @@ __global__ __launch_bounds__(kThreads, 2) void shared_walk(SharedArgs a, Index x
 
 // Few and short requests: a workgroup walks all that 16 rows of a request and head see, the
 // prefix as the request's own table names it, with nothing to divide before and nothing to
-// join behind it.  Bound by the chain of lengths, block ids and keys, then by 0.6 us per
-// unit of bf16, 1.0 of fp32, and with many requests by the keys, prefixes out of L2.
-// Replayed, divided and like this: 8 requests of a row and 1024 keys 12.9 and 8.3 us, of
-// 2048 keys 16.2 and 18.1; fp32, 8 of 256 keys 14.2 and 9.1, of 512 16.2 and 14.1, but 2 of
-// 512 11.8 and 14.2.  All tiles' keys together: 128 requests of eight heads, 1000 keys, 141 of
-// them common, 101 and 84, 875 common 31 and 29; 250 such 42 and 52.  With several tiles,
-// which read the same keys: 64 requests of nine rows, 256 keys, 31 and 28, 512 keys 37 and 52
-// (fp32, where the divided walk takes few rows too: 256 keys 64 and 58).
+// join behind it; eight wavefronts in bf16 where every tile has a compute unit of its own.
+// Bound by the chain of lengths, block ids and keys, then by 0.6 us per unit of bf16, 1.0
+// of fp32, and with many requests by the keys, prefixes out of L2.  Replayed, divided and
+// like this, head dim 128: 8 requests of a row and 128 keys 10.4 and 4.2 us, of 2000 keys,
+// 1000 of them common, 16.2 and 14.6 (of 3000 19.4 and 19.7); head dim 64, 2 requests of 4000
+// keys 13.1 and 12.3.  fp32, 8 of 256 keys 14.2 and 9.1; 2 of 512 11.8 and 14.2, of head dim 64
+// and 700 keys 11.7 and 11.9.  All tiles' keys together: 64 requests of eight heads, 2000 keys,
+// 250 of them common, 94 and 83, 1750 common 25.5 and 27.4; head dim 64, 2200 keys 43 and 34,
+// 20 and 19, 3000 keys 52 and 48, 21 and 25.  With several tiles in bf16, which read the same
+// keys again: 20 requests of nine rows and 2000 keys 35 and 30, but more tiles than fit at
+// once, 64 such requests, 256 keys 31 and 28, 512 keys 37 and 52.
 //
 // Workgroup (head, request, tile).
-template <typename T, int D>
-__global__ __launch_bounds__(kThreads, 2) void shared_short(SharedArgs a, Index x) {
-    __shared__ __attribute__((aligned(16))) uint8_t smem[kWaves * (D / 16) * 1024];
+template <typename T, int D, int W>
+__global__ __launch_bounds__(W * kWave, 2) void shared_short(SharedArgs a, Index x) {
+    __shared__ __attribute__((aligned(16))) uint8_t smem[W * (D / 16) * 1024];
     const int i = blockIdx.y;
     const int q0 = clamp_to(x.q_start[i], 0, a.total_q), n = clamp_to(x.q_start[i + 1], q0, a.total_q) - q0;
     Piece p{};
@@ -1181,10 +1190,11 @@ __global__ __launch_bounds__(kThreads, 2) void shared_short(SharedArgs a, Index 
     for (p.row0 = blockIdx.z * 16; p.row0 < rows; p.row0 += gridDim.z * 16) {
         p.rows = min(16, rows - p.row0);
         p.min_pos = p.pos0 + p.row0 / a.group;
-        const int seen = p.pos0 + (p.row0 + p.rows - 1) / a.group + 1, unit = kBlockTokens << a.unit_shift;
-        p.u1 = (max(0, seen) + unit - 1) / unit;
-        if constexpr (sizeof(T) == 2) walk_flat<D, true>(a, x, p, smem);
-        else walk_flat_f32<D, 1, true>(a, x, p, smem);
+        const int seen = p.pos0 + (p.row0 + p.rows - 1) / a.group + 1;
+        constexpr int kUnit = W * kBlockTokens * (sizeof(T) == 2 ? 2 : 1);
+        p.u1 = (max(0, seen) + kUnit - 1) / kUnit;
+        if constexpr (sizeof(T) == 2) walk_flat<D, true, W>(a, x, p, smem);
+        else walk_flat_f32<D, 1, true, W>(a, x, p, smem);
     }
 }
 
@@ -1272,7 +1282,7 @@ struct SharedPlan {
     int nwg, tile_a, tile_b;
     int64_t slots_a, slots_b, segs;
     bool inlined, weighted;
-    int short_tiles;  // row tiles of a request where all are short (shared_short), or 0
+    int short_tiles, short_waves;  // row tiles of a request where all are short (shared_short), or 0
     int split;  // groups of threads that share a row's pieces in the pass that joins
     size_t o_bytes, ml_bytes, total;
 };
@@ -1297,9 +1307,10 @@ int plan_shared(const verify_attn_params* p, int32_t total_q, int32_t max_q_len,
     // (rounded up, so that fewer rows in smaller tiles never need more)
     const int64_t keys = std::min<int64_t>(max_seq_len, (int64_t)p->max_blocks_per_seq * kBlockTokens);
     const int64_t tiles16 = (own_rows + 15) / 16, pairs16 = tiles16 * p->num_seqs * p->num_kv_heads;
-    const int64_t most = f32 ? kShortF32 : kShort, rounds = f32 || tiles16 == 1 ? 2 : 1;
-    s.short_tiles = keys <= most && pairs16 * keys <= rounds * s.nwg * most && p->num_seqs <= 65535 ? (int)tiles16 : 0;
+    const int64_t share = short_share(f32, D) / (!f32 && tiles16 > 1 && pairs16 > s.nwg ? 2 : 1);
+    s.short_tiles = keys <= short_keys(f32, D) && pairs16 * keys <= s.nwg * share && p->num_seqs <= 65535 ? (int)tiles16 : 0;
     if (s.short_tiles) {
+        s.short_waves = !f32 && 2 * pairs16 <= s.nwg ? 8 : kWaves;
         s.total = 0;
         return VERIFY_OK;
     }
@@ -1346,7 +1357,14 @@ bool is_plain(const verify_attn_params* p, int32_t num_groups, int32_t max_prefi
 template <typename T, int D>
 void launch_shared(const SharedArgs& a, const Index& x, const SharedPlan& plan, hipStream_t stream) {
     if (plan.short_tiles) {
-        hipLaunchKernelGGL((shared_short<T, D>), dim3(a.hkv, a.num_seqs, plan.short_tiles), dim3(kThreads), 0, stream, a, x);
+        const dim3 grid(a.hkv, a.num_seqs, plan.short_tiles);
+        if constexpr (sizeof(T) == 2) {
+            if (plan.short_waves == 8) {
+                hipLaunchKernelGGL((shared_short<T, D, 8>), grid, dim3(8 * kWave), 0, stream, a, x);
+                return;
+            }
+        }
+        hipLaunchKernelGGL((shared_short<T, D, kWaves>), grid, dim3(kThreads), 0, stream, a, x);
         return;
     }
     const int split = plan.split;

@@ -53,7 +53,7 @@ class SharedBatch:
         for i, b in unmapped:
             self.table[i, b] = [-1, total, 2 ** 31 - 1][b % 3]
         if wide:
-            self.table = np.pad(self.table, ((0, 0), (0, max(0, 100 - self.table.shape[1]))), constant_values=-1)
+            self.table = np.pad(self.table, ((0, 0), (0, max(0, 260 - self.table.shape[1]))), constant_values=-1)
         self.max_seq_len = 16 * self.table.shape[1] if wide else int(self.S.max(initial=0))
         self.sinks = torch.as_tensor(rng.standard_normal(hq), dtype=torch.float32) if sinks else None
 

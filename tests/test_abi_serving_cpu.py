@@ -91,9 +91,9 @@ def test_count_tokens(kw, want):
     assert _count(**kw) == want
 
 
-def _shared(attn=None, T=5, mq=3, ms=2000, G=1, mp=64, q=DUMMY, kc=DUMMY, vc=DUMMY, gs=DUMMY, pl=DUMMY, out=DUMMY, ws=DUMMY,
+def _shared(attn=None, T=5, mq=3, ms=5000, G=1, mp=64, q=DUMMY, kc=DUMMY, vc=DUMMY, gs=DUMMY, pl=DUMMY, out=DUMMY, ws=DUMMY,
             size=None):
-    params = attn or _attn(max_blocks_per_seq=200)
+    params = attn or _attn(max_blocks_per_seq=400)
     if size is None:
         n = ctypes.c_size_t(0)
         rc = av.library().verify_attention_shared_workspace_size(ctypes.byref(params), T, mq, ms, G, mp, ctypes.byref(n))
@@ -125,14 +125,14 @@ def _shared_size(params, T, mq, ms, G, mp):
 
 @pytest.mark.parametrize("dtype", [av.BF16, av.F32])
 @pytest.mark.parametrize("heads", [(8, 8), (32, 8), (5, 1), (64, 1)])
-@pytest.mark.parametrize("keys", [448, 1000, 3000])
+@pytest.mark.parametrize("keys", [448, 1000, 3000, 6000])
 def test_shared_workspace_covers_smaller_batches(keys, heads, dtype):
     sizes = {}
     for B in (1, 2, 7, 40, 300):
         for T in (1, 3, 4, 9, 10, 33, 40, 130, 300, 1000, 5000):
             for mq in (1, 9, 300):
                 p = _attn(num_seqs=B, num_q_heads=heads[0], num_kv_heads=heads[1], head_dim=64, dtype=dtype,
-                          max_blocks_per_seq=200)
+                          max_blocks_per_seq=400)
                 sizes[B, T, mq] = _shared_size(p, T, mq, keys, 2, 64)
     for (B, T, mq), size in sizes.items():
         assert all(other <= size for (b, t, m), other in sizes.items() if b <= B and t <= T and m == mq)
@@ -142,13 +142,13 @@ def test_shared_workspace_covers_smaller_batches(keys, heads, dtype):
 def test_shared_workspace_covers_smaller_batches_of_many_heads(dtype, d):
     """One row more may mean larger tiles, of every head."""
     for heads, mq in (((4096, 4096), 10 ** 6), ((4096, 4096), 20), ((8192, 4096), 33)):
-        sizes = [_shared_size(_attn(num_seqs=2, num_q_heads=heads[0], num_kv_heads=heads[1], head_dim=d, dtype=dtype),
-                              T, mq, 1000, 1, 64) for T in range(1, 200)]
+        sizes = [_shared_size(_attn(num_seqs=2, num_q_heads=heads[0], num_kv_heads=heads[1], head_dim=d, dtype=dtype, max_blocks_per_seq=400),
+                              T, mq, 5000, 1, 64) for T in range(1, 200)]
         assert sizes == sorted(sizes)
 
 
 def test_short_requests_need_no_workspace():
-    for keys, dtype, blocks, want in ((1024, av.BF16, 200, True), (1025, av.BF16, 200, False), (5000, av.BF16, 64, True),
+    for keys, dtype, blocks, want in ((2048, av.BF16, 200, True), (2049, av.BF16, 200, False), (5000, av.BF16, 128, True),
                                       (448, av.F32, 200, True), (449, av.F32, 200, False), (5000, av.F32, 28, True)):
         size = lambda B, mq: _shared_size(_attn(num_seqs=B, max_blocks_per_seq=blocks, dtype=dtype), 300, mq, keys, 1, 64)
         assert (size(2, 3) == 0) == want

@@ -88,12 +88,14 @@ def test_more_requests_than_a_workgroup_counts_itself(batch, wide):
     b.check(b.call(DEV))
 
 
-@pytest.mark.parametrize("keys,dtype,short", [(1024, "bf16", True), (1025, "bf16", False), (448, "f32", True), (449, "f32", False)])
-def test_short_requests_need_no_workspace(keys, dtype, short):
+@pytest.mark.parametrize("keys,dtype,d,short", [
+    (2048, "bf16", 128, True), (2049, "bf16", 128, False), (4096, "bf16", 64, True), (4097, "bf16", 64, False),
+    (448, "f32", 128, True), (449, "f32", 128, False), (704, "f32", 64, True), (705, "f32", 64, False)])
+def test_short_requests_need_no_workspace(keys, dtype, d, short):
     """On both sides of the longest short request, with more rows than one tile and than
     max_q_len."""
     n = [1, 9, 30]
-    b = SharedBatch(keys, [(2, 333)], [keys, 340, keys - 50], n, hq=10, hkv=2, d=64, dtype=dtype, sinks=True)
+    b = SharedBatch(keys, [(2, 333)], [keys, 340, keys - 50], n, hq=10, hkv=2, d=d, dtype=dtype, sinks=True)
     args = b.to(DEV)
     assert (av.attention_shared_workspace_size(args[0], args[1], args[3], num_groups=1, **b.bounds) == 0) == short
     b.check(b.call(DEV, args))
@@ -148,7 +150,7 @@ def test_captured_and_replayed_on_new_lengths(wide):
     b = SharedBatch(4, [(3, 320)], [500, 400, 350], [4, 2, 9], hq=8, hkv=2, d=64, dtype="bf16", sinks=True, wide=wide)
     args = b.to(DEV)
     sinks = b.sinks.to(DEV)
-    bounds = dict(max_q_len=9, max_seq_len=1600 if wide else 600, max_prefix_len=400)
+    bounds = dict(max_q_len=9, max_seq_len=4160 if wide else 600, max_prefix_len=400)
     ws = torch.empty(av.attention_shared_workspace_size(args[0], args[1], args[3], num_groups=1, **bounds),
                      dtype=torch.uint8, device=DEV)
     out = torch.empty_like(args[0])
