@@ -31,7 +31,7 @@
 // one row, 8192 keys of their own, 2.1 GB in 374 us.
 // Many rows (tall): the wavefronts take the rows, and the keys pass through a ring of
 // LDS stages that all of them read.  Bound by the matrix units, the exponentials and the
-// latencies between them: 288 rows behind 65536 common keys, 309 GFLOP in 292 us.
+// latencies between them: 288 rows behind 65536 common keys, 309 GFLOP in 300 us.
 // Both at once: 32 requests of nine rows, 512 to 4096 keys behind 8192 common ones, 87 us
 // (the walk 75, of which each kind of work alone would take about 45).
 #include <type_traits>
