@@ -1357,7 +1357,8 @@ bool is_plain(const verify_attn_params* p, int32_t num_groups, int32_t max_prefi
 template <typename T, int D>
 void launch_shared(const SharedArgs& a, const Index& x, const SharedPlan& plan, hipStream_t stream) {
     if (plan.short_tiles) {
-        const dim3 grid(a.hkv, a.num_seqs, plan.short_tiles);
+        // 65535 in z at most: a workgroup takes every gridDim.z-th tile
+        const dim3 grid(a.hkv, a.num_seqs, std::min(plan.short_tiles, 65535));
         if constexpr (sizeof(T) == 2) {
             if (plan.short_waves == 8) {
                 hipLaunchKernelGGL((shared_short<T, D, 8>), grid, dim3(8 * kWave), 0, stream, a, x);
