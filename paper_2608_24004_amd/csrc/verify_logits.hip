@@ -471,7 +471,7 @@ extern "C" int verify_count_tokens(int32_t num_seqs, int32_t total_tokens, int64
                                    const int32_t* slots, int32_t prompt, int32_t* counts, uint32_t* seen,
                                    hipStream_t stream) {
     if (num_seqs < 0 || total_tokens < 0 || num_slots < 0 || vocab < 1 || (prompt != 0 && prompt != 1)) return VERIFY_EINVAL;
-    if (vocab > INT32_MAX - 31 || num_seqs > 65535) return VERIFY_EUNSUPPORTED;
+    if (vocab >= INT32_MAX - 31 || num_seqs > 65535) return VERIFY_EUNSUPPORTED;
     if (num_seqs == 0 || total_tokens == 0 || num_slots == 0) return VERIFY_OK;
     if (!tokens || !token_start || !seen || (!prompt && !counts)) return VERIFY_EINVAL;
     const CountArgs a{counts, seen, tokens, token_start, num_tokens, slots, (int)vocab, (int)((vocab + 31) / 32),
