@@ -33,8 +33,8 @@
  *                       logits of every scored position are computed from the
  *                       final hidden states and reduced to the argmax on the
  *                       fly, never stored.
- *   verify_check_batch -- the batch descriptor's preconditions, checked on the
- *                       device.
+ *   verify_check_batch, verify_check_groups -- the batch descriptor's preconditions,
+ *                       and those of groups of requests, checked on the device.
  *   verify_rotary, verify_rotary_append -- the scored rows' queries and keys
  *                       rotated to explicit positions on one or several axes;
  *                       the second stores the keys and values like
@@ -470,6 +470,35 @@ int verify_check_batch(int32_t num_seqs, int32_t total_q, int32_t max_q_len,
                        const int32_t *q_start, const verify_attn_params *params,
                        int32_t max_seq_len, const int32_t *seq_lens,
                        const int32_t *block_tables, int32_t *counts, hipStream_t stream);
+
+/*
+ * verify_check_groups -- the same for the groups of verify_attention_shared, which reads a
+ * common prefix through the table of the group's first request, or through each
+ * request's own: where the two differ, so do its results.
+ *
+ *   num_groups, group_start, prefix_lens, max_prefix_len   as for verify_attention_shared
+ *   params       the attention layer's shape (num_seqs, block_size 16)
+ *   max_seq_len, seq_lens, block_tables   as for verify_attention_shared
+ *   counts       int32[VERIFY_CHECK_GROUPS_COUNTS] on the device, reset and written by the
+ *                call (asynchronously, on `stream`):
+ *     [VERIFY_CHECK_GROUPS_BOUNDS] groups k whose group_start[k] < 0,
+ *                                  group_start[k + 1] < group_start[k] or > num_seqs
+ *     [VERIFY_CHECK_GROUPS_TABLE]  requests with a block id other than that of their
+ *                                  group's first request among the prefix's whole blocks,
+ *                                  as far as both have cached keys there
+ *     [VERIFY_CHECK_GROUPS_FIRST]  the lowest group with one of them, INT32_MAX if none
+ * VERIFY_EINVAL (nothing enqueued) on negative sizes, NULL params or counts, or an array
+ * missing; VERIFY_EUNSUPPORTED from 65536 groups or requests on.  The arrays are read only
+ * within their stated sizes, whatever they hold.
+ */
+#define VERIFY_CHECK_GROUPS_BOUNDS 0
+#define VERIFY_CHECK_GROUPS_TABLE 1
+#define VERIFY_CHECK_GROUPS_FIRST 2
+#define VERIFY_CHECK_GROUPS_COUNTS 3
+int verify_check_groups(const verify_attn_params *params, int32_t max_seq_len, int32_t num_groups,
+                        int32_t max_prefix_len, const int32_t *group_start,
+                        const int32_t *prefix_lens, const int32_t *seq_lens,
+                        const int32_t *block_tables, int32_t *counts, hipStream_t stream);
 
 /*
  * Rotary positions.  Dims f and f + R/2 of a head (interleaved: 2f and 2f + 1) are

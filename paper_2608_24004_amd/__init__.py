@@ -14,6 +14,8 @@ If the library is missing, every entry point raises -- there is no fallback.
     check_batch(...)           the batch descriptor's preconditions, checked on
                                the device (the calls above take ``check=True``,
                                or every call does with AGENTSPEC_VERIFY_CHECK=1)
+    check_groups(...)          those of groups of requests, which
+                               verify_attention_shared checks beside them
     verify_rotary(...), verify_rotary_append(...)
                                queries and keys rotated to positions on one or
                                several axes, alone or with the append
@@ -47,7 +49,7 @@ __all__ = ["verify_attention", "verify_accept", "verify_accept_noalloc", "verify
            "verify_norm_rotary", "verify_norm_rotary_append", "verify_adjust_logits", "verify_count_tokens",
            "verify_attention_shared", "attention_shared_workspace_size",
            "verify_key_weights", "verify_evict_plan", "verify_kv_compact",
-           "key_weights_workspace_size", "evict_plan_workspace_size", "check_batch", "BatchError", "VerifyError", "library",
+           "key_weights_workspace_size", "evict_plan_workspace_size", "check_batch", "check_groups", "BatchError", "VerifyError", "library",
            "abi_version", "F32", "BF16"]
 
 OK, EINVAL, EUNSUPPORTED, EWORKSPACE, EHIP = 0, -1, -2, -3, -4
@@ -57,6 +59,8 @@ F32, BF16 = 0, 1
 # then the first offending request (VERIFY_CHECK_FIRST)
 CHECK_KINDS = ("rows", "q_len", "short_seq", "long_seq", "block_id")
 CHECK_COUNTS = 6
+# verify_check_groups' counts, likewise, then the first offending group
+CHECK_GROUPS_KINDS = ("bounds", "table")
 ROTARY_MAX_AXES = 4  # VERIFY_ROTARY_MAX_AXES
 CHECK_BY_DEFAULT = os.environ.get("AGENTSPEC_VERIFY_CHECK", "0") == "1"
 
@@ -70,12 +74,13 @@ class VerifyError(RuntimeError):
 class BatchError(ValueError):
     """A batch descriptor that fails verify_check_batch: ``counts`` maps each
     kind in CHECK_KINDS to its number of offending requests, ``first`` is the
-    lowest offending request."""
+    lowest offending request.  Or one whose groups fail verify_check_groups: then the
+    kinds are CHECK_GROUPS_KINDS and ``first`` is the lowest offending group."""
 
-    def __init__(self, where: str, counts: dict, first: int):
+    def __init__(self, where: str, counts: dict, first: int, of: str = "request"):
         self.counts, self.first = counts, first
         bad = ", ".join("%s %d" % (k, v) for k, v in counts.items() if v)
-        super().__init__("%s: bad batch descriptor (%s; first request %d)" % (where, bad, first))
+        super().__init__("%s: bad batch descriptor (%s; first %s %d)" % (where, bad, of, first))
 
 
 class AttnParams(ctypes.Structure):
@@ -171,6 +176,8 @@ def library(path: Optional[str] = None):
     lib.verify_budget.restype = ctypes.c_int
     lib.verify_check_batch.argtypes = [i32, i32, i32, vp, P, i32, vp, vp, vp, vp]
     lib.verify_check_batch.restype = ctypes.c_int
+    lib.verify_check_groups.argtypes = [P, i32, i32, i32, vp, vp, vp, vp, vp, vp]
+    lib.verify_check_groups.restype = ctypes.c_int
     RP, f32 = ctypes.POINTER(RotaryParams), ctypes.c_float
     lib.verify_rotary.argtypes = [RP, i32, i32, i32, vp, i64, vp, i64, vp, vp, vp, i64, vp, i64, vp]
     lib.verify_rotary.restype = ctypes.c_int
@@ -398,6 +405,34 @@ def check_batch(q_start, total_q: int, *, max_q_len: int = 0, seq_lens=None, blo
     (stream if stream is not None else torch.cuda.current_stream(dev)).synchronize()
     c = counts.cpu().tolist()
     return dict(zip(CHECK_KINDS, c[:len(CHECK_KINDS)])), (c[-1] if c[-1] != 2 ** 31 - 1 else -1)
+
+
+def check_groups(group_start, prefix_lens, seq_lens, block_tables, *, max_prefix_len: int, max_seq_len: int, stream=None):
+    """The preconditions of groups of requests (see verify_attention_shared), checked on
+    the device by verify_check_groups: that group_start ascends within the batch, and that
+    the requests of a group name the same blocks for their common prefix.  Waits for the
+    call's stream and returns (counts, first): offenders per kind of CHECK_GROUPS_KINDS,
+    groups and requests, and the lowest group with one (-1 if none)."""
+    import torch
+    i32, dev = torch.int32, group_start.device
+    if group_start.dim() != 1 or group_start.shape[0] < 1:
+        raise ValueError("group_start must be [G + 1], got %s" % (tuple(group_start.shape),))
+    if block_tables.dim() != 2 or block_tables.shape[1] < 1:
+        raise ValueError("block_tables must be [B, max_blocks], got %s" % (tuple(block_tables.shape),))
+    B, G = block_tables.shape[0], group_start.shape[0] - 1
+    _expect(group_start, "group_start", None, i32, dev)
+    _expect(prefix_lens, "prefix_lens", (G,), i32, dev)
+    _expect(seq_lens, "seq_lens", (B,), i32, dev)
+    _expect(block_tables, "block_tables", None, i32, dev)
+    params = AttnParams(num_seqs=B, block_size=16, max_blocks_per_seq=block_tables.shape[1])
+    arrays = [_dev_ptr(group_start, "group_start"), _dev_ptr(prefix_lens, "prefix_lens"), _dev_ptr(seq_lens, "seq_lens"),
+              _dev_ptr(block_tables, "block_tables")]
+    counts = torch.empty(len(CHECK_GROUPS_KINDS) + 1, dtype=i32, device=dev)
+    _launch("verify_check_groups", dev.index, ctypes.byref(params), int(max_seq_len), G, int(max_prefix_len), *arrays,
+            counts.data_ptr(), _stream_ptr(stream, dev))
+    (stream if stream is not None else torch.cuda.current_stream(dev)).synchronize()
+    c = counts.cpu().tolist()
+    return dict(zip(CHECK_GROUPS_KINDS, c)), (c[-1] if c[-1] != 2 ** 31 - 1 else -1)
 
 
 def _checked(check, where, **kw):
@@ -1089,7 +1124,8 @@ def verify_attention_shared(q, k_cache, v_cache, block_tables, seq_lens, q_start
     group_start [G + 1] int32: requests group_start[k] .. group_start[k + 1] - 1 form
     group k; prefix_lens [G] int32: their first prefix_lens[k] // 16 block table entries
     are the same; max_prefix_len bounds them.  k_cache, v_cache and workspace are 16-byte
-    aligned.  Other arguments and the result as for verify_attention without a window."""
+    aligned.  check also refuses groups that fail check_groups.  Other arguments and the
+    result as for verify_attention without a window."""
     import torch
     if q.dim() != 3:
         raise ValueError("q must be [T, Hq, D], got %s" % (tuple(q.shape),))
@@ -1108,6 +1144,10 @@ def verify_attention_shared(q, k_cache, v_cache, block_tables, seq_lens, q_start
     if check or check is None and CHECK_BY_DEFAULT:
         _checked(check, "verify_attention_shared", q_start=q_start, total_q=T, max_q_len=max_q_len, seq_lens=seq_lens,
                  block_tables=block_tables, num_blocks=k_cache.shape[0], max_seq_len=max_seq_len, stream=stream)
+        bad, first = check_groups(group_start, prefix_lens, seq_lens, block_tables, max_prefix_len=max_prefix_len,
+                                  max_seq_len=max_seq_len, stream=stream)
+        if any(bad.values()):
+            raise BatchError("verify_attention_shared", bad, first, "group")
     if scale != 0.0:
         params.scale = scale
     bounds = T, int(max_q_len), int(max_seq_len), G, int(max_prefix_len)

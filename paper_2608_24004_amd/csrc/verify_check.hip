@@ -1,6 +1,6 @@
 // verify_check.hip -- device-side validation of a verify batch's descriptor
-// (q_start, seq_lens, block_tables) against the preconditions the other
-// calls state.  Those calls never read device data on the host and define
+// (q_start, seq_lens, block_tables), and of the groups whose requests share a prefix,
+// against the preconditions the other calls state.  Those calls never read device data on the host and define
 // what they do with ids outside the cache (skip them); this call reports such
 // data instead, for callers that want to catch a bad batch before it runs.
 //
@@ -23,9 +23,10 @@ struct CArgs {
     int num_seqs, total_q, max_q_len, max_seq_len, max_blocks, num_blocks, window;
 };
 
-__global__ __launch_bounds__(kWave) void check_reset(int32_t* __restrict__ counts) {
+// `kinds` counts, and behind them the first offender.
+__global__ __launch_bounds__(kWave) void check_reset(int32_t* __restrict__ counts, int kinds) {
     const int t = threadIdx.x;
-    if (t < VERIFY_CHECK_COUNTS) counts[t] = t == VERIFY_CHECK_FIRST ? INT32_MAX : 0;
+    if (t <= kinds) counts[t] = t == kinds ? INT32_MAX : 0;
 }
 
 __global__ __launch_bounds__(kCheckThreads) void check_batch(CArgs a, const int32_t* __restrict__ q_start,
@@ -72,6 +73,47 @@ __global__ __launch_bounds__(kCheckThreads) void check_batch(CArgs a, const int3
     }
 }
 
+struct GArgs {
+    int num_seqs, num_groups, max_prefix, max_len, max_blocks;
+};
+
+// Workgroup i: the bounds of group i, and request i's blocks beside those of its group's
+// first request.
+__global__ __launch_bounds__(kCheckThreads) void check_groups(GArgs a, const int32_t* __restrict__ group_start,
+                                                              const int32_t* __restrict__ prefix_lens,
+                                                              const int32_t* __restrict__ seq_lens,
+                                                              const int32_t* __restrict__ block_tables,
+                                                              int32_t* __restrict__ counts) {
+    for (int i = blockIdx.x; i < std::max(a.num_groups, a.num_seqs); i += gridDim.x) {
+        if (i < a.num_groups && threadIdx.x == 0 &&
+            (group_start[i] < 0 || group_start[i + 1] < group_start[i] || group_start[i + 1] > a.num_seqs)) {
+            atomicAdd(&counts[VERIFY_CHECK_GROUPS_BOUNDS], 1);
+            atomicMin(&counts[VERIFY_CHECK_GROUPS_FIRST], i);
+        }
+        if (i >= a.num_seqs) continue;
+        // the last group that begins at or before the request, if it holds it
+        int k = 0, hi = a.num_groups - 1;
+        while (k < hi) {
+            const int mid = (k + hi + 1) >> 1;
+            if (group_start[mid] <= i) k = mid; else hi = mid - 1;
+        }
+        const int first = std::max(group_start[k], 0);
+        int differs = 0;
+        if (first < i && i < group_start[k + 1]) {
+            auto cached = [&](int r) { return std::max(0, std::min(seq_lens[r], a.max_len)); };
+            const int blocks = std::min(std::max(0, std::min(std::min(prefix_lens[k], a.max_prefix), cached(first))) / kBlockTokens,
+                                        (cached(i) + kBlockTokens - 1) / kBlockTokens);
+            const int32_t* row = block_tables + (int64_t)i * a.max_blocks;
+            const int32_t* common = block_tables + (int64_t)first * a.max_blocks;
+            for (int b = threadIdx.x; b < blocks; b += kCheckThreads) differs |= row[b] != common[b];
+        }
+        if (__syncthreads_or(differs) && threadIdx.x == 0) {
+            atomicAdd(&counts[VERIFY_CHECK_GROUPS_TABLE], 1);
+            atomicMin(&counts[VERIFY_CHECK_GROUPS_FIRST], k);
+        }
+    }
+}
+
 }  // namespace
 }  // namespace averify
 
@@ -101,10 +143,29 @@ extern "C" int verify_check_batch(int32_t num_seqs, int32_t total_q, int32_t max
         a.num_blocks = params->num_blocks;
         a.window = params->sliding_window;
     }
-    hipLaunchKernelGGL(check_reset, dim3(1), dim3(kWave), 0, stream, counts);
+    hipLaunchKernelGGL(check_reset, dim3(1), dim3(kWave), 0, stream, counts, VERIFY_CHECK_FIRST);
     if (num_seqs > 0)
         hipLaunchKernelGGL(check_batch, dim3((unsigned)std::min(num_seqs, kCheckMaxWorkgroups)),
                            dim3(kCheckThreads), 0, stream, a, q_start, params ? seq_lens : nullptr,
                            params ? block_tables : nullptr, counts);
+    return check_launch();
+}
+
+extern "C" int verify_check_groups(const verify_attn_params* params, int32_t max_seq_len, int32_t num_groups,
+                                   int32_t max_prefix_len, const int32_t* group_start, const int32_t* prefix_lens,
+                                   const int32_t* seq_lens, const int32_t* block_tables, int32_t* counts,
+                                   hipStream_t stream) {
+    if (!params || !counts || max_seq_len < 0 || num_groups < 0 || max_prefix_len < 0) return VERIFY_EINVAL;
+    if (params->num_seqs < 0 || params->block_size != kBlockTokens || params->max_blocks_per_seq <= 0) return VERIFY_EINVAL;
+    if (num_groups > 65535 || params->num_seqs > 65535) return VERIFY_EUNSUPPORTED;
+    if (num_groups > 0 && (!group_start || !prefix_lens)) return VERIFY_EINVAL;
+    if (num_groups > 0 && params->num_seqs > 0 && (!seq_lens || !block_tables)) return VERIFY_EINVAL;
+    const GArgs a{params->num_seqs, num_groups, max_prefix_len,
+                  (int)std::min<int64_t>(max_seq_len, (int64_t)kBlockTokens * params->max_blocks_per_seq),
+                  params->max_blocks_per_seq};
+    hipLaunchKernelGGL(check_reset, dim3(1), dim3(kWave), 0, stream, counts, VERIFY_CHECK_GROUPS_FIRST);
+    if (num_groups > 0)
+        hipLaunchKernelGGL(check_groups, dim3((unsigned)std::min(std::max(num_groups, params->num_seqs), kCheckMaxWorkgroups)),
+                           dim3(kCheckThreads), 0, stream, a, group_start, prefix_lens, seq_lens, block_tables, counts);
     return check_launch();
 }

@@ -1,9 +1,13 @@
 """Bounds of the serving calls at their exact values, on the host."""
 from __future__ import annotations
 
+import ctypes
+
 import pytest
+import torch
 
 import paper_2608_24004_amd as av
+from test_abi_bounded_cpu import DUMMY, _attn
 from test_abi_serving_cpu import _adjust, _count
 
 
@@ -22,3 +26,30 @@ def test_adjust_logits_refuses_vocabularies_from_the_stated_one_on(vocab, want):
 def test_requests(batch, want):
     assert _count(B=batch, tokens=None) == want
     assert _adjust(B=batch, logits=None) == want
+
+
+def _groups(params=True, ms=100, G=2, mp=64, gs=DUMMY, pl=DUMMY, lens=DUMMY, bt=DUMMY, counts=DUMMY, **kw):
+    p = _attn(**kw)
+    return av.library().verify_check_groups(ctypes.byref(p) if params else None, ms, G, mp, gs, pl, lens, bt, counts, None)
+
+
+@pytest.mark.parametrize("kw,want", [
+    (dict(params=False), av.EINVAL), (dict(counts=None), av.EINVAL), (dict(ms=-1), av.EINVAL), (dict(G=-1), av.EINVAL),
+    (dict(mp=-1), av.EINVAL), (dict(num_seqs=-1), av.EINVAL), (dict(block_size=32), av.EINVAL),
+    (dict(max_blocks_per_seq=0), av.EINVAL), (dict(G=65536), av.EUNSUPPORTED), (dict(num_seqs=65536), av.EUNSUPPORTED),
+    (dict(gs=None), av.EINVAL), (dict(pl=None), av.EINVAL), (dict(lens=None), av.EINVAL), (dict(bt=None), av.EINVAL),
+])
+def test_check_groups(kw, want):
+    assert _groups(**kw) == want
+
+
+def test_the_binding_refuses_groups():
+    i32 = torch.int32
+    good = [torch.zeros(3, dtype=i32), torch.zeros(2, dtype=i32), torch.zeros(4, dtype=i32), torch.zeros((4, 5), dtype=i32)]
+    bounds = dict(max_prefix_len=16, max_seq_len=80)
+    for at, t in [(0, good[0][:0]), (0, good[3]), (0, good[0].long()), (1, good[1][:1]), (2, good[2][:3]), (3, good[3][0]),
+                  (3, good[3][:, :0]), (3, good[3].float()), (0, good[0])]:
+        args = list(good)
+        args[at] = t
+        with pytest.raises((ValueError, TypeError)):
+            av.check_groups(*args, **bounds)
