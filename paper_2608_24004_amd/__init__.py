@@ -861,10 +861,11 @@ def _rotary_args(q, T, D, positions, inv_freq, axes, interleaved, scale, idx, de
     p_freq = _arg(inv_freq, "inv_freq", None, torch.float64, idx, dev)
     try:
         # of the usual 64 small numbers a string of bytes is made, hashed and compared in
-        # half of a tuple's time
-        turned = None if axes is None else bytes(axes)
+        # half of a tuple's time; of others than a list bytes() may take the memory (arrays)
+        # or a length (a tensor of one number)
+        turned = None if axes is None else bytes(axes if type(axes) in (list, tuple) else [int(x) for x in axes])
     except (TypeError, ValueError):
-        turned = tuple(axes)
+        turned = tuple(int(x) for x in axes)
     key = (D, F, num_axes, bool(interleaved), float(scale), q.dtype, turned)
     params = _rotary_params.get(key)
     if params is None:

@@ -3,6 +3,7 @@ from __future__ import annotations
 
 import ctypes
 
+import numpy as np
 import pytest
 import torch
 
@@ -53,3 +54,21 @@ def test_the_binding_refuses_groups():
         args[at] = t
         with pytest.raises((ValueError, TypeError)):
             av.check_groups(*args, **bounds)
+
+
+def test_axes_of_any_kind_name_the_same_frequencies():
+    """A layer's parameters are kept by what the axes say, not by how they are given: a
+    tensor of one axis is a number too."""
+    q, freq = torch.zeros((2, 1, 64)), torch.ones(1, dtype=torch.float64)
+    pos = torch.zeros((3, 2), dtype=torch.int32)
+    for axes in (torch.tensor([2]), (0,), np.array([1]), [1], torch.tensor([1]), (2,), np.array([0], dtype=np.uint8), [0.0],
+                 range(1, 2), b"\2"):
+        params, _, _ = av._rotary_args(q, 2, 64, pos, freq, axes, False, 0.0, -1, q.device)
+        assert list(params.axis[:1]) == [int(axes[0])]
+    freq = torch.ones(3, dtype=torch.float64)
+    for axes in (torch.tensor([2, 0, 1]), (0, 0, 2), np.array([1, 2, 0]), [0.0, 1.0, 2.0], range(3)):
+        params, _, _ = av._rotary_args(q, 2, 64, pos, freq, axes, False, 0.0, -1, q.device)
+        assert list(params.axis[:3]) == [int(x) for x in axes]
+    for axes in ((3,), (-1,), (300,), torch.tensor([3]), np.array([-1], dtype=np.int8)):
+        with pytest.raises(ValueError, match="axes"):
+            av._rotary_args(q, 2, 64, pos, freq[:1], axes, False, 0.0, -1, q.device)
