@@ -54,8 +54,18 @@ __device__ __forceinline__ float group_sum(float v, int sh) {
 // Query or key heads of a workgroup at most (six prompts of 12 thousand rows in all: 54.3 us
 // with 16, 56.8 with 8).
 constexpr int kNormHeads = 16;
-// Workgroups that a compute unit holds, by their registers or their wavefronts.
-constexpr int resident(bool append, bool wide, bool inter) { return !wide ? 8 : !inter ? 5 : append ? 6 : 8; }
+// Workgroups of a compute unit that the choice of heads counts with.  A unit holds, wide,
+// by registers five with pairs of halves (fp32 heads of 64 dims seven), eight of
+// neighbouring pairs without and, by the values' LDS, five (128 dims) or seven (64) with the
+// append.  Counting with those instead is not faster on the average of 16 lengths, 700 to
+// 8000 rows of 40 heads: neighbouring pairs with the append, fp32 of 128 dims, 1.8 % slower,
+// of 64 dims, bf16 and fp32, 3.1 % slower and the same; halves, fp32 of 64 dims, 2.3 % slower,
+// with the append the same.  For bf16 of 128 dims five instead of six are 2.9 % faster (1000
+// rows 10.2 and 13.2 us).
+constexpr int resident(bool append, bool wide, bool inter, bool f32, int d) {
+    if (!wide || (inter && !append)) return 8;
+    return inter && (f32 || d == 64) ? 6 : 5;
+}
 // (row, head) units of a thread in flight, 64 bytes.
 constexpr int units(bool inter) { return inter ? 4 : 2; }
 
@@ -289,7 +299,8 @@ int norm_call(NormArgs& na, const verify_rotary_params& p, hipStream_t stream) {
     // take (2500 rows of 40 heads: eight, in one round, 14.0 us; three, in not quite two, 18.2;
     // 8000 rows: eight, in two, 39.4; 16, in one and a sixth, 41.5).  Of long inputs all
     // that a workgroup takes.
-    const int64_t tiles = ((int64_t)a.total_q + kTile - 1) / kTile, fit = (int64_t)resident(APPEND, wide, p.interleaved) * device_cus();
+    const int64_t tiles = ((int64_t)a.total_q + kTile - 1) / kTile,
+                  fit = (int64_t)resident(APPEND, wide, p.interleaved, esize == 4, p.head_dim) * device_cus();
     auto groups = [&](int64_t heads, int h) { return (heads + h - 1) / h; };
     auto wgs = [&](int h) { return tiles * (groups(a.hq, h) + groups(a.hkv, h) + a.value_wgs); };
     auto cost = [&](int h) { return ((wgs(h) + fit - 1) / fit * fit + wgs(h)) * (h + 4); };
