@@ -11,15 +11,16 @@
 //
 // What bounds it: memory, 2 V bytes in and out per row (288 rows of 151936 with all changes
 // 36.4 us, a copy 37), and with single rows the latencies that lead to a span's logits
-// (256 of them 61 us, a copy 32).  The request's state is small
+// (256 of them 61 to 64 us, a copy 32).  The request's state is small
 // beside them: a bit per token tells whether a count need be read at all, so V / 4
 // bytes of bits and the counts of the few tokens that were had.  A workgroup takes
 // kSpan tokens of one request and all of its rows: state and biases become a bit and a
 // summand per token in registers, eight tokens to a thread; a draft changes those of
 // one token on the way to the next row.  What hides the memory's latency is the number
-// of wavefronts: counts and biases, which only a draft needs again, lie in LDS (with them
-// and the next rows in registers, four wavefronts per SIMD instead of eight, the 288 rows
-// took 60 us; six, in a loop over spans that reads a request's parameters once, 40).  Wavefronts whose tokens nothing changes move bits.
+// of wavefronts, seven per SIMD in bf16 (by LDS) and six in fp32 (by registers): counts and
+// biases, which only a draft needs again, lie in LDS (with them and the next rows in registers,
+// four wavefronts, the 288 rows took 60 us; in a loop over spans that reads a request's
+// parameters once, six, 40).  Wavefronts whose tokens nothing changes move bits.
 #include <type_traits>
 
 #include "common.h"
