@@ -23,17 +23,23 @@
 //                  results of both products are its eight keys 8 lg .. 8 lg + 7 of 32;
 //   O^T += V^T P^T the same instruction, A = V^T: a lane's 16 bytes are the eight keys
 //                  8 lg .. 8 lg + 7 of dim l16, B = P^T as the scores left it.
-// Nothing but the operands of several wavefronts goes through LDS.
+// Nothing but the operands of several wavefronts goes through LDS.  bf16's weights enter the
+// second product in bf16, as verify_attention's do; maxima, sums and outputs are in fp32, and
+// the sum is that of the unrounded weights.  The rounding takes the output's error from
+// the 0.0017 of its norm that the store alone leaves to 0.0022-0.0023.  A second product with
+// what the rounding takes off leaves 0.0017 and costs a third more where the matrix units count: 288
+// rows behind 65536 keys 297 -> 391 us, 32 requests of nine rows 87 -> 100, 64 single rows 52.6 ->
+// 54.9 (fp32 inputs have fp32 weights and products).
 //
 // Few rows (flat): the four wavefronts of a workgroup take 32 of a unit's 128 keys each,
 // with all rows, straight from memory into operand registers, the next unit's keys
 // asked for as soon as this one's scores are done.  Bound by memory: 64 requests of
-// one row, 8192 keys of their own, 2.1 GB in 374 us.
+// one row, 8192 keys of their own, 2.1 GB in 372 to 415 us by what ran before (5.8 to 5.2 TB/s).
 // Many rows (tall): the wavefronts take the rows, and the keys pass through a ring of
 // LDS stages that all of them read.  Bound by the matrix units, the exponentials and the
-// latencies between them: 288 rows behind 65536 common keys, 309 GFLOP in 300 us.
-// Both at once: 32 requests of nine rows, 512 to 4096 keys behind 8192 common ones, 87 us
-// (the walk 75, of which each kind of work alone would take about 45).
+// latencies between them: 288 rows behind 65536 common keys, 309 GFLOP in 303 us.
+// Both at once: 32 requests of nine rows, 512 to 4096 keys behind 8192 common ones, 86 us
+// (the walk 77, of which each kind of work alone would take about 45).
 #include <type_traits>
 
 #include "common.h"
@@ -72,7 +78,7 @@ constexpr float kNoMax = -3.0e38f;  // a maximum over no key
 // raised: with a maximum that need not be exact the raise is rare.
 constexpr float kSlackLog2 = 8.f;
 // 16-row tiles of a flat walk at most.  In bf16 two of them and the keys under way do not
-// fit 256 registers, and the ring serves 32 rows as well (5.1 TB/s; flat, with 16 rows, 5.8;
+// fit 256 registers, and the ring serves 32 rows as well (5.2 TB/s; flat, with 16 rows, 5.6;
 // with Q in LDS three fit, but 32 requests of nine rows take 71 us instead of 65).  In fp32
 // more rows read the keys less often: 288 rows behind 65536 common keys, 309 GFLOP, take
 // 2.55 ms (121 TFLOP/s) with three tiles, 2.81 with two.
@@ -1166,8 +1172,10 @@ __global__ __launch_bounds__(kThreads, 2) void shared_walk(SharedArgs a, Index x
 // of fp32, and with many requests by the keys, prefixes out of L2.  Replayed, divided and
 // like this, head dim 128: 8 requests of a row and 128 keys 10.4 and 4.2 us, of 2000 keys,
 // 1000 of them common, 16.2 and 14.6 (of 3000 19.4 and 19.7); head dim 64, 2 requests of 4000
-// keys 13.1 and 12.3.  fp32, 8 of 256 keys 14.2 and 9.1; 2 of 512 11.8 and 14.2, of head dim 64
-// and 700 keys 11.7 and 11.9.  All tiles' keys together: 64 requests of eight heads, 2000 keys,
+// keys 13.1 and 12.3.  fp32, 8 of 256 keys 14.2 and 9.1; two of 440 keys, half of them common,
+// 11.8 and 12.8, three quarters common 13.5 and 12.8; two of 512 13.8 and 15.4, but eight of nine
+// rows and 520 keys 29.8 and 16.4: with more tiles the division takes longer, which the limit
+// on keys alone leaves out; head dim 64, two of 700 keys 12.4 and 11.8.  All tiles' keys together: 64 requests of eight heads, 2000 keys,
 // 250 of them common, 94 and 83, 1750 common 25.5 and 27.4; head dim 64, 2200 keys 43 and 34,
 // 20 and 19, 3000 keys 52 and 48, 21 and 25.  With several tiles in bf16, which read the same
 // keys again: 20 requests of nine rows and 2000 keys 35 and 30, but more tiles than fit at
