@@ -852,8 +852,9 @@ const char *verify_status_string(int status);
 /* Library ABI version (major * 10000 + minor * 100 + patch): 1.9.0.  Since 1.9.0
  * verify_attention_plan reports whole pairs (-1), and the size that
  * verify_attention_workspace_size returns covers batches of fewer requests.  The
- * rotary and bounded-cache calls were added to it without a change to any other: a
- * caller that may load a library of 1.9.0 without them looks for their symbols. */
+ * rotary and bounded-cache calls, the norms with rotary positions, shared attention,
+ * changed logits and verify_check_groups were added to it without a change to any other:
+ * a caller that may load a library of 1.9.0 without them looks for their symbols. */
 int verify_abi_version(void);
 
 #ifdef __cplusplus
